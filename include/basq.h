@@ -303,6 +303,101 @@ int basq_calibrate_bias(const void* X, int64_t M, int32_t K, int64_t ldx, int32_
  * int8 (Paley type-I construction over GF(27) = GF(3)[t]/(t^3 + 2t + 1)). */
 int basq_hadamard28(int8_t* out_host);
 
+/* ---- around the linear layer: norm, rotary positions, INT4 cache, attention ------------------- */
+
+/*
+ * The residual's addition and the root-mean-square norm in front of a linear layer.  For each token m:
+ *
+ *     h_k = bf16(X[m,k] + residual[m,k])                             (X[m,k] without a residual)
+ *     y_k = (h_k * rstd) * weight_k ,   rstd = 1 / sqrt(mean_k h_k^2 + eps)          fp32
+ *     Y8[m,k] = e4m3(y_k / s_m) ,   s_m = max_k |y_k| / 448          (1 if not a positive finite number)
+ *
+ *   X, residual  bf16 [M, ldx], [M, ldr]; residual may be NULL.   weight  bf16 [K]
+ *   res_out      out, bf16 [M, ldro]: h, or NULL.  May be X or residual (with that one's stride)
+ *   Y            out, bf16 [M, ldy], or NULL where Y8 is given.  May be X or residual
+ *   Y8, y8_scale out, OCP e4m3 [M, ldy8] and fp32 [M] (for a projection that is kept in 8 bits), or NULL
+ * K % 8 == 0, K <= 32768; strides multiples of 8; base pointers 16-byte aligned (Y8: 8, y8_scale: 4).  M == 0 does nothing.
+ */
+int basq_add_rms_norm(const void* X, const void* residual, const void* weight, int64_t M, int32_t K, int64_t ldx, int64_t ldr,
+                      float eps, void* res_out, int64_t ldro, void* Y, int64_t ldy, uint8_t* Y8, int64_t ldy8, float* y8_scale,
+                      void* stream);
+
+/*
+ * Cosines and sines for basq_rope_append, computed in fp64 (offline): row p holds cos(p f_j), j < rot_dim/2, then sin(p f_j),
+ * with f_j = base^(-2j/rot_dim), and for long contexts
+ *   BASQ_ROPE_LINEAR  f_j / factor
+ *   BASQ_ROPE_BANDS   u f_j + (1 - u) f_j / factor, u = clamp((t_j - low) / (high - low), 0, 1), t_j = original_len f_j / 2 pi
+ *                     the turns that pair j makes over the original length
+ *   BASQ_ROPE_YARN    the same with u linear in j, between the pairs that make `high` and `low` turns (rounded outwards), and
+ *                     cosines and sines times 0.1 ln(factor) + 1 (factor > 1)
+ * factor is read by all but BASQ_ROPE_PLAIN; low, high and original_len by the last two.
+ *   cos_sin   out, fp32 [positions, rot_dim]
+ */
+#define BASQ_ROPE_PLAIN  0
+#define BASQ_ROPE_LINEAR 1
+#define BASQ_ROPE_BANDS  2
+#define BASQ_ROPE_YARN   3
+int basq_rope_table(int32_t rot_dim, int64_t positions, double base, int32_t scaling, double factor, double low, double high,
+                    double original_len, float* cos_sin, void* stream);
+
+/*
+ * The paged INT4 cache of keys and values (Sec. 5 "Deployment Details": per-head asymmetric INT4): uint8 [num_pages, kv_heads,
+ * page_size * (head_dim + 16)].  With P = page_size, D = head_dim, one head of one page holds
+ *     K codes [P, D/2] canonical | V codes [P, D/2] canonical | K ranges fp32 [P, 2] = (scale, lo) | V ranges fp32 [P, 2]
+ * and stands for scale * code + lo.  Slot s of a layer's cache is token s % P of page s / P.
+ * head_dim 64 or 128; page_size a power of two from 16 to 1024; fewer than 2^31 tokens in all pages; 16-byte aligned.
+ * basq_kv_page_bytes: bytes of one page (all heads), 0 for an unsupported shape.
+ */
+size_t basq_kv_page_bytes(int32_t kv_heads, int32_t head_dim, int32_t page_size);
+
+/*
+ * New tokens' heads on their way into the cache: rotary positions and the online per-head Hadamard rotation of q and k (Sec. 4;
+ * the rotation cancels in q . k), the INT4 quantisation of k and v (Eq. 4 per head, Sec. 5).  For each token t, in fp32, each
+ * operation rounded on its own:
+ *     rope     (a, b) -> (a cos - b sin, b cos + a sin) for the pairs of the first rot_dim channels: (i, i + rot_dim/2), or
+ *              (2i, 2i + 1) where interleaved, with the cosines and sines of row positions[t]; the other channels stay
+ *     rotate   sums and differences (a + b, a - b) of the channels 1, 2, 4, ... D/2 apart, then times fp32(1/sqrt(D))
+ *     k, v     lo, hi, s, q as in basq_rotate_quant, over each head; code and (s, lo) go to slots[t] of the cache
+ *     k_hat, v_hat   bf16(fma(s, q, lo)), what the cache stands for (the prompt's own attention)
+ *   q, k, v    bf16 [T, heads, D], [T, kv_heads, D] twice, heads side by side, token strides ldq, ldk, ldv (the three parts of one
+ *              fused projection's output, say).  heads or kv_heads may be 0 (no q, or neither k nor v)
+ *   positions  int32 [T]; a token whose position is negative or >= table_rows is padding: nothing of it is read or written.
+ *              Not read where cos_sin is NULL (no rotary positions)
+ *   cos_sin    fp32 [table_rows, rot_dim] (basq_rope_table); rot_dim a multiple of 16 up to D
+ *   slots      int32 [T], each at most once; one that is negative or past the cache is not stored.  cache may be NULL (not stored)
+ *   bits       must be 4 (else BASQ_EUNSUPPORTED)
+ *   q_out      out, bf16 [T, heads, D], token stride ldqo; may be q.  k_hat, v_hat: out, bf16 [T, kv_heads, D], token stride ldh,
+ *              or NULL; may be k and v
+ * T == 0 does nothing.
+ */
+int basq_rope_append(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int64_t T, int32_t heads,
+                     int32_t kv_heads, int32_t head_dim, const int32_t* positions, const float* cos_sin, int64_t table_rows,
+                     int32_t rot_dim, int32_t interleaved, int32_t rotate, float clip_lo, float clip_hi, int32_t bits,
+                     const int32_t* slots, uint8_t* cache, int32_t num_pages, int32_t page_size, void* q_out, int64_t ldqo,
+                     void* k_hat, void* v_hat, int64_t ldh, void* stream);
+
+/*
+ * Attention of the q_len newest tokens of each sequence over its cache, in which they are stored already.  With k_t, v_t what the
+ * cache stands for, for new token j = 0 .. q_len - 1 of sequence b and each head (head h reads kv head h / (heads/kv_heads)):
+ *     s_t = scale q . k_t ;   s_t = softcap tanh(s_t / softcap) where softcap > 0
+ *     out = sum_t softmax(s)_t v_t ,   lse = ln sum_t e^(s_t)
+ * over the tokens t < n, n = lengths[b] - (q_len - 1 - j), and t >= n - window where window > 0.  No token: out = 0, lse = -inf.
+ *   q          bf16 [B * q_len, heads, D], token stride ldq (q_out of basq_rope_append)
+ *   page_table int32 [B, table_stride]: token t of sequence b is token t % page_size of page page_table[b, t / page_size].  Entries
+ *              past a length are not read; tokens of a page that is negative or >= num_pages count as not there
+ *   lengths    int32 [B], the new tokens among them; more than max_len counts as max_len (negative as 0)
+ *   max_len    host: the longest length there can be; the work is laid out for it.  At most table_stride * page_size
+ *   out        out, bf16 [B * q_len, heads, D], token stride ldo; may be q.   lse   out, fp32 [B * q_len, heads], or NULL
+ *   workspace  basq_paged_attention_workspace_bytes, 256-byte aligned (BASQ_EWORKSPACE where it is smaller); NULL where that is 0
+ * The result does not depend on where pages lie.  B == 0 does nothing.
+ */
+size_t basq_paged_attention_workspace_bytes(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                                            int32_t max_len, int32_t window);
+int basq_paged_attention(const void* q, int64_t ldq, int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                         int32_t bits, const uint8_t* cache, int32_t num_pages, int32_t page_size, const int32_t* page_table,
+                         int64_t table_stride, const int32_t* lengths, int32_t max_len, float scale, float softcap, int32_t window,
+                         void* out, int64_t ldo, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- diagnostics: what this machine sustains (used by the benchmark's measured ceilings), single tilings, bounds ---- */
 
 /*

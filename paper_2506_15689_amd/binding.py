@@ -23,6 +23,7 @@ STREAM_MAX_TOKENS = 128      # calls of more tokens never take the weight-stream
 
 EXPORTS = ["basq_version", "basq_last_error", "basq_rotate_quant", "basq_w4a4_gemm", "basq_workspace_bytes",
            "basq_w4a4_gemm_grouped", "basq_group_colsums", "basq_fp6_bytes", "basq_pack_fp6", "basq_decode_bytes", "basq_pack_decode", "basq_linear_fused", "basq_linear_fused_static", "basq_rotate_weights", "basq_quantize_weights", "basq_fused_bias", "basq_prepare_weights", "basq_calibrate_bias",
+           "basq_add_rms_norm", "basq_rope_table", "basq_kv_page_bytes", "basq_rope_append", "basq_paged_attention_workspace_bytes", "basq_paged_attention",
            "basq_hadamard28", "basq_diag_stream", "basq_diag_read", "basq_diag_mfma_i8", "basq_diag_mfma_f6",
            "basq_diag_fp6_tiling", "basq_diag_w4a4_gemm_fp6", "basq_diag_fp6_split_tiling", "basq_diag_w4a4_gemm_fp6_split",
            "basq_diag_grouped_tiling", "basq_diag_w4a4_gemm_grouped_fp6", "basq_diag_grouped_wide_strays", "basq_diag_block_vector_channels",
@@ -87,6 +88,21 @@ def load() -> ctypes.CDLL:
     lib.basq_prepare_weights.argtypes = [vp, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.basq_calibrate_bias.restype = c.c_int
     lib.basq_calibrate_bias.argtypes = [vp, i64, i32, i64, i32, vp, vp, vp, c.c_size_t, vp]
+    f64 = c.c_double
+    lib.basq_add_rms_norm.restype = c.c_int
+    lib.basq_add_rms_norm.argtypes = [vp, vp, vp, i64, i32, i64, i64, f32, vp, i64, vp, i64, vp, i64, vp, vp]
+    lib.basq_rope_table.restype = c.c_int
+    lib.basq_rope_table.argtypes = [i32, i64, f64, i32, f64, f64, f64, f64, vp, vp]
+    lib.basq_kv_page_bytes.restype = c.c_size_t
+    lib.basq_kv_page_bytes.argtypes = [i32, i32, i32]
+    lib.basq_rope_append.restype = c.c_int
+    lib.basq_rope_append.argtypes = [vp, i64, vp, i64, vp, i64, i64, i32, i32, i32, vp, vp, i64, i32, i32, i32, f32, f32, i32,
+                                     vp, vp, i32, i32, vp, i64, vp, vp, i64, vp]
+    lib.basq_paged_attention_workspace_bytes.restype = c.c_size_t
+    lib.basq_paged_attention_workspace_bytes.argtypes = [i32] * 7
+    lib.basq_paged_attention.restype = c.c_int
+    lib.basq_paged_attention.argtypes = [vp, i64, i32, i32, i32, i32, i32, i32, vp, i32, i32, vp, i64, vp, i32, f32, f32, i32,
+                                         vp, i64, vp, vp, c.c_size_t, vp]
     lib.basq_hadamard28.restype = c.c_int
     lib.basq_hadamard28.argtypes = [vp]
     lib.basq_diag_stream.restype = c.c_int
@@ -335,6 +351,141 @@ def basq_calibrate_bias(X: torch.Tensor, rot_size: int, act_scale: Optional[torc
                                       _stream(stream)))
 
 
+# ---- around the linear layer: norm, rotary positions, INT4 cache, attention --------------------
+
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BANDS, ROPE_YARN = 0, 1, 2, 3      # BASQ_ROPE_* of include/basq.h
+
+
+def _rows(t: torch.Tensor, shape, name: str, dtype=torch.bfloat16) -> int:
+    """The row stride of a tensor of this shape and type whose rows are contiguous.  (One row has no stride of its own.)"""
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype} {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
+    if len(shape) == 3:
+        width = shape[1] * shape[2]
+        contiguous = (t.stride(2) == 1 or shape[2] < 2) and (t.stride(1) == shape[2] or shape[1] < 2)
+    else:
+        width = shape[1]
+        contiguous = t.stride(1) == 1 or width < 2
+    if not contiguous and t.numel() > 0:
+        raise ValueError(f"the values of one row of {name} must lie side by side")
+    return t.stride(0) if shape[0] > 1 else width
+
+
+def _vector(t: torch.Tensor, n: int, name: str, dtype) -> None:
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous {dtype} of {n} values, not {t.dtype} {tuple(t.shape)}")
+
+
+def _page_size(cache: torch.Tensor, D: int) -> int:
+    if cache.dtype != torch.uint8 or cache.dim() != 3 or not cache.is_contiguous() or cache.shape[2] % (D + 16) != 0:
+        raise ValueError(f"cache must be contiguous uint8 [pages, kv heads, page_size * {D + 16}], not {cache.dtype} {tuple(cache.shape)}")
+    return cache.shape[2] // (D + 16)
+
+
+def basq_add_rms_norm(X: torch.Tensor, residual: Optional[torch.Tensor], weight: torch.Tensor, eps: float,
+                      Y: Optional[torch.Tensor], res_out: Optional[torch.Tensor] = None, *, Y8: Optional[torch.Tensor] = None,
+                      y8_scale: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """X, residual, res_out, Y bf16 [M, K] (any row strides); weight bf16 [K]; Y8 float8_e4m3fn [M, K] with y8_scale fp32 [M].
+    res_out = X + residual, Y = its norm; res_out and Y may be X or residual."""
+    M, K = shape = X.shape
+    _vector(weight, K, "weight", torch.bfloat16)
+    if Y8 is not None and y8_scale is not None:
+        _vector(y8_scale, M, "y8_scale", torch.float32)
+    _check(load().basq_add_rms_norm(
+        _p(X), _p(residual), _p(weight), M, K, _rows(X, shape, "X"), 0 if residual is None else _rows(residual, shape, "residual"),
+        eps, _p(res_out), 0 if res_out is None else _rows(res_out, shape, "res_out"), _p(Y), 0 if Y is None else _rows(Y, shape, "Y"),
+        _p(Y8), 0 if Y8 is None else _rows(Y8, shape, "Y8", torch.float8_e4m3fn), _p(y8_scale), _stream(stream)))
+
+
+def basq_rope_table(cos_sin: torch.Tensor, base: float, *, scaling: int = ROPE_PLAIN, factor: float = 1.0, low: float = 1.0,
+                    high: float = 32.0, original_len: float = 8192.0, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """cos_sin fp32 [positions, rot_dim], filled with cosines, then sines, of every position."""
+    positions, rot_dim = cos_sin.shape
+    _vector(cos_sin, positions * rot_dim, "cos_sin", torch.float32)
+    _check(load().basq_rope_table(rot_dim, positions, base, scaling, factor, low, high, original_len, _p(cos_sin), _stream(stream)))
+
+
+def basq_kv_page_bytes(kv_heads: int, head_dim: int, page_size: int) -> int:
+    return int(load().basq_kv_page_bytes(kv_heads, head_dim, page_size))
+
+
+def basq_rope_append(q: Optional[torch.Tensor], k: Optional[torch.Tensor], v: Optional[torch.Tensor],
+                     positions: Optional[torch.Tensor], cos_sin: Optional[torch.Tensor], slots: Optional[torch.Tensor],
+                     cache: Optional[torch.Tensor], clip_lo: float, clip_hi: float, q_out: Optional[torch.Tensor],
+                     k_hat: Optional[torch.Tensor] = None, v_hat: Optional[torch.Tensor] = None, *, interleaved: bool = False,
+                     rotate: bool = True, bits: int = 4, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """q, q_out bf16 [T, heads, D]; k, v, k_hat, v_hat bf16 [T, kv_heads, D] (any token strides, k_hat's and v_hat's the same);
+    positions, slots int32 [T]; cos_sin fp32 [rows, rot_dim]; cache uint8 [pages, kv_heads, page_size * (D + 16)]
+    (alloc_kv_cache).  q alone: k, v, slots and cache None; keys and values alone: q and q_out None."""
+    some = q if q is not None else k
+    if some is None or (k is None) != (v is None):
+        raise ValueError("q, or k and v, must be given")
+    T, _, D = some.shape
+    heads = ldq = ldqo = 0
+    if q is not None:
+        heads, ldq = q.shape[1], _rows(q, q.shape, "q")
+        if q_out is None:
+            raise ValueError("q_out must be given with q")
+        ldqo = _rows(q_out, q.shape, "q_out")
+    kv_heads = ldk = ldv = ldh = pages = page_size = 0
+    if k is not None:
+        shape = (T, k.shape[1], D)
+        kv_heads, ldk, ldv = k.shape[1], _rows(k, shape, "k"), _rows(v, shape, "v")
+        if cache is not None:
+            pages, page_size = cache.shape[0], _page_size(cache, D)
+            if cache.shape[1] != kv_heads:
+                raise ValueError(f"the cache has {cache.shape[1]} kv heads, k has {kv_heads}")
+            if slots is None:
+                raise ValueError("slots must be given with cache")
+            _vector(slots, T, "slots", torch.int32)
+        if k_hat is not None:
+            ldh = _rows(k_hat, shape, "k_hat")
+        if v_hat is not None:
+            ldv_hat = _rows(v_hat, shape, "v_hat")
+            if k_hat is not None and ldv_hat != ldh:
+                raise ValueError("k_hat and v_hat must have the same token stride")
+            ldh = ldv_hat
+    table_rows = rot_dim = 0
+    if cos_sin is not None:
+        table_rows, rot_dim = cos_sin.shape
+        _vector(cos_sin, table_rows * rot_dim, "cos_sin", torch.float32)
+        if positions is None:
+            raise ValueError("positions must be given with cos_sin")
+        _vector(positions, T, "positions", torch.int32)
+    _check(load().basq_rope_append(_p(q), ldq, _p(k), ldk, _p(v), ldv, T, heads, kv_heads, D, _p(positions), _p(cos_sin), table_rows,
+                                   rot_dim, interleaved, rotate, clip_lo, clip_hi, bits, _p(slots), _p(cache), pages, page_size,
+                                   _p(q_out), ldqo, _p(k_hat), _p(v_hat), ldh, _stream(stream)))
+
+
+def basq_paged_attention_workspace_bytes(B: int, q_len: int, heads: int, kv_heads: int, head_dim: int, max_len: int,
+                                         window: int = 0) -> int:
+    return int(load().basq_paged_attention_workspace_bytes(B, q_len, heads, kv_heads, head_dim, max_len, window))
+
+
+def basq_paged_attention(q: torch.Tensor, cache: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, max_len: int,
+                         scale: float, out: torch.Tensor, workspace: Optional[torch.Tensor], *, q_len: int = 1,
+                         softcap: float = 0.0, window: int = 0, lse: Optional[torch.Tensor] = None, bits: int = 4,
+                         stream: Optional[torch.cuda.Stream] = None) -> None:
+    """q, out bf16 [B * q_len, heads, D] (any token strides); cache uint8 [pages, kv_heads, page_size * (D + 16)]; page_table
+    int32 [B, pages of a sequence] (any row stride); lengths int32 [B]; lse fp32 [B * q_len, heads] or None."""
+    rows, heads, D = q.shape
+    B = lengths.shape[0]
+    if rows != B * q_len:
+        raise ValueError(f"q has {rows} rows, {B} sequences of {q_len} new tokens need {B * q_len}")
+    if page_table.dtype != torch.int32 or page_table.dim() != 2 or page_table.shape[0] != B or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+        raise ValueError(f"page_table must be int32 [{B}, pages of a sequence], not {page_table.dtype} {tuple(page_table.shape)}")
+    _vector(lengths, B, "lengths", torch.int32)
+    if lse is not None:
+        _vector(lse, rows * heads, "lse", torch.float32)
+    page_size = _page_size(cache, D)
+    if max_len > page_table.shape[1] * page_size:
+        raise ValueError(f"max_len = {max_len} is more than the {page_table.shape[1]} pages of {page_size} tokens of a sequence hold")
+    _check(load().basq_paged_attention(
+        _p(q), _rows(q, q.shape, "q"), B, q_len, heads, cache.shape[1], D, bits, _p(cache), cache.shape[0], page_size, _p(page_table),
+        page_table.stride(0) if B > 1 else page_table.shape[1], _p(lengths), max_len, scale, softcap, window, _p(out),
+        _rows(out, q.shape, "out"), _p(lse), _p(workspace), 0 if workspace is None else workspace.nbytes, _stream(stream)))
+
+
 def basq_diag_stream(src: torch.Tensor, dst: torch.Tensor, meta: torch.Tensor, tokens: int, K: int, *,
                      stream: Optional[torch.cuda.Stream] = None) -> None:
     _check(load().basq_diag_stream(_p(src), _p(dst), _p(meta), tokens, K, _stream(stream)))
@@ -433,6 +584,13 @@ def alloc_activation_buffers(M: int, K: int, device="cuda") -> Tuple[torch.Tenso
 def alloc_fp6_buffer(rows: int, K: int, device="cuda") -> torch.Tensor:
     """out6 uint8 [basq_fp6_bytes(rows, K)] for basq_pack_fp6 / the Aq6 output of basq_rotate_quant."""
     return torch.empty(basq_fp6_bytes(rows, K), dtype=torch.uint8, device=device)
+
+
+def alloc_kv_cache(num_pages: int, kv_heads: int, head_dim: int, page_size: int, device="cuda") -> torch.Tensor:
+    """cache uint8 [num_pages, kv_heads, page_size * (head_dim + 16)] for basq_rope_append / basq_paged_attention."""
+    if basq_kv_page_bytes(kv_heads, head_dim, page_size) == 0:
+        raise ValueError(f"unsupported cache shape: {kv_heads} heads of {head_dim} channels, pages of {page_size}")
+    return torch.empty((num_pages, kv_heads, page_size * (head_dim + 16)), dtype=torch.uint8, device=device)
 
 
 def alloc_weight_buffers(N: int, K: int, device="cuda"):

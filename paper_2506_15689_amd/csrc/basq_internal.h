@@ -117,6 +117,71 @@ int launch_fused_bias(const uint8_t* Wq, int32_t N, int32_t K, const uint16_t* w
 int launch_f32_to_bf16(const float* in, uint16_t* out, int64_t count, hipStream_t s);
 int launch_column_mean(const float* r, int64_t M, int32_t K, const float* act_scale, float* out, hipStream_t s);
 
+// ---- the operators around the linear layer (api_block.hip) ------------------------------------
+struct RmsNormArgs {
+    const uint16_t* X;        // bf16 bits
+    const uint16_t* residual; // optional
+    const uint16_t* weight;
+    uint16_t* res_out;        // optional
+    uint16_t* Y;              // optional
+    uint8_t* Y8;              // optional, e4m3
+    float* y8_scale;          // with Y8
+    int64_t M;
+    int32_t K;
+    int64_t ldx, ldr, ldro, ldy, ldy8;
+    float eps;
+};
+int launch_add_rms_norm(const RmsNormArgs& a, hipStream_t s);     // rms_norm.hip
+
+struct RopeAppendArgs {
+    const uint16_t *q, *k, *v;                                    // [T, heads, D], [T, kv_heads, D] twice; bf16 bits
+    int64_t T, ldq, ldk, ldv;
+    int32_t heads, kv_heads, D;
+    const int32_t* positions; // [T]; with cos_sin
+    const float* cos_sin;     // optional, [table_rows, rot]: cosines, then sines
+    int64_t table_rows;
+    int32_t rot, interleaved, rotate;
+    float norm;               // 1/sqrt(D)
+    const int32_t* slots;     // [T], optional
+    uint8_t* cache;
+    int32_t num_pages, page_log2;
+    float clip_lo, clip_hi;
+    uint16_t* q_out;
+    int64_t ldqo;
+    uint16_t *k_hat, *v_hat;  // optional
+    int64_t ldh;
+};
+int launch_rope_append(const RopeAppendArgs& a, hipStream_t s);   // rope_append.hip
+struct RopeScaling {
+    int32_t kind;             // BASQ_ROPE_*
+    double base, factor, low, high, original_len;
+};
+int launch_rope_table(float* out, int64_t rows, int32_t rot, const RopeScaling& k, hipStream_t s);
+
+struct PagedAttentionArgs {
+    const uint16_t* q;        // [B * q_len, heads, D], bf16 bits
+    int64_t ldq;
+    int32_t B, q_len, heads, kv_heads, D;
+    const uint8_t* cache;
+    int32_t num_pages, page_log2;
+    const int32_t* page_table;                                    // [B, table_stride]
+    int64_t table_stride;
+    const int32_t* lengths;   // [B]
+    int32_t max_len;
+    float scale, softcap;
+    int32_t window;
+    uint16_t* out;            // [B * q_len, heads, D]
+    int64_t ldo;
+    float* lse;               // optional, [B * q_len, heads]
+    int32_t splits, chunk;    // parts of a context, tokens of a part (paged_attention_split)
+    float* part_o;            // [B * q_len, heads, splits, D] where there are several
+    float2* part_ml;          // [B * q_len, heads, splits]: reference and sum
+    float inv_cap, cap_log2e; // set by the launcher
+};
+void paged_attention_split(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t max_len, int32_t window,
+                           int32_t* splits, int32_t* chunk);
+int launch_paged_attention(PagedAttentionArgs a, hipStream_t s);  // paged_attention.hip
+
 // 28 x 28 Paley type-I matrix, row-major, built on the host at first use (hadamard28.hip).
 const int8_t* hadamard28_host();
 

@@ -1,0 +1,145 @@
+// Root-mean-square norm with the residual's addition (the step in front of every W4A4 linear layer of a transformer block):
+//
+//     h = bf16(x + residual),   y = (h * rstd) * w,   rstd = 1 / sqrt(mean_k h_k^2 + eps)
+//
+// with y in bf16 and / or in e4m3 with one scale per token, s = max_k |y_k| / 448.  h is rounded before the norm, so that the norm
+// is that of the stored stream; sums, rstd and y are fp32.
+//
+// Bound by memory: 8 bytes a channel with everything in bf16 and about ten vector instructions.  A token stays in registers from
+// its only read to its only write: a workgroup (or, up to 2048 channels, one wavefront, without a barrier) holds it in 16-byte
+// pieces, thread t those of number t, t + THREADS, ...
+#include "basq_internal.h"
+
+namespace basq {
+
+namespace {
+
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+typedef float v2f __attribute__((ext_vector_type(2)));
+
+// two fp32 -> two bf16 in one register, round-half-to-even
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f){a, b}, v2bf));
+}
+__device__ __forceinline__ float low_f32(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high_f32(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+template <int THREADS, class Op>
+__device__ __forceinline__ float across(float v, float* scratch, Op op) {
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) v = op(v, __shfl_xor(v, off, 64));
+    if constexpr (THREADS > 64) {
+        if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = scratch[0];
+#pragma unroll
+        for (int w = 1; w < THREADS / 64; ++w) v = op(v, scratch[w]);
+    }
+    return v;
+}
+
+template <int THREADS, int PIECES, bool RES>
+__global__ __launch_bounds__(THREADS) void add_rms_norm_kernel(RmsNormArgs a) {
+    __shared__ float scratch[2][THREADS / 64];
+    const int64_t m = blockIdx.x;
+    const int tid = threadIdx.x, pieces = a.K / 8;
+    const uint4* x = reinterpret_cast<const uint4*>(a.X + m * a.ldx);
+    const uint4* r = reinterpret_cast<const uint4*>(RES ? a.residual + m * a.ldr : nullptr);
+    const uint4* w = reinterpret_cast<const uint4*>(a.weight);
+    uint4 h[PIECES], g[PIECES];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const int p = tid + i * THREADS;
+        h[i] = make_uint4(0, 0, 0, 0);
+        g[i] = make_uint4(0, 0, 0, 0);
+        if (p < pieces) {
+            h[i] = x[p];
+            if (RES) g[i] = r[p];
+        }
+    }
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        uint32_t* hw = reinterpret_cast<uint32_t*>(&h[i]);
+        const uint32_t* gw = reinterpret_cast<const uint32_t*>(&g[i]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (RES) hw[j] = pack_bf16(low_f32(hw[j]) + low_f32(gw[j]), high_f32(hw[j]) + high_f32(gw[j]));
+            sum = fmaf(low_f32(hw[j]), low_f32(hw[j]), sum);
+            sum = fmaf(high_f32(hw[j]), high_f32(hw[j]), sum);
+        }
+        const int p = tid + i * THREADS;
+        if (a.res_out && p < pieces) reinterpret_cast<uint4*>(a.res_out + m * a.ldro)[p] = h[i];
+    }
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const int p = tid + i * THREADS;
+        g[i] = make_uint4(0, 0, 0, 0);
+        if (p < pieces) g[i] = w[p];
+    }
+    sum = across<THREADS>(sum, scratch[0], [](float u, float v) { return u + v; });
+    const float rstd = rsqrtf(sum / (float)a.K + a.eps);
+
+    float top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const int p = tid + i * THREADS;
+        const uint32_t* hw = reinterpret_cast<const uint32_t*>(&h[i]);
+        const uint32_t* gw = reinterpret_cast<const uint32_t*>(&g[i]);
+        uint4 out;
+        uint32_t* ow = reinterpret_cast<uint32_t*>(&out);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float u = low_f32(hw[j]) * rstd * low_f32(gw[j]), v = high_f32(hw[j]) * rstd * high_f32(gw[j]);
+            ow[j] = pack_bf16(u, v);
+            top = fmaxf(top, fmaxf(fabsf(u), fabsf(v)));
+        }
+        if (a.Y && p < pieces) reinterpret_cast<uint4*>(a.Y + m * a.ldy)[p] = out;
+    }
+    if (!a.Y8) return;
+    top = across<THREADS>(top, scratch[1], [](float u, float v) { return fmaxf(u, v); });
+    float scale = __fdiv_rn(top, 448.0f);
+    if (!(scale > 0.0f && scale < INFINITY)) scale = 1.0f;
+    const float inv = __fdiv_rn(1.0f, scale);
+    if (tid == 0) a.y8_scale[m] = scale;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const int p = tid + i * THREADS;
+        if (p >= pieces) break;
+        const uint32_t* hw = reinterpret_cast<const uint32_t*>(&h[i]);
+        const uint32_t* gw = reinterpret_cast<const uint32_t*>(&g[i]);
+        uint32_t c[2];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            // (a product may be one rounding over the largest number; NaN stays NaN)
+            float u = low_f32(hw[j]) * rstd * low_f32(gw[j]) * inv, v = high_f32(hw[j]) * rstd * high_f32(gw[j]) * inv;
+            if (fabsf(u) > 448.0f) u = copysignf(448.0f, u);
+            if (fabsf(v) > 448.0f) v = copysignf(448.0f, v);
+            c[j / 2] = j % 2 ? __builtin_amdgcn_cvt_pk_fp8_f32(u, v, c[j / 2], true) : __builtin_amdgcn_cvt_pk_fp8_f32(u, v, 0, false);
+        }
+        reinterpret_cast<uint2*>(a.Y8 + m * a.ldy8)[p] = make_uint2(c[0], c[1]);
+    }
+}
+
+template <int THREADS, int PIECES>
+void launch(const RmsNormArgs& a, hipStream_t s) {
+    if (a.residual) hipLaunchKernelGGL((add_rms_norm_kernel<THREADS, PIECES, true>), dim3((unsigned)a.M), dim3(THREADS), 0, s, a);
+    else hipLaunchKernelGGL((add_rms_norm_kernel<THREADS, PIECES, false>), dim3((unsigned)a.M), dim3(THREADS), 0, s, a);
+}
+
+}  // namespace
+
+int launch_add_rms_norm(const RmsNormArgs& a, hipStream_t s) {
+    if (a.M == 0) return BASQ_OK;
+    const int pieces = a.K / 8;
+    if (pieces <= 64) launch<64, 1>(a, s);
+    else if (pieces <= 128) launch<64, 2>(a, s);
+    else if (pieces <= 256) launch<64, 4>(a, s);
+    else if (pieces <= 512) launch<256, 2>(a, s);
+    else if (pieces <= 1024) launch<256, 4>(a, s);
+    else if (pieces <= 2048) launch<256, 8>(a, s);
+    else launch<512, 8>(a, s);
+    return check_hip(hipGetLastError(), "add_rms_norm launch");
+}
+
+}  // namespace basq
