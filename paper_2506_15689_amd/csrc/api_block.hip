@@ -35,8 +35,13 @@ int check_cache(const void* cache, int32_t num_pages, int32_t page_size, int32_t
     return BASQ_OK;
 }
 
-size_t split_bytes(int64_t rows, int32_t head_dim, int32_t splits) {
-    return splits > 1 ? (size_t)rows * (size_t)splits * (4u * (size_t)head_dim + 8u) : 0;
+int64_t attention_segments(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads) {
+    return (int64_t)B * kv_heads * (((int64_t)(heads / kv_heads) * q_len + 15) / 16);
+}
+
+// parts of 16 rows of D sums with their reference and sum, and a segment's place (PagedAttentionArgs)
+size_t parts_bytes(int32_t workers, int32_t head_dim, int64_t segments) {
+    return workers > 0 ? 2 * (size_t)workers * 16 * (4 * (size_t)head_dim + 8) + 8 * (size_t)segments : 0;
 }
 
 }  // namespace
@@ -148,9 +153,8 @@ int basq_rope_append(const void* q, int64_t ldq, const void* k, int64_t ldk, con
 size_t basq_paged_attention_workspace_bytes(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t head_dim,
                                             int32_t max_len, int32_t window) {
     if (B < 1 || q_len < 1 || heads < 1 || kv_heads < 1 || heads % kv_heads != 0 || (head_dim != 64 && head_dim != 128) || max_len < 0) return 0;
-    int32_t splits, chunk;
-    paged_attention_split(B, q_len, heads, kv_heads, max_len, window, &splits, &chunk);
-    return split_bytes((int64_t)B * q_len * heads, head_dim, splits);
+    const int workers = paged_attention_workers(B, q_len, heads, kv_heads, head_dim, max_len, window);
+    return workers < 0 ? 0 : parts_bytes(workers, head_dim, attention_segments(B, q_len, heads, kv_heads));
 }
 
 int basq_paged_attention(const void* q, int64_t ldq, int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t head_dim,
@@ -177,9 +181,9 @@ int basq_paged_attention(const void* q, int64_t ldq, int32_t B, int32_t q_len, i
     if (rc != BASQ_OK) return rc;
     if ((max_len > 0 && !page_table) || !lengths || !aligned(page_table, 4) || !aligned(lengths, 4) || !aligned(lse, 4))
         return fail(BASQ_EINVAL, "page_table and lengths must be given; they and lse must be 4-byte aligned");
-    paged_attention_split(B, q_len, heads, kv_heads, max_len, window, &a.splits, &a.chunk);
-    const int64_t rows = (int64_t)B * q_len * heads;
-    const size_t need = split_bytes(rows, head_dim, a.splits);
+    a.workers = paged_attention_workers(B, q_len, heads, kv_heads, head_dim, max_len, window);
+    if (a.workers < 0) return fail(BASQ_EUNSUPPORTED, "2^31 or more parts of 128 tokens, or rows of a head");
+    const size_t need = parts_bytes(a.workers, head_dim, attention_segments(B, q_len, heads, kv_heads));
     if (need > 0) {
         if (!workspace || !aligned(workspace, 256)) return fail(BASQ_EINVAL, "workspace is null or not 256-byte aligned");
         if (workspace_bytes < need) return fail(BASQ_EWORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes, need);
@@ -191,7 +195,8 @@ int basq_paged_attention(const void* q, int64_t ldq, int32_t B, int32_t q_len, i
     a.scale = scale; a.softcap = softcap; a.window = window;
     a.out = static_cast<uint16_t*>(out); a.ldo = ldo; a.lse = lse;
     a.part_o = static_cast<float*>(workspace);
-    a.part_ml = reinterpret_cast<float2*>(a.part_o + (size_t)rows * a.splits * head_dim);
+    a.part_ml = reinterpret_cast<float2*>(a.part_o + 2 * (size_t)a.workers * 16 * head_dim);
+    a.part_of = reinterpret_cast<int2*>(a.part_ml + 2 * (size_t)a.workers * 16);
     return launch_paged_attention(a, static_cast<hipStream_t>(stream));
 }
 

@@ -173,13 +173,13 @@ struct PagedAttentionArgs {
     uint16_t* out;            // [B * q_len, heads, D]
     int64_t ldo;
     float* lse;               // optional, [B * q_len, heads]
-    int32_t splits, chunk;    // parts of a context, tokens of a part (paged_attention_split)
-    float* part_o;            // [B * q_len, heads, splits, D] where there are several
-    float2* part_ml;          // [B * q_len, heads, splits]: reference and sum
+    int32_t workers;          // workgroups that share the work (paged_attention_workers), 0: one to a segment
+    float* part_o;            // [2 * workers, 16, D]: a workgroup's last part of a segment begun before, and its part of one that goes on
+    float2* part_ml;          // [2 * workers, 16]: reference and sum
+    int2* part_of;            // [segments]: the workgroup in which a segment begins, and its number of parts
     float inv_cap, cap_log2e; // set by the launcher
 };
-void paged_attention_split(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t max_len, int32_t window,
-                           int32_t* splits, int32_t* chunk);
+int paged_attention_workers(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t max_len, int32_t window);
 int launch_paged_attention(PagedAttentionArgs a, hipStream_t s);  // paged_attention.hip
 
 // 28 x 28 Paley type-I matrix, row-major, built on the host at first use (hadamard28.hip).

@@ -14,11 +14,13 @@
 // no value changes lanes between the two products, and M, l and the rescaling are per lane.  The step's loads (codes and ranges) are
 // requested while the step before is worked on.
 //
-// A code's bit pattern, taken for an fp16 number, is the code times 2^-24 (and the code in the next nibble, left in place, 16 times
-// that): exact, two codes to an instruction, and no conversion.  Query rows are brought to fp16 times a power of two of their own
-// (a bf16 value fits it exactly while it is within 2^-30 of the row's largest); weights p_t vs_t are rounded to fp16 (2^-12
-// relative, against 2^-9 of the bf16 output) near 2^5 of their running maximum, far from either end of fp16.  l, M and both sums are
-// fp32.
+// Codes become fp16 numbers without a conversion, two to an instruction.  The values' as they lie: a bit pattern of 0 .. 15, taken for
+// an fp16 number, is the code times 2^-24, and the code in the next nibble, left in place, 16 times that.  The matrix cores drop low
+// bits of products with such subnormal operands (2^-21 of the sum of magnitudes, 200 times what they do with others; measured), which
+// is nothing to a bf16 output but shows in lse; so the keys' codes are put into the mantissa of 1024, and 8 more than that subtracted.
+// Query rows are brought to fp16 times a power of two of their own (a bf16 value fits it exactly while it is within 2^-30 of the
+// row's largest); weights p_t vs_t are rounded to fp16 (2^-12 relative, against 2^-9 of the bf16 output) near 2^5 of their running
+// maximum, far from either end of fp16.  l, M and both sums are fp32.
 #include "basq_internal.h"
 
 #include <type_traits>
@@ -30,17 +32,21 @@ namespace {
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+typedef int v4i __attribute__((ext_vector_type(4)));
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef float v2f __attribute__((ext_vector_type(2)));
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 
 constexpr int PA_WAVES = 4, PA_STEP = 32;                        // tokens of a wave's step
-constexpr float UNSET = -1e30f;                                  // M before the first token that counts
+constexpr int PA_UNIT = PA_WAVES * PA_STEP;
+constexpr int PA_STAGES = 2;                                      // steps of a wave in LDS
+constexpr float UNSET = -1e30f;                                  // M of a row that has seen no token
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
-// eight codes (one dword, low nibble first) as fp16: codes 0, 4, 2, 6 times 2^-24 and 1, 5, 3, 7 times 2^-20, in the order
-// 0 4 | 1 5 | 2 6 | 3 7
+// eight codes (one dword, low nibble first) as fp16 numbers 2^-20 times the code, in the order 0 4 | 1 5 | 2 6 | 3 7
 __device__ __forceinline__ v8h spread(uint32_t x) {
-    const v4u w = {x & 0x000F000Fu, x & 0x00F000F0u, (x >> 8) & 0x000F000Fu, (x >> 8) & 0x00F000F0u};
+    constexpr uint32_t MASK = 0x00F000F0u;
+    const v4u w = {(x << 4) & MASK, x & MASK, (x >> 4) & MASK, (x >> 8) & MASK};
     return __builtin_bit_cast(v8h, w);
 }
 __device__ __forceinline__ float quarters_max(float v) {
@@ -52,46 +58,76 @@ __device__ __forceinline__ float quarters_sum(float v) {
     return v + __shfl_xor(v, 32, 64);
 }
 
-// What a step reads: for block j of 16 tokens the keys of token lane % 16 (channels D/4 * (lane / 16) ..), and for the four tokens
-// 4 * (lane / 16) .. the values of channels D/16 * (lane % 16) .. and both ranges.
+#define PA_LDS_PTR(p) ((__attribute__((address_space(3))) void*)(p))
+
+// A block of 16 tokens in LDS: its keys, its values, its ranges (4 KB would be the next power of two; blocks lie end to end).
 template <int D>
-struct Step {
-    typedef typename std::conditional<D == 128, uint4, uint2>::type Keys;
-    typedef typename std::conditional<D == 128, uint32_t, uint16_t>::type Values;
-    Keys k[2];
-    Values v[2][4];
-    float4 kr[2][2], vr[2][2];                                   // (scale, lo) of two tokens each
+struct Block {
+    static constexpr int V_AT = 8 * D, R_AT = 16 * D, BYTES = 16 * D + 256;
+    static constexpr int LOADS = D == 128 ? 3 : 2;               // direct loads that bring it
 };
 
-template <int D, bool CAP>
-__global__ __launch_bounds__(PA_WAVES * 64, 2) void paged_attention_kernel(PagedAttentionArgs a) {
+// N neighbouring channels of a row's result, from its sums at reference M: out = x / l (0 where no token counted), lse.
+template <int N>
+__device__ __forceinline__ void finish(const PagedAttentionArgs& a, int64_t token, int head, int D, int channel, const float (&x)[N], float M, float l) {
+    const float inv = l > 0.0f ? __fdiv_rn(1.0f, l) : l;         // (0 and NaN stay)
+    uint32_t y[N / 2];
+#pragma unroll
+    for (int c = 0; c < N; c += 2) y[c / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f){x[c] * inv, x[c + 1] * inv}, v2bf));
+    uint16_t* dst = a.out + token * a.ldo + head * D + channel;
+    if constexpr (N == 8) *reinterpret_cast<uint4*>(dst) = make_uint4(y[0], y[1], y[2], y[3]);
+    else *reinterpret_cast<uint2*>(dst) = make_uint2(y[0], y[1]);
+    if (a.lse && channel == 0) a.lse[token * a.heads + head] = l == 0.0f ? -INFINITY : (M + __log2f(l)) * LN2;
+}
+
+// Tokens of a sequence that new tokens j_first .. j_last of it see, in units of PA_UNIT from `begin` (a multiple of 16).
+struct Span {
+    int begin, end;
+};
+__device__ __forceinline__ Span span_of(const PagedAttentionArgs& a, int len, int j_first, int j_last) {
+    return {a.window > 0 ? max(len - (a.q_len - 1) + j_first - a.window, 0) & ~15 : 0, len - (a.q_len - 1) + j_last};
+}
+__device__ __forceinline__ int length_of(const PagedAttentionArgs& a, int b) { return min(max(a.lengths[b], 0), a.max_len); }
+// units of sequence b, the same for all its segments; at least one, whose taker also writes the zeros of rows that see nothing
+__device__ __forceinline__ int units_of(const PagedAttentionArgs& a, int b) {
+    const Span s = span_of(a, length_of(a, b), 0, a.q_len - 1);
+    return max((s.end - s.begin + PA_UNIT - 1) / PA_UNIT, 1);
+}
+
+template <int D>
+struct Shared {
+    union {
+        uint8_t ring[PA_WAVES][PA_STAGES][2][Block<D>::BYTES];
+        float o[PA_WAVES][16][D + 4];
+    };
+    float ml[PA_WAVES][2][16];
+};
+
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+// A segment, one kv head and tile of 16 query rows of sequence b: `taken` of its `units`, from number `unit` on.
+template <int D, bool CAP, bool FOLD>
+__device__ __forceinline__ void attend(const PagedAttentionArgs& a, Shared<D>& lds, int b, int segment, int unit, int taken, int units) {
     constexpr int TILES = D / 16;                                // channel tiles of the second product: channel TILES * n + c
     constexpr int KS = D / 32;                                   // 32-channel steps of the first
-    __shared__ float lds_o[PA_WAVES][16][D + 4];
-    __shared__ float lds_ml[PA_WAVES][2][16];
-
+    constexpr int MINE = FOLD ? 4 : 8;                           // tokens of a lane in a step
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quarter = lane >> 4;
     const int group = a.heads / a.kv_heads, rows = group * a.q_len, row_tiles = (rows + 15) / 16;
-    int id = blockIdx.x;
-    const int split = id % a.splits;
-    id /= a.splits;
-    const int row_tile = id % row_tiles;
-    id /= row_tiles;
-    const int kv_head = id % a.kv_heads, b = id / a.kv_heads;
-
-    const int len = min(max(a.lengths[b], 0), a.max_len);
-    // this lane's query row: new token j, head, and the tokens [begin, end) that it sees
-    const int row = row_tile * 16 + col, j = min(row, rows - 1) / group, head = kv_head * group + min(row, rows - 1) - j * group;
-    const int end = len - (a.q_len - 1) + j, begin = a.window > 0 ? max(end - a.window, 0) : 0;
-    // the tokens of all rows of the tile, in whole blocks from the first's, and this workgroup's part of them
-    const int j_first = row_tile * 16 / group, j_last = min(row_tile * 16 + 15, rows - 1) / group;
-    const int all_end = len - (a.q_len - 1) + j_last, all_begin = a.window > 0 ? max(len - (a.q_len - 1) + j_first - a.window, 0) & ~15 : 0;
-    const int from = all_begin + split * a.chunk, to = min(all_end, from + a.chunk);
-    if (split > 0 && from >= to) return;                          // (the first part of an empty row writes its zeros)
-
+    const int kv_head = __builtin_amdgcn_readfirstlane(segment / row_tiles), row_tile = segment - kv_head * row_tiles;
     const int P = 1 << a.page_log2;
     const int64_t head_bytes = (int64_t)P * (D + 16);
+    const int len = __builtin_amdgcn_readfirstlane(length_of(a, b));
+    // this lane's query row: new token j, head, and the tokens [begin, end) that it sees
+    const int row = min(row_tile * 16 + (FOLD ? col & 7 : col), rows - 1), j = row / group, head = kv_head * group + row - j * group;
+    const int end = len - (a.q_len - 1) + j, begin = a.window > 0 ? max(end - a.window, 0) : 0;
+    // the tokens of this part that any row of the tile sees
+    const int j_first = __builtin_amdgcn_readfirstlane(row_tile * 16 / group), j_last = __builtin_amdgcn_readfirstlane(min(row_tile * 16 + 15, rows - 1) / group);
+    const Span all = span_of(a, len, 0, a.q_len - 1), mine = span_of(a, len, j_first, j_last);
+    const int from = max(all.begin + unit * PA_UNIT, mine.begin), to = min(all.begin + (unit + taken) * PA_UNIT, mine.end);
     const int32_t* pages = a.page_table + (int64_t)b * a.table_stride;
 
     // query rows
@@ -120,121 +156,161 @@ __global__ __launch_bounds__(PA_WAVES * 64, 2) void paged_attention_kernel(Paged
         // the largest becomes 2^14 .. 2^15 (exponent field of top, 127 = 2^0)
         const int e = min(max(141 - (int)(__float_as_uint(top) >> 23), -100), 100);
         const float up = __uint_as_float((uint32_t)(127 + e) << 23);
-        c1 = a.scale * LOG2E * __uint_as_float((uint32_t)(127 - e) << 23) * 0x1p24f;
+        c1 = a.scale * LOG2E * __uint_as_float((uint32_t)(127 - e) << 23) * 0x1p20f;
         qs = a.scale * LOG2E * sum;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-            const float* y = x + 8 * s;
-            const float odd = up * 0.0625f;
-            q[s] = (v8h){(_Float16)(y[0] * up), (_Float16)(y[4] * up), (_Float16)(y[1] * odd), (_Float16)(y[5] * odd),
-                         (_Float16)(y[2] * up), (_Float16)(y[6] * up), (_Float16)(y[3] * odd), (_Float16)(y[7] * odd)};
+            constexpr int ORDER[8] = {0, 4, 1, 5, 2, 6, 3, 7};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[s][i] = (_Float16)(x[8 * s + ORDER[i]] * up);
         }
     }
 
     v4f o[TILES];
 #pragma unroll
     for (int c = 0; c < TILES; ++c) o[c] = (v4f){0.f, 0.f, 0.f, 0.f};
-    float M = UNSET, l = 0.0f, lows = 0.0f;                       // l and lows: this lane's tokens
+    float M = 0.0f, l = 0.0f, lows = 0.0f;                        // l and lows: this lane's tokens
+    bool set = false;                                             // M is a reference: the row has seen a token
 
-    // byte offsets of the lane's pieces inside one head of one page
-    const uint32_t k_at = col * (D / 2) + quarter * (D / 8);
-    const uint32_t v_at = P * (D / 2) + 4 * quarter * (D / 2) + col * (D / 32);
-    const uint32_t r_at = P * D + 4 * quarter * 8;
+    // What a lane requests, as byte offsets into one head of one page, and where it reads what it works on.  Row i of the first
+    // product's results is token 4 * (i % 4) + i / 4 of a block, so quarter g of the wave works on tokens g, 4 + g, 8 + g, 12 + g:
+    // for each of the four, the wave reads 256 (128) bytes of values side by side.  Keys lie in 16-byte pieces whose place
+    // inside their row changes from token to token, so that 16 lanes read from all banks; ranges lie by quarter.
+    uint32_t code_from[Block<D>::LOADS - 1];
+    if constexpr (D == 128) {
+        code_from[0] = 16 * ((lane & 60) | ((lane ^ (lane >> 4)) & 3));
+        code_from[1] = P * 64 + 16 * lane;
+    } else {
+        code_from[0] = lane < 32 ? 16 * ((lane & 30) | ((lane ^ (lane >> 4)) & 1)) : P * 32 + 16 * (lane - 32);
+    }
+    const uint32_t range_from = P * D + (lane >> 5) * 8 * P + 8 * (4 * ((lane >> 1) & 3) + ((lane >> 3) & 3)) + 4 * (lane & 1);
+    const int token = 4 * (col & 3) + (col >> 2);
+    const int k_at = D == 128 ? token * 64 + ((quarter ^ token >> 2) & 3) * 16 : token * 32 + ((quarter >> 1) ^ (token >> 3)) * 16 + (quarter & 1) * 8;
+    const int v_at = Block<D>::V_AT + quarter * (D / 2) + col * (D / 32), r_at = Block<D>::R_AT + quarter * 32 + (FOLD ? (col >> 3) * Block<D>::BYTES : 0);
+    uint8_t* const ring = &lds.ring[wave][0][0][0];
 
-    // Page ids of this wave's next 32 steps, block 2i + h of them on lane 2i + h; -1 for blocks past the end and for no page.
-    int ids = 0;
-    const int first = from + wave * PA_STEP;
-    auto fetch_ids = [&](int t0) {
-        const int t = t0 + (lane >> 1) * (PA_WAVES * PA_STEP) + (lane & 1) * 16;
+    // This wave's next 32 steps: where block 2i + h of 16 tokens begins in the cache, on lane 2i + h; and whether it is there (not
+    // past the end, of a page that exists; the others are read from the first page, and masked).
+    int64_t place = 0;
+    uint64_t there = 0;
+    constexpr int STRIDE = PA_WAVES * PA_STEP;
+    auto fetch = [&](int t0) {
+        const int t = t0 + (lane >> 1) * STRIDE + (lane & 1) * 16;
         int id = -1;
         if (t < to) id = pages[t >> a.page_log2];
-        ids = id >= 0 && id < a.num_pages ? id : -1;
+        const bool ok = id >= 0 && id < a.num_pages;
+        there = __ballot(ok);
+        place = ((int64_t)(ok ? id : 0) * a.kv_heads + kv_head) * head_bytes;
     };
-    auto load = [&](int i, int t, Step<D>& s) {                   // step i of the fetched ids, tokens t ..
+    // requests step i of the fetched ones, tokens t .., into a stage of the ring; nothing (which counts as loads) behind the last
+    auto load = [&](int i, int last, int t, int stage) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int id = max(__builtin_amdgcn_readlane(ids, 2 * i + h), 0);
-            const uint8_t* base = a.cache + ((int64_t)id * a.kv_heads + kv_head) * head_bytes;
+            const int from_lane = (2 * i + h) & 63;
+            const uint32_t low = __builtin_amdgcn_readlane((int)place, from_lane), high = __builtin_amdgcn_readlane((int)(place >> 32), from_lane);
+            const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.cache) + (int64_t)((uint64_t)high << 32 | low), 0,
+                                                                                  i <= last ? (int)head_bytes : 0, 0x00020000);
             const int at = (t + 16 * h) & (P - 1);
-            const uint8_t* codes = base + at * (D / 2);
-            s.k[h] = *reinterpret_cast<const typename Step<D>::Keys*>(codes + k_at);
+            uint8_t* dst = ring + (stage * 2 + h) * Block<D>::BYTES;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) s.v[h][r] = *reinterpret_cast<const typename Step<D>::Values*>(codes + v_at + r * (D / 2));
-            const float4* kr = reinterpret_cast<const float4*>(base + at * 8 + r_at);
-            const float4* vr = reinterpret_cast<const float4*>(base + at * 8 + r_at + 8 * P);
-            s.kr[h][0] = kr[0]; s.kr[h][1] = kr[1];
-            s.vr[h][0] = vr[0]; s.vr[h][1] = vr[1];
+            for (int n = 0; n < Block<D>::LOADS - 1; ++n)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, PA_LDS_PTR(dst + 1024 * n), 16, (int)code_from[n], at * (D / 2), 0, 2);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, PA_LDS_PTR(dst + Block<D>::R_AT), 4, (int)range_from, at * 8, 0, 2);
         }
     };
     // whether no row of the tile masks any token of the step
     const int inner_begin = a.window > 0 ? max(len - (a.q_len - 1) + j_last - a.window, 0) : 0, inner_end = len - (a.q_len - 1) + j_first;
 
-    auto work = [&](int i, int t, const Step<D>& s) {
-        float sc[8], vs[8], vl[8];
+    auto row_max = [&](float v) {
+        v = quarters_max(v);
+        return FOLD ? fmaxf(v, __shfl_xor(v, 8, 64)) : v;
+    };
+    // log2(e) cap tanh(y), y = x / (log2(e) cap): tanh(y) = 1 - 2 / (e^2y + 1), whose rounding near 0 is that of 1, and there its
+    // series, 2^-23 of the value off at most up to 1/4
+    auto capped = [&](float x) {
+        const float y = x * a.inv_cap, y2 = y * y;
+        const float far = 1.0f - 2.0f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * (2.0f * LOG2E)) + 1.0f);
+        const float near = y * fmaf(y2, fmaf(y2, fmaf(y2, fmaf(y2, 62.0f / 2835, -17.0f / 315), 2.0f / 15), -1.0f / 3), 1.0f);
+        return a.cap_log2e * (fabsf(y) < 0.25f ? near : far);
+    };
+    auto work = [&](int i, int t, int stage) {
+        const uint8_t* blocks = ring + stage * 2 * Block<D>::BYTES;
+        v4f acc[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            v4f acc = {0.f, 0.f, 0.f, 0.f};
-            const uint32_t* kw = reinterpret_cast<const uint32_t*>(&s.k[h]);
+            // (as integers, here and below: in front of a float-typed read of LDS the compiler waits for every direct load)
+            typedef int Keys __attribute__((ext_vector_type(KS)));
+            const Keys kw = *reinterpret_cast<const Keys*>(blocks + h * Block<D>::BYTES + k_at);
+            acc[h] = (v4f){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int n = 0; n < KS; ++n) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(spread(kw[n]), q[n], acc, 0, 0, 0);
-            const float* kr = reinterpret_cast<const float*>(&s.kr[h]);
-            const float* vr = reinterpret_cast<const float*>(&s.vr[h]);
+            for (int n = 0; n < KS; ++n) acc[h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(spread(kw[n]), q[n], acc[h], 0, 0, 0);
+        }
+        // folded, columns 8 .. 15 are the rows of 0 .. 7 again, for the second block
+        if constexpr (FOLD)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                float x = fmaf(kr[2 * r], acc[r] * c1, kr[2 * r + 1] * qs);
-                if (CAP) {
-                    // log2(e) cap tanh(y), y = x / (log2(e) cap): tanh(y) = 1 - 2 / (e^2y + 1), whose rounding near 0 is that of 1,
-                    // and there its series, below 2^-23 of the value off up to 1/4
-                    const float y = x * a.inv_cap, y2 = y * y;
-                    const float far = 1.0f - 2.0f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * (2.0f * LOG2E)) + 1.0f);
-                    const float near = y * fmaf(y2, fmaf(y2, fmaf(y2, fmaf(y2, 62.0f / 2835, -17.0f / 315), 2.0f / 15), -1.0f / 3), 1.0f);
-                    x = a.cap_log2e * (fabsf(y) < 0.25f ? near : far);
+            for (int r = 0; r < 4; ++r) acc[0][r] = col & 8 ? acc[1][r] : acc[0][r];
+        float sc[MINE], vs[MINE], vl[MINE];
+        float least = INFINITY;                                   // scale of a value
+#pragma unroll
+        for (int h = 0; h < MINE / 4; ++h) {
+            const uint8_t* ranges = blocks + h * Block<D>::BYTES + r_at;
+#pragma unroll
+            for (int r = 0; r < 4; r += 2) {                       // (scale, lo) of two tokens each
+                const v4f kr = __builtin_bit_cast(v4f, *reinterpret_cast<const v4i*>(ranges + 8 * r));
+                const v4f vr = __builtin_bit_cast(v4f, *reinterpret_cast<const v4i*>(ranges + 128 + 8 * r));
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    // less M; with a cap, M goes off behind it
+                    const float x = fmaf(kr[2 * n], acc[h][r + n] * c1, CAP ? kr[2 * n + 1] * qs : fmaf(kr[2 * n + 1], qs, -M));
+                    sc[4 * h + r + n] = CAP ? capped(x) - M : x;
+                    vs[4 * h + r + n] = vr[2 * n];
+                    vl[4 * h + r + n] = vr[2 * n + 1];
+                    least = fminf(least, vr[2 * n]);
                 }
-                sc[4 * h + r] = x;
-                vs[4 * h + r] = vr[2 * r];
-                vl[4 * h + r] = vr[2 * r + 1];
             }
         }
-        const int id0 = __builtin_amdgcn_readlane(ids, 2 * i), id1 = __builtin_amdgcn_readlane(ids, 2 * i + 1);
-        if ((id0 | id1) < 0 || t < inner_begin || t + PA_STEP > inner_end) {
+        const unsigned both = (unsigned)(there >> (2 * i)) & 3u;
+        if (both != 3u || t < inner_begin || t + PA_STEP > inner_end) {
+            asm volatile("");                                     // (a branch: few steps come here)
             // what is masked may hold anything, also ranges that are no numbers
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int at = t + 16 * h + 4 * quarter + r;
-                    const bool seen = at >= begin && at < end && (h ? id1 : id0) >= 0;
-                    sc[4 * h + r] = seen ? sc[4 * h + r] : -INFINITY;
-                    vs[4 * h + r] = seen ? vs[4 * h + r] : 0.0f;
-                    vl[4 * h + r] = seen ? vl[4 * h + r] : 0.0f;
-                }
-        }
-        float p[8], w[8], top = 0.0f;
-        auto weigh = [&]() {
-            top = 0.0f;
-#pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                p[r] = __builtin_amdgcn_exp2f(sc[r] - M);
-                w[r] = p[r] * vs[r];
+            for (int n = 0; n < MINE; ++n) {
+                const int h = FOLD ? col >> 3 : n / 4, at = t + 16 * h + 4 * (n % 4) + quarter;
+                const bool seen = at >= begin && at < end && (both >> h & 1u);
+                sc[n] = seen ? sc[n] : -INFINITY;
+                vs[n] = seen ? vs[n] : 0.0f;
+                vl[n] = seen ? vl[n] : 0.0f;
             }
-            // (a token whose scale is 0 has no w: its p counts once it nears the end of fp32)
+        }
+        float p[MINE], w[MINE];
+        auto weigh = [&]() {
+            float top = 0.0f;
 #pragma unroll
-            for (int r = 0; r < 8; ++r) top = fmaxf(top, fabsf(w[r]));
-            float most = p[0];
-#pragma unroll
-            for (int r = 1; r < 8; ++r) most = fmaxf(most, p[r]);
-            top = fmaxf(top, most * 0x1p-60f);
+            for (int r = 0; r < MINE; ++r) {
+                p[r] = __builtin_amdgcn_exp2f(sc[r]);
+                w[r] = p[r] * vs[r];
+                top = fmaxf(top, w[r]);
+            }
+            return top;
         };
-        weigh();
-        // A row whose weights leave fp16's range (its first token does) gets a new reference: its largest weight becomes 2^5.
-        if (__any(top > 0x1p15f)) {
+        float top = weigh();
+        // A row's first tokens, and weights that leave fp16's range, give it a new reference: its largest weight becomes 2^5.
+        // (Where a scale is next to 0, p itself counts once it nears the end of fp32.)
+        if (__any(top > 0x1p15f || !set || !(least >= 0x1p-60f))) {
+            asm volatile("");
             float best = -INFINITY;
 #pragma unroll
-            for (int r = 0; r < 8; ++r) best = fmaxf(best, sc[r] + fmaxf(__builtin_amdgcn_logf(vs[r]), -60.0f));
-            const bool mine = quarters_max(top) > 0x1p15f;
-            const float next = mine ? quarters_max(best) - 5.0f : M;
-            const float f = __builtin_amdgcn_exp2f(M - next);
-            M = next;
+            for (int r = 0; r < MINE; ++r) {
+                best = fmaxf(best, sc[r] + fmaxf(__builtin_amdgcn_logf(vs[r]), -60.0f));
+                top = fmaxf(top, fmaxf(fabsf(w[r]), p[r] * 0x1p-60f));
+            }
+            best = row_max(best);
+            const float up = (row_max(top) > 0x1p15f || !set) && best > -INFINITY ? best - 5.0f : 0.0f;
+            set = set || best > -INFINITY;
+            const float f = __builtin_amdgcn_exp2f(-up);
+            M += up;
+#pragma unroll
+            for (int r = 0; r < MINE; ++r) sc[r] -= up;
             l *= f;
             lows *= f;
 #pragma unroll
@@ -242,20 +318,37 @@ __global__ __launch_bounds__(PA_WAVES * 64, 2) void paged_attention_kernel(Paged
             weigh();
         }
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
+        for (int r = 0; r < MINE; ++r) {
             l += p[r];
             lows = fmaf(p[r], vl[r], lows);
         }
-        const v8h pw = {(_Float16)w[0], (_Float16)w[1], (_Float16)w[2], (_Float16)w[3], (_Float16)w[4], (_Float16)w[5], (_Float16)w[6], (_Float16)w[7]};
+        v8h pw;
+        if constexpr (FOLD) {
+            // the second block's weights from eight lanes further on (in columns 8 .. 15, whose results nobody reads, the first's)
+            v4u both_w;
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                both_w[n] = __builtin_bit_cast(uint32_t, (v2h){(_Float16)w[2 * n], (_Float16)w[2 * n + 1]});
+                both_w[2 + n] = (uint32_t)__builtin_amdgcn_mov_dpp((int)both_w[n], 0x128, 0xF, 0xF, true);
+            }
+            pw = __builtin_bit_cast(v8h, both_w);
+        } else {
+#pragma unroll
+            for (int n = 0; n < 8; ++n) pw[n] = (_Float16)w[n];
+        }
         // channels x tokens of the values: pairs of tokens side by side, then a code of both per instruction
+        uint32_t v[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            const uint8_t* from = blocks + (r / 4) * Block<D>::BYTES + v_at + (r % 4) * (2 * D);
+            v[r] = D == 128 ? (uint32_t)*reinterpret_cast<const int*>(from) : *reinterpret_cast<const uint16_t*>(from);
+        }
         constexpr int HALVES = D == 128 ? 2 : 1;
 #pragma unroll
         for (int half = 0; half < HALVES; ++half) {
             uint32_t x[4];
 #pragma unroll
-            for (int i2 = 0; i2 < 4; ++i2)
-                x[i2] = __builtin_amdgcn_perm((uint32_t)s.v[i2 / 2][2 * (i2 % 2) + 1], (uint32_t)s.v[i2 / 2][2 * (i2 % 2)],
-                                              half ? 0x07060302u : 0x05040100u);
+            for (int r = 0; r < 4; ++r) x[r] = __builtin_amdgcn_perm(v[2 * r + 1], v[2 * r], half ? 0x07060302u : 0x05040100u);
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 const uint32_t mask = c & 1 ? 0x00F000F0u : 0x000F000Fu;
@@ -266,141 +359,214 @@ __global__ __launch_bounds__(PA_WAVES * 64, 2) void paged_attention_kernel(Paged
         }
     };
 
-    constexpr int STRIDE = PA_WAVES * PA_STEP;
-    for (int t0 = first; t0 < to; t0 += 32 * STRIDE) {
-        fetch_ids(t0);
-        const int steps = min(32, (to - t0 + STRIDE - 1) / STRIDE);
-        Step<D> s[2];
-        load(0, t0, s[0]);
-        for (int i = 0; i < steps; i += 2) {
-            if (i + 1 < steps) load(i + 1, t0 + (i + 1) * STRIDE, s[1]);
-            work(i, t0 + i * STRIDE, s[0]);
-            if (i + 1 >= steps) break;
-            if (i + 2 < steps) load(i + 2, t0 + (i + 2) * STRIDE, s[0]);
-            work(i + 1, t0 + (i + 1) * STRIDE, s[1]);
+    // PA_STAGES - 1 steps are under way while one is worked on.
+    for (int t0 = from + wave * PA_STEP; t0 < to; t0 += 32 * STRIDE) {
+        fetch(t0);
+        const int last = min(32, (to - t0 + STRIDE - 1) / STRIDE) - 1;
+#pragma unroll
+        for (int i = 0; i < PA_STAGES - 1; ++i) load(i, last, t0 + i * STRIDE, i);
+        int stage = 0;
+        for (int i = 0; i <= last; ++i) {
+            load(i + PA_STAGES - 1, last, t0 + (i + PA_STAGES - 1) * STRIDE, stage == 0 ? PA_STAGES - 1 : stage - 1);
+            wait_loads<(PA_STAGES - 1) * 2 * Block<D>::LOADS>();
+            work(i, t0 + i * STRIDE, stage);
+            asm volatile("" ::: "memory");                        // (the stage is read before it is requested anew)
+            stage = stage == PA_STAGES - 1 ? 0 : stage + 1;
         }
+        wait_loads<0>();
     }
 
     // join the four waves: sums brought to the largest reference
+    if (!set) M = UNSET;
     l = quarters_sum(l);
     lows = quarters_sum(lows);
+    if constexpr (FOLD) {
+        l += __shfl_xor(l, 8, 64);
+        lows += __shfl_xor(lows, 8, 64);
+    }
     if (quarter == 0) {
-        lds_ml[wave][0][col] = M;
-        lds_ml[wave][1][col] = l;
+        lds.ml[wave][0][col] = M;
+        lds.ml[wave][1][col] = l;
     }
     __syncthreads();
     float best = UNSET;
 #pragma unroll
-    for (int w = 0; w < PA_WAVES; ++w) best = fmaxf(best, lds_ml[w][0][col]);
+    for (int w = 0; w < PA_WAVES; ++w) best = fmaxf(best, lds.ml[w][0][col]);
     const float f = __builtin_amdgcn_exp2f(M - best);
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int c = 0; c < TILES; ++c)
-            lds_o[wave][col][TILES * (4 * quarter + r) + c] = f * fmaf(o[c][r], c & 1 ? 0x1p20f : 0x1p24f, lows);
+            lds.o[wave][col][TILES * (4 * quarter + r) + c] = f * fmaf(o[c][r], c & 1 ? 0x1p20f : 0x1p24f, lows);
     __syncthreads();
     // sixteen threads to a row, D/16 neighbouring channels each
     const int out_col = threadIdx.x / 16, piece = threadIdx.x % 16, out_row = row_tile * 16 + out_col;
     if (out_row >= rows) return;
-    float x[TILES], total = 0.0f;
+    float x[TILES] = {}, total = 0.0f;
     best = UNSET;
 #pragma unroll
-    for (int w = 0; w < PA_WAVES; ++w) best = fmaxf(best, lds_ml[w][0][out_col]);
-#pragma unroll
-    for (int c = 0; c < TILES; ++c) x[c] = 0.0f;
+    for (int w = 0; w < PA_WAVES; ++w) best = fmaxf(best, lds.ml[w][0][out_col]);
 #pragma unroll
     for (int w = 0; w < PA_WAVES; ++w) {
-        total = fmaf(lds_ml[w][1][out_col], __builtin_amdgcn_exp2f(lds_ml[w][0][out_col] - best), total);
+        total = fmaf(lds.ml[w][1][out_col], __builtin_amdgcn_exp2f(lds.ml[w][0][out_col] - best), total);
 #pragma unroll
-        for (int c = 0; c < TILES; ++c) x[c] += lds_o[w][out_col][TILES * piece + c];
+        for (int c = 0; c < TILES; ++c) x[c] += lds.o[w][out_col][TILES * piece + c];
     }
-    const int out_j = out_row / group, out_head = kv_head * group + out_row - out_j * group;
-    const int64_t token = (int64_t)b * a.q_len + out_j;
-    if (a.splits > 1) {
-        const int64_t at = (token * a.heads + out_head) * a.splits + split;
+    if (taken < units) {
+        // the part of a workgroup that the segment began before, and the one that begins in it
+        const int64_t at = (2 * (int64_t)blockIdx.x + (unit == 0)) * 16 + out_col;
 #pragma unroll
         for (int c = 0; c < TILES; c += 4)
             *reinterpret_cast<float4*>(a.part_o + at * D + TILES * piece + c) = make_float4(x[c], x[c + 1], x[c + 2], x[c + 3]);
         if (piece == 0) a.part_ml[at] = make_float2(best, total);
         return;
     }
-    const float inv = total > 0.0f ? __fdiv_rn(1.0f, total) : total == 0.0f ? 0.0f : total;      // (NaN stays)
-    uint32_t y[TILES / 2];
-#pragma unroll
-    for (int c = 0; c < TILES; c += 2) y[c / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f){x[c] * inv, x[c + 1] * inv}, v2bf));
-    uint16_t* dst = a.out + token * a.ldo + out_head * D + TILES * piece;
-    if constexpr (TILES == 8) *reinterpret_cast<uint4*>(dst) = make_uint4(y[0], y[1], y[2], y[3]);
-    else *reinterpret_cast<uint2*>(dst) = make_uint2(y[0], y[1]);
-    if (a.lse && piece == 0) a.lse[token * a.heads + out_head] = total == 0.0f ? -INFINITY : (best + __log2f(total)) * LN2;
+    const int out_j = out_row / group;
+    finish<TILES>(a, (int64_t)b * a.q_len + out_j, kv_head * group + out_row - out_j * group, D, TILES * piece, x, best, total);
 }
 
-// Joins the parts of a row: one wavefront to a row.
+// Work is a row of units: sequence by sequence, in it segment by segment (kv head by kv head, row tile by row tile), in it token by
+// token.  With a.workers > 0 that many workgroups take equal shares of it, whatever the lengths are: a share begins and ends inside
+// segments, whose parts the second kernel joins.  Otherwise a workgroup takes a segment.
+template <int D, bool CAP, bool FOLD>
+__global__ __launch_bounds__(PA_WAVES * 64, 3) void paged_attention_kernel(PagedAttentionArgs a) {
+    __shared__ __attribute__((aligned(256))) Shared<D> lds;
+    const int lane = threadIdx.x & 63;
+    const int segments = a.kv_heads * ((a.heads / a.kv_heads * a.q_len + 15) / 16);              // of a sequence
+    int b = 0, segment, unit = 0, units, left, share = 1;
+    if (a.workers == 0) {
+        b = blockIdx.x / segments;
+        segment = blockIdx.x - b * segments;
+        left = units = units_of(a, b);
+    } else {
+        int total = 0;
+        for (int b0 = 0; b0 < a.B; b0 += 64) {
+            int u = b0 + lane < a.B ? units_of(a, b0 + lane) : 0;
+#pragma unroll
+            for (int off = 32; off >= 1; off >>= 1) u += __shfl_xor(u, off, 64);
+            total += u;
+        }
+        total = __builtin_amdgcn_readfirstlane(total) * segments;
+        share = (total + a.workers - 1) / a.workers;
+        const int first = blockIdx.x * share;
+        left = min(share, total - first);
+        if (left <= 0) return;
+        int before = 0;                                          // units of the sequences before b, that of unit `first`
+        for (;;) {
+            const int u = b + lane < a.B ? units_of(a, b + lane) : 0;
+            int sum = u;
+#pragma unroll
+            for (int off = 1; off < 64; off <<= 1) {
+                const int v = __shfl_up(sum, off, 64);
+                if (lane >= off) sum += v;
+            }
+            const uint64_t behind = __ballot((before + sum) * segments > first);
+            if (behind != 0) {                                   // (it is in one of the rounds: first < total)
+                const int n = __builtin_ctzll(behind);
+                before += __builtin_amdgcn_readlane(sum - u, n);
+                units = __builtin_amdgcn_readlane(u, n);
+                b += n;
+                break;
+            }
+            before += __builtin_amdgcn_readlane(sum, 63);
+            b += 64;
+        }
+        segment = (first - before * segments) / units;
+        unit = first - before * segments - segment * units;
+    }
+    // (all of these are the same on every lane, which has to be said of quotients)
+    auto same = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    b = same(b); segment = same(segment); unit = same(unit); units = same(units); left = same(left);
+    for (;;) {
+        const int taken = min(units - unit, left);
+        // a segment that begins here: its first part's workgroup, and how many parts it has
+        if (a.workers > 0 && unit == 0 && threadIdx.x == 0)
+            a.part_of[(int64_t)b * segments + segment] = make_int2(blockIdx.x, 1 + (units - taken + share - 1) / share);
+        attend<D, CAP, FOLD>(a, lds, b, segment, unit, taken, units);
+        left -= taken;
+        if (left == 0) return;
+        unit = 0;
+        if (++segment == segments) {
+            segment = 0;
+            units = same(units_of(a, ++b));
+        }
+        __syncthreads();                                         // LDS is written anew
+    }
+}
+
+// Joins the parts of the segments that have several: a workgroup to a row, groups of D/4 threads to a part, four channels each.
 template <int D>
 __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedAttentionArgs a) {
-    constexpr int PER = D / 64;
-    const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= (int64_t)a.B * a.q_len * a.heads) return;
-    const int64_t token = row / a.heads;
+    constexpr int LANES = D / 4, GROUPS = 256 / LANES;
+    __shared__ float4 lds_x[GROUPS][LANES];
+    __shared__ float lds_m[4], lds_l[GROUPS];
+    const int64_t row = blockIdx.x, token = row / a.heads;
     const int head = (int)(row - token * a.heads), b = (int)(token / a.q_len), j = (int)(token - (int64_t)b * a.q_len);
-    const int group = a.heads / a.kv_heads, rows = group * a.q_len;
-    const int row_tile = (j * group + head % group) / 16;
-    const int j_first = row_tile * 16 / group, j_last = min(row_tile * 16 + 15, rows - 1) / group;
-    const int len = min(max(a.lengths[b], 0), a.max_len);
-    const int all_end = len - (a.q_len - 1) + j_last, all_begin = a.window > 0 ? max(len - (a.q_len - 1) + j_first - a.window, 0) & ~15 : 0;
-    const int parts = max(1, (all_end - all_begin + a.chunk - 1) / a.chunk);     // those that have tokens, and the first
-    const float2* ml = a.part_ml + row * a.splits;
-    const float* po = a.part_o + row * a.splits * D + PER * lane;
+    const int group = a.heads / a.kv_heads, row_tiles = (group * a.q_len + 15) / 16, in_kv = j * group + head % group;
+    const int2 where = a.part_of[((int64_t)b * a.kv_heads + head / group) * row_tiles + in_kv / 16];
+    const int parts = where.y;
+    if (parts <= 1) return;
+    const int piece = threadIdx.x % LANES, part0 = threadIdx.x / LANES, at_col = in_kv % 16;
+    auto slot = [&](int p) { return (2 * ((int64_t)where.x + p) + (p == 0)) * 16 + at_col; };
     float best = UNSET;
-    for (int s = lane; s < parts; s += 64) best = fmaxf(best, ml[s].x);
+    for (int p = threadIdx.x; p < parts; p += 256) best = fmaxf(best, a.part_ml[slot(p)].x);
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) best = fmaxf(best, __shfl_xor(best, off, 64));
-    float total = 0.0f, x[PER] = {};
-    for (int s = 0; s < parts; ++s) {
-        const float2 m = ml[s];
-        const float f = __builtin_amdgcn_exp2f(m.x - best);
-        total = fmaf(m.y, f, total);
-#pragma unroll
-        for (int c = 0; c < PER; ++c) x[c] = fmaf(po[(int64_t)s * D + c], f, x[c]);
+    if ((threadIdx.x & 63) == 0) lds_m[threadIdx.x >> 6] = best;
+    __syncthreads();
+    best = fmaxf(fmaxf(lds_m[0], lds_m[1]), fmaxf(lds_m[2], lds_m[3]));
+    float total = 0.0f;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int p = part0; p < parts; p += GROUPS) {
+        const float2 ml = a.part_ml[slot(p)];
+        const float4 o = *reinterpret_cast<const float4*>(a.part_o + slot(p) * D + 4 * piece);
+        const float f = __builtin_amdgcn_exp2f(ml.x - best);
+        total = fmaf(ml.y, f, total);
+        x.x = fmaf(o.x, f, x.x); x.y = fmaf(o.y, f, x.y); x.z = fmaf(o.z, f, x.z); x.w = fmaf(o.w, f, x.w);
     }
-    const float inv = total > 0.0f ? __fdiv_rn(1.0f, total) : total == 0.0f ? 0.0f : total;
-    uint16_t* dst = a.out + token * a.ldo + head * D + PER * lane;
+    lds_x[part0][piece] = x;
+    if (piece == 0) lds_l[part0] = total;
+    __syncthreads();
+    if (part0 != 0) return;
 #pragma unroll
-    for (int c = 0; c < PER; ++c) dst[c] = f32_to_bf16(x[c] * inv);
-    if (a.lse && lane == 0) a.lse[row] = total == 0.0f ? -INFINITY : (best + __log2f(total)) * LN2;
+    for (int g = 1; g < GROUPS; ++g) {
+        const float4 o = lds_x[g][piece];
+        x.x += o.x; x.y += o.y; x.z += o.z; x.w += o.w;
+        total += lds_l[g];
+    }
+    const float y[4] = {x.x, x.y, x.z, x.w};
+    finish<4>(a, token, head, D, 4 * piece, y, best, total);
 }
 
 template <int D>
 int launch(const PagedAttentionArgs& a, hipStream_t s) {
-    const int rows = a.heads / a.kv_heads * a.q_len;
-    const int64_t blocks = (int64_t)a.B * a.kv_heads * ((rows + 15) / 16) * a.splits;
-    if (blocks > 0x7FFFFFFFll) return fail(BASQ_EUNSUPPORTED, "paged_attention: too many rows");
-    if (a.softcap > 0.0f) hipLaunchKernelGGL((paged_attention_kernel<D, true>), dim3((unsigned)blocks), dim3(PA_WAVES * 64), 0, s, a);
-    else hipLaunchKernelGGL((paged_attention_kernel<D, false>), dim3((unsigned)blocks), dim3(PA_WAVES * 64), 0, s, a);
-    int rc = check_hip(hipGetLastError(), "paged_attention launch");
-    if (rc != BASQ_OK || a.splits == 1) return rc;
-    const int64_t joins = ((int64_t)a.B * a.q_len * a.heads + 3) / 4;
-    hipLaunchKernelGGL((paged_attention_join_kernel<D>), dim3((unsigned)joins), dim3(256), 0, s, a);
+    const int64_t segments = (int64_t)a.B * a.kv_heads * ((a.heads / a.kv_heads * a.q_len + 15) / 16);
+    const unsigned blocks = (unsigned)(a.workers > 0 ? a.workers : segments);
+    const bool fold = a.heads / a.kv_heads * a.q_len <= 8;
+    auto kernel = a.softcap > 0.0f ? fold ? paged_attention_kernel<D, true, true> : paged_attention_kernel<D, true, false>
+                                   : fold ? paged_attention_kernel<D, false, true> : paged_attention_kernel<D, false, false>;
+    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(PA_WAVES * 64), 0, s, a);
+    const int rc = check_hip(hipGetLastError(), "paged_attention launch");
+    if (rc != BASQ_OK || a.workers == 0) return rc;
+    hipLaunchKernelGGL((paged_attention_join_kernel<D>), dim3((unsigned)((int64_t)a.B * a.q_len * a.heads)), dim3(256), 0, s, a);
     return check_hip(hipGetLastError(), "paged_attention join launch");
 }
 
 }  // namespace
 
-// How the contexts are split: enough workgroups to fill the chip four times over, and no part shorter than 128 tokens, a step of
-// each of a workgroup's waves.
-void paged_attention_split(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t max_len, int32_t window,
-                           int32_t* splits, int32_t* chunk) {
-    const int64_t base = (int64_t)B * kv_heads * (((int64_t)(heads / kv_heads) * q_len + 15) / 16);
-    // (a window is cut to whole blocks of 16 at its begin, and the rows of a tile have windows up to q_len - 1 tokens apart)
+// Short contexts, whose segments one workgroup each takes in a few steps, go without the second launch; -1 where there are too many
+// units to be numbered.
+int paged_attention_workers(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t max_len, int32_t window) {
+    const int64_t segments = (int64_t)B * kv_heads * (((int64_t)(heads / kv_heads) * q_len + 15) / 16);
+    // (a window is cut to whole blocks of 16 at its begin, and rows have windows up to q_len - 1 tokens apart)
     const int64_t range = window > 0 && window + (int64_t)q_len + 15 < max_len ? window + (int64_t)q_len + 15 : max_len;
-    constexpr int64_t PART = 128;
-    const int64_t most = (range + PART - 1) / PART, want = base > 0 ? (1024 + base - 1) / base : 1;
-    int64_t n = want < most ? want : most;
-    if (n < 1) n = 1;
-    int64_t each = ((range + n - 1) / n + PART - 1) / PART * PART;
-    if (each < PART) each = PART;
-    *chunk = (int32_t)each;
-    *splits = (int32_t)((range + each - 1) / each > 1 ? (range + each - 1) / each : 1);
+    const int64_t units = range > PA_UNIT ? (range + PA_UNIT - 1) / PA_UNIT : 1;
+    if (segments * units > 0x7FFFFFFFll || (int64_t)B * q_len * heads > 0x7FFFFFFFll) return -1;
+    if (units <= 4) return 0;
+    // as many as the chip holds at once
+    const int64_t most = head_dim == 64 ? 768 : 768;
+    return (int)(segments * units < most ? segments * units : most);
 }
 
 int launch_paged_attention(PagedAttentionArgs a, hipStream_t s) {
