@@ -177,7 +177,8 @@ struct PagedAttentionArgs {
     float* part_o;            // [2 * workers, 16, D]: a workgroup's last part of a segment begun before, and its part of one that goes on
     float2* part_ml;          // [2 * workers, 16]: reference and sum
     int2* part_of;            // [segments]: the workgroup in which a segment begins, and its number of parts
-    float inv_cap, cap_log2e; // set by the launcher
+    float inv_cap, cap_log2e; // these four are set by the launcher
+    int32_t group, row_tiles; // heads of a kv head, tiles of 16 of its query rows
 };
 int paged_attention_workers(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t max_len, int32_t window);
 int launch_paged_attention(PagedAttentionArgs a, hipStream_t s);  // paged_attention.hip

@@ -67,6 +67,15 @@ struct Block {
     static constexpr int LOADS = D == 128 ? 3 : 2;               // direct loads that bring it
 };
 
+// N neighbouring values (2, 4 or 8) in one go
+template <int N>
+__device__ __forceinline__ void store(float* to, const float (&x)[N]) {
+    if constexpr (N == 2) *reinterpret_cast<float2*>(to) = make_float2(x[0], x[1]);
+    else
+#pragma unroll
+        for (int c = 0; c < N; c += 4) *reinterpret_cast<float4*>(to + c) = make_float4(x[c], x[c + 1], x[c + 2], x[c + 3]);
+}
+
 // N neighbouring channels of a row's result, from its sums at reference M: out = x / l (0 where no token counted), lse.
 template <int N>
 __device__ __forceinline__ void finish(const PagedAttentionArgs& a, int64_t token, int head, int D, int channel, const float (&x)[N], float M, float l) {
@@ -76,103 +85,146 @@ __device__ __forceinline__ void finish(const PagedAttentionArgs& a, int64_t toke
     for (int c = 0; c < N; c += 2) y[c / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f){x[c] * inv, x[c + 1] * inv}, v2bf));
     uint16_t* dst = a.out + token * a.ldo + head * D + channel;
     if constexpr (N == 8) *reinterpret_cast<uint4*>(dst) = make_uint4(y[0], y[1], y[2], y[3]);
-    else *reinterpret_cast<uint2*>(dst) = make_uint2(y[0], y[1]);
+    else if constexpr (N == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(y[0], y[1]);
+    else *reinterpret_cast<uint32_t*>(dst) = y[0];
     if (a.lse && channel == 0) a.lse[token * a.heads + head] = l == 0.0f ? -INFINITY : (M + __log2f(l)) * LN2;
 }
 
-// Tokens of a sequence that new tokens j_first .. j_last of it see, in units of PA_UNIT from `begin` (a multiple of 16).
-struct Span {
-    int begin, end;
-};
-__device__ __forceinline__ Span span_of(const PagedAttentionArgs& a, int len, int j_first, int j_last) {
-    return {a.window > 0 ? max(len - (a.q_len - 1) + j_first - a.window, 0) & ~15 : 0, len - (a.q_len - 1) + j_last};
+// the length of a sequence that is the same for the whole wave (a scalar load: a vector load's wait would be for all direct loads too)
+__device__ __forceinline__ int clamped(const PagedAttentionArgs& a, int len) { return min(max(len, 0), a.max_len); }
+__device__ __forceinline__ int length_of(const PagedAttentionArgs& a, int b) {
+    return clamped(a, ((const __attribute__((address_space(4))) int32_t*)a.lengths)[b]);
 }
-__device__ __forceinline__ int length_of(const PagedAttentionArgs& a, int b) { return min(max(a.lengths[b], 0), a.max_len); }
-// units of sequence b, the same for all its segments; at least one, whose taker also writes the zeros of rows that see nothing
-__device__ __forceinline__ int units_of(const PagedAttentionArgs& a, int b) {
-    const Span s = span_of(a, length_of(a, b), 0, a.q_len - 1);
-    return max((s.end - s.begin + PA_UNIT - 1) / PA_UNIT, 1);
+// the first token that a new token sees, in whole blocks, when it sees those before `end`
+__device__ __forceinline__ int first_token(const PagedAttentionArgs& a, int end) { return a.window > 0 ? max(end - a.window, 0) & ~15 : 0; }
+// units of PA_UNIT tokens that any new token of a sequence sees, the same for all its segments; at least one, whose taker also writes
+// the zeros of rows that see nothing
+__device__ __forceinline__ int units_of(const PagedAttentionArgs& a, int len) {
+    return max((len - first_token(a, len - (a.q_len - 1)) + PA_UNIT - 1) / PA_UNIT, 1);
 }
 
-template <int D>
+// ROWS query rows at most in a tile.  LDS is allocated in steps of 1280 bytes: D = 128 with 8 rows takes 42 of the 128, three workgroups
+// to a compute unit.
+template <int D, int ROWS>
 struct Shared {
-    union {
-        uint8_t ring[PA_WAVES][PA_STAGES][2][Block<D>::BYTES];
-        float o[PA_WAVES][16][D + 4];
-    };
-    float ml[PA_WAVES][2][16];
+    uint8_t ring[PA_WAVES][PA_STAGES][2][Block<D>::BYTES];
+    int o[PA_WAVES][ROWS][D];                                    // fp32 (integers for the compiler, see below), groups of 4 in another order in each row
+    int ml[PA_WAVES][2][ROWS];
 };
+
+static_assert(sizeof(Shared<128, 8>) <= 42 * 1280, "three workgroups to a compute unit");
 
 template <int N>
 __device__ __forceinline__ void wait_loads() {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
+// (the compiler's own barrier waits for every load that is under way)
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+__device__ __forceinline__ int same(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-// A segment, one kv head and tile of 16 query rows of sequence b: `taken` of its `units`, from number `unit` on.
+// Some units of a segment, one kv head and tile of query rows of sequence b: `taken` of its `units`, from number `unit` on.
+struct Part {
+    int b, len, segment, unit, taken, units;
+    int kv_head, row_tile;
+    int from, to;                                                // the tokens of it that any row of the tile sees
+    int j_first;                                                 // the first row's new token
+    int inner_begin, inner_end;                                  // between these, all rows see all tokens
+};
+
+// Work is a row of units: sequence by sequence, in it segment by segment (kv head by kv head, row tile by row tile), in it token by
+// token.  With a.workers > 0 that many workgroups take equal shares of it, whatever the lengths are: a share begins and ends inside
+// segments, whose parts the second kernel joins.  Otherwise a workgroup takes a segment.
+//
+// FOLD: tiles of at most eight rows, which stand in columns 0 .. 7 and again in 8 .. 15; a lane works on the first block's scores, or
+// on the second's, instead of on both.
 template <int D, bool CAP, bool FOLD>
-__device__ __forceinline__ void attend(const PagedAttentionArgs& a, Shared<D>& lds, int b, int segment, int unit, int taken, int units) {
+__global__ __launch_bounds__(PA_WAVES * 64, D == 128 && !FOLD ? 2 : 3) void paged_attention_kernel(PagedAttentionArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)   // buffer resources are a device-only type; the host pass only needs the stub
     constexpr int TILES = D / 16;                                // channel tiles of the second product: channel TILES * n + c
     constexpr int KS = D / 32;                                   // 32-channel steps of the first
     constexpr int MINE = FOLD ? 4 : 8;                           // tokens of a lane in a step
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int ROWS = FOLD ? 8 : 16;
+    constexpr int STRIDE = PA_WAVES * PA_STEP;
+    __shared__ __attribute__((aligned(256))) Shared<D, ROWS> lds;
+    const int lane = threadIdx.x & 63, wave = same(threadIdx.x >> 6);
     const int col = lane & 15, quarter = lane >> 4;
-    const int group = a.heads / a.kv_heads, rows = group * a.q_len, row_tiles = (rows + 15) / 16;
-    const int kv_head = __builtin_amdgcn_readfirstlane(segment / row_tiles), row_tile = segment - kv_head * row_tiles;
+    const int group = a.group, rows = group * a.q_len, row_tiles = a.row_tiles;
+    const int segments = a.kv_heads * row_tiles;                 // of a sequence
     const int P = 1 << a.page_log2;
     const int64_t head_bytes = (int64_t)P * (D + 16);
-    const int len = __builtin_amdgcn_readfirstlane(length_of(a, b));
-    // this lane's query row: new token j, head, and the tokens [begin, end) that it sees
-    const int row = min(row_tile * 16 + (FOLD ? col & 7 : col), rows - 1), j = row / group, head = kv_head * group + row - j * group;
-    const int end = len - (a.q_len - 1) + j, begin = a.window > 0 ? max(end - a.window, 0) : 0;
-    // the tokens of this part that any row of the tile sees
-    const int j_first = __builtin_amdgcn_readfirstlane(row_tile * 16 / group), j_last = __builtin_amdgcn_readfirstlane(min(row_tile * 16 + 15, rows - 1) / group);
-    const Span all = span_of(a, len, 0, a.q_len - 1), mine = span_of(a, len, j_first, j_last);
-    const int from = max(all.begin + unit * PA_UNIT, mine.begin), to = min(all.begin + (unit + taken) * PA_UNIT, mine.end);
-    const int32_t* pages = a.page_table + (int64_t)b * a.table_stride;
 
-    // query rows
-    v8h q[KS];
-    float c1, qs;
-    {
-        const uint16_t* src = a.q + ((int64_t)b * a.q_len + j) * a.ldq + (int64_t)head * D + quarter * (D / 4);
-        float x[D / 4], top = 0.0f, sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < D / 4; i += 8) {
-            const uint4 w = *reinterpret_cast<const uint4*>(src + i);
-            const uint32_t* u = reinterpret_cast<const uint32_t*>(&w);
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                x[i + 2 * h] = __uint_as_float(u[h] << 16);
-                x[i + 2 * h + 1] = __uint_as_float(u[h] & 0xFFFF0000u);
+    // ---- this workgroup's first part, and the units that it has to take
+    int b = 0, len, segment, unit = 0, units, left, share = 1;
+    if (a.workers == 0) {
+        b = blockIdx.x / segments;
+        segment = blockIdx.x - b * segments;
+        len = length_of(a, b);
+        left = units = units_of(a, len);
+    } else {
+        int mine = 0, u = 0, sum = 0;                            // of sequence base + lane: length, units, units of all up to it
+        auto scan = [&](int base) {
+            mine = base + lane < a.B ? clamped(a, a.lengths[base + lane]) : 0;
+            u = base + lane < a.B ? units_of(a, mine) : 0;
+            sum = u;
+            sum += __builtin_amdgcn_update_dpp(0, sum, 0x111, 0xF, 0xF, true);       // rows of 16 lanes: shifts by 1, 2, 4, 8
+            sum += __builtin_amdgcn_update_dpp(0, sum, 0x112, 0xF, 0xF, true);
+            sum += __builtin_amdgcn_update_dpp(0, sum, 0x114, 0xF, 0xF, true);
+            sum += __builtin_amdgcn_update_dpp(0, sum, 0x118, 0xF, 0xF, true);
+            sum += __builtin_amdgcn_update_dpp(0, sum, 0x142, 0xA, 0xF, false);      // lane 15 into the second row, 47 into the fourth
+            sum += __builtin_amdgcn_update_dpp(0, sum, 0x143, 0xC, 0xF, false);      // lane 31 into the upper half
+            return __builtin_amdgcn_readlane(sum, 63);
+        };
+        int total = 0, last_round = 0;
+        for (int base = 0; base < a.B; base += 64) {
+            total += scan(base);
+            last_round = base;
+        }
+        total *= segments;
+        share = same((total + a.workers - 1) / a.workers);
+        const int first = blockIdx.x * share;
+        left = min(share, total - first);
+        if (left <= 0) return;
+        int before = 0;                                          // units of the sequences before b, that of unit `first`
+        for (;;) {
+            const int these = last_round > 0 ? scan(b) : __builtin_amdgcn_readlane(sum, 63);
+            const uint64_t behind = __ballot((before + sum) * segments > first);
+            if (behind != 0) {                                   // (it is in one of the rounds: first < total)
+                const int n = __builtin_ctzll(behind);
+                before += __builtin_amdgcn_readlane(sum - u, n);
+                units = __builtin_amdgcn_readlane(u, n);
+                len = __builtin_amdgcn_readlane(mine, n);
+                b += n;
+                break;
             }
+            before += these;
+            b += 64;
         }
-#pragma unroll
-        for (int i = 0; i < D / 4; ++i) {
-            top = fmaxf(top, fabsf(x[i]));
-            sum += x[i];
-        }
-        top = quarters_max(top);
-        sum = quarters_sum(sum);
-        // the largest becomes 2^14 .. 2^15 (exponent field of top, 127 = 2^0)
-        const int e = min(max(141 - (int)(__float_as_uint(top) >> 23), -100), 100);
-        const float up = __uint_as_float((uint32_t)(127 + e) << 23);
-        c1 = a.scale * LOG2E * __uint_as_float((uint32_t)(127 - e) << 23) * 0x1p20f;
-        qs = a.scale * LOG2E * sum;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            constexpr int ORDER[8] = {0, 4, 1, 5, 2, 6, 3, 7};
-#pragma unroll
-            for (int i = 0; i < 8; ++i) q[s][i] = (_Float16)(x[8 * s + ORDER[i]] * up);
-        }
+        segment = (first - before * segments) / units;
+        unit = first - before * segments - segment * units;
     }
 
-    v4f o[TILES];
-#pragma unroll
-    for (int c = 0; c < TILES; ++c) o[c] = (v4f){0.f, 0.f, 0.f, 0.f};
-    float M = 0.0f, l = 0.0f, lows = 0.0f;                        // l and lows: this lane's tokens
-    bool set = false;                                             // M is a reference: the row has seen a token
+    auto describe = [&](int b, int len, int segment, int unit, int units, int left) {
+        Part p;
+        p.b = b; p.len = len; p.segment = segment; p.unit = unit; p.units = units;
+        p.taken = min(units - unit, left);
+        p.kv_head = row_tiles == 1 ? segment : same(segment / row_tiles);
+        p.row_tile = segment - p.kv_head * row_tiles;
+        const int seen = len - (a.q_len - 1);                     // tokens that the first new token sees
+        const int j_first = row_tiles == 1 ? 0 : same(p.row_tile * 16 / group);
+        const int j_last = row_tiles == 1 ? a.q_len - 1 : same(min(p.row_tile * 16 + 15, rows - 1) / group);
+        const int begin = first_token(a, seen);
+        p.from = max(begin + unit * PA_UNIT, first_token(a, seen + j_first));
+        p.to = min(begin + (unit + p.taken) * PA_UNIT, seen + j_last);
+        p.inner_begin = a.window > 0 ? max(seen + j_last - a.window, 0) : 0;
+        p.inner_end = seen + j_first;
+        p.j_first = j_first;
+        return p;
+    };
+    // the lane's query row in a part's tile; the new token of a row
+    auto new_token = [&](int row) { return a.q_len == 1 ? 0 : row / group; };
+    auto row_of = [&](const Part& p) { return min(p.row_tile * 16 + (FOLD ? col & 7 : col), rows - 1); };
 
-    // What a lane requests, as byte offsets into one head of one page, and where it reads what it works on.  Row i of the first
+    // ---- what a lane requests, as byte offsets into one head of one page, and where it reads what it works on.  Row i of the first
     // product's results is token 4 * (i % 4) + i / 4 of a block, so quarter g of the wave works on tokens g, 4 + g, 8 + g, 12 + g:
     // for each of the four, the wave reads 256 (128) bytes of values side by side.  Keys lie in 16-byte pieces whose place
     // inside their row changes from token to token, so that 16 lanes read from all banks; ranges lie by quarter.
@@ -189,20 +241,20 @@ __device__ __forceinline__ void attend(const PagedAttentionArgs& a, Shared<D>& l
     const int v_at = Block<D>::V_AT + quarter * (D / 2) + col * (D / 32), r_at = Block<D>::R_AT + quarter * 32 + (FOLD ? (col >> 3) * Block<D>::BYTES : 0);
     uint8_t* const ring = &lds.ring[wave][0][0][0];
 
-    // This wave's next 32 steps: where block 2i + h of 16 tokens begins in the cache, on lane 2i + h; and whether it is there (not
+    // The wave's next 32 steps: where block 2i + h of 16 tokens begins in the cache, on lane 2i + h; and whether it is there (not
     // past the end, of a page that exists; the others are read from the first page, and masked).
     int64_t place = 0;
     uint64_t there = 0;
-    constexpr int STRIDE = PA_WAVES * PA_STEP;
-    auto fetch = [&](int t0) {
+    auto request_ids = [&](const Part& p, int t0) {
         const int t = t0 + (lane >> 1) * STRIDE + (lane & 1) * 16;
-        int id = -1;
-        if (t < to) id = pages[t >> a.page_log2];
+        return t < p.to ? a.page_table[(int64_t)p.b * a.table_stride + (t >> a.page_log2)] : -1;
+    };
+    auto take_ids = [&](const Part& p, int id) {
         const bool ok = id >= 0 && id < a.num_pages;
         there = __ballot(ok);
-        place = ((int64_t)(ok ? id : 0) * a.kv_heads + kv_head) * head_bytes;
+        place = ((int64_t)(ok ? id : 0) * a.kv_heads + p.kv_head) * head_bytes;
     };
-    // requests step i of the fetched ones, tokens t .., into a stage of the ring; nothing (which counts as loads) behind the last
+    // requests step i, tokens t .., into a stage of the ring; nothing (which counts as loads) behind the last
     auto load = [&](int i, int last, int t, int stage) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -218,8 +270,57 @@ __device__ __forceinline__ void attend(const PagedAttentionArgs& a, Shared<D>& l
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, PA_LDS_PTR(dst + Block<D>::R_AT), 4, (int)range_from, at * 8, 0, 2);
         }
     };
-    // whether no row of the tile masks any token of the step
-    const int inner_begin = a.window > 0 ? max(len - (a.q_len - 1) + j_last - a.window, 0) : 0, inner_end = len - (a.q_len - 1) + j_first;
+    auto last_step = [&](const Part& p, int t0) { return t0 < p.to ? min(32, (p.to - t0 + STRIDE - 1) / STRIDE) - 1 : -1; };
+    auto load_first = [&](const Part& p, int t0) {
+#pragma unroll
+        for (int i = 0; i < PA_STAGES - 1; ++i) load(i, last_step(p, t0), t0 + i * STRIDE, i);
+    };
+    uint4 raw[KS];                                               // the lane's D/4 channels of its query row
+    auto request_row = [&](const Part& p) {
+        const int row = row_of(p), j = new_token(row), head = p.kv_head * group + row - j * group;
+        const uint4* src = reinterpret_cast<const uint4*>(a.q + ((int64_t)p.b * a.q_len + j) * a.ldq + (int64_t)head * D + quarter * (D / 4));
+#pragma unroll
+        for (int i = 0; i < KS; ++i) raw[i] = src[i];
+    };
+
+    // ---- the state of a part
+    v8h q[KS];
+    float c1, qs;
+    int begin, end;                                               // the tokens that the lane's row sees
+    v4f o[TILES];
+    float M, l, lows;                                             // l and lows: this lane's tokens
+    bool set;                                                     // M is a reference: the row has seen a token
+    auto start = [&](const Part& p) {
+        end = p.inner_end - p.j_first + new_token(row_of(p));
+        begin = a.window > 0 ? max(end - a.window, 0) : 0;
+        float x[D / 4], top = 0.0f, sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < D / 4; i += 2) {
+            const uint32_t u = reinterpret_cast<const uint32_t*>(raw)[i / 2];
+            x[i] = __uint_as_float(u << 16);
+            x[i + 1] = __uint_as_float(u & 0xFFFF0000u);
+            top = fmaxf(top, fmaxf(fabsf(x[i]), fabsf(x[i + 1])));
+            sum += x[i];
+            sum += x[i + 1];
+        }
+        top = quarters_max(top);
+        sum = quarters_sum(sum);
+        // the largest becomes 2^14 .. 2^15 (exponent field of top, 127 = 2^0)
+        const int e = min(max(141 - (int)(__float_as_uint(top) >> 23), -100), 100);
+        const float up = __uint_as_float((uint32_t)(127 + e) << 23);
+        c1 = a.scale * LOG2E * __uint_as_float((uint32_t)(127 - e) << 23) * 0x1p20f;
+        qs = a.scale * LOG2E * sum;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            constexpr int ORDER[8] = {0, 4, 1, 5, 2, 6, 3, 7};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[s][i] = (_Float16)(x[8 * s + ORDER[i]] * up);
+        }
+#pragma unroll
+        for (int c = 0; c < TILES; ++c) o[c] = (v4f){0.f, 0.f, 0.f, 0.f};
+        M = l = lows = 0.0f;
+        set = false;
+    };
 
     auto row_max = [&](float v) {
         v = quarters_max(v);
@@ -233,7 +334,7 @@ __device__ __forceinline__ void attend(const PagedAttentionArgs& a, Shared<D>& l
         const float near = y * fmaf(y2, fmaf(y2, fmaf(y2, fmaf(y2, 62.0f / 2835, -17.0f / 315), 2.0f / 15), -1.0f / 3), 1.0f);
         return a.cap_log2e * (fabsf(y) < 0.25f ? near : far);
     };
-    auto work = [&](int i, int t, int stage) {
+    auto work = [&](const Part& part, int i, int t, int stage) {
         const uint8_t* blocks = ring + stage * 2 * Block<D>::BYTES;
         v4f acc[2];
 #pragma unroll
@@ -270,7 +371,7 @@ __device__ __forceinline__ void attend(const PagedAttentionArgs& a, Shared<D>& l
             }
         }
         const unsigned both = (unsigned)(there >> (2 * i)) & 3u;
-        if (both != 3u || t < inner_begin || t + PA_STEP > inner_end) {
+        if (both != 3u || t < part.inner_begin || t + PA_STEP > part.inner_end) {
             asm volatile("");                                     // (a branch: few steps come here)
             // what is masked may hold anything, also ranges that are no numbers
 #pragma unroll
@@ -359,197 +460,198 @@ __device__ __forceinline__ void attend(const PagedAttentionArgs& a, Shared<D>& l
         }
     };
 
-    // PA_STAGES - 1 steps are under way while one is worked on.
-    for (int t0 = from + wave * PA_STEP; t0 < to; t0 += 32 * STRIDE) {
-        fetch(t0);
-        const int last = min(32, (to - t0 + STRIDE - 1) / STRIDE) - 1;
+    // ---- the four waves' sums into one: written at each wave's own reference, read at the largest
+    auto finish_part = [&](const Part& p) {
+        // a segment that begins here: its first part's workgroup, and how many parts it has
+        if (a.workers > 0 && p.unit == 0 && threadIdx.x == 0)
+            a.part_of[(int64_t)p.b * segments + p.segment] = make_int2(blockIdx.x, 1 + (p.units - p.taken + share - 1) / share);
+        l = quarters_sum(l);
+        lows = quarters_sum(lows);
+        if constexpr (FOLD) {
+            l += __shfl_xor(l, 8, 64);
+            lows += __shfl_xor(lows, 8, 64);
+        }
+        lds_barrier();                                            // the part before is read
+        if (col < ROWS) {
+            if (quarter == 0) {
+                lds.ml[wave][0][col] = __float_as_int(set ? M : UNSET);
+                lds.ml[wave][1][col] = __float_as_int(l);
+            }
 #pragma unroll
-        for (int i = 0; i < PA_STAGES - 1; ++i) load(i, last, t0 + i * STRIDE, i);
-        int stage = 0;
-        for (int i = 0; i <= last; ++i) {
-            load(i + PA_STAGES - 1, last, t0 + (i + PA_STAGES - 1) * STRIDE, stage == 0 ? PA_STAGES - 1 : stage - 1);
-            wait_loads<(PA_STAGES - 1) * 2 * Block<D>::LOADS>();
-            work(i, t0 + i * STRIDE, stage);
-            asm volatile("" ::: "memory");                        // (the stage is read before it is requested anew)
-            stage = stage == PA_STAGES - 1 ? 0 : stage + 1;
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int c = 0; c < TILES; c += 4) {
+                    const v4f x = {fmaf(o[c][r], 0x1p24f, lows), fmaf(o[c + 1][r], 0x1p20f, lows), fmaf(o[c + 2][r], 0x1p24f, lows), fmaf(o[c + 3][r], 0x1p20f, lows)};
+                    *reinterpret_cast<v4i*>(&lds.o[wave][col][(TILES * (4 * quarter + r) + c) ^ (col & 7) * 4]) = __builtin_bit_cast(v4i, x);
+                }
+        }
+        lds_barrier();
+        // 16 (32) threads to a row, a few neighbouring channels each
+        constexpr int THREADS = PA_WAVES * 64 / ROWS, N = D / THREADS;
+        const int r = threadIdx.x / THREADS, piece = threadIdx.x % THREADS, row = p.row_tile * 16 + r;
+        if (row >= rows) return;
+        float x[N] = {}, total = 0.0f, best = UNSET;
+#pragma unroll
+        for (int w = 0; w < PA_WAVES; ++w) best = fmaxf(best, __int_as_float(lds.ml[w][0][r]));
+#pragma unroll
+        for (int w = 0; w < PA_WAVES; ++w) {
+            const float f = __builtin_amdgcn_exp2f(__int_as_float(lds.ml[w][0][r]) - best);
+            total = fmaf(__int_as_float(lds.ml[w][1][r]), f, total);
+#pragma unroll
+            for (int c = 0; c < N; ++c) x[c] = fmaf(__int_as_float(lds.o[w][r][(N * piece + c) ^ (r & 7) * 4]), f, x[c]);
+        }
+        if (p.taken < p.units) {
+            // the part of a workgroup that the segment began before, and the one that begins in it
+            const int64_t at = (2 * (int64_t)blockIdx.x + (p.unit == 0)) * 16 + r;
+            store<N>(a.part_o + at * D + N * piece, x);
+            if (piece == 0) a.part_ml[at] = make_float2(best, total);
+            return;
+        }
+        const int j = new_token(row);
+        finish<N>(a, (int64_t)p.b * a.q_len + j, p.kv_head * group + row - j * group, D, N * piece, x, best, total);
+    };
+
+    // ---- part by part; the first loads of the next are under way while the sums of one are joined
+    Part part = describe(same(b), same(len), same(segment), same(unit), same(units), same(left));
+    take_ids(part, request_ids(part, part.from + wave * PA_STEP));
+    request_row(part);
+    load_first(part, part.from + wave * PA_STEP);
+    left = same(left);
+    for (;;) {
+        left -= part.taken;
+        Part next = part;
+        int next_ids = -1;
+        if (left > 0) {
+            const bool same_b = part.segment + 1 < segments;
+            const int next_b = same_b ? part.b : part.b + 1, next_len = same_b ? part.len : length_of(a, next_b);
+            next = describe(next_b, next_len, same_b ? part.segment + 1 : 0, 0, same_b ? part.units : units_of(a, next_len), left);
+            next_ids = request_ids(next, next.from + wave * PA_STEP);
+        }
+        start(part);
+        // PA_STAGES - 1 steps are under way while one is worked on
+        for (int t0 = part.from + wave * PA_STEP; t0 < part.to; t0 += 32 * STRIDE) {
+            const int last = last_step(part, t0);
+            if (t0 >= part.from + 32 * STRIDE) {
+                take_ids(part, request_ids(part, t0));
+                load_first(part, t0);
+            }
+            int stage = 0;
+            for (int i = 0; i <= last; ++i) {
+                load(i + PA_STAGES - 1, last, t0 + (i + PA_STAGES - 1) * STRIDE, stage == 0 ? PA_STAGES - 1 : stage - 1);
+                wait_loads<(PA_STAGES - 1) * 2 * Block<D>::LOADS>();
+                work(part, i, t0 + i * STRIDE, stage);
+                asm volatile("" ::: "memory");                    // (the stage is read before it is requested anew)
+                stage = stage == PA_STAGES - 1 ? 0 : stage + 1;
+            }
         }
         wait_loads<0>();
-    }
-
-    // join the four waves: sums brought to the largest reference
-    if (!set) M = UNSET;
-    l = quarters_sum(l);
-    lows = quarters_sum(lows);
-    if constexpr (FOLD) {
-        l += __shfl_xor(l, 8, 64);
-        lows += __shfl_xor(lows, 8, 64);
-    }
-    if (quarter == 0) {
-        lds.ml[wave][0][col] = M;
-        lds.ml[wave][1][col] = l;
-    }
-    __syncthreads();
-    float best = UNSET;
-#pragma unroll
-    for (int w = 0; w < PA_WAVES; ++w) best = fmaxf(best, lds.ml[w][0][col]);
-    const float f = __builtin_amdgcn_exp2f(M - best);
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int c = 0; c < TILES; ++c)
-            lds.o[wave][col][TILES * (4 * quarter + r) + c] = f * fmaf(o[c][r], c & 1 ? 0x1p20f : 0x1p24f, lows);
-    __syncthreads();
-    // sixteen threads to a row, D/16 neighbouring channels each
-    const int out_col = threadIdx.x / 16, piece = threadIdx.x % 16, out_row = row_tile * 16 + out_col;
-    if (out_row >= rows) return;
-    float x[TILES] = {}, total = 0.0f;
-    best = UNSET;
-#pragma unroll
-    for (int w = 0; w < PA_WAVES; ++w) best = fmaxf(best, lds.ml[w][0][out_col]);
-#pragma unroll
-    for (int w = 0; w < PA_WAVES; ++w) {
-        total = fmaf(lds.ml[w][1][out_col], __builtin_amdgcn_exp2f(lds.ml[w][0][out_col] - best), total);
-#pragma unroll
-        for (int c = 0; c < TILES; ++c) x[c] += lds.o[w][out_col][TILES * piece + c];
-    }
-    if (taken < units) {
-        // the part of a workgroup that the segment began before, and the one that begins in it
-        const int64_t at = (2 * (int64_t)blockIdx.x + (unit == 0)) * 16 + out_col;
-#pragma unroll
-        for (int c = 0; c < TILES; c += 4)
-            *reinterpret_cast<float4*>(a.part_o + at * D + TILES * piece + c) = make_float4(x[c], x[c + 1], x[c + 2], x[c + 3]);
-        if (piece == 0) a.part_ml[at] = make_float2(best, total);
-        return;
-    }
-    const int out_j = out_row / group;
-    finish<TILES>(a, (int64_t)b * a.q_len + out_j, kv_head * group + out_row - out_j * group, D, TILES * piece, x, best, total);
-}
-
-// Work is a row of units: sequence by sequence, in it segment by segment (kv head by kv head, row tile by row tile), in it token by
-// token.  With a.workers > 0 that many workgroups take equal shares of it, whatever the lengths are: a share begins and ends inside
-// segments, whose parts the second kernel joins.  Otherwise a workgroup takes a segment.
-template <int D, bool CAP, bool FOLD>
-__global__ __launch_bounds__(PA_WAVES * 64, 3) void paged_attention_kernel(PagedAttentionArgs a) {
-    __shared__ __attribute__((aligned(256))) Shared<D> lds;
-    const int lane = threadIdx.x & 63;
-    const int segments = a.kv_heads * ((a.heads / a.kv_heads * a.q_len + 15) / 16);              // of a sequence
-    int b = 0, segment, unit = 0, units, left, share = 1;
-    if (a.workers == 0) {
-        b = blockIdx.x / segments;
-        segment = blockIdx.x - b * segments;
-        left = units = units_of(a, b);
-    } else {
-        int total = 0;
-        for (int b0 = 0; b0 < a.B; b0 += 64) {
-            int u = b0 + lane < a.B ? units_of(a, b0 + lane) : 0;
-#pragma unroll
-            for (int off = 32; off >= 1; off >>= 1) u += __shfl_xor(u, off, 64);
-            total += u;
+        if (left > 0) {
+            request_row(next);
+            take_ids(next, next_ids);
+            load_first(next, next.from + wave * PA_STEP);
         }
-        total = __builtin_amdgcn_readfirstlane(total) * segments;
-        share = (total + a.workers - 1) / a.workers;
-        const int first = blockIdx.x * share;
-        left = min(share, total - first);
+        finish_part(part);
         if (left <= 0) return;
-        int before = 0;                                          // units of the sequences before b, that of unit `first`
-        for (;;) {
-            const int u = b + lane < a.B ? units_of(a, b + lane) : 0;
-            int sum = u;
-#pragma unroll
-            for (int off = 1; off < 64; off <<= 1) {
-                const int v = __shfl_up(sum, off, 64);
-                if (lane >= off) sum += v;
-            }
-            const uint64_t behind = __ballot((before + sum) * segments > first);
-            if (behind != 0) {                                   // (it is in one of the rounds: first < total)
-                const int n = __builtin_ctzll(behind);
-                before += __builtin_amdgcn_readlane(sum - u, n);
-                units = __builtin_amdgcn_readlane(u, n);
-                b += n;
-                break;
-            }
-            before += __builtin_amdgcn_readlane(sum, 63);
-            b += 64;
-        }
-        segment = (first - before * segments) / units;
-        unit = first - before * segments - segment * units;
+        part = next;
     }
-    // (all of these are the same on every lane, which has to be said of quotients)
-    auto same = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
-    b = same(b); segment = same(segment); unit = same(unit); units = same(units); left = same(left);
-    for (;;) {
-        const int taken = min(units - unit, left);
-        // a segment that begins here: its first part's workgroup, and how many parts it has
-        if (a.workers > 0 && unit == 0 && threadIdx.x == 0)
-            a.part_of[(int64_t)b * segments + segment] = make_int2(blockIdx.x, 1 + (units - taken + share - 1) / share);
-        attend<D, CAP, FOLD>(a, lds, b, segment, unit, taken, units);
-        left -= taken;
-        if (left == 0) return;
-        unit = 0;
-        if (++segment == segments) {
-            segment = 0;
-            units = same(units_of(a, ++b));
-        }
-        __syncthreads();                                         // LDS is written anew
-    }
+#endif
 }
 
-// Joins the parts of the segments that have several: a workgroup to a row, groups of D/4 threads to a part, four channels each.
-template <int D>
+// Joins the parts of the segments that have several: WAVES wavefronts to a row, groups of D/4 lanes to a part, four channels each.
+// With few parts a row the kernel is three memory latencies: where the parts are, what they are, and the end.
+template <int D, int WAVES>
 __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedAttentionArgs a) {
-    constexpr int LANES = D / 4, GROUPS = 256 / LANES;
-    __shared__ float4 lds_x[GROUPS][LANES];
-    __shared__ float lds_m[4], lds_l[GROUPS];
-    const int64_t row = blockIdx.x, token = row / a.heads;
+    constexpr int LANES = D / 4, GROUPS = WAVES * 64 / LANES, AHEAD = 4;
+    __shared__ float lds[WAVES][LANES][6];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const uint32_t row = WAVES == 1 ? blockIdx.x * 4 + wave : blockIdx.x;            // (fewer than 2^31 rows)
+    if (row >= (uint32_t)a.B * a.q_len * a.heads) return;
+    const int64_t token = row / (uint32_t)a.heads;
     const int head = (int)(row - token * a.heads), b = (int)(token / a.q_len), j = (int)(token - (int64_t)b * a.q_len);
-    const int group = a.heads / a.kv_heads, row_tiles = (group * a.q_len + 15) / 16, in_kv = j * group + head % group;
-    const int2 where = a.part_of[((int64_t)b * a.kv_heads + head / group) * row_tiles + in_kv / 16];
+    const int in_kv = j * a.group + head % a.group;
+    const int2 where = a.part_of[((int64_t)b * a.kv_heads + head / a.group) * a.row_tiles + in_kv / 16];
     const int parts = where.y;
     if (parts <= 1) return;
-    const int piece = threadIdx.x % LANES, part0 = threadIdx.x / LANES, at_col = in_kv % 16;
-    auto slot = [&](int p) { return (2 * ((int64_t)where.x + p) + (p == 0)) * 16 + at_col; };
-    float best = UNSET;
-    for (int p = threadIdx.x; p < parts; p += 256) best = fmaxf(best, a.part_ml[slot(p)].x);
+    const int piece = lane % LANES, group0 = (WAVES == 1 ? 0 : wave * (64 / LANES)) + lane / LANES;
+    float best = UNSET, total = 0.0f, x[4] = {};
+    for (int p0 = group0; p0 < parts; p0 += AHEAD * GROUPS) {
+        float2 ml[AHEAD];
+        float4 o[AHEAD];
 #pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) best = fmaxf(best, __shfl_xor(best, off, 64));
-    if ((threadIdx.x & 63) == 0) lds_m[threadIdx.x >> 6] = best;
-    __syncthreads();
-    best = fmaxf(fmaxf(lds_m[0], lds_m[1]), fmaxf(lds_m[2], lds_m[3]));
-    float total = 0.0f;
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int p = part0; p < parts; p += GROUPS) {
-        const float2 ml = a.part_ml[slot(p)];
-        const float4 o = *reinterpret_cast<const float4*>(a.part_o + slot(p) * D + 4 * piece);
-        const float f = __builtin_amdgcn_exp2f(ml.x - best);
-        total = fmaf(ml.y, f, total);
-        x.x = fmaf(o.x, f, x.x); x.y = fmaf(o.y, f, x.y); x.z = fmaf(o.z, f, x.z); x.w = fmaf(o.w, f, x.w);
-    }
-    lds_x[part0][piece] = x;
-    if (piece == 0) lds_l[part0] = total;
-    __syncthreads();
-    if (part0 != 0) return;
+        for (int i = 0; i < AHEAD; ++i) {
+            const int p = p0 + i * GROUPS;
+            ml[i] = make_float2(UNSET, 0.0f);
+            o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (p < parts) {
+                const int64_t at = (2 * ((int64_t)where.x + p) + (p == 0)) * 16 + in_kv % 16;
+                ml[i] = a.part_ml[at];
+                o[i] = *reinterpret_cast<const float4*>(a.part_o + at * D + 4 * piece);
+            }
+        }
+        float next = best;
 #pragma unroll
-    for (int g = 1; g < GROUPS; ++g) {
-        const float4 o = lds_x[g][piece];
-        x.x += o.x; x.y += o.y; x.z += o.z; x.w += o.w;
-        total += lds_l[g];
+        for (int i = 0; i < AHEAD; ++i) next = fmaxf(next, ml[i].x);
+        const float back = __builtin_amdgcn_exp2f(best - next);
+        best = next;
+        total *= back;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) x[c] *= back;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const float f = __builtin_amdgcn_exp2f(ml[i].x - best), y[4] = {o[i].x, o[i].y, o[i].z, o[i].w};
+            total = fmaf(ml[i].y, f, total);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) x[c] = fmaf(y[c], f, x[c]);
+        }
     }
-    const float y[4] = {x.x, x.y, x.z, x.w};
-    finish<4>(a, token, head, D, 4 * piece, y, best, total);
+    // the groups of a wave, then the waves
+    auto join = [&](float m, float t, const float (&y)[4]) {
+        const float next = fmaxf(best, m), f = __builtin_amdgcn_exp2f(best - next), g = __builtin_amdgcn_exp2f(m - next);
+        best = next;
+        total = fmaf(total, f, t * g);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) x[c] = fmaf(x[c], f, y[c] * g);
+    };
+#pragma unroll
+    for (int off = LANES; off < 64; off <<= 1) {
+        float y[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) y[c] = __shfl_xor(x[c], off, 64);
+        join(__shfl_xor(best, off, 64), __shfl_xor(total, off, 64), y);
+    }
+    if constexpr (WAVES > 1) {
+        if (lane < LANES) {
+            float* mine = lds[wave][lane];
+            mine[0] = best; mine[1] = total;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) mine[2 + c] = x[c];
+        }
+        __syncthreads();
+        if (wave != 0) return;
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) {
+            const float* theirs = lds[w][piece];
+            const float y[4] = {theirs[2], theirs[3], theirs[4], theirs[5]};
+            join(theirs[0], theirs[1], y);
+        }
+    }
+    if (lane < LANES) finish<4>(a, token, head, D, 4 * piece, x, best, total);
 }
 
 template <int D>
 int launch(const PagedAttentionArgs& a, hipStream_t s) {
-    const int64_t segments = (int64_t)a.B * a.kv_heads * ((a.heads / a.kv_heads * a.q_len + 15) / 16);
+    const int64_t segments = (int64_t)a.B * a.kv_heads * a.row_tiles;
     const unsigned blocks = (unsigned)(a.workers > 0 ? a.workers : segments);
-    const bool fold = a.heads / a.kv_heads * a.q_len <= 8;
+    const bool fold = a.group * a.q_len <= 8;
     auto kernel = a.softcap > 0.0f ? fold ? paged_attention_kernel<D, true, true> : paged_attention_kernel<D, true, false>
                                    : fold ? paged_attention_kernel<D, false, true> : paged_attention_kernel<D, false, false>;
     hipLaunchKernelGGL(kernel, dim3(blocks), dim3(PA_WAVES * 64), 0, s, a);
     const int rc = check_hip(hipGetLastError(), "paged_attention launch");
     if (rc != BASQ_OK || a.workers == 0) return rc;
-    hipLaunchKernelGGL((paged_attention_join_kernel<D>), dim3((unsigned)((int64_t)a.B * a.q_len * a.heads)), dim3(256), 0, s, a);
+    // many rows have few parts each: a wavefront does
+    const int64_t rows = (int64_t)a.B * a.q_len * a.heads;
+    if (rows >= 512) hipLaunchKernelGGL((paged_attention_join_kernel<D, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((paged_attention_join_kernel<D, 4>), dim3((unsigned)rows), dim3(256), 0, s, a);
     return check_hip(hipGetLastError(), "paged_attention join launch");
 }
 
@@ -565,12 +667,14 @@ int paged_attention_workers(int32_t B, int32_t q_len, int32_t heads, int32_t kv_
     if (segments * units > 0x7FFFFFFFll || (int64_t)B * q_len * heads > 0x7FFFFFFFll) return -1;
     if (units <= 4) return 0;
     // as many as the chip holds at once
-    const int64_t most = head_dim == 64 ? 768 : 768;
+    const int64_t most = head_dim == 128 && heads / kv_heads * (int64_t)q_len > 8 ? 512 : 768;
     return (int)(segments * units < most ? segments * units : most);
 }
 
 int launch_paged_attention(PagedAttentionArgs a, hipStream_t s) {
     if (a.B == 0) return BASQ_OK;
+    a.group = a.heads / a.kv_heads;
+    a.row_tiles = (a.group * a.q_len + 15) / 16;
     a.cap_log2e = a.softcap * LOG2E;
     a.inv_cap = a.softcap > 0.0f ? 1.0f / a.cap_log2e : 0.0f;
     return a.D == 64 ? launch<64>(a, s) : launch<128>(a, s);
