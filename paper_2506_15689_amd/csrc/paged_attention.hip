@@ -7,20 +7,30 @@
 // so the codes go into the matrix cores as they are, and ranges into the scores and the weights: one pass over the cache, with the
 // running reference M of the softmax.
 //
-// Bound by reading the cache, D + 16 bytes a token and kv head.  A wavefront takes 32 tokens of one kv head at a time on 16 x 16 x 32
-// MFMAs whose 16 columns are the query rows that share the kv head (its heads, times the new tokens): tokens x channels of the keys
-// times channels x rows gives scores with the row on lane % 16, four tokens to a quarter of the wave and block of 16; these are, as
-// they lie, the weights' operand of channels x tokens of the values times tokens x rows, whose results keep the row on lane % 16.  So
-// no value changes lanes between the two products, and M, l and the rescaling are per lane.  The step's loads (codes and ranges) are
-// requested while the step before is worked on.
+// A wavefront takes 32 tokens of one kv head at a time on 16 x 16 x 32 MFMAs whose 16 columns are the query rows that share the kv head
+// (its heads, times the new tokens): tokens x channels of the keys times channels x rows gives scores with the row on lane % 16, four
+// tokens to a quarter of the wave and block of 16; these are, as they lie, the weights' operand of channels x tokens of the values
+// times tokens x rows, whose results keep the row on lane % 16.  So no value changes lanes between the two products, and M, l and the
+// rescaling are per lane.  Of up to eight rows, half the columns would be empty: there the rows stand twice, and a lane does one
+// block's softmax instead of two (166 vector instructions a step instead of 227).
 //
-// Codes become fp16 numbers without a conversion, two to an instruction.  The values' as they lie: a bit pattern of 0 .. 15, taken for
-// an fp16 number, is the code times 2^-24, and the code in the next nibble, left in place, 16 times that.  The matrix cores drop low
-// bits of products with such subnormal operands (2^-21 of the sum of magnitudes, 200 times what they do with others; measured), which
-// is nothing to a bf16 output but shows in lse; so the keys' codes are put into the mantissa of 1024, and 8 more than that subtracted.
-// Query rows are brought to fp16 times a power of two of their own (a bf16 value fits it exactly while it is within 2^-30 of the
-// row's largest); weights p_t vs_t are rounded to fp16 (2^-12 relative, against 2^-9 of the bf16 output) near 2^5 of their running
-// maximum, far from either end of fp16.  l, M and both sums are fp32.
+// Codes become fp16 numbers without a conversion, two to an instruction, by masks: a bit pattern of 0 .. 15, taken for an fp16 number,
+// is the code times 2^-24, and the code in the next nibble, left in place, 16 times that.  The matrix cores drop low bits of products
+// with subnormal operands, the more the smaller they are: with patterns of 0 .. 15 scores are 2.4e-6 off, with 16 times that 3.5e-7
+// (q of standard deviation 1.8, D = 128; fp32 arithmetic 2.5e-7), so the keys' codes are all brought to the second nibble; the values',
+// whose products end in bf16, are not.  Query rows are brought to fp16 times a power of two of their own (a bf16 value fits it exactly
+// while it is within 2^-30 of the row's largest); weights p_t vs_t are rounded to fp16 (2^-11 relative at most, against 2^-8 of the
+// bf16 output) near 2^5 of their running maximum, far from either end of fp16.  l, M and both sums are fp32.
+//
+// Codes and ranges come by direct loads into a ring of LDS stages that the wave has to itself, a step ahead of the one that is
+// worked on: registers hold none of it, and three workgroups of four waves fit a compute unit.  (Loads into registers, two
+// workgroups: 85 us for 64 contexts of 4340 tokens on average, 64 heads over 8; as built 66.)  The loads carry the non-temporal hint:
+// nothing is read twice (77 -> 66 us).
+//
+// Bound: reading the cache, D + 16 bytes a token and kv head, and nearly as much the vector instructions.  That workload is 327 MB and
+// takes 66 us, 4.9 TB/s; from a cache of one page, so without the memory, 55 us; a kernel that only reads as many bytes 49 us.
+// What is left is the start of a workgroup (5 us until its first loads are in: lengths, page ids, codes, one after the other), and
+// the end, when the workgroup of a compute unit that started first is done earlier than the others (39, 45 and 52 us).
 #include "basq_internal.h"
 
 #include <type_traits>
@@ -407,8 +417,8 @@ __global__ __launch_bounds__(PA_WAVES * 64, D == 128 && !FOLD ? 2 : 3) void page
             }
             best = row_max(best);
             const float up = (row_max(top) > 0x1p15f || !set) && best > -INFINITY ? best - 5.0f : 0.0f;
+            const float f = set ? __builtin_amdgcn_exp2f(-up) : 0.0f;            // (the sums of a row without a reference are 0)
             set = set || best > -INFINITY;
-            const float f = __builtin_amdgcn_exp2f(-up);
             M += up;
 #pragma unroll
             for (int r = 0; r < MINE; ++r) sc[r] -= up;

@@ -269,9 +269,10 @@ int launch_rope_append(const RopeAppendArgs& a, hipStream_t s) {
 }
 
 int launch_rope_table(float* out, int64_t rows, int32_t rot, const RopeScaling& k, hipStream_t s) {
+    if (rows == 0) return BASQ_OK;
     const int64_t blocks = (rows * (rot / 2) + 255) / 256;
     if (blocks > 0x7FFFFFFFll) return fail(BASQ_EUNSUPPORTED, "rope_table: too many positions");
-    if (blocks > 0) hipLaunchKernelGGL(rope_table_kernel, dim3((unsigned)blocks), dim3(256), 0, s, out, rows, rot, k);
+    hipLaunchKernelGGL(rope_table_kernel, dim3((unsigned)blocks), dim3(256), 0, s, out, rows, rot, k);
     return check_hip(hipGetLastError(), "rope_table launch");
 }
 

@@ -1,0 +1,159 @@
+"""The operators around the linear layer without a GPU: what they refuse, before anything would be launched."""
+import ctypes
+import os
+
+import pytest
+import torch
+
+from paper_2506_15689_amd import binding as B
+
+FAKE = ctypes.c_void_p(0x1000)
+ODD = ctypes.c_void_p(0x1008)
+BF16 = torch.bfloat16
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(B.LIB_PATH):
+        from paper_2506_15689_amd import build
+        build.build_lib(verbose=False)
+    return B.load()
+
+
+def norm(lib, **kw):
+    a = dict(X=FAKE, residual=FAKE, weight=FAKE, M=4, K=64, ldx=64, ldr=64, eps=1e-5, res_out=FAKE, ldro=64, Y=FAKE, ldy=64, Y8=None,
+             ldy8=0, y8_scale=None)
+    assert set(kw) <= set(a)
+    a.update(kw)
+    return lib.basq_add_rms_norm(*a.values(), None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(M=-1), B.BASQ_EINVAL), (dict(M=1 << 31), B.BASQ_EINVAL), (dict(K=0), B.BASQ_EINVAL), (dict(K=60), B.BASQ_EINVAL),
+    (dict(K=32776, ldx=32776), B.BASQ_EUNSUPPORTED), (dict(eps=-1.0), B.BASQ_EINVAL), (dict(eps=float("nan")), B.BASQ_EINVAL),
+    (dict(X=None), B.BASQ_EINVAL), (dict(X=ODD), B.BASQ_EINVAL), (dict(ldx=56), B.BASQ_EINVAL), (dict(ldx=68), B.BASQ_EINVAL),
+    (dict(residual=ODD), B.BASQ_EINVAL), (dict(ldr=60), B.BASQ_EINVAL), (dict(weight=None), B.BASQ_EINVAL),
+    (dict(res_out=ODD), B.BASQ_EINVAL), (dict(ldro=0), B.BASQ_EINVAL), (dict(Y=None), B.BASQ_EINVAL), (dict(Y=ODD), B.BASQ_EINVAL),
+    (dict(ldy=63), B.BASQ_EINVAL), (dict(Y8=FAKE, ldy8=64), B.BASQ_EINVAL), (dict(Y8=FAKE, ldy8=60, y8_scale=FAKE), B.BASQ_EINVAL),
+    (dict(Y8=ctypes.c_void_p(0x1004), ldy8=64, y8_scale=FAKE), B.BASQ_EINVAL),
+    (dict(Y8=FAKE, ldy8=64, y8_scale=ctypes.c_void_p(0x1002)), B.BASQ_EINVAL),
+])
+def test_norm_refuses(lib, kw, code):
+    assert norm(lib, **kw) == code and B.basq_last_error()
+
+
+def test_empty_calls_do_nothing(lib):
+    assert norm(lib, M=0, X=None, Y=None) == B.BASQ_OK
+    assert append(lib, T=0, q=None, k=None, v=None, q_out=None, positions=None, slots=None) == B.BASQ_OK
+    assert attention(lib, B=0, q=None, out=None, page_table=None, lengths=None) == B.BASQ_OK
+    assert lib.basq_rope_table(64, 0, 10000.0, 0, 1.0, 1.0, 2.0, 1.0, None, None) == B.BASQ_OK
+
+
+def append(lib, **kw):
+    a = dict(q=FAKE, ldq=512, k=FAKE, ldk=256, v=FAKE, ldv=256, T=4, heads=4, kv_heads=2, head_dim=128, positions=FAKE, cos_sin=FAKE,
+             table_rows=16, rot_dim=128, interleaved=0, rotate=1, clip_lo=0.9, clip_hi=0.9, bits=4, slots=FAKE, cache=FAKE, num_pages=4,
+             page_size=16, q_out=FAKE, ldqo=512, k_hat=None, v_hat=None, ldh=0)
+    assert set(kw) <= set(a)
+    a.update(kw)
+    return lib.basq_rope_append(*a.values(), None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(T=-1), B.BASQ_EINVAL), (dict(head_dim=96), B.BASQ_EUNSUPPORTED), (dict(heads=-1), B.BASQ_EINVAL),
+    (dict(heads=0, kv_heads=0), B.BASQ_EINVAL), (dict(bits=8), B.BASQ_EUNSUPPORTED), (dict(q=None), B.BASQ_EINVAL),
+    (dict(q=ODD), B.BASQ_EINVAL), (dict(ldq=504), B.BASQ_EINVAL), (dict(ldq=516), B.BASQ_EINVAL), (dict(k=None), B.BASQ_EINVAL),
+    (dict(v=None), B.BASQ_EINVAL), (dict(ldv=128), B.BASQ_EINVAL), (dict(q_out=None), B.BASQ_EINVAL), (dict(ldqo=0), B.BASQ_EINVAL),
+    (dict(positions=None), B.BASQ_EINVAL), (dict(slots=None), B.BASQ_EINVAL), (dict(cos_sin=ODD), B.BASQ_EINVAL),
+    (dict(table_rows=0), B.BASQ_EINVAL), (dict(rot_dim=0), B.BASQ_EUNSUPPORTED), (dict(rot_dim=24), B.BASQ_EUNSUPPORTED),
+    (dict(rot_dim=144), B.BASQ_EUNSUPPORTED), (dict(clip_lo=0.0), B.BASQ_EINVAL), (dict(clip_hi=1.5), B.BASQ_EINVAL),
+    (dict(cache=None), B.BASQ_EINVAL), (dict(cache=ODD), B.BASQ_EINVAL), (dict(num_pages=0), B.BASQ_EINVAL),
+    (dict(num_pages=1 << 27), B.BASQ_EINVAL), (dict(page_size=8), B.BASQ_EUNSUPPORTED), (dict(page_size=48), B.BASQ_EUNSUPPORTED),
+    (dict(page_size=2048), B.BASQ_EUNSUPPORTED), (dict(k_hat=FAKE, ldh=128), B.BASQ_EINVAL), (dict(v_hat=ODD, ldh=256), B.BASQ_EINVAL),
+    (dict(positions=ctypes.c_void_p(0x1002)), B.BASQ_EINVAL),
+])
+def test_append_refuses(lib, kw, code):
+    assert append(lib, **kw) == code and B.basq_last_error()
+
+
+@pytest.mark.parametrize("args", [
+    (0, 4, 1e4, 0, 1.0, 1.0, 2.0, 1.0), (63, 4, 1e4, 0, 1.0, 1.0, 2.0, 1.0), (64, -1, 1e4, 0, 1.0, 1.0, 2.0, 1.0),
+    (64, 4, 1.0, 0, 1.0, 1.0, 2.0, 1.0), (64, 4, 1e4, 1, 0.0, 1.0, 2.0, 1.0), (64, 4, 1e4, 2, 8.0, 4.0, 1.0, 8192.0),
+    (64, 4, 1e4, 3, 8.0, 1.0, 32.0, 0.0), (64, 4, float("inf"), 0, 1.0, 1.0, 2.0, 1.0),
+])
+def test_table_refuses(lib, args):
+    assert lib.basq_rope_table(*args, FAKE, None) == B.BASQ_EINVAL
+    assert lib.basq_rope_table(64, 4, 1e4, 4, 1.0, 1.0, 2.0, 1.0, FAKE, None) == B.BASQ_EUNSUPPORTED
+    assert lib.basq_rope_table(64, 4, 1e4, 0, 1.0, 1.0, 2.0, 1.0, None, None) == B.BASQ_EINVAL
+
+
+def attention(lib, **kw):
+    a = dict(q=FAKE, ldq=512, B=2, q_len=1, heads=4, kv_heads=2, head_dim=128, bits=4, cache=FAKE, num_pages=64, page_size=16,
+             page_table=FAKE, table_stride=32, lengths=FAKE, max_len=512, scale=0.1, softcap=0.0, window=0, out=FAKE, ldo=512, lse=None,
+             workspace=None, workspace_bytes=0)
+    assert set(kw) <= set(a)
+    a.update(kw)
+    return lib.basq_paged_attention(*a.values(), None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(B=-1), B.BASQ_EINVAL), (dict(q_len=0), B.BASQ_EINVAL), (dict(heads=0), B.BASQ_EINVAL), (dict(kv_heads=0), B.BASQ_EINVAL),
+    (dict(heads=5), B.BASQ_EINVAL), (dict(head_dim=256), B.BASQ_EUNSUPPORTED), (dict(bits=8), B.BASQ_EUNSUPPORTED),
+    (dict(max_len=-1), B.BASQ_EINVAL), (dict(max_len=513), B.BASQ_EINVAL), (dict(table_stride=-1), B.BASQ_EINVAL),
+    (dict(scale=float("inf")), B.BASQ_EINVAL), (dict(softcap=-1.0), B.BASQ_EINVAL), (dict(softcap=float("nan")), B.BASQ_EINVAL),
+    (dict(window=-1), B.BASQ_EINVAL), (dict(cache=None), B.BASQ_EINVAL), (dict(cache=ODD), B.BASQ_EINVAL), (dict(num_pages=0), B.BASQ_EINVAL),
+    (dict(page_size=24), B.BASQ_EUNSUPPORTED), (dict(q=None), B.BASQ_EINVAL), (dict(ldq=511), B.BASQ_EINVAL), (dict(out=None), B.BASQ_EINVAL),
+    (dict(ldo=256), B.BASQ_EINVAL), (dict(page_table=None), B.BASQ_EINVAL), (dict(lengths=None), B.BASQ_EINVAL),
+    (dict(lse=ctypes.c_void_p(0x1002)), B.BASQ_EINVAL),
+    (dict(B=1 << 20, max_len=1 << 19, table_stride=1 << 15), B.BASQ_EUNSUPPORTED),
+    # a call that splits its contexts needs a workspace
+    (dict(max_len=8192, table_stride=512), B.BASQ_EINVAL), (dict(max_len=8192, table_stride=512, workspace=ctypes.c_void_p(0x1010)), B.BASQ_EINVAL),
+    (dict(max_len=8192, table_stride=512, workspace=FAKE, workspace_bytes=64), B.BASQ_EWORKSPACE),
+])
+def test_attention_refuses(lib, kw, code):
+    assert attention(lib, **kw) == code and B.basq_last_error()
+
+
+def test_sizes(lib):
+    assert B.basq_kv_page_bytes(8, 128, 64) == 8 * 64 * 144 and B.basq_kv_page_bytes(1, 64, 16) == 16 * 80
+    assert [B.basq_kv_page_bytes(*s) for s in [(0, 128, 64), (8, 96, 64), (8, 128, 8), (8, 128, 48), (8, 128, 2048)]] == [0] * 5
+    W = B.basq_paged_attention_workspace_bytes
+    # short contexts (a window shortens them too) need none; longer ones no more than the workgroups' parts, whatever the batch
+    assert W(4, 1, 32, 8, 128, 512) == 0 and W(4, 1, 32, 8, 128, 100000, 300) == 0 and W(4, 1, 32, 8, 128, 100000, 1000) > 0
+    assert 0 < W(1, 1, 64, 8, 128, 131072) <= W(64, 1, 64, 8, 128, 131072) < 16 << 20
+    assert W(0, 1, 32, 8, 128, 512) == W(4, 0, 32, 8, 128, 512) == W(4, 1, 30, 8, 128, 512) == W(1 << 20, 1, 4, 2, 128, 1 << 19) == 0
+
+
+def test_binding_refuses_tensors_that_do_not_fit(lib):
+    """Shapes, types and layouts are checked before a raw pointer is passed."""
+    z = lambda *s, dtype=BF16: torch.zeros(s, dtype=dtype)  # noqa: E731
+    x, w = z(4, 64), z(64)
+    bad = [
+        lambda: B.basq_add_rms_norm(x, z(4, 56), w, 1e-5, z(4, 64)),
+        lambda: B.basq_add_rms_norm(x, None, z(56), 1e-5, z(4, 64)),
+        lambda: B.basq_add_rms_norm(x, None, w.float(), 1e-5, z(4, 64)),
+        lambda: B.basq_add_rms_norm(x, None, w, 1e-5, z(64, 4).t()),
+        lambda: B.basq_add_rms_norm(x, None, w, 1e-5, z(3, 64)),
+        lambda: B.basq_add_rms_norm(x, None, w, 1e-5, None, Y8=z(4, 64, dtype=torch.uint8), y8_scale=z(4, dtype=torch.float32)),
+        lambda: B.basq_add_rms_norm(x, None, w, 1e-5, None, Y8=z(4, 64, dtype=torch.float8_e4m3fn), y8_scale=z(3, dtype=torch.float32)),
+    ]
+    q, k, cache = z(3, 4, 64), z(3, 2, 64), z(5, 2, 16 * 80, dtype=torch.uint8)
+    i32 = lambda n: z(n, dtype=torch.int32)  # noqa: E731
+    table = z(8, 64, dtype=torch.float32)
+    good = dict(q=q, k=k, v=k, positions=i32(3), cos_sin=table, slots=i32(3), cache=cache, clip_lo=0.9, clip_hi=0.9, q_out=z(3, 4, 64))
+    for change in [dict(q_out=None), dict(q_out=z(3, 4, 32)), dict(v=None), dict(v=z(3, 4, 64)), dict(positions=z(3, dtype=torch.int64)),
+                   dict(positions=i32(2)), dict(slots=None), dict(slots=z(3, dtype=torch.int64)), dict(positions=None),
+                   dict(cache=z(5, 4, 16 * 80, dtype=torch.uint8)), dict(cache=z(5, 2, 1000, dtype=torch.uint8)), dict(cache=z(5, 2, 16 * 80)),
+                   dict(cos_sin=z(8, 64)), dict(q=z(3, 64, 4).transpose(1, 2)), dict(k_hat=z(3, 2, 32)),
+                   dict(k_hat=z(3, 2, 64), v_hat=z(3, 4, 64)[:, :2]), dict(q=None, k=None, v=None)]:
+        bad.append(lambda change=change: B.basq_rope_append(**{**good, **change}))
+    attend = dict(q=q, cache=cache, page_table=z(3, 4, dtype=torch.int32), lengths=i32(3), max_len=64, scale=0.1, out=z(3, 4, 64), workspace=None)
+    for change in [dict(max_len=65), dict(q_len=2), dict(lengths=z(3, dtype=torch.int64)), dict(page_table=z(3, 4, dtype=torch.int64)),
+                   dict(page_table=z(2, 4, dtype=torch.int32)), dict(out=z(3, 4, 32)), dict(lse=z(3, 4)), dict(lse=z(2, 4, dtype=torch.float32)),
+                   dict(cache=cache[:, :, :-16])]:
+        bad.append(lambda change=change: B.basq_paged_attention(**{**attend, **change}))
+    bad.append(lambda: B.basq_rope_table(z(8, 64), 1e4))
+    bad.append(lambda: B.alloc_kv_cache(4, 2, 96, 16, device="cpu"))
+    for n, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+            pytest.fail(f"call {n} was not refused")

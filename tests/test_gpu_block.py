@@ -1,0 +1,534 @@
+"""The operators around the linear layer on the GPU, against their definitions (block_ref.py).  Tolerances are stated where they are
+used, with what they follow from."""
+import math
+
+import pytest
+import torch
+
+from paper_2506_15689_amd import binding as B
+
+import block_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+BF16 = torch.bfloat16
+UNTOUCHED = 0xA5
+
+
+def gen(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def randn(g, *shape):
+    return torch.randn(shape, generator=g, device=DEV)
+
+
+def strided(t, pad):
+    """The same values in rows that are `pad` elements further apart."""
+    if pad == 0:
+        return t.contiguous()
+    M, width = t.shape[0], t[0].numel()
+    wide = torch.full((M, width + pad), 7.0, dtype=torch.float32, device=t.device).to(t.dtype)
+    view = wide[:, :width].unflatten(1, t.shape[1:]) if t.dim() == 3 else wide[:, :width]
+    view.copy_(t)
+    return view
+
+
+def check_stored(got, want, slack):
+    """bf16 values against fp64 ones that the arithmetic in front of the store may miss by `slack`: rounding is monotonic, so what is
+    stored lies between the roundings of the ends."""
+    got, low, high = ref.f64(got), (want - slack).to(BF16).double(), (want + slack).to(BF16).double()
+    bad = ~((got >= low) & (got <= high))
+    assert not bad.any(), f"{int(bad.sum())} of {bad.numel()} values; the furthest {float(((got - want).abs() / slack)[bad].max())} times the slack away"
+
+
+# ---- norm ----------------------------------------------------------------------------------------
+
+def check_norm(y, want):
+    # fp32: a sum of squares in runs of up to 64 and a tree behind, three roundings and rsqrt: under 2^-16
+    check_stored(y, want, want.abs() * 2.0 ** -16)
+
+
+@pytest.mark.parametrize("M,K", [(1, 8), (3, 520), (2, 512), (5, 1016), (4, 2048), (3, 2056), (61, 4096), (1, 8192), (7, 11008), (5, 14336), (2, 16392), (2, 32768)])
+@pytest.mark.parametrize("with_residual", [True, False])
+def test_norm(M, K, with_residual):
+    g = gen(M * K)
+    x, r = (randn(g, M, K) * 3).to(BF16), randn(g, M, K).to(BF16) if with_residual else None
+    w = (1 + 0.2 * randn(g, K)).to(BF16)
+    x = strided(x, 24)
+    r = strided(r, 8) if with_residual else None
+    y, h = strided(torch.zeros(M, K, dtype=BF16, device=DEV), 16), torch.zeros(M, K, dtype=BF16, device=DEV)
+    y8, s8 = torch.zeros(M, K + 8, dtype=torch.uint8, device=DEV).view(torch.float8_e4m3fn)[:, :K], torch.zeros(M, device=DEV)
+    B.basq_add_rms_norm(x, r, w, 1e-5, y, h, Y8=y8, y8_scale=s8)
+    want_h, want = ref.add_rms_norm(x, r, w, 1e-5)
+    assert torch.equal(h.cpu(), want_h)
+    check_norm(y, want)
+    if M > 1:
+        assert (y._base[:, K:] == 7).all(), "the gaps between rows were written"
+    top = want.abs().amax(1)
+    assert ((ref.f64(s8) - top / 448).abs() <= top / 448 * 2.0 ** -16).all()
+    # e4m3: half of a step, 2^-4 of a normal number, 2^-10 of the scale below; and fp32 in front
+    got = ref.f64(y8.float()) * ref.f64(s8)[:, None]
+    tol = torch.maximum(want.abs() * 2.0 ** -4, ref.f64(s8)[:, None] * 2.0 ** -10) * (1 + 2.0 ** -10)
+    assert ((got - want).abs() <= tol).all()
+    # either output alone, in place of the inputs
+    x2 = x.contiguous().clone()
+    r2 = None if r is None else r.contiguous().clone()
+    B.basq_add_rms_norm(x2, r2, w, 1e-5, x2, r2)
+    assert torch.equal(x2, y) and (r2 is None or torch.equal(r2, h))
+    y8b, s8b = torch.zeros_like(y8.contiguous()), torch.zeros_like(s8)
+    B.basq_add_rms_norm(x, r, w, 1e-5, None, Y8=y8b, y8_scale=s8b)
+    assert torch.equal(y8b.view(torch.uint8), y8.contiguous().view(torch.uint8)) and torch.equal(s8b, s8)
+
+
+def test_norm_of_unusual_rows():
+    """Zeros, infinities and NaN stay in their rows; tiny and huge rows are normed like others as far as fp32 squares go."""
+    g = gen(1)
+    K = 4096
+    x = randn(g, 8, K).to(BF16)
+    clean = x.clone()
+    x[1] = 0
+    x[2, 5] = float("inf")
+    x[3, 7] = float("nan")
+    x[4] *= 1e-15
+    x[5] *= 1e15
+    w = torch.ones(K, dtype=BF16, device=DEV)
+    y, y8, s8 = torch.empty_like(x), torch.empty(8, K, dtype=torch.float8_e4m3fn, device=DEV), torch.empty(8, device=DEV)
+    B.basq_add_rms_norm(x, None, w, 0.0, y, Y8=y8, y8_scale=s8)
+    y0 = torch.empty_like(x)
+    B.basq_add_rms_norm(clean, None, w, 0.0, y0)
+    for m in (0, 6, 7):
+        assert torch.equal(y[m], y0[m])
+    for m in (4, 5):
+        check_norm(y[m:m + 1], ref.add_rms_norm(x[m:m + 1], None, w, 0.0)[1])
+    assert torch.isnan(y[3]).all() and torch.isnan(y[2, 5])
+    B.basq_add_rms_norm(x, None, w, 1e-5, y, Y8=y8, y8_scale=s8)
+    assert (y[1] == 0).all() and (y8[1].float() == 0).all() and s8[1] == 1.0
+
+
+# ---- rotary positions, rotation, cache -----------------------------------------------------------
+
+@pytest.mark.parametrize("scaling,kw", [
+    (B.ROPE_PLAIN, {}), (B.ROPE_LINEAR, dict(factor=4.0)), (B.ROPE_BANDS, dict(factor=8.0, low=1.0, high=4.0, original_len=8192.0)),
+    (B.ROPE_YARN, dict(factor=16.0, low=1.0, high=32.0, original_len=4096.0)),
+])
+def test_rope_table(scaling, kw):
+    for rot, base, n in [(128, 500000.0, 1000), (32, 10000.0, 77), (2, 10000.0, 1)]:
+        t = torch.empty(n, rot, device=DEV)
+        B.basq_rope_table(t, base, scaling=scaling, **kw)
+        want = ref.rope_table(n, rot, base, scaling, **kw)
+        # fp64 inside (positions of a thousand: angles to 2^-40), rounded to fp32 once
+        assert ((ref.f64(t) - want).abs() <= 2.0 ** -24 * want.abs() + 2.0 ** -38).all()
+    t = torch.empty(1 << 20, 2, device=DEV)[-4:]                    # far positions, by the table's last rows
+    big = torch.empty(1 << 20, 16, device=DEV)
+    B.basq_rope_table(big, 10000.0, scaling=scaling, **kw)
+    want = ref.rope_table(1 << 20, 16, 10000.0, scaling, **kw)
+    assert ((ref.f64(big) - want).abs() <= 2.0 ** -24 * want.abs() + 2.0 ** -30).all()
+
+
+def append_case(seed, T, heads, kv_heads, D, P, rot, pages=None):
+    g = gen(seed)
+    x = randn(g, T, heads + 2 * kv_heads, D)
+    x[:, :, :3] += 5
+    x = x.to(BF16)
+    rows = 50
+    table = torch.empty(rows, rot, device=DEV) if rot else None
+    if rot:
+        B.basq_rope_table(table, 10000.0)
+    pages = pages or -(-2 * T // P) + 1
+    cache = torch.full((pages, max(kv_heads, 1), P * (D + 16)), UNTOUCHED, dtype=torch.uint8, device=DEV)
+    slots = torch.randperm(pages * P, generator=g, device=DEV)[:T].to(torch.int32)
+    positions = torch.randint(0, rows, (T,), generator=g, device=DEV, dtype=torch.int32)
+    return x, table, cache, slots, positions
+
+
+@pytest.mark.parametrize("T,heads,kv_heads,D,P,rot,interleaved,rotate", [
+    (1, 32, 32, 128, 64, 128, False, True),
+    (5, 8, 2, 128, 16, 64, True, True),
+    (37, 7, 1, 64, 32, 64, False, True),
+    (3, 71, 1, 64, 16, 16, True, False),
+    (130, 28, 4, 128, 128, 32, False, False),
+    (9, 5, 5, 64, 16, 0, False, True),
+    (2, 3, 3, 128, 1024, 112, False, True),
+    (11, 6, 6, 128, 16, 48, True, True),
+    (700, 2, 1, 128, 64, 128, False, True),
+    (4, 1, 9, 64, 16, 64, False, False),
+])
+def test_append_is_the_definition_bit_for_bit(T, heads, kv_heads, D, P, rot, interleaved, rotate):
+    x, table, cache, slots, positions = append_case(T * heads + D, T, heads, kv_heads, D, P, rot)
+    want_cache = cache.cpu().clone()
+    slots[0] = -1 if T > 2 else slots[0]                            # not stored
+    if T > 4:
+        slots[1] = cache.shape[0] * P                               # nor this one
+        positions[2], positions[3] = -1, 50                         # padding, if there are positions
+    q, k, v = x[:, :heads], x[:, heads:heads + kv_heads], x[:, heads + kv_heads:]
+    q_out = torch.full((T, heads, D), 9.0, dtype=BF16, device=DEV)
+    hats = [strided(torch.full((T, kv_heads, D), 9.0, dtype=BF16, device=DEV), 8) for _ in range(2)]
+    B.basq_rope_append(q, k, v, positions if rot else None, table, slots, cache, 0.9, 0.8, q_out, *hats, interleaved=interleaved, rotate=rotate)
+
+    skipped = torch.zeros(T, dtype=torch.bool)
+    if rot:
+        skipped = (positions.cpu() < 0) | (positions.cpu() >= 50)
+    keep = (~skipped)[:, None, None]
+    nine = torch.tensor(9.0, dtype=BF16)
+    want_q = ref.turn(q, table, positions, interleaved, rotate)
+    assert torch.equal(q_out.cpu(), torch.where(keep, want_q.to(BF16), nine))
+    stored = torch.where(skipped, torch.tensor(-1, dtype=torch.int32), slots.cpu())
+    for which, part in enumerate([ref.turn(k, table, positions, interleaved, rotate), v.cpu().float()]):
+        codes, s, lo = ref.quantise(part, 0.9, 0.8)
+        ref.put(want_cache, D, stored, which, codes, s, lo)
+        assert torch.equal(hats[which].cpu(), torch.where(keep, ref.dequantise(codes, s, lo).to(BF16), nine))
+    assert torch.equal(cache.cpu(), want_cache)
+    # and in 64 bits: the transform's sums of up to D values lose 2^-24 a stage, of the vector's length
+    exact = ref.turn(q, table, positions, interleaved, rotate, torch.float64)
+    length = q.cpu().double().norm(dim=-1, keepdim=True)
+    check_stored(q_out.cpu()[~skipped], exact[~skipped], (16 * 2.0 ** -24 * length + 0 * exact)[~skipped])
+
+
+def test_append_parts_and_places():
+    """q alone, keys and values alone, without a cache, in place: the same values as all together."""
+    T, heads, kv_heads, D, P = 33, 8, 4, 128, 16
+    x, table, cache, slots, positions = append_case(3, T, heads, kv_heads, D, P, 128)
+    q, k, v = x[:, :heads], x[:, heads:heads + kv_heads], x[:, heads + kv_heads:]
+    q_out = torch.empty(T, heads, D, dtype=BF16, device=DEV)
+    hats = [torch.empty(T, kv_heads, D, dtype=BF16, device=DEV) for _ in range(2)]
+    B.basq_rope_append(q, k, v, positions, table, slots, cache, 0.9, 0.9, q_out, *hats)
+    q2 = torch.empty_like(q_out)
+    B.basq_rope_append(q, None, None, positions, table, None, None, 0.9, 0.9, q2)
+    assert torch.equal(q2, q_out)
+    cache2 = torch.full_like(cache, UNTOUCHED)
+    B.basq_rope_append(None, k, v, positions, table, slots, cache2, 0.9, 0.9, None)
+    assert torch.equal(cache2, cache)
+    inplace = x.clone()
+    B.basq_rope_append(inplace[:, :heads], inplace[:, heads:heads + kv_heads], inplace[:, heads + kv_heads:], positions, table, None, None,
+                       0.9, 0.9, inplace[:, :heads], inplace[:, heads:heads + kv_heads], inplace[:, heads + kv_heads:])
+    assert torch.equal(inplace[:, :heads], q_out)
+    assert torch.equal(inplace[:, heads:heads + kv_heads], hats[0]) and torch.equal(inplace[:, heads + kv_heads:], hats[1])
+
+
+def test_append_of_unusual_vectors():
+    """Constant, zero, infinite and NaN vectors: the quantiser's rules for them, and no other vector changes."""
+    T, D, P = 6, 64, 16
+    x, _, cache, slots, _ = append_case(4, T, 1, 2, D, P, 0)
+    k, v = x[:, 1:3], x[:, 3:5]
+    k[0, 0], v[1, 1], v[2, 0], k[3, 1], v[4, 0, 5] = 0, 2.5, float("inf"), float("nan"), float("nan")
+    clean = cache.clone()
+    B.basq_rope_append(None, k, v, None, None, slots, cache, 0.9, 0.9, None, rotate=False)
+    codes, ranges = ref.cache_views(cache.cpu(), D)
+    place = [(s // P, s % P) for s in slots.tolist()]
+    at = lambda t, h, which: ranges[place[t][0], h, which, place[t][1]]  # noqa: E731
+    assert at(0, 0, 0).tolist() == [1.0, 0.0] and at(2, 0, 1)[0] == 1.0 and at(3, 1, 0)[0] == 1.0
+    # (a constant: 0.9 of it at both ends)
+    assert at(1, 1, 1).tolist() == [1.0, float(torch.tensor(0.9) * 2.5)]
+    for t, h, which, part in [(5, 0, 0, k), (5, 1, 1, v), (0, 1, 0, k), (1, 0, 1, v), (4, 1, 1, v)]:
+        want, s, lo = ref.quantise(part[t, h].cpu().float(), 0.9, 0.9)
+        c = codes[place[t][0], h, which, place[t][1]]
+        assert torch.equal(torch.stack([c & 15, c >> 4], -1).flatten().float(), want) and at(t, h, which).tolist() == [float(s), float(lo)]
+    assert not torch.equal(clean, cache)
+
+
+def test_append_agrees_with_the_per_head_quantiser():
+    """k without rotary positions is what basq_rotate_quant with rot_size = group_size = 128 makes of it, but for the order of sums."""
+    T, heads, D, P = 300, 4, 128, 64
+    x, _, cache, slots, _ = append_case(5, T, 0, heads, D, P, 0)
+    k, v = x[:, :heads].contiguous(), x[:, heads:]
+    B.basq_rope_append(None, k, v, None, None, slots, cache, 0.9, 0.9, None)
+    Aq = torch.empty(T, heads * D // 2, dtype=torch.uint8, device=DEV)
+    meta = torch.empty(T * heads, 4, dtype=torch.int32, device=DEV)
+    B.basq_rotate_quant(k.view(T, heads * D), D, None, None, 0.9, 0.9, Aq, meta, group_size=D)
+    codes, ranges = ref.cache_views(cache, D)
+    s = slots.long()
+    mine, theirs = codes[s // P, :, 0, s % P], Aq.view(T, heads, D // 2)
+    # another order of fp32 sums moves a code in some ten thousand at most
+    assert (mine != theirs).float().mean() <= 1e-4
+    r = meta.view(torch.float32).view(T, heads, 4)[..., :2]
+    torch.testing.assert_close(ranges[s // P, :, 0, s % P], r, rtol=1e-5, atol=1e-5)
+
+
+# ---- attention -----------------------------------------------------------------------------------
+
+def attention_case(seed, lengths, heads, kv_heads, D, P, q_len, spare=2, holes=0, scale_of_values=0.36):
+    """A cache whose pages are in random order, and whatever lies outside the contexts is 0xFF: codes of 15, ranges that are NaN."""
+    g = gen(seed)
+    Bn = len(lengths)
+    used = [max(-(-n // P), 0) for n in lengths]
+    pages = sum(used) + spare
+    cache = torch.full((pages, kv_heads, P * (D + 16)), 0xFF, dtype=torch.uint8, device=DEV)
+    codes, ranges = ref.cache_views(cache, D)
+    order = torch.randperm(pages, generator=g, device=DEV)
+    table = torch.full((Bn, max(used + [1]) + 1), -7, dtype=torch.int32, device=DEV)
+    at = 0
+    for b, n in enumerate(lengths):
+        mine = order[at:at + used[b]]
+        at += used[b]
+        table[b, :used[b]] = mine.to(torch.int32)
+        if n > 0:
+            t = torch.arange(n, device=DEV)
+            page, off = mine[t // P], t % P
+            codes[page, :, :, off] = torch.randint(0, 256, (n, kv_heads, 2, D // 2), generator=g, device=DEV, dtype=torch.uint8)
+            s = torch.exp(0.3 * randn(g, n, kv_heads, 2)) * 0.36
+            s[..., 1] *= scale_of_values / 0.36
+            ranges[page, :, :, off] = torch.stack([s, s * (-7.5 + 0.5 * randn(g, n, kv_heads, 2))], -1)
+    for _ in range(holes):                                           # pages that are not there
+        b = int(torch.randint(0, Bn, (1,), generator=g, device=DEV))
+        if used[b] > 1:
+            table[b, int(torch.randint(0, used[b], (1,), generator=g, device=DEV))] = pages if holes % 2 else -1
+            holes -= 1
+    q = (1.8 * randn(g, Bn * q_len, heads, D)).to(BF16)
+    return q, cache, table, torch.tensor(lengths, dtype=torch.int32, device=DEV)
+
+
+def attend(q, cache, table, lengths, max_len, q_len=1, softcap=0.0, window=0, scale=None, pad=0, guard=True):
+    rows, heads, D = q.shape
+    scale = 1 / math.sqrt(D) if scale is None else scale
+    need = B.basq_paged_attention_workspace_bytes(lengths.numel(), q_len, heads, cache.shape[1], D, max_len, window)
+    # (the workspace is full of NaN, and one byte longer would be seen)
+    ws = torch.full((need + 256,), 0xFF, dtype=torch.uint8, device=DEV)
+    out = strided(torch.full((rows, heads, D), 9.0, dtype=BF16, device=DEV), pad)
+    lse = torch.full((rows, heads), 9.0, device=DEV)
+    B.basq_paged_attention(q, cache, table, lengths, max_len, scale, out, ws[:need] if need else None, q_len=q_len, softcap=softcap, window=window, lse=lse)
+    if guard:
+        assert (ws[need:] == 0xFF).all()
+    return out, lse
+
+
+def check_attention(q, cache, table, lengths, max_len, q_len=1, softcap=0.0, window=0, scale=None, pad=0):
+    out, lse = attend(q, cache, table, lengths, max_len, q_len, softcap, window, scale, pad)
+    scale = 1 / math.sqrt(q.shape[2]) if scale is None else scale
+    want, want_lse, slack, slack_lse = ref.paged_attention(q, cache, table, lengths, max_len, scale, q_len, softcap, window)
+    got, got_lse = ref.f64(out), ref.f64(lse)
+    empty = torch.isinf(want_lse)
+    assert torch.equal(got_lse[empty], want_lse[empty]) and (got[empty] == 0).all()
+    check_stored(out.cpu()[~empty], want[~empty], slack[~empty])
+    err_lse = (got_lse - want_lse).abs()[~empty]
+    assert (err_lse <= slack_lse[~empty]).all(), f"lse: {float((err_lse / slack_lse[~empty]).max())} of the tolerance"
+    return out, lse
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("heads,kv_heads", [(4, 4), (16, 2), (9, 1), (16, 1), (35, 1), (14, 2)])
+def test_attention_lengths(heads, kv_heads, D):
+    """Lengths of zero, one, ends inside a block, a page, a unit and a step, and one behind; with one workgroup to a segment and with
+    shared work (which the bound on the lengths decides)."""
+    lengths = [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 300, 512]
+    case = attention_case(heads + D, lengths, heads, kv_heads, D, 16, 1)
+    a = check_attention(*case, 512, pad=8)
+    table = torch.nn.functional.pad(case[2], (0, 100), value=-7)
+    b = check_attention(case[0], case[1], table, case[3], 2000)
+    # the same work in other shares: other orders of fp32 sums
+    torch.testing.assert_close(a[1][2:], b[1][2:], rtol=0, atol=1e-5)
+
+
+@pytest.mark.parametrize("P", [16, 32, 64, 128, 1024])
+def test_attention_pages(P):
+    """Page sizes, long and ragged contexts, and pages that are not there."""
+    check_attention(*attention_case(P, [5000, 1, 2777, 0, 901, 64], 8, 2, 128, P, 1, holes=3), 5000)
+    check_attention(*attention_case(P + 1, [3001, 130], 4, 4, 64, P, 1, holes=1), 3001)
+
+
+@pytest.mark.parametrize("q_len,heads,kv_heads", [(2, 8, 2), (4, 28, 4), (5, 3, 1), (16, 2, 2), (33, 4, 1), (8, 71, 1)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_of_several_new_tokens(q_len, heads, kv_heads, D):
+    """Each new token sees those before it; a sequence may hold fewer tokens than there are new ones."""
+    case = attention_case(q_len + D, [q_len, 700, q_len - 1, 90, 1, 0], heads, kv_heads, D, 16, q_len)
+    check_attention(*case, 700, q_len)
+
+
+@pytest.mark.parametrize("window", [1, 15, 16, 17, 100, 128, 1000, 100000])
+@pytest.mark.parametrize("q_len", [1, 3])
+def test_attention_windows(window, q_len):
+    case = attention_case(window, [3, 16, 129, 1500, 0, 2100], 8, 4, 128, 32, q_len)
+    check_attention(*case, 2100, q_len, window=window)
+    check_attention(*case, 2100, q_len, window=window, softcap=20.0)
+
+
+def test_attention_with_many_new_tokens_in_a_window():
+    """Row tiles with different windows: most units of a segment are outside a tile's."""
+    check_attention(*attention_case(9, [900, 640], 4, 2, 64, 16, 300), 900, 300, window=70)
+
+
+@pytest.mark.parametrize("softcap", [1e-3, 5.0, 50.0, 1e6])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_softcap(softcap, D):
+    check_attention(*attention_case(7, [1, 40, 777], 12, 4, D, 16, 1), 777, softcap=softcap)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.1, 1e-6, 3.0])
+def test_attention_scales(scale):
+    """Score scales of zero, below zero, and so large that one token takes all."""
+    check_attention(*attention_case(8, [1, 700, 33], 8, 2, 128, 16, 1), 700, scale=scale)
+
+
+@pytest.mark.parametrize("size", [1e-12, 1e-4, 1e4, 1e12])
+def test_attention_of_small_and_large_values(size):
+    """Weights times scales are kept near the middle of fp16 whatever the values' scales are, also where they change on the way."""
+    check_attention(*attention_case(11, [900, 64], 8, 2, 128, 16, 1, scale_of_values=size), 900)
+    q, cache, table, lengths = attention_case(12, [900, 64], 8, 2, 128, 16, 1)
+    _, ranges = ref.cache_views(cache, 128)
+    ranges[::3, :, 1] *= size
+    check_attention(q, cache, table, lengths, 900)
+
+
+def test_attention_reference_moves():
+    """Scores that grow all along the context, by hundreds: the reference moves on again and again."""
+    q, cache, table, lengths = attention_case(13, [2000], 8, 1, 128, 16, 1)
+    codes, ranges = ref.cache_views(cache, 128)
+    P = 16
+    for t in range(0, 2000):
+        ranges[int(table[0, t // P]), :, 0, t % P] *= 1 + t / 50
+    check_attention(q, cache, table, lengths, 2000)
+
+
+def test_attention_of_zero_scales():
+    """Vectors whose scale is 0 stand for their lower bound, also where a page of zeros is attended to."""
+    q, cache, table, lengths = attention_case(14, [300, 40], 8, 2, 128, 16, 1)
+    _, ranges = ref.cache_views(cache, 128)
+    ranges[:, :, 1, 3::5, 0] = 0
+    ranges[:, :, 0, 1::7, 0] = 0
+    check_attention(q, cache, table, lengths, 300)
+    cache.zero_()
+    out, lse = attend(q, cache, table, lengths, 300)
+    assert (out == 0).all() and torch.allclose(lse[0], torch.full_like(lse[0], math.log(300)), atol=1e-5)
+
+
+def test_attention_clamps_lengths():
+    """More than max_len counts as max_len, less than nothing as nothing."""
+    q, cache, table, lengths = attention_case(15, [600, 600, 600], 8, 2, 64, 16, 1)
+    lengths.copy_(torch.tensor([600, 1 << 30, -5]))
+    check_attention(q, cache, table, lengths, 400)
+
+
+def test_attention_nan_stays_in_its_row():
+    """A NaN in a query, or in a range that is seen, reaches the rows that read it and no other."""
+    q, cache, table, lengths = attention_case(16, [300, 200, 900], 8, 2, 128, 16, 1)
+    good, good_lse = attend(q, cache, table, lengths, 900)
+    q2 = q.clone()
+    q2[1, 3, 7] = float("nan")
+    out, lse = attend(q2, cache, table, lengths, 900)
+    assert torch.isnan(out[1, 3]).all() and torch.isnan(lse[1, 3])
+    rest = torch.ones(3, 8, dtype=torch.bool)
+    rest[1, 3] = False
+    assert torch.equal(out[rest], good[rest]) and torch.equal(lse[rest], good_lse[rest])
+    _, ranges = ref.cache_views(cache, 128)
+    ranges[int(table[0, 2]), 1, 1, 5, 1] = float("nan")
+    out, _ = attend(q, cache, table, lengths, 900)
+    assert torch.isnan(out[0, 4:]).all()
+    assert torch.equal(out[0, :4], good[0, :4]) and torch.equal(out[1:], good[1:])
+
+
+def test_attention_of_infinite_query():
+    q, cache, table, lengths = attention_case(17, [40, 30], 4, 2, 64, 16, 1)
+    good, _ = attend(q, cache, table, lengths, 40)
+    q[0, 1, 0] = float("inf")
+    out, _ = attend(q, cache, table, lengths, 40)
+    assert torch.equal(out[0, 2:], good[0, 2:]) and torch.equal(out[1], good[1]) and torch.equal(out[0, 0], good[0, 0])
+
+
+def test_attention_many_sequences():
+    """More sequences than a wavefront has lanes, so that the shares are found in several rounds."""
+    lengths = [(37 * i) % 257 for i in range(200)]
+    check_attention(*attention_case(18, lengths, 4, 2, 64, 16, 1), 5000 if False else 272)
+    q, cache, table, lens = attention_case(19, lengths, 4, 2, 64, 16, 1)
+    table = torch.nn.functional.pad(table, (0, 400), value=-1)
+    check_attention(q, cache, table, lens, 5000)
+
+
+def test_attention_is_the_same_every_time_and_anywhere():
+    """Bits do not depend on the run, on where pages lie, or on the batch's other rows' values."""
+    q, cache, table, lengths = attention_case(20, [4000, 77, 1300], 16, 2, 128, 16, 1)
+    a = attend(q, cache, table, lengths, 4000)
+    for _ in range(3):
+        b = attend(q, cache, table, lengths, 4000)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    perm = torch.randperm(cache.shape[0], device=DEV)
+    moved = torch.empty_like(cache)
+    moved[perm] = cache
+    there = table >= 0
+    new_table = torch.where(there, perm[table.clamp(min=0).long()].to(torch.int32), table)
+    b = attend(q, moved, new_table, lengths, 4000)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_attention_past_four_gigabytes():
+    """Pages beyond the 32-bit range of byte offsets, and append to them."""
+    P, kv_heads, D = 64, 8, 128
+    page_bytes = B.basq_kv_page_bytes(kv_heads, D, P)
+    pages = (9 << 30) // page_bytes
+    cache = torch.empty((pages, kv_heads, P * (D + 16)), dtype=torch.uint8, device=DEV)
+    g = gen(21)
+    T = 200
+    ids = torch.tensor([pages - 1, pages // 2, 3, pages - 2], dtype=torch.int32, device=DEV)
+    cache[ids.long()] = 0xFF
+    k, v = randn(g, T, kv_heads, D).to(BF16), randn(g, T, kv_heads, D).to(BF16)
+    t = torch.arange(T, device=DEV)
+    slots = (ids.long()[t // P] * P + t % P).to(torch.int32)
+    B.basq_rope_append(None, k, v, None, None, slots, cache, 0.9, 0.9, None)
+    q = randn(g, 1, 16, D).to(BF16)
+    lengths = torch.tensor([T], dtype=torch.int32, device=DEV)
+    small = cache[ids.long()].clone()
+    here = torch.arange(4, dtype=torch.int32, device=DEV)[None]
+    want = check_attention(q, small, here, lengths, T)
+    for max_len in (T, 256):
+        out, lse = attend(q, cache, ids[None].contiguous(), lengths, max_len)
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
+def test_attention_output_may_be_the_query():
+    q, cache, table, lengths = attention_case(22, [700, 50], 8, 2, 128, 16, 1)
+    for max_len in (700, 512):
+        lengths.clamp_(max=max_len)
+        out, _ = attend(q, cache, table, lengths, max_len)
+        q2 = q.clone()
+        need = B.basq_paged_attention_workspace_bytes(2, 1, 8, 2, 128, max_len)
+        ws = torch.empty(need, dtype=torch.uint8, device=DEV) if need else None
+        B.basq_paged_attention(q2, cache, table, lengths, max_len, 1 / math.sqrt(128), q2, ws)
+        assert torch.equal(q2, out)
+
+
+def test_on_another_stream_and_in_a_graph():
+    """A whole step -- norm, append, attention -- on a side stream, and replayed from a graph between eager work."""
+    heads, kv_heads, D, P, Bn = 16, 4, 128, 16, 3
+    lengths = [900, 17, 333]
+    q0, cache, table, lens = attention_case(23, lengths, heads, kv_heads, D, P, 1)
+    g = gen(24)
+    x = randn(g, Bn, heads * D).to(BF16)
+    w = torch.ones(heads * D, dtype=BF16, device=DEV)
+    qkv = randn(g, Bn, heads + 2 * kv_heads, D).to(BF16)
+    cos_sin = torch.empty(1000, D, device=DEV)
+    B.basq_rope_table(cos_sin, 10000.0)
+    positions = lens - 1
+    slots = (table.long().gather(1, (positions // P).long()[:, None])[:, 0] * P + positions % P).to(torch.int32)
+    need = B.basq_paged_attention_workspace_bytes(Bn, 1, heads, kv_heads, D, 900)
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    bufs = [torch.empty_like(x), torch.empty_like(x), torch.empty(Bn, heads, D, dtype=BF16, device=DEV), torch.empty(Bn, heads, D, dtype=BF16, device=DEV)]
+
+    def step():
+        B.basq_add_rms_norm(x, x, w, 1e-5, bufs[0], bufs[1])
+        B.basq_rope_append(qkv[:, :heads], qkv[:, heads:heads + kv_heads], qkv[:, heads + kv_heads:], positions, cos_sin, slots, cache, 0.9, 0.9, bufs[2])
+        B.basq_paged_attention(bufs[2], cache, table, lens, 900, 1 / math.sqrt(D), bufs[3], ws)
+
+    step()
+    torch.cuda.synchronize()
+    want = [b.clone() for b in bufs]
+    side = torch.cuda.Stream()
+    for b in bufs:
+        b.zero_()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, bufs))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(4):
+        for b in bufs:
+            b.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, bufs))
+        step()
+        torch.cuda.synchronize()
