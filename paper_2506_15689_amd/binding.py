@@ -356,30 +356,21 @@ def basq_calibrate_bias(X: torch.Tensor, rot_size: int, act_scale: Optional[torc
 ROPE_PLAIN, ROPE_LINEAR, ROPE_BANDS, ROPE_YARN = 0, 1, 2, 3      # BASQ_ROPE_* of include/basq.h
 
 
-def _rows(t: torch.Tensor, shape, name: str, dtype=torch.bfloat16) -> int:
-    """The row stride of a tensor of this shape and type whose rows are contiguous.  (One row has no stride of its own.)"""
-    if t.shape != shape or t.dtype != dtype:
-        raise ValueError(f"{name} must be {dtype} {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
-    if len(shape) == 3:
-        width = shape[1] * shape[2]
-        contiguous = (t.stride(2) == 1 or shape[2] < 2) and (t.stride(1) == shape[2] or shape[1] < 2)
-    else:
-        width = shape[1]
-        contiguous = t.stride(1) == 1 or width < 2
-    if not contiguous and t.numel() > 0:
-        raise ValueError(f"the values of one row of {name} must lie side by side")
-    return t.stride(0) if shape[0] > 1 else width
+# Calls of a decode step are a few microseconds of GPU work each: their arguments are checked and marshalled in a compiled module.
+_block = None
 
 
-def _vector(t: torch.Tensor, n: int, name: str, dtype) -> None:
-    if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous {dtype} of {n} values, not {t.dtype} {tuple(t.shape)}")
-
-
-def _page_size(cache: torch.Tensor, D: int) -> int:
-    if cache.dtype != torch.uint8 or cache.dim() != 3 or not cache.is_contiguous() or cache.shape[2] % (D + 16) != 0:
-        raise ValueError(f"cache must be contiguous uint8 [pages, kv heads, page_size * {D + 16}], not {cache.dtype} {tuple(cache.shape)}")
-    return cache.shape[2] // (D + 16)
+def _load_block():
+    global _block
+    if _block is None:
+        load()
+        try:
+            from . import _block as module
+        except ImportError as e:
+            raise ImportError(f"{os.path.join(_PKG, '_block.so')} is missing or does not load: build it with "
+                              "`python -m paper_2506_15689_amd.build`; there is no fallback path") from e
+        _block = module
+    return _block
 
 
 def basq_add_rms_norm(X: torch.Tensor, residual: Optional[torch.Tensor], weight: torch.Tensor, eps: float,
@@ -387,21 +378,17 @@ def basq_add_rms_norm(X: torch.Tensor, residual: Optional[torch.Tensor], weight:
                       y8_scale: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
     """X, residual, res_out, Y bf16 [M, K] (any row strides); weight bf16 [K]; Y8 float8_e4m3fn [M, K] with y8_scale fp32 [M].
     res_out = X + residual, Y = its norm; res_out and Y may be X or residual."""
-    M, K = shape = X.shape
-    _vector(weight, K, "weight", torch.bfloat16)
-    if Y8 is not None and y8_scale is not None:
-        _vector(y8_scale, M, "y8_scale", torch.float32)
-    _check(load().basq_add_rms_norm(
-        _p(X), _p(residual), _p(weight), M, K, _rows(X, shape, "X"), 0 if residual is None else _rows(residual, shape, "residual"),
-        eps, _p(res_out), 0 if res_out is None else _rows(res_out, shape, "res_out"), _p(Y), 0 if Y is None else _rows(Y, shape, "Y"),
-        _p(Y8), 0 if Y8 is None else _rows(Y8, shape, "Y8", torch.float8_e4m3fn), _p(y8_scale), _stream(stream)))
+    rc = (_block or _load_block()).add_rms_norm(X, residual, weight, eps, Y, res_out, Y8, y8_scale, _stream, stream)
+    if rc != BASQ_OK:
+        _check(rc)
 
 
 def basq_rope_table(cos_sin: torch.Tensor, base: float, *, scaling: int = ROPE_PLAIN, factor: float = 1.0, low: float = 1.0,
                     high: float = 32.0, original_len: float = 8192.0, stream: Optional[torch.cuda.Stream] = None) -> None:
     """cos_sin fp32 [positions, rot_dim], filled with cosines, then sines, of every position."""
     positions, rot_dim = cos_sin.shape
-    _vector(cos_sin, positions * rot_dim, "cos_sin", torch.float32)
+    if cos_sin.dtype != torch.float32 or not cos_sin.is_contiguous() or not cos_sin.is_cuda:
+        raise ValueError(f"cos_sin must be contiguous fp32 on the GPU, not {cos_sin.dtype} {tuple(cos_sin.shape)}")
     _check(load().basq_rope_table(rot_dim, positions, base, scaling, factor, low, high, original_len, _p(cos_sin), _stream(stream)))
 
 
@@ -417,44 +404,10 @@ def basq_rope_append(q: Optional[torch.Tensor], k: Optional[torch.Tensor], v: Op
     """q, q_out bf16 [T, heads, D]; k, v, k_hat, v_hat bf16 [T, kv_heads, D] (any token strides, k_hat's and v_hat's the same);
     positions, slots int32 [T]; cos_sin fp32 [rows, rot_dim]; cache uint8 [pages, kv_heads, page_size * (D + 16)]
     (alloc_kv_cache).  q alone: k, v, slots and cache None; keys and values alone: q and q_out None."""
-    some = q if q is not None else k
-    if some is None or (k is None) != (v is None):
-        raise ValueError("q, or k and v, must be given")
-    T, _, D = some.shape
-    heads = ldq = ldqo = 0
-    if q is not None:
-        heads, ldq = q.shape[1], _rows(q, q.shape, "q")
-        if q_out is None:
-            raise ValueError("q_out must be given with q")
-        ldqo = _rows(q_out, q.shape, "q_out")
-    kv_heads = ldk = ldv = ldh = pages = page_size = 0
-    if k is not None:
-        shape = (T, k.shape[1], D)
-        kv_heads, ldk, ldv = k.shape[1], _rows(k, shape, "k"), _rows(v, shape, "v")
-        if cache is not None:
-            pages, page_size = cache.shape[0], _page_size(cache, D)
-            if cache.shape[1] != kv_heads:
-                raise ValueError(f"the cache has {cache.shape[1]} kv heads, k has {kv_heads}")
-            if slots is None:
-                raise ValueError("slots must be given with cache")
-            _vector(slots, T, "slots", torch.int32)
-        if k_hat is not None:
-            ldh = _rows(k_hat, shape, "k_hat")
-        if v_hat is not None:
-            ldv_hat = _rows(v_hat, shape, "v_hat")
-            if k_hat is not None and ldv_hat != ldh:
-                raise ValueError("k_hat and v_hat must have the same token stride")
-            ldh = ldv_hat
-    table_rows = rot_dim = 0
-    if cos_sin is not None:
-        table_rows, rot_dim = cos_sin.shape
-        _vector(cos_sin, table_rows * rot_dim, "cos_sin", torch.float32)
-        if positions is None:
-            raise ValueError("positions must be given with cos_sin")
-        _vector(positions, T, "positions", torch.int32)
-    _check(load().basq_rope_append(_p(q), ldq, _p(k), ldk, _p(v), ldv, T, heads, kv_heads, D, _p(positions), _p(cos_sin), table_rows,
-                                   rot_dim, interleaved, rotate, clip_lo, clip_hi, bits, _p(slots), _p(cache), pages, page_size,
-                                   _p(q_out), ldqo, _p(k_hat), _p(v_hat), ldh, _stream(stream)))
+    rc = (_block or _load_block()).rope_append(q, k, v, positions, cos_sin, slots, cache, clip_lo, clip_hi, q_out, k_hat, v_hat, interleaved,
+                                               rotate, bits, _stream, stream)
+    if rc != BASQ_OK:
+        _check(rc)
 
 
 def basq_paged_attention_workspace_bytes(B: int, q_len: int, heads: int, kv_heads: int, head_dim: int, max_len: int,
@@ -468,22 +421,10 @@ def basq_paged_attention(q: torch.Tensor, cache: torch.Tensor, page_table: torch
                          stream: Optional[torch.cuda.Stream] = None) -> None:
     """q, out bf16 [B * q_len, heads, D] (any token strides); cache uint8 [pages, kv_heads, page_size * (D + 16)]; page_table
     int32 [B, pages of a sequence] (any row stride); lengths int32 [B]; lse fp32 [B * q_len, heads] or None."""
-    rows, heads, D = q.shape
-    B = lengths.shape[0]
-    if rows != B * q_len:
-        raise ValueError(f"q has {rows} rows, {B} sequences of {q_len} new tokens need {B * q_len}")
-    if page_table.dtype != torch.int32 or page_table.dim() != 2 or page_table.shape[0] != B or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
-        raise ValueError(f"page_table must be int32 [{B}, pages of a sequence], not {page_table.dtype} {tuple(page_table.shape)}")
-    _vector(lengths, B, "lengths", torch.int32)
-    if lse is not None:
-        _vector(lse, rows * heads, "lse", torch.float32)
-    page_size = _page_size(cache, D)
-    if max_len > page_table.shape[1] * page_size:
-        raise ValueError(f"max_len = {max_len} is more than the {page_table.shape[1]} pages of {page_size} tokens of a sequence hold")
-    _check(load().basq_paged_attention(
-        _p(q), _rows(q, q.shape, "q"), B, q_len, heads, cache.shape[1], D, bits, _p(cache), cache.shape[0], page_size, _p(page_table),
-        page_table.stride(0) if B > 1 else page_table.shape[1], _p(lengths), max_len, scale, softcap, window, _p(out),
-        _rows(out, q.shape, "out"), _p(lse), _p(workspace), 0 if workspace is None else workspace.nbytes, _stream(stream)))
+    rc = (_block or _load_block()).paged_attention(q, cache, page_table, lengths, max_len, scale, out, workspace, q_len, softcap, window, lse,
+                                                   bits, _stream, stream)
+    if rc != BASQ_OK:
+        _check(rc)
 
 
 def basq_diag_stream(src: torch.Tensor, dst: torch.Tensor, meta: torch.Tensor, tokens: int, K: int, *,

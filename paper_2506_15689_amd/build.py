@@ -1,15 +1,18 @@
-"""Builds libbasq.so (the HIP kernels and the C ABI) for gfx950 with hipcc, in-tree."""
+"""Builds libbasq.so (the HIP kernels and the C ABI) for gfx950 with hipcc, and _block.so (a Python module on top of it, host code
+only) with the host compiler, both in-tree."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libbasq.so")
+BLOCK = os.path.join(PKG, "_block.so")
 
 SOURCES = ["api.hip", "hadamard28.hip", "rotate_quant.hip", "rotate_quant_pow2.hip", "rotate_quant_k28.hip", "rotate_quant_head.hip", "rotate_quant_block.hip", "gemm_w4a4.hip", "gemm_w4a4_direct.hip", "gemm_w4a4_fp6.hip", "gemm_w4a4_grouped.hip", "gemm_w4a4_grouped_fp6.hip", "gemm_w4a4_grouped_wide.hip", "fp6_pack.hip", "gemv_w4a4.hip", "linear_decode.hip", "linear_small.hip", "api_block.hip", "rms_norm.hip", "rope_append.hip", "paged_attention.hip", "weights.hip", "diag.hip"]
 
@@ -58,8 +61,32 @@ def _compile(src: str) -> str:
     return obj
 
 
+def _compile_block() -> str:
+    """The object of the Python module; it needs torch's headers, and no GPU."""
+    import torch
+    root = os.path.dirname(torch.__file__)
+    obj = os.path.join(BUILD, "binding_block.o")
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(root, "include"),
+           "-c", os.path.join(CSRC, "binding_block.cpp"), "-o", obj]
+    proc = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    if proc.returncode != 0:
+        raise RuntimeError("binding_block.cpp failed:\n" + proc.stdout)
+    return obj
+
+
+def _link_block(obj: str) -> None:
+    import torch
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+    cmd = [os.environ.get("CXX", "g++"), "-shared", "-o", BLOCK, obj, "-L", PKG, "-l:libbasq.so", "-Wl,-rpath,$ORIGIN",
+           "-L", libs, "-lc10", "-ltorch_cpu", "-ltorch_python", "-Wl,--no-as-needed"]
+    proc = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    if proc.returncode != 0:
+        raise RuntimeError("link of _block.so failed:\n" + proc.stdout)
+
+
 def build_lib(verbose: bool = True, extra_flags=(), out: str = LIB) -> str:
-    """Compile every translation unit and link libbasq.so.  Always recompiles.
+    """Compile every translation unit, link libbasq.so and the Python module.  Always recompiles.
     `extra_flags` (e.g. -D tuning macros) and `out` exist for tuning experiments."""
     global BUILD
     if out != LIB:
@@ -67,11 +94,14 @@ def build_lib(verbose: bool = True, extra_flags=(), out: str = LIB) -> str:
     os.makedirs(BUILD, exist_ok=True)
     HIPCC_FLAGS.extend(extra_flags)
     with ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as ex:
+        block = ex.submit(_compile_block) if out == LIB else None      # (a library of another name goes without the module)
         objs = list(ex.map(_compile, SOURCES))
     cmd = [_hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", "-Wl,-z,defs", "-o", out, *objs]
     proc = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     if proc.returncode != 0:
         raise RuntimeError("link failed:\n" + proc.stdout)
+    if block is not None:
+        _link_block(block.result())
     if verbose:
         print(f"built {out}")
     return out

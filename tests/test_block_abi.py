@@ -154,6 +154,15 @@ def test_binding_refuses_tensors_that_do_not_fit(lib):
     bad.append(lambda: B.basq_rope_table(z(8, 64), 1e4))
     bad.append(lambda: B.alloc_kv_cache(4, 2, 96, 16, device="cpu"))
     for n, call in enumerate(bad):
-        with pytest.raises(ValueError):
+        with pytest.raises(ValueError) as refused:
             call()
             pytest.fail(f"call {n} was not refused")
+        # by its own fault, not because all of this is on the CPU
+        assert "on the GPU of" not in str(refused.value), n
+    for call in [lambda: B.basq_add_rms_norm(x, None, w, 1e-5, z(4, 64)), lambda: B.basq_rope_append(**good), lambda: B.basq_paged_attention(**attend)]:
+        with pytest.raises(ValueError, match="is not on the GPU"):
+            call()
+    with pytest.raises(TypeError):
+        B.basq_add_rms_norm(x, None, w, "small", z(4, 64))
+    with pytest.raises(ValueError, match="must be a tensor"):
+        B.basq_add_rms_norm(x, None, w.tolist(), 1e-5, z(4, 64))
