@@ -19,7 +19,7 @@ namespace {
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef float v2f __attribute__((ext_vector_type(2)));
 
-constexpr int RA_WAVES = 4;
+constexpr int RA_WAVES = 4, AHEAD = 2;                           // steps of a wave under way
 
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v) {
@@ -144,15 +144,18 @@ __global__ __launch_bounds__(RA_WAVES * 64) void rope_append_kernel(RopeAppendAr
         const int head = head_of(step, kind);
         uint4 w = make_uint4(0, 0, 0, 0);
         const uint16_t* x = kind == 0 ? a.q + t * a.ldq : kind == 1 ? a.k + t * a.ldk : a.v + t * a.ldv;
-        if (head < (kind == 0 ? a.heads : a.kv_heads)) w = *reinterpret_cast<const uint4*>(x + head * D + c0);
+        if (head < (kind == 0 ? a.heads : a.kv_heads)) w = nt_load16(x + head * D + c0);
         return w;
     };
 
-    uint4 next = make_uint4(0, 0, 0, 0);
-    if (part * per < end) next = request(part * per);
+    uint4 next[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) next[i] = part * per + i < end ? request(part * per + i) : make_uint4(0, 0, 0, 0);
     for (int step = part * per; step < end; ++step) {
-        const uint4 w = next;
-        if (step + 1 < end) next = request(step + 1);
+        const uint4 w = next[0];
+#pragma unroll
+        for (int i = 0; i + 1 < AHEAD; ++i) next[i] = next[i + 1];
+        if (step + AHEAD < end) next[AHEAD - 1] = request(step + AHEAD);
         int kind;
         const int head = head_of(step, kind);
         float x[8];
@@ -178,7 +181,7 @@ __global__ __launch_bounds__(RA_WAVES * 64) void rope_append_kernel(RopeAppendAr
             if (a.rotate) hadamard<D>(x, lane, a.norm);
         }
         if (kind == 0) {
-            if (head < a.heads) *reinterpret_cast<uint4*>(a.q_out + t * a.ldqo + head * D + c0) = narrow(x);
+            if (head < a.heads) nt_store16(a.q_out + t * a.ldqo + head * D + c0, narrow(x));
             continue;
         }
         const float lo = a.clip_lo * over_head<D>(x, [](float u, float v) { return fminf(u, v); });
@@ -210,7 +213,7 @@ __global__ __launch_bounds__(RA_WAVES * 64) void rope_append_kernel(RopeAppendAr
                 x[2 * i] = fmaf(s, (float)((even >> (8 * i)) & 255u), lo);
                 x[2 * i + 1] = fmaf(s, (float)((odd >> (8 * i)) & 255u), lo);
             }
-            *reinterpret_cast<uint4*>(hat + t * a.ldh + head * D + c0) = narrow(x);
+            nt_store16(hat + t * a.ldh + head * D + c0, narrow(x));
         }
     }
 }
@@ -219,8 +222,9 @@ template <int D>
 int launch(const RopeAppendArgs& a, hipStream_t s) {
     constexpr int HEADS = 512 / D;
     const int steps = (a.heads + HEADS - 1) / HEADS + 2 * ((a.kv_heads + HEADS - 1) / HEADS);
-    // a wave to a token once that fills the chip, otherwise its steps are spread over several
-    int64_t parts = (4096 + a.T - 1) / a.T;
+    // eight thousand waves while a token has steps for several of them (32 a compute unit; 4096 tokens of 64 and 8 heads: 41.8 us with half
+    // as many and one step under way, 37.4 with twice as many, as built 35.4 .. 36.9), and one to a token from there on
+    int64_t parts = (8192 + a.T - 1) / a.T;
     if (parts > steps) parts = steps;
     const int per = (int)((steps + parts - 1) / parts);
     parts = (steps + per - 1) / per;
