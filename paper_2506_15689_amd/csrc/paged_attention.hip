@@ -49,6 +49,7 @@ typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 
 constexpr int PA_WAVES = 4, PA_STEP = 32;                        // tokens of a wave's step
 constexpr int PA_UNIT = PA_WAVES * PA_STEP;
+constexpr int PA_START = 2;                                       // what the start and the end of a part cost, in units
 constexpr int PA_STAGES = 2;                                      // steps of a wave in LDS
 constexpr float UNSET = -1e30f;                                  // M of a row that has seen no token
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
@@ -142,8 +143,9 @@ struct Part {
 };
 
 // Work is a row of units: sequence by sequence, in it segment by segment (kv head by kv head, row tile by row tile), in it token by
-// token.  With a.workers > 0 that many workgroups take equal shares of it, whatever the lengths are: a share begins and ends inside
-// segments, whose parts the second kernel joins.  Otherwise a workgroup takes a segment.
+// token; in front of each segment stand PA_START units that are no tokens, for what a part costs besides its tokens.  With a.workers > 0
+// that many workgroups take equal shares of it, whatever the lengths are: a share begins and ends inside segments, whose parts the
+// second kernel joins.  Otherwise a workgroup takes a segment.
 //
 // FOLD: tiles of at most eight rows, which stand in columns 0 .. 7 and again in 8 .. 15; a lane works on the first block's scores, or
 // on the second's, instead of on both.
@@ -164,17 +166,18 @@ __global__ __launch_bounds__(PA_WAVES * 64, D == 128 && !FOLD ? 2 : 3) void page
     const int64_t head_bytes = (int64_t)P * (D + 16);
 
     // ---- this workgroup's first part, and the units that it has to take
-    int b = 0, len, segment, unit = 0, units, left, share = 1;
+    int b = 0, len, segment, unit = 0, units, left, share = 1;   // left: with PA_START units for each segment that begins
     if (a.workers == 0) {
         b = blockIdx.x / segments;
         segment = blockIdx.x - b * segments;
         len = length_of(a, b);
-        left = units = units_of(a, len);
+        units = units_of(a, len);
+        left = units + PA_START;
     } else {
         int mine = 0, u = 0, sum = 0;                            // of sequence base + lane: length, units, units of all up to it
         auto scan = [&](int base) {
             mine = base + lane < a.B ? clamped(a, a.lengths[base + lane]) : 0;
-            u = base + lane < a.B ? units_of(a, mine) : 0;
+            u = base + lane < a.B ? units_of(a, mine) + PA_START : 0;
             sum = u;
             sum += __builtin_amdgcn_update_dpp(0, sum, 0x111, 0xF, 0xF, true);       // rows of 16 lanes: shifts by 1, 2, 4, 8
             sum += __builtin_amdgcn_update_dpp(0, sum, 0x112, 0xF, 0xF, true);
@@ -192,7 +195,7 @@ __global__ __launch_bounds__(PA_WAVES * 64, D == 128 && !FOLD ? 2 : 3) void page
         total *= segments;
         share = same((total + a.workers - 1) / a.workers);
         const int first = blockIdx.x * share;
-        left = min(share, total - first);
+        left = min(share, total - first);                        // (not above 0 behind the last)
         if (left <= 0) return;
         int before = 0;                                          // units of the sequences before b, that of unit `first`
         for (;;) {
@@ -201,7 +204,7 @@ __global__ __launch_bounds__(PA_WAVES * 64, D == 128 && !FOLD ? 2 : 3) void page
             if (behind != 0) {                                   // (it is in one of the rounds: first < total)
                 const int n = __builtin_ctzll(behind);
                 before += __builtin_amdgcn_readlane(sum - u, n);
-                units = __builtin_amdgcn_readlane(u, n);
+                units = __builtin_amdgcn_readlane(u, n) - PA_START;
                 len = __builtin_amdgcn_readlane(mine, n);
                 b += n;
                 break;
@@ -209,14 +212,21 @@ __global__ __launch_bounds__(PA_WAVES * 64, D == 128 && !FOLD ? 2 : 3) void page
             before += these;
             b += 64;
         }
-        segment = (first - before * segments) / units;
-        unit = first - before * segments - segment * units;
+        segment = (first - before * segments) / (units + PA_START);
+        unit = first - before * segments - segment * (units + PA_START) - PA_START;
+        if (unit < 0) {                                          // some of the start is this share's
+            left += unit + PA_START;
+            unit = 0;
+        } else {
+            left += PA_START;
+        }
+        if (left <= PA_START) return;
     }
 
     auto describe = [&](int b, int len, int segment, int unit, int units, int left) {
         Part p;
         p.b = b; p.len = len; p.segment = segment; p.unit = unit; p.units = units;
-        p.taken = min(units - unit, left);
+        p.taken = min(units - unit, left - PA_START);
         p.kv_head = row_tiles == 1 ? segment : same(segment / row_tiles);
         p.row_tile = segment - p.kv_head * row_tiles;
         const int seen = len - (a.q_len - 1);                     // tokens that the first new token sees
@@ -528,10 +538,10 @@ __global__ __launch_bounds__(PA_WAVES * 64, D == 128 && !FOLD ? 2 : 3) void page
     load_first(part, part.from + wave * PA_STEP);
     left = same(left);
     for (;;) {
-        left -= part.taken;
+        left -= part.taken + PA_START;
         Part next = part;
         int next_ids = -1;
-        if (left > 0) {
+        if (left > PA_START) {
             const bool same_b = part.segment + 1 < segments;
             const int next_b = same_b ? part.b : part.b + 1, next_len = same_b ? part.len : length_of(a, next_b);
             next = describe(next_b, next_len, same_b ? part.segment + 1 : 0, 0, same_b ? part.units : units_of(a, next_len), left);
@@ -555,13 +565,13 @@ __global__ __launch_bounds__(PA_WAVES * 64, D == 128 && !FOLD ? 2 : 3) void page
             }
         }
         wait_loads<0>();
-        if (left > 0) {
+        if (left > PA_START) {
             request_row(next);
             take_ids(next, next_ids);
             load_first(next, next.from + wave * PA_STEP);
         }
         finish_part(part);
-        if (left <= 0) return;
+        if (left <= PA_START) return;
         part = next;
     }
 #endif
@@ -674,7 +684,7 @@ int paged_attention_workers(int32_t B, int32_t q_len, int32_t heads, int32_t kv_
     // (a window is cut to whole blocks of 16 at its begin, and rows have windows up to q_len - 1 tokens apart)
     const int64_t range = window > 0 && window + (int64_t)q_len + 15 < max_len ? window + (int64_t)q_len + 15 : max_len;
     const int64_t units = range > PA_UNIT ? (range + PA_UNIT - 1) / PA_UNIT : 1;
-    if (segments * units > 0x7FFFFFFFll || (int64_t)B * q_len * heads > 0x7FFFFFFFll) return -1;
+    if (segments * (units + PA_START) > 0x7FFFFFFFll || (int64_t)B * q_len * heads > 0x7FFFFFFFll) return -1;
     if (units <= 4) return 0;
     // as many as the chip holds at once
     const int64_t most = head_dim == 128 && heads / kv_heads * (int64_t)q_len > 8 ? 512 : 768;
