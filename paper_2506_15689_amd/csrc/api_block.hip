@@ -153,7 +153,10 @@ int basq_rope_append(const void* q, int64_t ldq, const void* k, int64_t ldk, con
 size_t basq_paged_attention_workspace_bytes(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t head_dim,
                                             int32_t max_len, int32_t window) {
     if (B < 1 || q_len < 1 || heads < 1 || kv_heads < 1 || heads % kv_heads != 0 || (head_dim != 64 && head_dim != 128) || max_len < 0) return 0;
-    const int workers = paged_attention_workers(B, q_len, heads, kv_heads, head_dim, max_len, window);
+    // (whether scores are capped is not known here: what the larger of both needs)
+    int workers = paged_attention_workers(B, q_len, heads, kv_heads, head_dim, max_len, window, false);
+    const int capped = paged_attention_workers(B, q_len, heads, kv_heads, head_dim, max_len, window, true);
+    if (capped > workers) workers = capped;
     return workers < 0 ? 0 : parts_bytes(workers, head_dim, attention_segments(B, q_len, heads, kv_heads));
 }
 
@@ -181,7 +184,7 @@ int basq_paged_attention(const void* q, int64_t ldq, int32_t B, int32_t q_len, i
     if (rc != BASQ_OK) return rc;
     if ((max_len > 0 && !page_table) || !lengths || !aligned(page_table, 4) || !aligned(lengths, 4) || !aligned(lse, 4))
         return fail(BASQ_EINVAL, "page_table and lengths must be given; they and lse must be 4-byte aligned");
-    a.workers = paged_attention_workers(B, q_len, heads, kv_heads, head_dim, max_len, window);
+    a.workers = paged_attention_workers(B, q_len, heads, kv_heads, head_dim, max_len, window, softcap > 0.0f);
     if (a.workers < 0) return fail(BASQ_EUNSUPPORTED, "2^31 or more parts of 128 tokens, or rows of a head");
     const size_t need = parts_bytes(a.workers, head_dim, attention_segments(B, q_len, heads, kv_heads));
     if (need > 0) {

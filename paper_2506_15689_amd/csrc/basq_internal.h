@@ -180,7 +180,7 @@ struct PagedAttentionArgs {
     float inv_cap, cap_log2e; // these four are set by the launcher
     int32_t group, row_tiles; // heads of a kv head, tiles of 16 of its query rows
 };
-int paged_attention_workers(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t max_len, int32_t window);
+int paged_attention_workers(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t max_len, int32_t window, bool cap);
 int launch_paged_attention(PagedAttentionArgs a, hipStream_t s);  // paged_attention.hip
 
 // 28 x 28 Paley type-I matrix, row-major, built on the host at first use (hadamard28.hip).

@@ -346,14 +346,6 @@ __global__ __launch_bounds__(PA_WAVES * 64, D == 128 && !FOLD ? 2 : 3) void page
         v = quarters_max(v);
         return FOLD ? fmaxf(v, __shfl_xor(v, 8, 64)) : v;
     };
-    // log2(e) cap tanh(y), y = x / (log2(e) cap): tanh(y) = 1 - 2 / (e^2y + 1), whose rounding near 0 is that of 1, and there its
-    // series, 2^-23 of the value off at most up to 1/4
-    auto capped = [&](float x) {
-        const float y = x * a.inv_cap, y2 = y * y;
-        const float far = 1.0f - 2.0f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * (2.0f * LOG2E)) + 1.0f);
-        const float near = y * fmaf(y2, fmaf(y2, fmaf(y2, fmaf(y2, 62.0f / 2835, -17.0f / 315), 2.0f / 15), -1.0f / 3), 1.0f);
-        return a.cap_log2e * (fabsf(y) < 0.25f ? near : far);
-    };
     auto work = [&](const Part& part, int i, int t, int stage) {
         const uint8_t* blocks = ring + stage * 2 * Block<D>::BYTES;
         v4f acc[2];
@@ -381,14 +373,37 @@ __global__ __launch_bounds__(PA_WAVES * 64, D == 128 && !FOLD ? 2 : 3) void page
                 const v4f vr = __builtin_bit_cast(v4f, *reinterpret_cast<const v4i*>(ranges + 128 + 8 * r));
 #pragma unroll
                 for (int n = 0; n < 2; ++n) {
-                    // less M; with a cap, M goes off behind it
+                    // less M; with a cap, M goes off behind that
                     const float x = fmaf(kr[2 * n], acc[h][r + n] * c1, CAP ? kr[2 * n + 1] * qs : fmaf(kr[2 * n + 1], qs, -M));
-                    sc[4 * h + r + n] = CAP ? capped(x) - M : x;
+                    sc[4 * h + r + n] = x;
                     vs[4 * h + r + n] = vr[2 * n];
                     vl[4 * h + r + n] = vr[2 * n + 1];
                     least = fminf(least, vr[2 * n]);
                 }
             }
+        }
+        if constexpr (CAP) {
+            // log2(e) cap tanh(y), y = x / (log2(e) cap).  Up to 3/8 by its series, under 2^-24 of the value off, which is all that most
+            // steps need; beyond, 1 - 2 / (e^2y + 1), whose rounding is that of 1.
+            bool far = false;
+            float y[MINE];
+#pragma unroll
+            for (int n = 0; n < MINE; ++n) {
+                y[n] = sc[n] * a.inv_cap;
+                far = far || !(fabsf(y[n]) < 0.375f);
+                const float y2 = y[n] * y[n];
+                sc[n] = y[n] * fmaf(y2, fmaf(y2, fmaf(y2, fmaf(y2, fmaf(y2, -1382.0f / 155925, 62.0f / 2835), -17.0f / 315), 2.0f / 15), -1.0f / 3), 1.0f);
+            }
+            if (__any(far)) {
+                asm volatile("");
+#pragma unroll
+                for (int n = 0; n < MINE; ++n) {
+                    const float t = 1.0f - 2.0f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y[n] * (2.0f * LOG2E)) + 1.0f);
+                    sc[n] = fabsf(y[n]) < 0.375f ? sc[n] : t;
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < MINE; ++n) sc[n] = fmaf(sc[n], a.cap_log2e, -M);
         }
         const unsigned both = (unsigned)(there >> (2 * i)) & 3u;
         if (both != 3u || t < part.inner_begin || t + PA_STEP > part.inner_end) {
@@ -677,17 +692,31 @@ int launch(const PagedAttentionArgs& a, hipStream_t s) {
 
 }  // namespace
 
-// Short contexts, whose segments one workgroup each takes in a few steps, go without the second launch; -1 where there are too many
-// units to be numbered.
-int paged_attention_workers(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t max_len, int32_t window) {
+// How many workgroups share the work; 0 where each takes a segment, which goes without the second launch; -1 where there are too many
+// units to be numbered.  Both in microseconds behind the start: a unit takes a workgroup 0.73 while it has a compute unit to itself or
+// nearly so, and 0.47 for each of the two or three that it has for company; the second launch and the parts' ends are 6.  Measured, one
+// workgroup to a segment against shares, contexts of one length: 32 segments of 512, 1024, 2048 tokens 7.7, 10.6, 16.2 us (of 512,
+// always one each), 10.5, 11.4; 256 segments of 640, 1024, 2048 tokens 9.0, 11.1, 16.8 against 14.0, 15.8, 20.3.  But a context that is
+// longer than the others keeps its workgroup alone, and shares do not mind: they are taken to have 55 % of the longest's work.
+int paged_attention_workers(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t max_len, int32_t window, bool cap) {
     const int64_t segments = (int64_t)B * kv_heads * (((int64_t)(heads / kv_heads) * q_len + 15) / 16);
     // (a window is cut to whole blocks of 16 at its begin, and rows have windows up to q_len - 1 tokens apart)
     const int64_t range = window > 0 && window + (int64_t)q_len + 15 < max_len ? window + (int64_t)q_len + 15 : max_len;
     const int64_t units = range > PA_UNIT ? (range + PA_UNIT - 1) / PA_UNIT : 1;
     if (segments * (units + PA_START) > 0x7FFFFFFFll || (int64_t)B * q_len * heads > 0x7FFFFFFFll) return -1;
-    if (units <= 4) return 0;
     // as many as the chip holds at once
     const int64_t most = head_dim == 128 && heads / kv_heads * (int64_t)q_len > 8 ? 512 : 768;
+    constexpr double CUS = 256, EACH = 0.47, JOIN = 6.0, FILLED = 0.55;
+    const double ALONE = cap ? 0.95 : 0.73;                      // (a tanh a score)
+    auto unit_us = [&](double workgroups) {
+        const double company = (workgroups < (double)most ? workgroups : (double)most) / CUS * EACH;
+        return company > ALONE ? company : ALONE;
+    };
+    const double rounds = segments > most ? (double)segments / (double)most : 1.0;
+    const int64_t share = (segments * (units + PA_START) + most - 1) / most;
+    const double segment_each = (double)units * unit_us((double)segments) * rounds;
+    const double shared = JOIN + FILLED * (double)share * unit_us((double)(segments * units));
+    if (units <= 4 || segment_each <= shared) return 0;
     return (int)(segments * units < most ? segments * units : most);
 }
 
