@@ -495,6 +495,7 @@ __global__ __launch_bounds__(PA_WAVES * 64, D == 128 && !FOLD ? 2 : 3) void page
         }
     };
 
+    bool joined = false;
     // ---- the four waves' sums into one: written at each wave's own reference, read at the largest
     auto finish_part = [&](const Part& p) {
         // a segment that begins here: its first part's workgroup, and how many parts it has
@@ -506,7 +507,8 @@ __global__ __launch_bounds__(PA_WAVES * 64, D == 128 && !FOLD ? 2 : 3) void page
             l += __shfl_xor(l, 8, 64);
             lows += __shfl_xor(lows, 8, 64);
         }
-        lds_barrier();                                            // the part before is read
+        if (joined) lds_barrier();                                // the part before is read
+        joined = true;
         if (col < ROWS) {
             if (quarter == 0) {
                 lds.ml[wave][0][col] = __float_as_int(set ? M : UNSET);
@@ -593,10 +595,10 @@ __global__ __launch_bounds__(PA_WAVES * 64, D == 128 && !FOLD ? 2 : 3) void page
 }
 
 // Joins the parts of the segments that have several: WAVES wavefronts to a row, groups of D/4 lanes to a part, four channels each.
-// With few parts a row the kernel is three memory latencies: where the parts are, what they are, and the end.
+// It is memory latencies: where the parts are, and what they are, all of them (up to 128 of D = 128 with eight waves) at once.
 template <int D, int WAVES>
-__global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedAttentionArgs a) {
-    constexpr int LANES = D / 4, GROUPS = WAVES * 64 / LANES, AHEAD = 4;
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void paged_attention_join_kernel(PagedAttentionArgs a) {
+    constexpr int LANES = D / 4, GROUPS = WAVES * 64 / LANES, AHEAD = WAVES == 1 ? 4 : 8;
     __shared__ float lds[WAVES][LANES][6];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const uint32_t row = WAVES == 1 ? blockIdx.x * 4 + wave : blockIdx.x;            // (fewer than 2^31 rows)
@@ -686,7 +688,7 @@ int launch(const PagedAttentionArgs& a, hipStream_t s) {
     // many rows have few parts each: a wavefront does
     const int64_t rows = (int64_t)a.B * a.q_len * a.heads;
     if (rows >= 512) hipLaunchKernelGGL((paged_attention_join_kernel<D, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((paged_attention_join_kernel<D, 4>), dim3((unsigned)rows), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((paged_attention_join_kernel<D, 8>), dim3((unsigned)rows), dim3(512), 0, s, a);
     return check_hip(hipGetLastError(), "paged_attention join launch");
 }
 
