@@ -145,7 +145,7 @@ struct Part {
 // Work is a row of units: sequence by sequence, in it segment by segment (kv head by kv head, row tile by row tile), in it token by
 // token; in front of each segment stand PA_START units that are no tokens, for what a part costs besides its tokens.  With a.workers > 0
 // that many workgroups take equal shares of it, whatever the lengths are: a share begins and ends inside segments, whose parts the
-// second kernel joins.  Otherwise a workgroup takes a segment.
+// second kernel joins.  Otherwise a workgroup takes whole segments, every gridDim.x-th.
 //
 // FOLD: tiles of at most eight rows, which stand in columns 0 .. 7 and again in 8 .. 15; a lane works on the first block's scores, or
 // on the second's, instead of on both.
@@ -554,14 +554,25 @@ __global__ __launch_bounds__(PA_WAVES * 64, D == 128 && !FOLD ? 2 : 3) void page
     request_row(part);
     load_first(part, part.from + wave * PA_STEP);
     left = same(left);
+    uint32_t round = 1;
     for (;;) {
         left -= part.taken + PA_START;
+        const bool more = a.workers > 0 ? left > PA_START : (uint32_t)blockIdx.x + round * gridDim.x < (uint32_t)(a.B * segments);
         Part next = part;
         int next_ids = -1;
-        if (left > PA_START) {
-            const bool same_b = part.segment + 1 < segments;
-            const int next_b = same_b ? part.b : part.b + 1, next_len = same_b ? part.len : length_of(a, next_b);
-            next = describe(next_b, next_len, same_b ? part.segment + 1 : 0, 0, same_b ? part.units : units_of(a, next_len), left);
+        if (more) {
+            int next_b = part.b, next_segment = part.segment + 1;
+            if (a.workers == 0) {
+                const int index = blockIdx.x + round++ * gridDim.x;
+                next_b = same(index / segments);
+                next_segment = index - next_b * segments;
+            } else if (next_segment == segments) {
+                ++next_b;
+                next_segment = 0;
+            }
+            const int next_len = next_b == part.b ? part.len : length_of(a, next_b), next_units = units_of(a, next_len);
+            if (a.workers == 0) left = next_units + PA_START;
+            next = describe(next_b, next_len, next_segment, 0, next_units, left);
             next_ids = request_ids(next, next.from + wave * PA_STEP);
         }
         start(part);
@@ -582,13 +593,13 @@ __global__ __launch_bounds__(PA_WAVES * 64, D == 128 && !FOLD ? 2 : 3) void page
             }
         }
         wait_loads<0>();
-        if (left > PA_START) {
+        if (more) {
             request_row(next);
             take_ids(next, next_ids);
             load_first(next, next.from + wave * PA_STEP);
         }
         finish_part(part);
-        if (left <= PA_START) return;
+        if (!more) return;
         part = next;
     }
 #endif
@@ -675,10 +686,22 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void paged_attention
     if (lane < LANES) finish<4>(a, token, head, D, 4 * piece, x, best, total);
 }
 
+// units of the longest context that there can be (a window is cut to whole blocks of 16 at its begin, and rows have windows up to
+// q_len - 1 tokens apart)
+int64_t longest_units(int32_t q_len, int32_t max_len, int32_t window) {
+    const int64_t range = window > 0 && window + (int64_t)q_len + 15 < max_len ? window + (int64_t)q_len + 15 : max_len;
+    return range > PA_UNIT ? (range + PA_UNIT - 1) / PA_UNIT : 1;
+}
+// workgroups that the chip holds at once, `rows` query rows to a kv head
+int resident(int32_t head_dim, int64_t rows) { return head_dim == 128 && rows > 8 ? 512 : 768; }
+
 template <int D>
 int launch(const PagedAttentionArgs& a, hipStream_t s) {
     const int64_t segments = (int64_t)a.B * a.kv_heads * a.row_tiles;
-    const unsigned blocks = (unsigned)(a.workers > 0 ? a.workers : segments);
+    // Where segments go whole, each has a workgroup of its own, and the next free compute unit takes the next one; but where all are
+    // short, starting is most of it, and a workgroup prepares its next segment beside the one that it works on.
+    const bool brief = a.workers == 0 && longest_units(a.q_len, a.max_len, a.window) <= 4;
+    const unsigned blocks = (unsigned)(a.workers > 0 ? a.workers : brief && segments > resident(D, a.group * a.q_len) ? resident(D, a.group * a.q_len) : segments);
     const bool fold = a.group * a.q_len <= 8;
     auto kernel = a.softcap > 0.0f ? fold ? paged_attention_kernel<D, true, true> : paged_attention_kernel<D, true, false>
                                    : fold ? paged_attention_kernel<D, false, true> : paged_attention_kernel<D, false, false>;
@@ -702,12 +725,9 @@ int launch(const PagedAttentionArgs& a, hipStream_t s) {
 // longer than the others keeps its workgroup alone, and shares do not mind: they are taken to have 55 % of the longest's work.
 int paged_attention_workers(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t max_len, int32_t window, bool cap) {
     const int64_t segments = (int64_t)B * kv_heads * (((int64_t)(heads / kv_heads) * q_len + 15) / 16);
-    // (a window is cut to whole blocks of 16 at its begin, and rows have windows up to q_len - 1 tokens apart)
-    const int64_t range = window > 0 && window + (int64_t)q_len + 15 < max_len ? window + (int64_t)q_len + 15 : max_len;
-    const int64_t units = range > PA_UNIT ? (range + PA_UNIT - 1) / PA_UNIT : 1;
+    const int64_t units = longest_units(q_len, max_len, window);
     if (segments * (units + PA_START) > 0x7FFFFFFFll || (int64_t)B * q_len * heads > 0x7FFFFFFFll) return -1;
-    // as many as the chip holds at once
-    const int64_t most = head_dim == 128 && heads / kv_heads * (int64_t)q_len > 8 ? 512 : 768;
+    const int64_t most = resident(head_dim, heads / kv_heads * (int64_t)q_len);
     constexpr double CUS = 256, EACH = 0.47, JOIN = 6.0, FILLED = 0.55;
     const double ALONE = cap ? 0.95 : 0.73;                      // (a tanh a score)
     auto unit_us = [&](double workgroups) {
