@@ -120,7 +120,7 @@ template <int D, int ROWS>
 struct Shared {
     uint8_t ring[PA_WAVES][PA_STAGES][2][Block<D>::BYTES];
     int o[PA_WAVES][ROWS][D];                                    // fp32 (integers for the compiler, see below), groups of 4 in another order in each row
-    int ml[PA_WAVES][2][ROWS];
+    int ml[PA_WAVES][3][ROWS];                                    // M, l, lows of each wave
 };
 
 static_assert(sizeof(Shared<128, 8>) <= 42 * 1280, "three workgroups to a compute unit");
@@ -310,9 +310,11 @@ __global__ __launch_bounds__(PA_WAVES * 64, D == 128 && !FOLD ? 2 : 3) void page
     v4f o[TILES];
     float M, l, lows;                                             // l and lows: this lane's tokens
     bool set;                                                     // M is a reference: the row has seen a token
+    bool fresh;                                                   // all sums are 0
     auto start = [&](const Part& p) {
         end = p.inner_end - p.j_first + new_token(row_of(p));
         begin = a.window > 0 ? max(end - a.window, 0) : 0;
+        // (sums of pairs by the dot product with 1, 1)
         float x[D / 4], top = 0.0f, sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < D / 4; i += 2) {
@@ -320,26 +322,31 @@ __global__ __launch_bounds__(PA_WAVES * 64, D == 128 && !FOLD ? 2 : 3) void page
             x[i] = __uint_as_float(u << 16);
             x[i + 1] = __uint_as_float(u & 0xFFFF0000u);
             top = fmaxf(top, fmaxf(fabsf(x[i]), fabsf(x[i + 1])));
-            sum += x[i];
-            sum += x[i + 1];
+            sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2bf, u), (v2bf){(__bf16)1.0f, (__bf16)1.0f}, sum, false);
         }
         top = quarters_max(top);
         sum = quarters_sum(sum);
-        // the largest becomes 2^14 .. 2^15 (exponent field of top, 127 = 2^0)
-        const int e = min(max(141 - (int)(__float_as_uint(top) >> 23), -100), 100);
-        const float up = __uint_as_float((uint32_t)(127 + e) << 23);
-        c1 = a.scale * LOG2E * __uint_as_float((uint32_t)(127 - e) << 23) * 0x1p20f;
         qs = a.scale * LOG2E * sum;
+        c1 = a.scale * LOG2E * 0x1p20f;
+        // rows whose largest value is not between 2^-3 and 2^15 are brought to 2^14 .. 2^15 (exponent field of top, 127 = 2^0)
+        if (__any(!(top >= 0.125f && top < 32768.0f))) {
+            const int e = min(max(141 - (int)(__float_as_uint(top) >> 23), -100), 100);
+            const float up = __uint_as_float((uint32_t)(127 + e) << 23);
+            c1 *= __uint_as_float((uint32_t)(127 - e) << 23);
+#pragma unroll
+            for (int i = 0; i < D / 4; ++i) x[i] *= up;
+        }
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             constexpr int ORDER[8] = {0, 4, 1, 5, 2, 6, 3, 7};
 #pragma unroll
-            for (int i = 0; i < 8; ++i) q[s][i] = (_Float16)(x[8 * s + ORDER[i]] * up);
+            for (int i = 0; i < 8; ++i) q[s][i] = (_Float16)x[8 * s + ORDER[i]];
         }
 #pragma unroll
         for (int c = 0; c < TILES; ++c) o[c] = (v4f){0.f, 0.f, 0.f, 0.f};
         M = l = lows = 0.0f;
         set = false;
+        fresh = true;
     };
 
     auto row_max = [&](float v) {
@@ -442,17 +449,20 @@ __global__ __launch_bounds__(PA_WAVES * 64, D == 128 && !FOLD ? 2 : 3) void page
             }
             best = row_max(best);
             const float up = (row_max(top) > 0x1p15f || !set) && best > -INFINITY ? best - 5.0f : 0.0f;
-            const float f = set ? __builtin_amdgcn_exp2f(-up) : 0.0f;            // (the sums of a row without a reference are 0)
-            set = set || best > -INFINITY;
             M += up;
 #pragma unroll
             for (int r = 0; r < MINE; ++r) sc[r] -= up;
-            l *= f;
-            lows *= f;
+            if (!fresh) {
+                const float f = set ? __builtin_amdgcn_exp2f(-up) : 0.0f;        // (the sums of a row without a reference are 0)
+                l *= f;
+                lows *= f;
 #pragma unroll
-            for (int c = 0; c < TILES; ++c) o[c] *= f;
+                for (int c = 0; c < TILES; ++c) o[c] *= f;
+            }
+            set = set || best > -INFINITY;
             weigh();
         }
+        fresh = false;
 #pragma unroll
         for (int r = 0; r < MINE; ++r) {
             l += p[r];
@@ -513,30 +523,34 @@ __global__ __launch_bounds__(PA_WAVES * 64, D == 128 && !FOLD ? 2 : 3) void page
             if (quarter == 0) {
                 lds.ml[wave][0][col] = __float_as_int(set ? M : UNSET);
                 lds.ml[wave][1][col] = __float_as_int(l);
+                lds.ml[wave][2][col] = __float_as_int(lows);
             }
 #pragma unroll
             for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int c = 0; c < TILES; c += 4) {
-                    const v4f x = {fmaf(o[c][r], 0x1p24f, lows), fmaf(o[c + 1][r], 0x1p20f, lows), fmaf(o[c + 2][r], 0x1p24f, lows), fmaf(o[c + 3][r], 0x1p20f, lows)};
-                    *reinterpret_cast<v4i*>(&lds.o[wave][col][(TILES * (4 * quarter + r) + c) ^ (col & 7) * 4]) = __builtin_bit_cast(v4i, x);
-                }
+                for (int c = 0; c < TILES; c += 4)
+                    *reinterpret_cast<v4i*>(&lds.o[wave][col][(TILES * (4 * quarter + r) + c) ^ (col & 7) * 4]) =
+                        __builtin_bit_cast(v4i, (v4f){o[c][r], o[c + 1][r], o[c + 2][r], o[c + 3][r]});
         }
         lds_barrier();
         // 16 (32) threads to a row, a few neighbouring channels each
         constexpr int THREADS = PA_WAVES * 64 / ROWS, N = D / THREADS;
         const int r = threadIdx.x / THREADS, piece = threadIdx.x % THREADS, row = p.row_tile * 16 + r;
         if (row >= rows) return;
-        float x[N] = {}, total = 0.0f, best = UNSET;
+        float x[N] = {}, total = 0.0f, bias = 0.0f, best = UNSET;
 #pragma unroll
         for (int w = 0; w < PA_WAVES; ++w) best = fmaxf(best, __int_as_float(lds.ml[w][0][r]));
 #pragma unroll
         for (int w = 0; w < PA_WAVES; ++w) {
             const float f = __builtin_amdgcn_exp2f(__int_as_float(lds.ml[w][0][r]) - best);
             total = fmaf(__int_as_float(lds.ml[w][1][r]), f, total);
+            bias = fmaf(__int_as_float(lds.ml[w][2][r]), f, bias);
 #pragma unroll
             for (int c = 0; c < N; ++c) x[c] = fmaf(__int_as_float(lds.o[w][r][(N * piece + c) ^ (r & 7) * 4]), f, x[c]);
         }
+        // (codes of even channels went in 2^-24 times their size, those of odd ones 2^-20)
+#pragma unroll
+        for (int c = 0; c < N; ++c) x[c] = fmaf(x[c], c & 1 ? 0x1p20f : 0x1p24f, bias);
         if (p.taken < p.units) {
             // the part of a workgroup that the segment began before, and the one that begins in it
             const int64_t at = (2 * (int64_t)blockIdx.x + (p.unit == 0)) * 16 + r;
@@ -558,10 +572,8 @@ __global__ __launch_bounds__(PA_WAVES * 64, D == 128 && !FOLD ? 2 : 3) void page
     for (;;) {
         left -= part.taken + PA_START;
         const bool more = a.workers > 0 ? left > PA_START : (uint32_t)blockIdx.x + round * gridDim.x < (uint32_t)(a.B * segments);
-        Part next = part;
-        int next_ids = -1;
+        int next_ids = -1, next_b = part.b, next_segment = part.segment + 1, next_len = 0, next_units = 0;
         if (more) {
-            int next_b = part.b, next_segment = part.segment + 1;
             if (a.workers == 0) {
                 const int index = blockIdx.x + round++ * gridDim.x;
                 next_b = same(index / segments);
@@ -570,9 +582,10 @@ __global__ __launch_bounds__(PA_WAVES * 64, D == 128 && !FOLD ? 2 : 3) void page
                 ++next_b;
                 next_segment = 0;
             }
-            const int next_len = next_b == part.b ? part.len : length_of(a, next_b), next_units = units_of(a, next_len);
+            next_len = next_b == part.b ? part.len : length_of(a, next_b);
+            next_units = units_of(a, next_len);
             if (a.workers == 0) left = next_units + PA_START;
-            next = describe(next_b, next_len, next_segment, 0, next_units, left);
+            const Part next = describe(next_b, next_len, next_segment, 0, next_units, left);
             next_ids = request_ids(next, next.from + wave * PA_STEP);
         }
         start(part);
@@ -593,14 +606,15 @@ __global__ __launch_bounds__(PA_WAVES * 64, D == 128 && !FOLD ? 2 : 3) void page
             }
         }
         wait_loads<0>();
-        if (more) {
+        if (more) {                                               // (described anew: two parts' descriptions fill the scalar registers)
+            const Part next = describe(next_b, next_len, next_segment, 0, next_units, left);
             request_row(next);
             take_ids(next, next_ids);
             load_first(next, next.from + wave * PA_STEP);
         }
         finish_part(part);
         if (!more) return;
-        part = next;
+        part = describe(next_b, next_len, next_segment, 0, next_units, left);
     }
 #endif
 }
