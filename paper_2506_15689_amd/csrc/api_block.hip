@@ -154,8 +154,8 @@ size_t basq_paged_attention_workspace_bytes(int32_t B, int32_t q_len, int32_t he
                                             int32_t max_len, int32_t window) {
     if (B < 1 || q_len < 1 || heads < 1 || kv_heads < 1 || heads % kv_heads != 0 || (head_dim != 64 && head_dim != 128) || max_len < 0) return 0;
     // (whether scores are capped is not known here: what the larger of both needs)
-    int workers = paged_attention_workers(B, q_len, heads, kv_heads, head_dim, max_len, window, false);
-    const int capped = paged_attention_workers(B, q_len, heads, kv_heads, head_dim, max_len, window, true);
+    int workers = paged_attention_plan(B, q_len, heads, kv_heads, head_dim, max_len, window, false).workers;
+    const int capped = paged_attention_plan(B, q_len, heads, kv_heads, head_dim, max_len, window, true).workers;
     if (capped > workers) workers = capped;
     return workers < 0 ? 0 : parts_bytes(workers, head_dim, attention_segments(B, q_len, heads, kv_heads));
 }
@@ -184,7 +184,9 @@ int basq_paged_attention(const void* q, int64_t ldq, int32_t B, int32_t q_len, i
     if (rc != BASQ_OK) return rc;
     if ((max_len > 0 && !page_table) || !lengths || !aligned(page_table, 4) || !aligned(lengths, 4) || !aligned(lse, 4))
         return fail(BASQ_EINVAL, "page_table and lengths must be given; they and lse must be 4-byte aligned");
-    a.workers = paged_attention_workers(B, q_len, heads, kv_heads, head_dim, max_len, window, softcap > 0.0f);
+    const AttentionPlan plan = paged_attention_plan(B, q_len, heads, kv_heads, head_dim, max_len, window, softcap > 0.0f);
+    a.workers = plan.workers;
+    a.waves = plan.waves;
     if (a.workers < 0) return fail(BASQ_EUNSUPPORTED, "2^31 or more parts of 128 tokens, or rows of a head");
     const size_t need = parts_bytes(a.workers, head_dim, attention_segments(B, q_len, heads, kv_heads));
     if (need > 0) {

@@ -173,14 +173,17 @@ struct PagedAttentionArgs {
     uint16_t* out;            // [B * q_len, heads, D]
     int64_t ldo;
     float* lse;               // optional, [B * q_len, heads]
-    int32_t workers;          // workgroups that share the work (paged_attention_workers), 0: one to a segment
+    int32_t workers, waves;   // workgroups that share the work, 0: one to a segment; waves of a workgroup (paged_attention_plan)
     float* part_o;            // [2 * workers, 16, D]: a workgroup's last part of a segment begun before, and its part of one that goes on
     float2* part_ml;          // [2 * workers, 16]: reference and sum
     int2* part_of;            // [segments]: the workgroup in which a segment begins, and its number of parts
     float inv_cap, cap_log2e; // these four are set by the launcher
     int32_t group, row_tiles; // heads of a kv head, tiles of 16 of its query rows
 };
-int paged_attention_workers(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t max_len, int32_t window, bool cap);
+struct AttentionPlan {
+    int32_t workers, waves;
+};
+AttentionPlan paged_attention_plan(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t max_len, int32_t window, bool cap);
 int launch_paged_attention(PagedAttentionArgs a, hipStream_t s);  // paged_attention.hip
 
 // 28 x 28 Paley type-I matrix, row-major, built on the host at first use (hadamard28.hip).

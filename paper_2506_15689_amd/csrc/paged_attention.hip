@@ -47,8 +47,8 @@ typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef float v2f __attribute__((ext_vector_type(2)));
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 
-constexpr int PA_WAVES = 4, PA_STEP = 32;                        // tokens of a wave's step
-constexpr int PA_UNIT = PA_WAVES * PA_STEP;
+constexpr int PA_STEP = 32;                                      // tokens of a wave's step
+constexpr int PA_UNIT = 4 * PA_STEP;                             // a step of each of four waves: what work is counted in
 constexpr int PA_START = 2;                                       // what the start and the end of a part cost, in units
 constexpr int PA_STAGES = 2;                                      // steps of a wave in LDS
 constexpr float UNSET = -1e30f;                                  // M of a row that has seen no token
@@ -116,14 +116,14 @@ __device__ __forceinline__ int units_of(const PagedAttentionArgs& a, int len) {
 
 // ROWS query rows at most in a tile.  LDS is allocated in steps of 1280 bytes: D = 128 with 8 rows takes 42 of the 128, three workgroups
 // to a compute unit.
-template <int D, int ROWS>
+template <int D, int WAVES, int ROWS>
 struct Shared {
-    uint8_t ring[PA_WAVES][PA_STAGES][2][Block<D>::BYTES];
-    int o[PA_WAVES][ROWS][D];                                    // fp32 (integers for the compiler, see below), groups of 4 in another order in each row
-    int ml[PA_WAVES][3][ROWS];                                    // M, l, lows of each wave
+    uint8_t ring[WAVES][PA_STAGES][2][Block<D>::BYTES];
+    int o[WAVES][ROWS][D];                                    // fp32 (integers for the compiler, see below), groups of 4 in another order in each row
+    int ml[WAVES][3][ROWS];                                    // M, l, lows of each wave
 };
 
-static_assert(sizeof(Shared<128, 8>) <= 42 * 1280, "three workgroups to a compute unit");
+static_assert(sizeof(Shared<128, 4, 8>) <= 42 * 1280, "three workgroups to a compute unit");
 
 template <int N>
 __device__ __forceinline__ void wait_loads() {
@@ -149,15 +149,15 @@ struct Part {
 //
 // FOLD: tiles of at most eight rows, which stand in columns 0 .. 7 and again in 8 .. 15; a lane works on the first block's scores, or
 // on the second's, instead of on both.
-template <int D, bool CAP, bool FOLD>
-__global__ __launch_bounds__(PA_WAVES * 64, D == 128 && !FOLD ? 2 : 3) void paged_attention_kernel(PagedAttentionArgs a) {
+template <int D, int WAVES, bool CAP, bool FOLD>
+__global__ __launch_bounds__(WAVES * 64, WAVES == 8 || (D == 128 && !FOLD) ? 2 : 3) void paged_attention_kernel(PagedAttentionArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)   // buffer resources are a device-only type; the host pass only needs the stub
     constexpr int TILES = D / 16;                                // channel tiles of the second product: channel TILES * n + c
     constexpr int KS = D / 32;                                   // 32-channel steps of the first
     constexpr int MINE = FOLD ? 4 : 8;                           // tokens of a lane in a step
     constexpr int ROWS = FOLD ? 8 : 16;
-    constexpr int STRIDE = PA_WAVES * PA_STEP;
-    __shared__ __attribute__((aligned(256))) Shared<D, ROWS> lds;
+    constexpr int STRIDE = WAVES * PA_STEP;
+    __shared__ __attribute__((aligned(256))) Shared<D, WAVES, ROWS> lds;
     const int lane = threadIdx.x & 63, wave = same(threadIdx.x >> 6);
     const int col = lane & 15, quarter = lane >> 4;
     const int group = a.group, rows = group * a.q_len, row_tiles = a.row_tiles;
@@ -533,15 +533,15 @@ __global__ __launch_bounds__(PA_WAVES * 64, D == 128 && !FOLD ? 2 : 3) void page
                         __builtin_bit_cast(v4i, (v4f){o[c][r], o[c + 1][r], o[c + 2][r], o[c + 3][r]});
         }
         lds_barrier();
-        // 16 (32) threads to a row, a few neighbouring channels each
-        constexpr int THREADS = PA_WAVES * 64 / ROWS, N = D / THREADS;
+        // 16 to 64 threads to a row, 2 to 8 neighbouring channels each
+        constexpr int THREADS = WAVES * 64 / ROWS < D / 2 ? WAVES * 64 / ROWS : D / 2, N = D / THREADS;
         const int r = threadIdx.x / THREADS, piece = threadIdx.x % THREADS, row = p.row_tile * 16 + r;
-        if (row >= rows) return;
+        if (r >= ROWS || row >= rows) return;
         float x[N] = {}, total = 0.0f, bias = 0.0f, best = UNSET;
 #pragma unroll
-        for (int w = 0; w < PA_WAVES; ++w) best = fmaxf(best, __int_as_float(lds.ml[w][0][r]));
+        for (int w = 0; w < WAVES; ++w) best = fmaxf(best, __int_as_float(lds.ml[w][0][r]));
 #pragma unroll
-        for (int w = 0; w < PA_WAVES; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             const float f = __builtin_amdgcn_exp2f(__int_as_float(lds.ml[w][0][r]) - best);
             total = fmaf(__int_as_float(lds.ml[w][1][r]), f, total);
             bias = fmaf(__int_as_float(lds.ml[w][2][r]), f, bias);
@@ -709,6 +709,14 @@ int64_t longest_units(int32_t q_len, int32_t max_len, int32_t window) {
 // workgroups that the chip holds at once, `rows` query rows to a kv head
 int resident(int32_t head_dim, int64_t rows) { return head_dim == 128 && rows > 8 ? 512 : 768; }
 
+template <int D, int WAVES>
+void launch_waves(const PagedAttentionArgs& a, unsigned blocks, hipStream_t s) {
+    const bool fold = a.group * a.q_len <= 8;
+    auto kernel = a.softcap > 0.0f ? fold ? paged_attention_kernel<D, WAVES, true, true> : paged_attention_kernel<D, WAVES, true, false>
+                                   : fold ? paged_attention_kernel<D, WAVES, false, true> : paged_attention_kernel<D, WAVES, false, false>;
+    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(WAVES * 64), 0, s, a);
+}
+
 template <int D>
 int launch(const PagedAttentionArgs& a, hipStream_t s) {
     const int64_t segments = (int64_t)a.B * a.kv_heads * a.row_tiles;
@@ -716,10 +724,8 @@ int launch(const PagedAttentionArgs& a, hipStream_t s) {
     // short, starting is most of it, and a workgroup prepares its next segment beside the one that it works on.
     const bool brief = a.workers == 0 && longest_units(a.q_len, a.max_len, a.window) <= 4;
     const unsigned blocks = (unsigned)(a.workers > 0 ? a.workers : brief && segments > resident(D, a.group * a.q_len) ? resident(D, a.group * a.q_len) : segments);
-    const bool fold = a.group * a.q_len <= 8;
-    auto kernel = a.softcap > 0.0f ? fold ? paged_attention_kernel<D, true, true> : paged_attention_kernel<D, true, false>
-                                   : fold ? paged_attention_kernel<D, false, true> : paged_attention_kernel<D, false, false>;
-    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(PA_WAVES * 64), 0, s, a);
+    if (a.waves == 8) launch_waves<D, 8>(a, blocks, s);
+    else launch_waves<D, 4>(a, blocks, s);
     const int rc = check_hip(hipGetLastError(), "paged_attention launch");
     if (rc != BASQ_OK || a.workers == 0) return rc;
     // many rows have few parts each: a wavefront does
@@ -731,29 +737,33 @@ int launch(const PagedAttentionArgs& a, hipStream_t s) {
 
 }  // namespace
 
-// How many workgroups share the work; 0 where each takes a segment, which goes without the second launch; -1 where there are too many
-// units to be numbered.  Both in microseconds behind the start: a unit takes a workgroup 0.73 while it has a compute unit to itself or
-// nearly so, and 0.47 for each of the two or three that it has for company; the second launch and the parts' ends are 6.  Measured, one
-// workgroup to a segment against shares, contexts of one length: 32 segments of 512, 1024, 2048 tokens 7.7, 10.6, 16.2 us (of 512,
-// always one each), 10.5, 11.4; 256 segments of 640, 1024, 2048 tokens 9.0, 11.1, 16.8 against 14.0, 15.8, 20.3.  But a context that is
-// longer than the others keeps its workgroup alone, and shares do not mind: they are taken to have 55 % of the longest's work.
-int paged_attention_workers(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t max_len, int32_t window, bool cap) {
+// Who takes the work: that many workgroups in equal shares, or (workers = 0) one to a segment, of four waves or, while there are no
+// more than compute units, of eight.  workers = -1 where there are too many units to be numbered.
+//
+// By microseconds behind the start.  A step takes a wave 0.73 while the compute unit has four of them, 0.88 of eight, and 0.47 for each
+// four that it has, where they are more; eight waves' sums are joined 0.6 later than four's; the second launch and the parts' ends are 6.  A
+// context that is longer than the others keeps its workgroup alone, where shares do not mind: they are taken to have 55 % of the longest's
+// work.  Measured, contexts of one length, 128-channel heads, four waves, eight waves, shares: 32 segments of 256, 512, 1024, 2048 tokens
+// 6.2, 7.7, 10.6, 16.2 us; 6.7, 7.3, 9.2, 12.6; -, 10.2, 10.5, 11.4.  256 segments of 512, 1024, 2048 tokens 8.3, 11.1, 16.8; 7.9, 9.8, 15.2;
+// 13.4, 15.8, 20.3.
+AttentionPlan paged_attention_plan(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t max_len, int32_t window, bool cap) {
     const int64_t segments = (int64_t)B * kv_heads * (((int64_t)(heads / kv_heads) * q_len + 15) / 16);
     const int64_t units = longest_units(q_len, max_len, window);
-    if (segments * (units + PA_START) > 0x7FFFFFFFll || (int64_t)B * q_len * heads > 0x7FFFFFFFll) return -1;
+    if (segments * (units + PA_START) > 0x7FFFFFFFll || (int64_t)B * q_len * heads > 0x7FFFFFFFll) return {-1, 4};
     const int64_t most = resident(head_dim, heads / kv_heads * (int64_t)q_len);
-    constexpr double CUS = 256, EACH = 0.47, JOIN = 6.0, FILLED = 0.55;
-    const double ALONE = cap ? 0.95 : 0.73;                      // (a tanh a score)
-    auto unit_us = [&](double workgroups) {
-        const double company = (workgroups < (double)most ? workgroups : (double)most) / CUS * EACH;
-        return company > ALONE ? company : ALONE;
+    constexpr double CUS = 256, ALONE = 0.73, ALONE_EIGHT = 0.88, EACH = 0.47, END_EIGHT = 0.6, JOIN = 6.0, FILLED = 0.55;
+    const double tanhs = cap ? 0.22 : 0.0;                       // of a step's scores
+    auto step_us = [&](double fours, double alone) {             // fours: sets of four waves that the chip has
+        const double company = (fours < (double)most ? fours : (double)most) / CUS * EACH;
+        return company > alone + tanhs ? company : alone + tanhs;
     };
     const double rounds = segments > most ? (double)segments / (double)most : 1.0;
     const int64_t share = (segments * (units + PA_START) + most - 1) / most;
-    const double segment_each = (double)units * unit_us((double)segments) * rounds;
-    const double shared = JOIN + FILLED * (double)share * unit_us((double)(segments * units));
-    if (units <= 4 || segment_each <= shared) return 0;
-    return (int)(segments * units < most ? segments * units : most);
+    const double four = (double)units * step_us((double)segments, ALONE) * rounds;
+    const double eight = segments <= (int64_t)CUS ? END_EIGHT + (double)((units + 1) / 2) * step_us(2.0 * (double)segments, ALONE_EIGHT) : 2.0 * four;
+    const double shared = JOIN + FILLED * (double)share * step_us((double)(segments * units), ALONE);
+    if (units > 4 && shared < four && shared < eight) return {(int)(segments * units < most ? segments * units : most), 4};
+    return {0, eight < four ? 8 : 4};
 }
 
 int launch_paged_attention(PagedAttentionArgs a, hipStream_t s) {
