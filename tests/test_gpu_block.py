@@ -436,6 +436,21 @@ def test_attention_many_sequences():
     check_attention(q, cache, table, lens, 5000)
 
 
+@pytest.mark.parametrize("Bn,heads,kv_heads,D,longest", [(130, 16, 8, 128, 300), (40, 160, 16, 128, 150), (110, 8, 8, 64, 64), (100, 40, 8, 128, 700)])
+def test_attention_of_more_segments_than_the_chip_holds(Bn, heads, kv_heads, D, longest):
+    """Workgroups that take several short segments, and segments that wait for a place."""
+    lengths = [(31 * i) % (longest + 1) for i in range(Bn)]
+    check_attention(*attention_case(Bn, lengths, heads, kv_heads, D, 16, 1), longest)
+
+
+@pytest.mark.parametrize("heads,kv_heads,D", [(4, 4, 64), (4, 4, 128), (12, 1, 64), (12, 1, 128)])
+@pytest.mark.parametrize("longest", [513, 900, 1100])
+def test_attention_of_few_segments(heads, kv_heads, D, longest):
+    """Eight waves to a segment."""
+    check_attention(*attention_case(longest + D, [longest, 257, 0, 33], heads, kv_heads, D, 16, 1), longest)
+    check_attention(*attention_case(longest + D, [longest, 257, 0, 33], heads, kv_heads, D, 16, 2), longest, 2, softcap=30.0, window=longest // 2)
+
+
 def test_attention_is_the_same_every_time_and_anywhere():
     """Bits do not depend on the run, on where pages lie, or on the batch's other rows' values."""
     q, cache, table, lengths = attention_case(20, [4000, 77, 1300], 16, 2, 128, 16, 1)
