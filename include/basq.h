@@ -386,7 +386,8 @@ int basq_rope_append(const void* q, int64_t ldq, const void* k, int64_t ldk, con
  *   page_table int32 [B, table_stride]: token t of sequence b is token t % page_size of page page_table[b, t / page_size].  Entries
  *              past a length are not read; tokens of a page that is negative or >= num_pages count as not there
  *   lengths    int32 [B], the new tokens among them; more than max_len counts as max_len (negative as 0)
- *   max_len    host: the longest length there can be; the work is laid out for it.  At most table_stride * page_size
+ *   max_len    host: the longest length there can be; the work is laid out for it.  At most table_stride * page_size, and 2^31 - 2^16
+ *   q_len      up to 32768 (else BASQ_EUNSUPPORTED)
  *   out        out, bf16 [B * q_len, heads, D], token stride ldo; may be q.   lse   out, fp32 [B * q_len, heads], or NULL
  *   workspace  basq_paged_attention_workspace_bytes, 256-byte aligned (BASQ_EWORKSPACE where it is smaller); NULL where that is 0
  * The result does not depend on where pages lie.  B == 0 does nothing.

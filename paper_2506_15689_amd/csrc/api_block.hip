@@ -167,7 +167,9 @@ int basq_paged_attention(const void* q, int64_t ldq, int32_t B, int32_t q_len, i
     if (B < 0 || q_len < 1) return fail(BASQ_EINVAL, "B must be >= 0 and q_len >= 1 (got %d, %d)", B, q_len);
     int rc = check_heads(heads, kv_heads, head_dim, true);
     if (rc != BASQ_OK) return rc;
-    if ((int64_t)q_len * heads > 0x3FFFFFFFll) return fail(BASQ_EUNSUPPORTED, "q_len * heads must be less than 2^30");
+    // (the kernel counts tokens in 32 bits: a little room above the longest context, and below zero for what new tokens do not see)
+    if (q_len > 32768 || (int64_t)q_len * heads > 0x3FFFFFFFll) return fail(BASQ_EUNSUPPORTED, "q_len up to 32768 and q_len * heads < 2^30 are supported (got %d, %d)", q_len, heads);
+    if (max_len > 0x7FFF0000) return fail(BASQ_EUNSUPPORTED, "max_len up to 2^31 - 2^16 is supported (got %d)", max_len);
     if (bits != 4) return fail(BASQ_EUNSUPPORTED, "only bits == 4 is implemented (got %d)", bits);
     if (max_len < 0) return fail(BASQ_EINVAL, "max_len must be >= 0 (got %d)", max_len);
     if (!isfinite(scale)) return fail(BASQ_EINVAL, "scale must be finite (got %g)", (double)scale);
@@ -197,7 +199,8 @@ int basq_paged_attention(const void* q, int64_t ldq, int32_t B, int32_t q_len, i
     a.B = B; a.q_len = q_len; a.heads = heads; a.kv_heads = kv_heads; a.D = head_dim;
     a.cache = cache; a.num_pages = num_pages;
     a.page_table = page_table; a.table_stride = table_stride; a.lengths = lengths; a.max_len = max_len;
-    a.scale = scale; a.softcap = softcap; a.window = window;
+    a.scale = scale; a.softcap = softcap;
+    a.window = window < max_len ? window : 0;                     // (a window of all tokens is none)
     a.out = static_cast<uint16_t*>(out); a.ldo = ldo; a.lse = lse;
     a.part_o = static_cast<float*>(workspace);
     a.part_ml = reinterpret_cast<float2*>(a.part_o + 2 * (size_t)a.workers * 16 * head_dim);

@@ -601,7 +601,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 || (D == 128 && !FOLD) ? 2 :
                 load(i + PA_STAGES - 1, last, t0 + (i + PA_STAGES - 1) * STRIDE, stage == 0 ? PA_STAGES - 1 : stage - 1);
                 wait_loads<(PA_STAGES - 1) * 2 * Block<D>::LOADS>();
                 work(part, i, t0 + i * STRIDE, stage);
-                asm volatile("" ::: "memory");                    // (the stage is read before it is requested anew)
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // the stage is read before it is requested anew
                 stage = stage == PA_STAGES - 1 ? 0 : stage + 1;
             }
         }
@@ -749,7 +749,7 @@ int launch(const PagedAttentionArgs& a, hipStream_t s) {
 AttentionPlan paged_attention_plan(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t max_len, int32_t window, bool cap) {
     const int64_t segments = (int64_t)B * kv_heads * (((int64_t)(heads / kv_heads) * q_len + 15) / 16);
     const int64_t units = longest_units(q_len, max_len, window);
-    if (segments * (units + PA_START) > 0x7FFFFFFFll || (int64_t)B * q_len * heads > 0x7FFFFFFFll) return {-1, 4};
+    if (segments * (units + PA_START) > 0x7FFF0000ll || (int64_t)B * q_len * heads > 0x7FFFFFFFll) return {-1, 4};
     const int64_t most = resident(head_dim, heads / kv_heads * (int64_t)q_len);
     constexpr double CUS = 256, ALONE = 0.73, ALONE_EIGHT = 0.88, EACH = 0.47, END_EIGHT = 0.6, JOIN = 6.0, FILLED = 0.55;
     const double tanhs = cap ? 0.22 : 0.0;                       // of a step's scores

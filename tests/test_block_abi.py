@@ -98,6 +98,8 @@ def attention(lib, **kw):
 @pytest.mark.parametrize("kw,code", [
     (dict(B=-1), B.BASQ_EINVAL), (dict(q_len=0), B.BASQ_EINVAL), (dict(heads=0), B.BASQ_EINVAL), (dict(kv_heads=0), B.BASQ_EINVAL),
     (dict(heads=5), B.BASQ_EINVAL), (dict(head_dim=256), B.BASQ_EUNSUPPORTED), (dict(bits=8), B.BASQ_EUNSUPPORTED),
+    (dict(q_len=32769), B.BASQ_EUNSUPPORTED), (dict(q_len=32768, heads=32768, kv_heads=32768, ldq=1 << 22), B.BASQ_EUNSUPPORTED),
+    (dict(max_len=0x7FFF0001, table_stride=1 << 28), B.BASQ_EUNSUPPORTED),
     (dict(max_len=-1), B.BASQ_EINVAL), (dict(max_len=513), B.BASQ_EINVAL), (dict(table_stride=-1), B.BASQ_EINVAL),
     (dict(scale=float("inf")), B.BASQ_EINVAL), (dict(softcap=-1.0), B.BASQ_EINVAL), (dict(softcap=float("nan")), B.BASQ_EINVAL),
     (dict(window=-1), B.BASQ_EINVAL), (dict(cache=None), B.BASQ_EINVAL), (dict(cache=ODD), B.BASQ_EINVAL), (dict(num_pages=0), B.BASQ_EINVAL),

@@ -122,7 +122,7 @@ def test_rope_table(scaling, kw):
         want = ref.rope_table(n, rot, base, scaling, **kw)
         # fp64 inside (positions of a thousand: angles to 2^-40), rounded to fp32 once
         assert ((ref.f64(t) - want).abs() <= 2.0 ** -24 * want.abs() + 2.0 ** -38).all()
-    t = torch.empty(1 << 20, 2, device=DEV)[-4:]                    # far positions, by the table's last rows
+    # far positions
     big = torch.empty(1 << 20, 16, device=DEV)
     B.basq_rope_table(big, 10000.0, scaling=scaling, **kw)
     want = ref.rope_table(1 << 20, 16, 10000.0, scaling, **kw)
@@ -430,7 +430,7 @@ def test_attention_of_infinite_query():
 def test_attention_many_sequences():
     """More sequences than a wavefront has lanes, so that the shares are found in several rounds."""
     lengths = [(37 * i) % 257 for i in range(200)]
-    check_attention(*attention_case(18, lengths, 4, 2, 64, 16, 1), 5000 if False else 272)
+    check_attention(*attention_case(18, lengths, 4, 2, 64, 16, 1), 272)
     q, cache, table, lens = attention_case(19, lengths, 4, 2, 64, 16, 1)
     table = torch.nn.functional.pad(table, (0, 400), value=-1)
     check_attention(q, cache, table, lens, 5000)
