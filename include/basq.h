@@ -356,7 +356,7 @@ size_t basq_kv_page_bytes(int32_t kv_heads, int32_t head_dim, int32_t page_size)
  * operation rounded on its own:
  *     rope     (a, b) -> (a cos - b sin, b cos + a sin) for the pairs of the first rot_dim channels: (i, i + rot_dim/2), or
  *              (2i, 2i + 1) where interleaved, with the cosines and sines of row positions[t]; the other channels stay
- *     rotate   sums and differences (a + b, a - b) of the channels 1, 2, 4, ... D/2 apart, then times fp32(1/sqrt(D))
+ *     rotate   sums and differences (a + b, a - b) of the channels 1, 2, 4, ... D/2 apart, then times fp32(1/sqrt(D)); a zero is positive
  *     k, v     lo, hi, s, q as in basq_rotate_quant, over each head; code and (s, lo) go to slots[t] of the cache
  *     k_hat, v_hat   bf16(fma(s, q, lo)), what the cache stands for (the prompt's own attention)
  *   q, k, v    bf16 [T, heads, D], [T, kv_heads, D] twice, heads side by side, token strides ldq, ldk, ldv (the three parts of one

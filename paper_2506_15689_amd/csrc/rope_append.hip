@@ -8,8 +8,14 @@
 //
 // A head of D channels lies on D/8 lanes, eight neighbouring channels (16 bytes) each, so a wavefront takes 512 channels (four
 // or eight heads) per step.  The pair of a channel under rope is in the lane itself (interleaved) or rot/16 lanes away (halves);
-// the transform's stages over channel bits 0-2 are in the lane, the others are DPP moves; the range is a DPP reduction over the
-// head's lanes.  Nothing goes through LDS memory, and a token's cosines and sines stay in registers for all its heads.
+// the transform's stages over channel bits 0-2 are in the lane, the others are DPP operands; the range is a DPP reduction over the
+// head's lanes.  Nothing goes through LDS memory, and a token's cosines and sines stay in registers for all its heads.  A zero out of the
+// transform is positive.
+//
+// Bound by memory, with vector instructions not far behind (about 150 for a step of queries).  4096 tokens of 64 and 8 heads of 128 channels
+// move 173 MB in 34 us, 5.1 TB/s, 32768 tokens in 246 us, 5.6 (a large copy reaches 4.8); with the lanes' butterflies as two or three
+// instructions each and branches around loads and stores, 35.4 .. 36.5 and, for 1946 tokens of 40 and 40 heads of 64 channels, 17.9
+// instead of 16.2.  Sixteen tokens: 3.9 us, the launch and three loads one behind the other (position, cosines, heads).
 #include "basq_internal.h"
 
 namespace basq {
@@ -18,33 +24,45 @@ namespace {
 
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef float v2f __attribute__((ext_vector_type(2)));
+typedef uint32_t basq_v2u __attribute__((ext_vector_type(2)));
 
-constexpr int RA_WAVES = 4, AHEAD = 2;                           // steps of a wave under way
+constexpr int RA_WAVES = 4;
+constexpr int NT = 2;                                            // non-temporal
+constexpr int BEYOND = 0x7FFFFFF0;                               // behind the end of any buffer here
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void* p, int bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00020000);
+}
 
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v) {
     return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xF, 0xF, true));
 }
-constexpr int XOR1 = 0xB1, XOR2 = 0x4E, XOR3 = 0x1B, HALF_MIRROR = 0x141, MIRROR = 0x140, XOR8 = 0x128;
+constexpr int XOR1 = 0xB1, XOR2 = 0x4E, HALF_MIRROR = 0x141, MIRROR = 0x140;
 
-// the value of the lane whose number differs in bit BIT (0..3)
-template <int BIT>
-__device__ __forceinline__ float neighbour(float v) {
-    if constexpr (BIT == 0) return dpp<XOR1>(v);
-    else if constexpr (BIT == 1) return dpp<XOR2>(v);
-    else if constexpr (BIT == 2) return dpp<HALF_MIRROR>(dpp<XOR3>(v));        // 7 ^ 3
-    else return dpp<XOR8>(v);                                                  // a rotation by half a row
-}
+// The piece of eight channels that is on a head's lane (and the lane that a piece is on): pieces 4 .. 7 of eight lie backwards, so that the
+// mirror of eight lanes exchanges pieces whose numbers differ in bit 2 alone.
+__device__ __forceinline__ int piece_of(int lane) { return lane ^ (lane & 4 ? 3 : 0); }
 
-template <int BIT>
-__device__ __forceinline__ void stage(float (&x)[8], int lane) {
-    const uint32_t sign = (uint32_t)((lane >> BIT) & 1) << 31;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = neighbour<BIT>(x[i]) + __uint_as_float(__float_as_uint(x[i]) ^ sign);
-}
+// Butterflies over lanes, a + b where the piece's bit is clear and a - b where it is set, one instruction each: the latter lane's sum is kept
+// with the other sign (x - neighbour), as the lanes that it meets in later stages keep theirs.  (What an instruction writes may be another
+// lane's operand two instructions later: a s_nop in front, the eight values in turn behind it.)
+#define RA_STAGE(x, sign, CTRL)                                                                                                        \
+    asm("s_nop 1\n\t"                                                                                                                  \
+        "v_fmac_f32_dpp %0, %0, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                                                            \
+        "v_fmac_f32_dpp %1, %1, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                                                            \
+        "v_fmac_f32_dpp %2, %2, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                                                            \
+        "v_fmac_f32_dpp %3, %3, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                                                            \
+        "v_fmac_f32_dpp %4, %4, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                                                            \
+        "v_fmac_f32_dpp %5, %5, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                                                            \
+        "v_fmac_f32_dpp %6, %6, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                                                            \
+        "v_fmac_f32_dpp %7, %7, %8 " CTRL " row_mask:0xf bank_mask:0xf"                                                                \
+        : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(x[4]), "+v"(x[5]), "+v"(x[6]), "+v"(x[7])                               \
+        : "v"(sign))
 
+// norm: with the sign of a lane's sums (see above), signs[b]: -1 where the piece's bit b is set, else 1
 template <int D>
-__device__ __forceinline__ void hadamard(float (&x)[8], int lane, float norm) {
+__device__ __forceinline__ void hadamard(float (&x)[8], const float (&signs)[4], float norm) {
 #pragma unroll
     for (int step = 1; step < 8; step *= 2)
 #pragma unroll
@@ -54,12 +72,12 @@ __device__ __forceinline__ void hadamard(float (&x)[8], int lane, float norm) {
                 x[i] = a + b;
                 x[i + step] = a - b;
             }
-    stage<0>(x, lane);
-    stage<1>(x, lane);
-    stage<2>(x, lane);
-    if constexpr (D == 128) stage<3>(x, lane);
+    RA_STAGE(x, signs[0], "quad_perm:[1,0,3,2]");
+    RA_STAGE(x, signs[1], "quad_perm:[2,3,0,1]");
+    RA_STAGE(x, signs[2], "row_half_mirror");
+    if constexpr (D == 128) RA_STAGE(x, signs[3], "row_ror:8");
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] *= norm;
+    for (int i = 0; i < 8; ++i) x[i] = fmaf(x[i], norm, 0.0f);                 // (+ 0: a zero is positive, with either sign of norm)
 }
 
 template <int D, class Op>
@@ -72,43 +90,40 @@ __device__ __forceinline__ float over_head(const float (&x)[8], Op op) {
     return v;
 }
 
-__device__ __forceinline__ void widen(const uint4& w, float (&x)[8]) {
-    const uint32_t* u = reinterpret_cast<const uint32_t*>(&w);
+__device__ __forceinline__ void widen(const basq_v4u& w, float (&x)[8]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        x[2 * i] = __uint_as_float(u[i] << 16);
-        x[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
     }
 }
-__device__ __forceinline__ uint4 narrow(const float (&x)[8]) {
-    uint4 w;
-    uint32_t* u = reinterpret_cast<uint32_t*>(&w);
+__device__ __forceinline__ basq_v4u narrow(const float (&x)[8]) {
+    basq_v4u w;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        u[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f){x[2 * i], x[2 * i + 1]}, v2bf));
+    for (int i = 0; i < 4; ++i) w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f){x[2 * i], x[2 * i + 1]}, v2bf));
     return w;
 }
 
 // A wave takes `per` consecutive steps of one token; the steps of a token are its q heads, its k heads and its v heads, each
 // rounded up to whole steps.
 template <int D, bool INTERLEAVED>
-__global__ __launch_bounds__(RA_WAVES * 64) void rope_append_kernel(RopeAppendArgs a, int parts, int per) {
+__global__ __launch_bounds__(RA_WAVES * 64, 8) void rope_append_kernel(RopeAppendArgs a, int parts, int per) {
     constexpr int LANES = D / 8, HEADS = 64 / LANES;             // lanes of a head, heads of a step
     const int lane = threadIdx.x & 63;
     const uint32_t wave = blockIdx.x * (uint32_t)RA_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t t = wave / (uint32_t)parts;
+    const int64_t t = (uint32_t)__builtin_amdgcn_readfirstlane(wave / (uint32_t)parts);
     if (t >= a.T) return;
     const int part = (int)(wave - (uint32_t)t * (uint32_t)parts);
-    const int sub = lane % LANES, in_step = lane / LANES, c0 = 8 * sub;
+    const int sub = lane % LANES, in_step = lane / LANES, piece = piece_of(sub), c0 = 8 * piece;
     const int q_steps = (a.heads + HEADS - 1) / HEADS, kv_steps = (a.kv_heads + HEADS - 1) / HEADS;
     const int end = min(q_steps + 2 * kv_steps, (part + 1) * per);
 
     int position = 0;
     if (a.cos_sin) {
-        position = a.positions[t];
+        position = __builtin_amdgcn_readfirstlane(a.positions[t]);
         if (position < 0 || position >= a.table_rows) return;   // padding
     }
-    const int slot = a.slots && a.kv_heads ? a.slots[t] : -1;
+    const int slot = a.slots && a.kv_heads ? __builtin_amdgcn_readfirstlane(a.slots[t]) : -1;
 
     // out = x * co + pair * si
     float co[8], si[8];
@@ -116,7 +131,7 @@ __global__ __launch_bounds__(RA_WAVES * 64) void rope_append_kernel(RopeAppendAr
     const int half = a.rot / 2;
     const bool second = !INTERLEAVED && c0 >= half;
     // the lane that holds the pairs of this one's channels (itself where they are not turned)
-    const int pair_lane = INTERLEAVED || !turned ? lane : second ? lane - half / 8 : lane + half / 8;
+    const int pair_lane = INTERLEAVED || !turned ? lane : lane - sub + piece_of(second ? piece - half / 8 : piece + half / 8);
     if (turned) {
         const float* row = a.cos_sin + (int64_t)position * a.rot;
         if (INTERLEAVED) {
@@ -135,55 +150,54 @@ __global__ __launch_bounds__(RA_WAVES * 64) void rope_append_kernel(RopeAppendAr
         }
     }
 
-    auto head_of = [&](int step, int& kind) {
-        kind = step < q_steps ? 0 : step < q_steps + kv_steps ? 1 : 2;
-        return (step - (kind == 0 ? 0 : kind == 1 ? q_steps : q_steps + kv_steps)) * HEADS + in_step;
-    };
-    auto request = [&](int step) {
-        int kind;
-        const int head = head_of(step, kind);
-        uint4 w = make_uint4(0, 0, 0, 0);
-        const uint16_t* x = kind == 0 ? a.q + t * a.ldq : kind == 1 ? a.k + t * a.ldk : a.v + t * a.ldv;
-        if (head < (kind == 0 ? a.heads : a.kv_heads)) w = nt_load16(x + head * D + c0);
-        return w;
-    };
+    float signs[4], norm = a.norm;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        signs[b] = (piece >> b) & 1 ? -1.0f : 1.0f;
+        norm *= signs[b];
+    }
 
-    uint4 next[AHEAD];
+    // Loads and stores go through buffer descriptors that end with the heads there are: what lies behind them, and steps behind the last one,
+    // moves nothing, without a branch, so that a wait is for the one load it needs.
+    const uint32_t mine = 2 * (in_step * D + c0);
+    auto first_head = [&](int step) { return (step < q_steps ? step : step < q_steps + kv_steps ? step - q_steps : step - q_steps - kv_steps) * HEADS; };
+    auto request = [&](int step) {
+        const int first = first_head(step);
+        const uint16_t* row = step < q_steps ? a.q + t * a.ldq : step < q_steps + kv_steps ? a.k + t * a.ldk : a.v + t * a.ldv;
+        return __builtin_amdgcn_raw_buffer_load_b128(buffer(row + first * D, step < end ? ((step < q_steps ? a.heads : a.kv_heads) - first) * D * 2 : 0), mine, 0, NT);
+    };
+    auto turn = [&](const basq_v4u& w, float (&x)[8]) {
+        if (a.cos_sin) {
+            float p[8];
+            if (INTERLEAVED) {
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) next[i] = part * per + i < end ? request(part * per + i) : make_uint4(0, 0, 0, 0);
-    for (int step = part * per; step < end; ++step) {
-        const uint4 w = next[0];
+                for (int i = 0; i < 8; ++i) p[i] = x[i ^ 1];
+            } else {
+                basq_v4u other;
 #pragma unroll
-        for (int i = 0; i + 1 < AHEAD; ++i) next[i] = next[i + 1];
-        if (step + AHEAD < end) next[AHEAD - 1] = request(step + AHEAD);
-        int kind;
-        const int head = head_of(step, kind);
+                for (int i = 0; i < 4; ++i) other[i] = __shfl(w[i], pair_lane, 64);
+                widen(other, p);
+            }
+            if (turned)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = x[i] * co[i] + p[i] * si[i];
+        }
+        if (a.rotate) hadamard<D>(x, signs, norm);
+    };
+    auto query = [&](int step, const basq_v4u& w) {
         float x[8];
         widen(w, x);
-        if (kind < 2) {
-            if (a.cos_sin) {
-                float p[8];
-                if (INTERLEAVED) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) p[i] = x[i ^ 1];
-                } else {
-                    uint4 other;
-                    other.x = __shfl(w.x, pair_lane, 64);
-                    other.y = __shfl(w.y, pair_lane, 64);
-                    other.z = __shfl(w.z, pair_lane, 64);
-                    other.w = __shfl(w.w, pair_lane, 64);
-                    widen(other, p);
-                }
-                if (turned)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = x[i] * co[i] + p[i] * si[i];
-            }
-            if (a.rotate) hadamard<D>(x, lane, a.norm);
-        }
-        if (kind == 0) {
-            if (head < a.heads) nt_store16(a.q_out + t * a.ldqo + head * D + c0, narrow(x));
-            continue;
-        }
+        turn(w, x);
+        const int first = step * HEADS;
+        __builtin_amdgcn_raw_buffer_store_b128(narrow(x), buffer(a.q_out + t * a.ldqo + first * D, (a.heads - first) * D * 2), mine, 0, NT);
+    };
+    const int P = 1 << a.page_log2, page = slot >> a.page_log2, at = slot & (P - 1), pitch = P * (D + 16);
+    const bool stored = slot >= 0 && page < a.num_pages;
+    auto key_or_value = [&](int step, const basq_v4u& w) {
+        const bool value = step >= q_steps + kv_steps;
+        float x[8];
+        widen(w, x);
+        if (!value) turn(w, x);
         const float lo = a.clip_lo * over_head<D>(x, [](float u, float v) { return fminf(u, v); });
         const float hi = a.clip_hi * over_head<D>(x, [](float u, float v) { return fmaxf(u, v); });
         float s = __fdiv_rn(hi - lo, 15.0f);
@@ -198,23 +212,44 @@ __global__ __launch_bounds__(RA_WAVES * 64) void rope_append_kernel(RopeAppendAr
             even = __builtin_amdgcn_cvt_pk_u8_f32(x[2 * i], i, even);          // round-half-to-even, NaN -> 0
             odd = __builtin_amdgcn_cvt_pk_u8_f32(x[2 * i + 1], i, odd);
         }
-        if (head >= a.kv_heads) continue;
-        const int page = slot >> a.page_log2, at = slot & ((1 << a.page_log2) - 1);
-        if (slot >= 0 && page < a.num_pages) {
-            const int P = 1 << a.page_log2, which = kind - 1;
-            uint8_t* mine = a.cache + ((int64_t)page * a.kv_heads + head) * ((int64_t)P * (D + 16));
-            *reinterpret_cast<uint32_t*>(mine + (int64_t)(which * P + at) * (D / 2) + 4 * sub) = even | (odd << 4);
-            if (sub == 0) *reinterpret_cast<float2*>(mine + (int64_t)P * D + (which * P + at) * 8) = make_float2(s, lo);
-        }
-        uint16_t* hat = kind == 1 ? a.k_hat : a.v_hat;
+        const int first = first_head(step), row = value ? P + at : at;
+        const auto blocks = buffer(a.cache + ((int64_t)page * a.kv_heads + first) * pitch, stored ? min(a.kv_heads - first, HEADS) * pitch : 0);
+        __builtin_amdgcn_raw_buffer_store_b32(even | (odd << 4), blocks, in_step * pitch + row * (D / 2) + 4 * piece, 0, 0);
+        const basq_v2u range = {__float_as_uint(s), __float_as_uint(lo)};
+        __builtin_amdgcn_raw_buffer_store_b64(range, blocks, sub == 0 ? in_step * pitch + P * D + row * 8 : BEYOND, 0, 0);
+        uint16_t* hat = value ? a.v_hat : a.k_hat;
         if (hat) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 x[2 * i] = fmaf(s, (float)((even >> (8 * i)) & 255u), lo);
                 x[2 * i + 1] = fmaf(s, (float)((odd >> (8 * i)) & 255u), lo);
             }
-            nt_store16(hat + t * a.ldh + head * D + c0, narrow(x));
+            __builtin_amdgcn_raw_buffer_store_b128(narrow(x), buffer(hat + t * a.ldh + first * D, (a.kv_heads - first) * D * 2), mine, 0, NT);
         }
+    };
+
+    basq_v4u even_step = request(part * per), odd_step = request(part * per + 1);
+    int step = part * per;
+    for (const int last = min(end, q_steps) - 1; step < last; step += 2) {
+        basq_v4u w = even_step;
+        even_step = request(step + 2);
+        query(step, w);
+        w = odd_step;
+        odd_step = request(step + 3);
+        query(step + 1, w);
+    }
+    auto any = [&](int step, const basq_v4u& w) {
+        if (step < q_steps) query(step, w);
+        else key_or_value(step, w);
+    };
+    for (; step < end; step += 2) {
+        basq_v4u w = even_step;
+        even_step = request(step + 2);
+        any(step, w);
+        if (step + 1 == end) break;
+        w = odd_step;
+        odd_step = request(step + 3);
+        any(step + 1, w);
     }
 }
 
@@ -222,8 +257,9 @@ template <int D>
 int launch(const RopeAppendArgs& a, hipStream_t s) {
     constexpr int HEADS = 512 / D;
     const int steps = (a.heads + HEADS - 1) / HEADS + 2 * ((a.kv_heads + HEADS - 1) / HEADS);
-    // eight thousand waves while a token has steps for several of them (32 a compute unit; 4096 tokens of 64 and 8 heads: 41.8 us with half
-    // as many and one step under way, 37.4 with twice as many, as built 35.4 .. 36.9), and one to a token from there on
+    // eight thousand waves, as many as the chip holds, while a token has steps for several of them, and one to a token from there on (half as
+    // many, as built, twice as many: 4096 tokens of 64 and 8 heads 35.2, 34.0, 33.7 us; 1946 of 40 and 40 heads of 64 channels 16.0, 16.2,
+    // 16.9; 668 of 64 and 8 8.6, 8.8, 10.8)
     int64_t parts = (8192 + a.T - 1) / a.T;
     if (parts > steps) parts = steps;
     const int per = (int)((steps + parts - 1) / parts);

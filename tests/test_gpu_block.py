@@ -209,6 +209,29 @@ def test_append_parts_and_places():
     assert torch.equal(inplace[:, heads:heads + kv_heads], hats[0]) and torch.equal(inplace[:, heads + kv_heads:], hats[1])
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_append_of_heads_whose_sums_cancel(D):
+    """Heads of zeros, of one value, of alternating values and of one channel: the transform's zeros are positive, every bit of the
+    cache as defined."""
+    T, P = 5, 16
+    x, _, cache, slots, _ = append_case(6, T, 2, 2, D, P, 0)
+    x[:, :4:2] = 0
+    x[1, :] = 1.5
+    x[2, :, ::2], x[2, :, 1::2] = -3.0, 3.0
+    x[3, 1:3] = 0
+    x[3, 1, D - 1], x[3, 2, 9] = 7.0, -7.0
+    want_cache = cache.cpu().clone()
+    q, k, v = x[:, :2], x[:, 2:4], x[:, 4:]
+    q_out = torch.empty(T, 2, D, dtype=BF16, device=DEV)
+    B.basq_rope_append(q, k, v, None, None, slots, cache, 0.9, 0.8, q_out)
+    bits = lambda y: y.cpu().to(BF16).contiguous().view(torch.int16)  # noqa: E731
+    assert torch.equal(bits(q_out), bits(ref.turn(q, None, None, False, True)))
+    for which, part in enumerate([ref.turn(k, None, None, False, True), v.cpu().float()]):
+        codes, s, lo = ref.quantise(part, 0.9, 0.8)
+        ref.put(want_cache, D, slots.cpu(), which, codes, s, lo)
+    assert torch.equal(cache.cpu(), want_cache)
+
+
 def test_append_of_unusual_vectors():
     """Constant, zero, infinite and NaN vectors: the quantiser's rules for them, and no other vector changes."""
     T, D, P = 6, 64, 16
