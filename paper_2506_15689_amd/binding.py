@@ -1,5 +1,7 @@
-"""Thin ctypes binding of libbasq.so: same names as the C ABI (include/basq.h), torch tensors in,
-argument marshalling only.  Every step of the layer runs in the HIP kernels; there is no CPU
+"""Thin binding of libbasq.so: same names as the C ABI (include/basq.h), torch tensors in,
+argument marshalling only -- by ctypes, and for the calls around the linear layer (norm, append,
+attention), whose small forms Python's marshalling would cost more than their kernels, in the compiled
+module _block (csrc/binding_block.cpp).  Every step of the layer runs in the HIP kernels; there is no CPU
 fallback -- if the library is missing or a call fails, an exception is raised."""
 from __future__ import annotations
 

@@ -23,14 +23,15 @@
 // bf16 output) near 2^5 of their running maximum, far from either end of fp16.  l, M and both sums are fp32.
 //
 // Codes and ranges come by direct loads into a ring of LDS stages that the wave has to itself, a step ahead of the one that is
-// worked on: registers hold none of it, and three workgroups of four waves fit a compute unit.  (Loads into registers, two
-// workgroups: 85 us for 64 contexts of 4340 tokens on average, 64 heads over 8; as built 66.)  The loads carry the non-temporal hint:
-// nothing is read twice (77 -> 66 us).
+// worked on: registers hold none of it, and three workgroups of four waves fit a compute unit (loads into registers and two workgroups took
+// a quarter longer; three or four stages and two workgroups, or four workgroups, gain nothing).  The loads carry the non-temporal hint:
+// nothing is read twice (without it a sixth longer).
 //
-// Bound: reading the cache, D + 16 bytes a token and kv head, and nearly as much the vector instructions.  That workload is 327 MB and
-// takes 66 us, 4.9 TB/s; from a cache of one page, so without the memory, 55 us; a kernel that only reads as many bytes 49 us.
-// What is left is the start of a workgroup (5 us until its first loads are in: lengths, page ids, codes, one after the other), and
-// the end, when the workgroup of a compute unit that started first is done earlier than the others (39, 45 and 52 us).
+// Bound: reading the cache, D + 16 bytes a token and kv head, and not far behind the vector instructions.  64 contexts of 4340 tokens on
+// average, 64 heads over 8, are 327 MB and take 62 us, 5.3 TB/s: 58 of this kernel and 4.7 of the join; from a cache of one page, so without
+// the memory, 53; a kernel that only reads as many bytes takes 49.  What is left is the start of a workgroup (5 us until its first loads are
+// in: lengths, page ids, codes, one after the other), its end, where the three workgroups of a compute unit are done one after the other,
+// and the join.  16 contexts of 2600 on average, 32 heads over 8: 15 us; one of 131072: 33.  A call with little to read is the start: 6 us.
 #include "basq_internal.h"
 
 #include <type_traits>

@@ -13,9 +13,9 @@
 // transform is positive.
 //
 // Bound by memory, with vector instructions not far behind (about 150 for a step of queries).  4096 tokens of 64 and 8 heads of 128 channels
-// move 173 MB in 34 us, 5.1 TB/s, 32768 tokens in 246 us, 5.6 (a large copy reaches 4.8); with the lanes' butterflies as two or three
-// instructions each and branches around loads and stores, 35.4 .. 36.5 and, for 1946 tokens of 40 and 40 heads of 64 channels, 17.9
-// instead of 16.2.  Sixteen tokens: 3.9 us, the launch and three loads one behind the other (position, cosines, heads).
+// move 173 MB in 33.6 us, 5.2 TB/s, 32768 tokens in 246 us, 5.6 (a large copy reaches 4.8).  With the lanes' butterflies as two or three
+// instructions each and branches around loads and stores 35.4 .. 36.5, and 17.9 instead of 15.7 for 1946 tokens of 40 and 40 heads of 64
+// channels; with the first heads requested behind the token's position 34.1 and 16.2.  Sixteen tokens: 3.6 us, the launch and three loads.
 #include "basq_internal.h"
 
 namespace basq {
@@ -118,12 +118,24 @@ __global__ __launch_bounds__(RA_WAVES * 64, 8) void rope_append_kernel(RopeAppen
     const int q_steps = (a.heads + HEADS - 1) / HEADS, kv_steps = (a.kv_heads + HEADS - 1) / HEADS;
     const int end = min(q_steps + 2 * kv_steps, (part + 1) * per);
 
+    // Loads and stores go through buffer descriptors that end with the heads there are: what lies behind them, and steps behind the last one,
+    // moves nothing, without a branch, so that a wait is for the one load it needs.
+    const uint32_t mine = 2 * (in_step * D + c0);
+    auto first_head = [&](int step) { return (step < q_steps ? step : step < q_steps + kv_steps ? step - q_steps : step - q_steps - kv_steps) * HEADS; };
+    auto request = [&](int step) {
+        const int first = first_head(step);
+        const uint16_t* row = step < q_steps ? a.q + t * a.ldq : step < q_steps + kv_steps ? a.k + t * a.ldk : a.v + t * a.ldv;
+        return __builtin_amdgcn_raw_buffer_load_b128(buffer(row + first * D, step < end ? ((step < q_steps ? a.heads : a.kv_heads) - first) * D * 2 : 0), mine, 0, NT);
+    };
+
+    // the first heads under way before the token's place is known (scalar loads: a vector load's wait would be for the heads too)
+    basq_v4u even_step = request(part * per), odd_step = request(part * per + 1);
     int position = 0;
     if (a.cos_sin) {
-        position = __builtin_amdgcn_readfirstlane(a.positions[t]);
+        position = ((const __attribute__((address_space(4))) int32_t*)a.positions)[t];
         if (position < 0 || position >= a.table_rows) return;   // padding
     }
-    const int slot = a.slots && a.kv_heads ? __builtin_amdgcn_readfirstlane(a.slots[t]) : -1;
+    const int slot = a.slots && a.kv_heads ? ((const __attribute__((address_space(4))) int32_t*)a.slots)[t] : -1;
 
     // out = x * co + pair * si
     float co[8], si[8];
@@ -157,15 +169,6 @@ __global__ __launch_bounds__(RA_WAVES * 64, 8) void rope_append_kernel(RopeAppen
         norm *= signs[b];
     }
 
-    // Loads and stores go through buffer descriptors that end with the heads there are: what lies behind them, and steps behind the last one,
-    // moves nothing, without a branch, so that a wait is for the one load it needs.
-    const uint32_t mine = 2 * (in_step * D + c0);
-    auto first_head = [&](int step) { return (step < q_steps ? step : step < q_steps + kv_steps ? step - q_steps : step - q_steps - kv_steps) * HEADS; };
-    auto request = [&](int step) {
-        const int first = first_head(step);
-        const uint16_t* row = step < q_steps ? a.q + t * a.ldq : step < q_steps + kv_steps ? a.k + t * a.ldk : a.v + t * a.ldv;
-        return __builtin_amdgcn_raw_buffer_load_b128(buffer(row + first * D, step < end ? ((step < q_steps ? a.heads : a.kv_heads) - first) * D * 2 : 0), mine, 0, NT);
-    };
     auto turn = [&](const basq_v4u& w, float (&x)[8]) {
         if (a.cos_sin) {
             float p[8];
@@ -228,7 +231,6 @@ __global__ __launch_bounds__(RA_WAVES * 64, 8) void rope_append_kernel(RopeAppen
         }
     };
 
-    basq_v4u even_step = request(part * per), odd_step = request(part * per + 1);
     int step = part * per;
     for (const int last = min(end, q_steps) - 1; step < last; step += 2) {
         basq_v4u w = even_step;
@@ -258,8 +260,8 @@ int launch(const RopeAppendArgs& a, hipStream_t s) {
     constexpr int HEADS = 512 / D;
     const int steps = (a.heads + HEADS - 1) / HEADS + 2 * ((a.kv_heads + HEADS - 1) / HEADS);
     // eight thousand waves, as many as the chip holds, while a token has steps for several of them, and one to a token from there on (half as
-    // many, as built, twice as many: 4096 tokens of 64 and 8 heads 35.2, 34.0, 33.7 us; 1946 of 40 and 40 heads of 64 channels 16.0, 16.2,
-    // 16.9; 668 of 64 and 8 8.6, 8.8, 10.8)
+    // many, as built, twice as many: 4096 tokens of 64 and 8 heads 35.0, 33.6, 33.0 us; 1946 of 40 and 40 heads of 64 channels 15.4, 15.7,
+    // 16.3; 668 of 64 and 8 8.2, 8.4, 10.0; 7081 of 28 and 4 15.5, 15.8, 18.5)
     int64_t parts = (8192 + a.T - 1) / a.T;
     if (parts > steps) parts = steps;
     const int per = (int)((steps + parts - 1) / parts);
