@@ -203,6 +203,15 @@ __device__ __forceinline__ void nt_store16(void* p, uint4 x) {
     __builtin_nontemporal_store(v, reinterpret_cast<basq_v4u*>(p));
 }
 
+// op of the values of lanes l, l ^ 16, l ^ 32 and l ^ 48 (lane by lane the same operands in the same order)
+template <class Op>
+__device__ __forceinline__ float across_rows(float v, Op op) {
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = op(__uint_as_float(p[0]), __uint_as_float(p[1]));
+    const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return op(__uint_as_float(q[0]), __uint_as_float(q[1]));
+}
+
 __device__ __forceinline__ float bf16_to_f32(uint16_t b) { return __uint_as_float(((uint32_t)b) << 16); }
 
 // fp32 -> bf16 bits, round-half-to-even, NaN kept quiet.

@@ -62,13 +62,13 @@ __device__ __forceinline__ v8h spread(uint32_t x) {
     return __builtin_bit_cast(v8h, w);
 }
 __device__ __forceinline__ float quarters_max(float v) {
-    v = fmaxf(v, __shfl_xor(v, 16, 64));
-    return fmaxf(v, __shfl_xor(v, 32, 64));
+    return across_rows(v, [](float a, float b) { return fmaxf(a, b); });
 }
 __device__ __forceinline__ float quarters_sum(float v) {
-    v += __shfl_xor(v, 16, 64);
-    return v + __shfl_xor(v, 32, 64);
+    return across_rows(v, [](float a, float b) { return a + b; });
 }
+// the value of lane ^ 8
+__device__ __forceinline__ float half_row_on(float v) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x128, 0xF, 0xF, true)); }
 
 #define PA_LDS_PTR(p) ((__attribute__((address_space(3))) void*)(p))
 
@@ -352,7 +352,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 || (D == 128 && !FOLD) ? 2 :
 
     auto row_max = [&](float v) {
         v = quarters_max(v);
-        return FOLD ? fmaxf(v, __shfl_xor(v, 8, 64)) : v;
+        return FOLD ? fmaxf(v, half_row_on(v)) : v;
     };
     auto work = [&](const Part& part, int i, int t, int stage) {
         const uint8_t* blocks = ring + stage * 2 * Block<D>::BYTES;
@@ -515,8 +515,8 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 || (D == 128 && !FOLD) ? 2 :
         l = quarters_sum(l);
         lows = quarters_sum(lows);
         if constexpr (FOLD) {
-            l += __shfl_xor(l, 8, 64);
-            lows += __shfl_xor(lows, 8, 64);
+            l += half_row_on(l);
+            lows += half_row_on(lows);
         }
         if (joined) lds_barrier();                                // the part before is read
         joined = true;

@@ -7,9 +7,9 @@
 //
 // Bound by memory: 8 bytes a channel with everything in bf16 and about ten vector instructions.  A token stays in registers from
 // its only read to its only write: a workgroup holds it in 16-byte pieces, thread t those of number t, t + THREADS, ...  4096 tokens of
-// 8192 channels, 268 MB: 42.5 us, 6.3 TB/s (a large copy reaches 4.8).  Eight pieces a thread 50 us, four 43.5; without the
-// non-temporal hint on what is read and on h 47.4; with it on y too, which the next kernel reads, 46.  One token: 2.0 us, of which the
-// launch is most.
+// 8192 channels, 268 MB: 41.5 us, 6.5 TB/s (a large copy reaches 4.8).  Eight pieces a thread 50 us, four 43.5; without the
+// non-temporal hint on what is read and on h 47.4; with it on y too, which the next kernel reads, 46; with the weight read behind the sum
+// and sums through LDS 42.1, 61 tokens 4.2 instead of 3.8.  One token: 1.8 us, of which the launch is most.
 #include "basq_internal.h"
 
 namespace basq {
@@ -26,10 +26,17 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 __device__ __forceinline__ float low_f32(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high_f32(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xF, 0xF, true));
+}
 template <int THREADS, class Op>
 __device__ __forceinline__ float across(float v, float* scratch, Op op) {
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) v = op(v, __shfl_xor(v, off, 64));
+    v = op(v, dpp<0xB1>(v));                                     // the lane beside, the pair beside, both halves of eight, of sixteen
+    v = op(v, dpp<0x4E>(v));
+    v = op(v, dpp<0x141>(v));
+    v = op(v, dpp<0x140>(v));
+    v = across_rows(v, op);
     if constexpr (THREADS > 64) {
         if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
         __syncthreads();
@@ -48,7 +55,7 @@ __global__ __launch_bounds__(THREADS) void add_rms_norm_kernel(RmsNormArgs a) {
     const uint4* x = reinterpret_cast<const uint4*>(a.X + m * a.ldx);
     const uint4* r = reinterpret_cast<const uint4*>(RES ? a.residual + m * a.ldr : nullptr);
     const uint4* w = reinterpret_cast<const uint4*>(a.weight);
-    uint4 h[PIECES], g[PIECES];
+    uint4 h[PIECES], g[PIECES], weight[PIECES];
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
         const int p = tid + i * THREADS;
@@ -58,6 +65,13 @@ __global__ __launch_bounds__(THREADS) void add_rms_norm_kernel(RmsNormArgs a) {
             h[i] = nt_load16(x + p);
             if (RES) g[i] = nt_load16(r + p);
         }
+    }
+    // (before anything is stored: a wait for them would be for the stores too)
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const int p = tid + i * THREADS;
+        weight[i] = make_uint4(0, 0, 0, 0);
+        if (p < pieces) weight[i] = w[p];
     }
     float sum = 0.0f;
 #pragma unroll
@@ -73,12 +87,6 @@ __global__ __launch_bounds__(THREADS) void add_rms_norm_kernel(RmsNormArgs a) {
         const int p = tid + i * THREADS;
         if (a.res_out && p < pieces) nt_store16(reinterpret_cast<uint4*>(a.res_out + m * a.ldro) + p, h[i]);
     }
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-        const int p = tid + i * THREADS;
-        g[i] = make_uint4(0, 0, 0, 0);
-        if (p < pieces) g[i] = w[p];
-    }
     sum = across<THREADS>(sum, scratch[0], [](float u, float v) { return u + v; });
     const float rstd = rsqrtf(sum / (float)a.K + a.eps);
 
@@ -87,12 +95,12 @@ __global__ __launch_bounds__(THREADS) void add_rms_norm_kernel(RmsNormArgs a) {
     for (int i = 0; i < PIECES; ++i) {
         const int p = tid + i * THREADS;
         const uint32_t* hw = reinterpret_cast<const uint32_t*>(&h[i]);
-        const uint32_t* gw = reinterpret_cast<const uint32_t*>(&g[i]);
+        const uint32_t* ww = reinterpret_cast<const uint32_t*>(&weight[i]);
         uint4 out;
         uint32_t* ow = reinterpret_cast<uint32_t*>(&out);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float u = low_f32(hw[j]) * rstd * low_f32(gw[j]), v = high_f32(hw[j]) * rstd * high_f32(gw[j]);
+            const float u = low_f32(hw[j]) * rstd * low_f32(ww[j]), v = high_f32(hw[j]) * rstd * high_f32(ww[j]);
             ow[j] = pack_bf16(u, v);
             top = fmaxf(top, fmaxf(fabsf(u), fabsf(v)));
         }
@@ -109,12 +117,12 @@ __global__ __launch_bounds__(THREADS) void add_rms_norm_kernel(RmsNormArgs a) {
         const int p = tid + i * THREADS;
         if (p >= pieces) break;
         const uint32_t* hw = reinterpret_cast<const uint32_t*>(&h[i]);
-        const uint32_t* gw = reinterpret_cast<const uint32_t*>(&g[i]);
+        const uint32_t* ww = reinterpret_cast<const uint32_t*>(&weight[i]);
         uint32_t c[2];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             // (a product may be one rounding over the largest number; NaN stays NaN)
-            float u = low_f32(hw[j]) * rstd * low_f32(gw[j]) * inv, v = high_f32(hw[j]) * rstd * high_f32(gw[j]) * inv;
+            float u = low_f32(hw[j]) * rstd * low_f32(ww[j]) * inv, v = high_f32(hw[j]) * rstd * high_f32(ww[j]) * inv;
             if (fabsf(u) > 448.0f) u = copysignf(448.0f, u);
             if (fabsf(v) > 448.0f) v = copysignf(448.0f, v);
             c[j / 2] = j % 2 ? __builtin_amdgcn_cvt_pk_fp8_f32(u, v, c[j / 2], true) : __builtin_amdgcn_cvt_pk_fp8_f32(u, v, 0, false);
