@@ -203,6 +203,13 @@ __device__ __forceinline__ void nt_store16(void* p, uint4 x) {
     __builtin_nontemporal_store(v, reinterpret_cast<basq_v4u*>(p));
 }
 
+// A grid of at least n workgroups, in rows of up to 2^20: one dimension's threads have to be fewer than 2^32.
+inline dim3 grid_of(int64_t n) {
+    const int64_t row = n < (1 << 20) ? n : 1 << 20;
+    return dim3((unsigned)row, (unsigned)((n + row - 1) / row));
+}
+__device__ __forceinline__ int64_t workgroup_of_grid() { return blockIdx.x + (int64_t)blockIdx.y * gridDim.x; }
+
 // op of the values of lanes l, l ^ 16, l ^ 32 and l ^ 48 (lane by lane the same operands in the same order)
 template <class Op>
 __device__ __forceinline__ float across_rows(float v, Op op) {

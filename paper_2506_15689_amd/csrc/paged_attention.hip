@@ -724,7 +724,7 @@ int launch(const PagedAttentionArgs& a, hipStream_t s) {
     // Where segments go whole, each has a workgroup of its own, and the next free compute unit takes the next one; but where all are
     // short, starting is most of it, and a workgroup prepares its next segment beside the one that it works on.
     const bool brief = a.workers == 0 && longest_units(a.q_len, a.max_len, a.window) <= 4;
-    const unsigned blocks = (unsigned)(a.workers > 0 ? a.workers : brief && segments > resident(D, a.group * a.q_len) ? resident(D, a.group * a.q_len) : segments);
+    const unsigned blocks = (unsigned)(a.workers > 0 ? a.workers : brief && segments > resident(D, a.group * a.q_len) ? resident(D, a.group * a.q_len) : segments < (1 << 20) ? segments : 1 << 20);
     if (a.waves == 8) launch_waves<D, 8>(a, blocks, s);
     else launch_waves<D, 4>(a, blocks, s);
     const int rc = check_hip(hipGetLastError(), "paged_attention launch");
@@ -776,7 +776,7 @@ int launch_paged_attention(PagedAttentionArgs a, hipStream_t s) {
     a.group = a.heads / a.kv_heads;
     a.row_tiles = (a.group * a.q_len + 15) / 16;
     a.cap_log2e = a.softcap * LOG2E;
-    a.inv_cap = a.softcap > 0.0f ? 1.0f / a.cap_log2e : 0.0f;
+    a.inv_cap = a.softcap > 0.0f ? fminf(1.0f / a.cap_log2e, 0x1p127f) : 0.0f;
     return a.D == 64 ? launch<64>(a, s) : launch<128>(a, s);
 }
 

@@ -50,7 +50,8 @@ __device__ __forceinline__ float across(float v, float* scratch, Op op) {
 template <int THREADS, int PIECES, bool RES>
 __global__ __launch_bounds__(THREADS) void add_rms_norm_kernel(RmsNormArgs a) {
     __shared__ float scratch[2][THREADS / 64];
-    const int64_t m = blockIdx.x;
+    const int64_t m = workgroup_of_grid();
+    if (m >= a.M) return;
     const int tid = threadIdx.x, pieces = a.K / 8;
     const uint4* x = reinterpret_cast<const uint4*>(a.X + m * a.ldx);
     const uint4* r = reinterpret_cast<const uint4*>(RES ? a.residual + m * a.ldr : nullptr);
@@ -133,8 +134,8 @@ __global__ __launch_bounds__(THREADS) void add_rms_norm_kernel(RmsNormArgs a) {
 
 template <int THREADS, int PIECES>
 void launch(const RmsNormArgs& a, hipStream_t s) {
-    if (a.residual) hipLaunchKernelGGL((add_rms_norm_kernel<THREADS, PIECES, true>), dim3((unsigned)a.M), dim3(THREADS), 0, s, a);
-    else hipLaunchKernelGGL((add_rms_norm_kernel<THREADS, PIECES, false>), dim3((unsigned)a.M), dim3(THREADS), 0, s, a);
+    if (a.residual) hipLaunchKernelGGL((add_rms_norm_kernel<THREADS, PIECES, true>), grid_of(a.M), dim3(THREADS), 0, s, a);
+    else hipLaunchKernelGGL((add_rms_norm_kernel<THREADS, PIECES, false>), grid_of(a.M), dim3(THREADS), 0, s, a);
 }
 
 }  // namespace

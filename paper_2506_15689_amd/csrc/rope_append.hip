@@ -110,7 +110,7 @@ template <int D, bool INTERLEAVED>
 __global__ __launch_bounds__(RA_WAVES * 64, 8) void rope_append_kernel(RopeAppendArgs a, int parts, int per) {
     constexpr int LANES = D / 8, HEADS = 64 / LANES;             // lanes of a head, heads of a step
     const int lane = threadIdx.x & 63;
-    const uint32_t wave = blockIdx.x * (uint32_t)RA_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t wave = (uint32_t)workgroup_of_grid() * RA_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t t = (uint32_t)__builtin_amdgcn_readfirstlane(wave / (uint32_t)parts);
     if (t >= a.T) return;
     const int part = (int)(wave - (uint32_t)t * (uint32_t)parts);
@@ -267,15 +267,15 @@ int launch(const RopeAppendArgs& a, hipStream_t s) {
     const int per = (int)((steps + parts - 1) / parts);
     parts = (steps + per - 1) / per;
     const int64_t blocks = (a.T * parts + RA_WAVES - 1) / RA_WAVES;
-    if (blocks * RA_WAVES > 0xFFFFFFFFll) return fail(BASQ_EUNSUPPORTED, "rope_append: too many tokens");
-    if (a.interleaved) hipLaunchKernelGGL((rope_append_kernel<D, true>), dim3((unsigned)blocks), dim3(RA_WAVES * 64), 0, s, a, (int)parts, per);
-    else hipLaunchKernelGGL((rope_append_kernel<D, false>), dim3((unsigned)blocks), dim3(RA_WAVES * 64), 0, s, a, (int)parts, per);
+    if (blocks * RA_WAVES > 0x7FFFFFFFll) return fail(BASQ_EUNSUPPORTED, "rope_append: too many tokens");
+    if (a.interleaved) hipLaunchKernelGGL((rope_append_kernel<D, true>), grid_of(blocks), dim3(RA_WAVES * 64), 0, s, a, (int)parts, per);
+    else hipLaunchKernelGGL((rope_append_kernel<D, false>), grid_of(blocks), dim3(RA_WAVES * 64), 0, s, a, (int)parts, per);
     return check_hip(hipGetLastError(), "rope_append launch");
 }
 
 __global__ __launch_bounds__(256) void rope_table_kernel(float* out, int64_t rows, int rot, RopeScaling k) {
     const int half = rot / 2;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t i = workgroup_of_grid() * 256 + threadIdx.x;
     if (i >= rows * half) return;
     const int64_t row = i / half;
     const int j = (int)(i - row * half);
@@ -314,7 +314,7 @@ int launch_rope_table(float* out, int64_t rows, int32_t rot, const RopeScaling& 
     if (rows == 0) return BASQ_OK;
     const int64_t blocks = (rows * (rot / 2) + 255) / 256;
     if (blocks > 0x7FFFFFFFll) return fail(BASQ_EUNSUPPORTED, "rope_table: too many positions");
-    hipLaunchKernelGGL(rope_table_kernel, dim3((unsigned)blocks), dim3(256), 0, s, out, rows, rot, k);
+    hipLaunchKernelGGL(rope_table_kernel, grid_of(blocks), dim3(256), 0, s, out, rows, rot, k);
     return check_hip(hipGetLastError(), "rope_table launch");
 }
 

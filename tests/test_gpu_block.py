@@ -570,3 +570,28 @@ def test_on_another_stream_and_in_a_graph():
         assert all(torch.equal(a, b) for a, b in zip(want, bufs))
         step()
         torch.cuda.synchronize()
+
+
+def test_more_tokens_than_one_grid_dimension_has_threads():
+    """2^26 and a few tokens, of which 64 threads each are 2^32: norm and append, the last tokens and those around 2^26."""
+    M, K = 2 ** 26 + 3, 8
+    picked = torch.tensor([0, 1, 2 ** 20 - 1, 2 ** 20, 2 ** 26 - 1, 2 ** 26, 2 ** 26 + 2], device=DEV)
+    x, y = torch.zeros(M, K, dtype=BF16, device=DEV), torch.full((M, K), 9.0, dtype=BF16, device=DEV)
+    x[picked] = randn(gen(20), len(picked), K).to(BF16)
+    w = torch.ones(K, dtype=BF16, device=DEV)
+    B.basq_add_rms_norm(x, None, w, 1e-5, y)
+    check_norm(y[picked], ref.add_rms_norm(x[picked], None, w, 1e-5)[1])
+    assert int((y != 0).any(1).sum()) == len(picked)
+    del x, y
+    q = torch.zeros(M, 1, 64, dtype=BF16, device=DEV)
+    q[picked] = randn(gen(21), len(picked), 1, 64).to(BF16)
+    want = ref.turn(q[picked], None, None, False, True).to(BF16)
+    B.basq_rope_append(q, None, None, None, None, None, None, 0.9, 0.9, q)
+    assert torch.equal(q[picked].cpu(), want)
+    assert int((q.view(torch.int64) != 0).flatten(1).any(1).sum()) == len(picked)
+
+
+@pytest.mark.parametrize("softcap", [1e-40, 1e-38])
+def test_attention_of_the_smallest_caps(softcap):
+    """1 / cap is past the end of fp32: all tokens count alike."""
+    check_attention(*attention_case(22, [1, 40, 300], 8, 2, 128, 16, 1), 300, softcap=softcap)
