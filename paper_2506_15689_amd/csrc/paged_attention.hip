@@ -356,15 +356,30 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 || (D == 128 && !FOLD) ? 2 :
     };
     auto work = [&](const Part& part, int i, int t, int stage) {
         const uint8_t* blocks = ring + stage * 2 * Block<D>::BYTES;
+        // All that the step reads from LDS, in the order of its use, before any of it is used.
+        // (As integers: in front of a float-typed read of LDS the compiler waits for every direct load.)
+        typedef int Keys __attribute__((ext_vector_type(KS)));
+        Keys kw[2];
+        v4i range[MINE / 4][4];                                   // (scale, lo) of a lane's tokens, two in each: keys', values'
+        uint32_t v[8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) kw[h] = *reinterpret_cast<const Keys*>(blocks + h * Block<D>::BYTES + k_at);
+#pragma unroll
+        for (int h = 0; h < MINE / 4; ++h)
+#pragma unroll
+            for (int n = 0; n < 4; ++n) range[h][n] = *reinterpret_cast<const v4i*>(blocks + h * Block<D>::BYTES + r_at + 128 * (n / 2) + 16 * (n % 2));
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            const uint8_t* from = blocks + (r / 4) * Block<D>::BYTES + v_at + (r % 4) * (2 * D);
+            v[r] = D == 128 ? (uint32_t)*reinterpret_cast<const int*>(from) : *reinterpret_cast<const uint16_t*>(from);
+        }
+        __builtin_amdgcn_sched_barrier(0);
         v4f acc[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            // (as integers, here and below: in front of a float-typed read of LDS the compiler waits for every direct load)
-            typedef int Keys __attribute__((ext_vector_type(KS)));
-            const Keys kw = *reinterpret_cast<const Keys*>(blocks + h * Block<D>::BYTES + k_at);
             acc[h] = (v4f){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int n = 0; n < KS; ++n) acc[h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(spread(kw[n]), q[n], acc[h], 0, 0, 0);
+            for (int n = 0; n < KS; ++n) acc[h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(spread(kw[h][n]), q[n], acc[h], 0, 0, 0);
         }
         // folded, columns 8 .. 15 are the rows of 0 .. 7 again, for the second block
         if constexpr (FOLD)
@@ -374,11 +389,9 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 || (D == 128 && !FOLD) ? 2 :
         float least = INFINITY;                                   // scale of a value
 #pragma unroll
         for (int h = 0; h < MINE / 4; ++h) {
-            const uint8_t* ranges = blocks + h * Block<D>::BYTES + r_at;
 #pragma unroll
-            for (int r = 0; r < 4; r += 2) {                       // (scale, lo) of two tokens each
-                const v4f kr = __builtin_bit_cast(v4f, *reinterpret_cast<const v4i*>(ranges + 8 * r));
-                const v4f vr = __builtin_bit_cast(v4f, *reinterpret_cast<const v4i*>(ranges + 128 + 8 * r));
+            for (int r = 0; r < 4; r += 2) {
+                const v4f kr = __builtin_bit_cast(v4f, range[h][r / 2]), vr = __builtin_bit_cast(v4f, range[h][2 + r / 2]);
 #pragma unroll
                 for (int n = 0; n < 2; ++n) {
                     // less M; with a cap, M goes off behind that
@@ -484,12 +497,6 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 || (D == 128 && !FOLD) ? 2 :
             for (int n = 0; n < 8; ++n) pw[n] = (_Float16)w[n];
         }
         // channels x tokens of the values: pairs of tokens side by side, then a code of both per instruction
-        uint32_t v[8];
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
-            const uint8_t* from = blocks + (r / 4) * Block<D>::BYTES + v_at + (r % 4) * (2 * D);
-            v[r] = D == 128 ? (uint32_t)*reinterpret_cast<const int*>(from) : *reinterpret_cast<const uint16_t*>(from);
-        }
         constexpr int HALVES = D == 128 ? 2 : 1;
 #pragma unroll
         for (int half = 0; half < HALVES; ++half) {
