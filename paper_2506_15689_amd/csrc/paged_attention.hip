@@ -25,13 +25,14 @@
 // Codes and ranges come by direct loads into a ring of LDS stages that the wave has to itself, a step ahead of the one that is
 // worked on: registers hold none of it, and three workgroups of four waves fit a compute unit (loads into registers and two workgroups took
 // a quarter longer; three or four stages and two workgroups, or four workgroups, gain nothing).  The loads carry the non-temporal hint:
-// nothing is read twice (without it a sixth longer).
+// nothing is read twice (without it a sixth longer).  With two steps under way, the second requested once the first is in registers, calls
+// take 1 .. 3 % longer.
 //
 // Bound: reading the cache, D + 16 bytes a token and kv head, and not far behind the vector instructions.  64 contexts of 4340 tokens on
-// average, 64 heads over 8, are 327 MB and take 62 us, 5.3 TB/s: 58 of this kernel and 4.7 of the join; from a cache of one page, so without
+// average, 64 heads over 8, are 327 MB and take 61 us, 5.4 TB/s: 56 .. 57 of this kernel and 4.7 of the join; from a cache of one page, so without
 // the memory, 53; a kernel that only reads as many bytes takes 49.  What is left is the start of a workgroup (5 us until its first loads are
 // in: lengths, page ids, codes, one after the other), its end, where the three workgroups of a compute unit are done one after the other,
-// and the join.  16 contexts of 2600 on average, 32 heads over 8: 15 us; one of 131072: 33.  A call with little to read is the start: 6 us.
+// and the join.  16 contexts of 2600 on average, 32 heads over 8: 15.4 us; one of 131072: 32.7.  A call with little to read is the start: 6 us.
 #include "basq_internal.h"
 
 #include <type_traits>
@@ -633,13 +634,14 @@ template <int D, int WAVES>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void paged_attention_join_kernel(PagedAttentionArgs a) {
     constexpr int LANES = D / 4, GROUPS = WAVES * 64 / LANES, AHEAD = WAVES == 1 ? 4 : 8;
     __shared__ float lds[WAVES][LANES][6];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int wave = same(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const uint32_t row = WAVES == 1 ? blockIdx.x * 4 + wave : blockIdx.x;            // (fewer than 2^31 rows)
     if (row >= (uint32_t)a.B * a.q_len * a.heads) return;
-    const int64_t token = row / (uint32_t)a.heads;
-    const int head = (int)(row - token * a.heads), b = (int)(token / a.q_len), j = (int)(token - (int64_t)b * a.q_len);
-    const int in_kv = j * a.group + head % a.group;
-    const int2 where = a.part_of[((int64_t)b * a.kv_heads + head / a.group) * a.row_tiles + in_kv / 16];
+    const uint32_t token = same(row / (uint32_t)a.heads);
+    const int head = same(row - token * a.heads), kv_head = same((uint32_t)head / (uint32_t)a.group);
+    const int b = a.q_len == 1 ? (int)token : same(token / (uint32_t)a.q_len), j = (int)token - b * a.q_len;
+    const int in_kv = j * a.group + head - kv_head * a.group;
+    const int2 where = a.part_of[((int64_t)b * a.kv_heads + kv_head) * a.row_tiles + in_kv / 16];
     const int parts = where.y;
     if (parts <= 1) return;
     const int piece = lane % LANES, group0 = (WAVES == 1 ? 0 : wave * (64 / LANES)) + lane / LANES;
