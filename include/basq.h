@@ -310,7 +310,8 @@ int basq_hadamard28(int8_t* out_host);
  *
  *     h_k = bf16(X[m,k] + residual[m,k])                             (X[m,k] without a residual)
  *     y_k = (h_k * rstd) * weight_k ,   rstd = 1 / sqrt(mean_k h_k^2 + eps)          fp32
- *     Y8[m,k] = e4m3(y_k / s_m) ,   s_m = max_k |y_k| / 448          (1 if not a positive finite number)
+ *     Y8[m,k] = e4m3(y_k / s_m) ,   s_m = max_k |y_k| / 448          fp32; s_m = 1 if not a positive finite number, quotients beyond
+ *                                                                    +-448 are +-448, NaN stays NaN
  *
  *   X, residual  bf16 [M, ldx], [M, ldr]; residual may be NULL.   weight  bf16 [K]
  *   res_out      out, bf16 [M, ldro]: h, or NULL.  May be X or residual (with that one's stride)

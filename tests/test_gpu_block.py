@@ -595,3 +595,42 @@ def test_more_tokens_than_one_grid_dimension_has_threads():
 def test_attention_of_the_smallest_caps(softcap):
     """1 / cap is past the end of fp32: all tokens count alike."""
     check_attention(*attention_case(22, [1, 40, 300], 8, 2, 128, 16, 1), 300, softcap=softcap)
+
+
+def test_norm_in_8_bits_is_a_quotient():
+    """y / s rounded to e4m3, code by code: h of 1 and -1 have rstd = 1, so that y is the weight; every 8-bit significand under every largest
+    one, among them quotients that lie between two codes, where a product with 1 / s comes out beside them."""
+    significands = torch.arange(128, 256).float()
+    for top in range(128, 256):
+        w = torch.cat([significands * 2.0 ** -k for k in range(9)])
+        w = w[w <= top]
+        w = torch.cat([w, w.new_zeros(-len(w) % 8)])
+        x = torch.ones(2, len(w))
+        x[1, ::2] = -1.0
+        y8, s8 = torch.empty(2, len(w), dtype=torch.float8_e4m3fn, device=DEV), torch.empty(2, device=DEV)
+        B.basq_add_rms_norm(x.to(DEV, BF16), None, w.to(DEV, BF16), 0.0, None, Y8=y8, y8_scale=s8)
+        s = torch.tensor(float(top)) / torch.tensor(448.0)
+        assert (s8.cpu() == s).all(), top
+        want = (x * w / s).clamp(-448, 448).to(torch.float8_e4m3fn)
+        assert torch.equal(y8.cpu().float(), want.float()), top
+
+
+@pytest.mark.parametrize("size", [1e-30, 1e-35, 1e-36, 1e-37])
+def test_norm_in_8_bits_of_tiny_rows(size):
+    """Scales whose reciprocal is past the end of fp32, down to subnormal ones; some outputs are 0."""
+    g = gen(25)
+    M, K = 5, 1032
+    x = randn(g, M, K).to(BF16)
+    x[:, ::7] = 0
+    w = (size * (1 + 0.2 * randn(g, K))).to(BF16)
+    y8, s8 = torch.empty(M, K, dtype=torch.float8_e4m3fn, device=DEV), torch.empty(M, device=DEV)
+    B.basq_add_rms_norm(x, None, w, 1e-5, None, Y8=y8, y8_scale=s8)
+    _, want = ref.add_rms_norm(x, None, w, 1e-5)
+    # fp32: 2^-16 as in check_norm, and half of the smallest subnormal number for each of three roundings
+    slack = want.abs() * 2.0 ** -16 + 2.0 ** -148
+    top, s = want.abs().amax(1), ref.f64(s8)
+    assert ((s - top / 448).abs() <= top / 448 * 2.0 ** -16 + 2.0 ** -148).all()
+    # monotonic roundings: a code lies between those of the ends
+    got = ref.f64(y8.float())
+    low, high = (((want + d) / s[:, None]).clamp(-448, 448).float().to(torch.float8_e4m3fn).double() for d in (-slack, slack))
+    assert ((got >= low) & (got <= high)).all()
