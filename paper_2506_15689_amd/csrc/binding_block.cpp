@@ -57,7 +57,10 @@ struct Call {
     }
 };
 
-void* data(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
+// Where a tensor's values are.  Asked for while the GIL is held: it throws for tensors without storage of their own (those that stand for
+// others under torch.vmap, say).
+template <class T = void>
+T* data(const at::Tensor* t) { return t ? static_cast<T*>(t->data_ptr()) : nullptr; }
 
 // a tensor [rows, ...] of this shape whose rows are contiguous: its row stride (one row has no stride of its own)
 int64_t rows_of(const at::Tensor& t, const at::Tensor& like, const char* name, at::ScalarType type) {
@@ -161,11 +164,12 @@ PyObject* add_rms_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
         const int64_t ldy8 = Y8 ? rows_of(*Y8, X, "Y8", at::kFloat8_e4m3fn) : 0;
         if (y8_scale) vector_of(*y8_scale, M, "y8_scale", at::kFloat);
         c.same_gpu();
+        const void *x = data(&X), *r = data(residual), *w = data(&weight);
+        void *h = data(res_out), *y = data(Y);
+        uint8_t* y8 = data<uint8_t>(Y8);
+        float* scale = data<float>(y8_scale);
         void* stream = stream_of(args[8], args[9]);
-        return without_gil([&] {
-            return basq_add_rms_norm(data(&X), data(residual), data(&weight), M, K, ldx, ldr, eps, data(res_out), ldro, data(Y), ldy,
-                                     (uint8_t*)data(Y8), ldy8, (float*)data(y8_scale), stream);
-        });
+        return without_gil([&] { return basq_add_rms_norm(x, r, w, M, K, ldx, ldr, eps, h, ldro, y, ldy, y8, ldy8, scale, stream); });
     });
 }
 
@@ -221,12 +225,15 @@ PyObject* rope_append(PyObject*, PyObject* const* args, Py_ssize_t n) {
             vector_of(*positions, T, "positions", at::kInt);
         }
         c.same_gpu();
+        const void *qs = data(q), *ks = data(k), *vs = data(v);
+        const int32_t *at = data<int32_t>(positions), *to = data<int32_t>(slots);
+        const float* table = data<float>(cos_sin);
+        uint8_t* blocks = data<uint8_t>(cache);
+        void *turned = data(q_out), *kh = data(k_hat), *vh = data(v_hat);
         void* stream = stream_of(args[15], args[16]);
         return without_gil([&] {
-            return basq_rope_append(data(q), ldq, data(k), ldk, data(v), ldv, T, heads, kv_heads, head_dim, (const int32_t*)data(positions),
-                                    (const float*)data(cos_sin), table_rows, rot, interleaved, rotate, clip_lo, clip_hi, bits,
-                                    (const int32_t*)data(slots), (uint8_t*)data(cache), pages, page_size, data(q_out), ldqo, data(k_hat),
-                                    data(v_hat), ldh, stream);
+            return basq_rope_append(qs, ldq, ks, ldk, vs, ldv, T, heads, kv_heads, head_dim, at, table, table_rows, rot, interleaved, rotate, clip_lo,
+                                    clip_hi, bits, to, blocks, pages, page_size, turned, ldqo, kh, vh, ldh, stream);
         });
     });
 }
@@ -261,12 +268,18 @@ PyObject* paged_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
         if (workspace && !workspace->is_contiguous()) refuse("workspace must be contiguous");
         const int32_t sequences = narrow(B, "B"), head_dim = narrow(D, "head_dim"), all_heads = narrow(heads, "heads");
         const int32_t kv_heads = narrow(cache.size(1), "kv_heads"), pages = narrow(cache.size(0), "pages");
+        const int64_t table_stride = B > 1 ? table.stride(0) : table.size(1);
+        const size_t room = workspace ? workspace->nbytes() : 0;
         c.same_gpu();
+        const void* rows_q = data(&q);
+        const uint8_t* blocks = data<uint8_t>(&cache);
+        const int32_t *page_of = data<int32_t>(&table), *lens = data<int32_t>(&lengths);
+        void *result = data(&out), *parts = data(workspace);
+        float* sums = data<float>(lse);
         void* stream = stream_of(args[13], args[14]);
         return without_gil([&] {
-            return basq_paged_attention(data(&q), ldq, sequences, q_len, all_heads, kv_heads, head_dim, bits, (const uint8_t*)data(&cache), pages,
-                                        page_size, (const int32_t*)data(&table), B > 1 ? table.stride(0) : table.size(1), (const int32_t*)data(&lengths), max_len, scale, softcap, window,
-                                        data(&out), ldo, (float*)data(lse), data(workspace), workspace ? workspace->nbytes() : 0, stream);
+            return basq_paged_attention(rows_q, ldq, sequences, q_len, all_heads, kv_heads, head_dim, bits, blocks, pages, page_size, page_of, table_stride,
+                                        lens, max_len, scale, softcap, window, result, ldo, sums, parts, room, stream);
         });
     });
 }

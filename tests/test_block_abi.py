@@ -1,6 +1,8 @@
 """The operators around the linear layer without a GPU: what they refuse, before anything would be launched."""
 import ctypes
 import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -168,3 +170,47 @@ def test_binding_refuses_tensors_that_do_not_fit(lib):
         B.basq_add_rms_norm(x, None, w, "small", z(4, 64))
     with pytest.raises(ValueError, match="must be a tensor"):
         B.basq_add_rms_norm(x, None, w.tolist(), 1e-5, z(4, 64))
+
+
+WRAPPED = """
+import types
+import torch
+from torch._subclasses.fake_tensor import FakeTensorMode
+from paper_2506_15689_amd import binding as B
+
+handle = types.SimpleNamespace(cuda_stream=0)
+bf16 = lambda *s: torch.empty(s, dtype=torch.bfloat16, device="cuda")
+i32 = lambda *s: torch.empty(s, dtype=torch.int32, device="cuda")
+refused = 0
+with FakeTensorMode():
+    x, w, q, k = bf16(2, 3, 64), bf16(64), bf16(2, 3, 4, 64), bf16(3, 2, 64)
+    cache = torch.empty((5, 2, 16 * 80), dtype=torch.uint8, device="cuda")
+
+    def norm(x):
+        B.basq_add_rms_norm(x, None, w, 1e-5, x, stream=handle)
+        return x
+
+    def append(q):
+        B.basq_rope_append(q, k, k, None, None, i32(3), cache, 0.9, 0.9, q, stream=handle)
+        return q
+
+    def attend(q):
+        B.basq_paged_attention(q, cache, i32(3, 4), i32(3), 64, 0.1, q, None, stream=handle)
+        return q
+
+    for call, t in [(norm, x), (append, q), (attend, q)]:
+        for wrapped in [lambda: torch.vmap(call)(t), lambda: torch.func.jvp(call, (t[0],), (t[0],))]:
+            try:
+                wrapped()
+            except RuntimeError as e:
+                refused += "storage" in str(e)
+print("refused", refused)
+"""
+
+
+def test_tensors_without_storage_are_an_error(lib):
+    """Tensors that stand for others (under torch.vmap, with a tangent) have no values of their own to point to: an exception, not the end
+    of the process."""
+    done = subprocess.run([sys.executable, "-c", WRAPPED], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
+                          stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=300)
+    assert done.returncode == 0 and done.stdout.split()[-2:] == ["refused", "6"], done.stdout[-2000:]
