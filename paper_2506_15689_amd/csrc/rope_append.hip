@@ -15,7 +15,8 @@
 // Bound by memory, with vector instructions not far behind (about 150 for a step of queries).  4096 tokens of 64 and 8 heads of 128 channels
 // move 173 MB in 33.6 us, 5.2 TB/s, 32768 tokens in 246 us, 5.6 (a large copy reaches 4.8).  With the lanes' butterflies as two or three
 // instructions each and branches around loads and stores 35.4 .. 36.5, and 17.9 instead of 15.7 for 1946 tokens of 40 and 40 heads of 64
-// channels; with the first heads requested behind the token's position 34.1 and 16.2.  Sixteen tokens: 3.6 us, the launch and three loads.
+// channels.  (The first heads are requested once the token's position is known: requested beside it, 1 .. 2 % less, but padding's would be read.)
+// Sixteen tokens: 3.6 us, the launch and four loads, one after the other.
 #include "basq_internal.h"
 
 namespace basq {
@@ -128,14 +129,14 @@ __global__ __launch_bounds__(RA_WAVES * 64, 8) void rope_append_kernel(RopeAppen
         return __builtin_amdgcn_raw_buffer_load_b128(buffer(row + first * D, step < end ? ((step < q_steps ? a.heads : a.kv_heads) - first) * D * 2 : 0), mine, 0, NT);
     };
 
-    // the first heads under way before the token's place is known (scalar loads: a vector load's wait would be for the heads too)
-    basq_v4u even_step = request(part * per), odd_step = request(part * per + 1);
+    // where the token stands and goes (scalar loads: a vector load's wait would be for the heads too); of padding no head is read
+    const int slot = a.slots && a.kv_heads ? ((const __attribute__((address_space(4))) int32_t*)a.slots)[t] : -1;
     int position = 0;
     if (a.cos_sin) {
         position = ((const __attribute__((address_space(4))) int32_t*)a.positions)[t];
-        if (position < 0 || position >= a.table_rows) return;   // padding
+        if (position < 0 || position >= a.table_rows) return;
     }
-    const int slot = a.slots && a.kv_heads ? ((const __attribute__((address_space(4))) int32_t*)a.slots)[t] : -1;
+    basq_v4u even_step = request(part * per), odd_step = request(part * per + 1);
 
     // out = x * co + pair * si
     float co[8], si[8];

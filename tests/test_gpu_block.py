@@ -634,3 +634,21 @@ def test_norm_in_8_bits_of_tiny_rows(size):
     got = ref.f64(y8.float())
     low, high = (((want + d) / s[:, None]).clamp(-448, 448).float().to(torch.float8_e4m3fn).double() for d in (-slack, slack))
     assert ((got >= low) & (got <= high)).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_append_of_padding_that_has_no_memory(D):
+    """Nothing of a padding token is read or written: rows that lie 128 GB apart, of which only the first is there."""
+    heads, kv_heads, P, far = 9, 3, 16, 1 << 36
+    x, table, cache, slots, _ = append_case(26, 3, heads, kv_heads, D, P, D)
+    q, k, v = (t[:1].contiguous() for t in (x[:, :heads], x[:, heads:heads + kv_heads], x[:, heads + kv_heads:]))
+    cache2 = cache.clone()
+    positions = torch.tensor([7, -1, 50], dtype=torch.int32, device=DEV)
+    want = [torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)]
+    B.basq_rope_append(q, k, v, positions[:1], table, slots[:1], cache2, 0.9, 0.8, *want)
+    got = [torch.full_like(t, 9.0) for t in want]
+    p = lambda t: t.data_ptr()  # noqa: E731
+    B._check(B.load().basq_rope_append(p(q), far, p(k), far, p(v), far, 3, heads, kv_heads, D, p(positions), p(table), 50, D, 0, 1, 0.9, 0.8, 4,
+                                       p(slots), p(cache), cache.shape[0], P, p(got[0]), far, p(got[1]), p(got[2]), far, B._stream(None)))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.equal(cache, cache2)
