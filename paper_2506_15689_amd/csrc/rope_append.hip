@@ -260,6 +260,7 @@ template <int D>
 int launch(const RopeAppendArgs& a, hipStream_t s) {
     constexpr int HEADS = 512 / D;
     const int steps = (a.heads + HEADS - 1) / HEADS + 2 * ((a.kv_heads + HEADS - 1) / HEADS);
+    if (a.T > 0x7FFFFFFFll) return fail(BASQ_EUNSUPPORTED, "rope_append: too many tokens");
     // eight thousand waves, as many as the chip holds, while a token has steps for several of them, and one to a token from there on (half as
     // many, as built, twice as many: 4096 tokens of 64 and 8 heads 35.0, 33.6, 33.0 us; 1946 of 40 and 40 heads of 64 channels 15.4, 15.7,
     // 16.3; 668 of 64 and 8 8.2, 8.4, 10.0; 7081 of 28 and 4 15.5, 15.8, 18.5)
@@ -313,8 +314,8 @@ int launch_rope_append(const RopeAppendArgs& a, hipStream_t s) {
 
 int launch_rope_table(float* out, int64_t rows, int32_t rot, const RopeScaling& k, hipStream_t s) {
     if (rows == 0) return BASQ_OK;
+    if (rows > 0x7FFFFFFFll * 256 / (rot / 2)) return fail(BASQ_EUNSUPPORTED, "rope_table: too many positions");
     const int64_t blocks = (rows * (rot / 2) + 255) / 256;
-    if (blocks > 0x7FFFFFFFll) return fail(BASQ_EUNSUPPORTED, "rope_table: too many positions");
     hipLaunchKernelGGL(rope_table_kernel, grid_of(blocks), dim3(256), 0, s, out, rows, rot, k);
     return check_hip(hipGetLastError(), "rope_table launch");
 }

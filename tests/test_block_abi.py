@@ -214,3 +214,25 @@ def test_tensors_without_storage_are_an_error(lib):
     done = subprocess.run([sys.executable, "-c", WRAPPED], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
                           stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=300)
     assert done.returncode == 0 and done.stdout.split()[-2:] == ["refused", "6"], done.stdout[-2000:]
+
+
+COUNTS = """
+import ctypes
+from paper_2506_15689_amd import binding as B
+
+lib, there = B.load(), ctypes.c_void_p(0x1000)
+codes = []
+for T in [1 << 31, 1 << 61, (1 << 63) - 8192, (1 << 63) - 1]:
+    codes.append(lib.basq_rope_append(there, 512, there, 256, there, 256, T, 4, 2, 128, there, there, 16, 128, 0, 1, 0.9, 0.9, 4, there, there, 4, 16,
+                                      there, 512, None, None, 0, None))
+for rot, positions in [(1024, 1 << 31), (64, 1 << 59), (64, 1 << 62), (1024, (1 << 63) - 1), (2, (1 << 63) - 1)]:
+    codes.append(lib.basq_rope_table(rot, positions, 1e4, 0, 1.0, 1.0, 2.0, 1.0, there, None))
+print("codes", *codes)
+"""
+
+
+def test_counts_past_what_a_grid_holds(lib):
+    """Tokens and positions up to the end of 64 bits are refused, not divided by what has wrapped to 0 (in a process of its own)."""
+    done = subprocess.run([sys.executable, "-c", COUNTS], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
+                          stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=300)
+    assert done.returncode == 0 and done.stdout.split()[-10:] == ["codes"] + [str(B.BASQ_EUNSUPPORTED)] * 9, done.stdout[-2000:]
