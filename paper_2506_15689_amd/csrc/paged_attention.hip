@@ -774,8 +774,11 @@ AttentionPlan paged_attention_plan(int32_t B, int32_t q_len, int32_t heads, int3
     const double shared = JOIN + FILLED * (double)share * step_us((double)(segments * units), ALONE);
     // Many segments keep the chip full by themselves, the next one going to the first free place: from two rounds on, and where two to a
     // compute unit are not long (ragged contexts, whole segments and shares: 2048 segments up to 3000 tokens 85 and 95 us, up to 1000 32 and
-    // 37; 800 up to 2000 26 and 30, up to 8000 88 and 81; 512 up to 4000 32 and 36, up to 8192 67 and 63).
-    const bool plenty = segments >= 2 * most || (segments >= 2 * (int64_t)CUS && units <= 32);
+    // 37; 800 up to 2000 26 and 30, up to 8000 88 and 81; 512 up to 4000 32 and 36, up to 8192 67 and 63).  Not where contexts can be very
+    // long: one among short ones then keeps its workgroup alone, which the host cannot know (1536 segments, of which those of one sequence are
+    // longest: 4096 tokens 30 and 38 us, 8192 50 and 38, 16384 89 and 39, 131072 648 and 63; all ragged up to 8192 172 and 173, up to 16384 318
+    // and 308).
+    const bool plenty = (segments >= 2 * most && units <= 64) || (segments >= 2 * (int64_t)CUS && units <= 32);
     if (units > 4 && !plenty && shared < four && shared < eight) return {(int)(segments * units < most ? segments * units : most), 4};
     return {0, eight < four ? 8 : 4};
 }

@@ -236,3 +236,11 @@ def test_counts_past_what_a_grid_holds(lib):
     done = subprocess.run([sys.executable, "-c", COUNTS], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
                           stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=300)
     assert done.returncode == 0 and done.stdout.split()[-10:] == ["codes"] + [str(B.BASQ_EUNSUPPORTED)] * 9, done.stdout[-2000:]
+
+
+@pytest.mark.parametrize("Bn", [1, 16, 64, 191, 192, 193, 1000])
+def test_long_contexts_are_shared_whatever_the_batch(lib, Bn):
+    """One sequence may be far longer than the others, which the host does not know: its workgroups must not be left with it."""
+    long_call = dict(B=Bn, heads=64, kv_heads=8, ldq=8192, ldo=8192, max_len=131072, table_stride=8192)
+    assert B.basq_paged_attention_workspace_bytes(Bn, 1, 64, 8, 128, 131072) > 0
+    assert attention(lib, **long_call) == B.BASQ_EINVAL and "workspace" in B.basq_last_error()

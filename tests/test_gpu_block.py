@@ -652,3 +652,10 @@ def test_append_of_padding_that_has_no_memory(D):
                                        p(slots), p(cache), cache.shape[0], P, p(got[0]), far, p(got[1]), p(got[2]), far, B._stream(None)))
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.equal(cache, cache2)
+
+
+@pytest.mark.parametrize("D,kv_heads,group", [(64, 16, 1), (128, 8, 9)])
+def test_attention_of_one_long_context_among_many_short_ones(D, kv_heads, group):
+    lengths = [(29 * i) % 100 for i in range(130)]
+    lengths[77] = 9000
+    check_attention(*attention_case(27, lengths, kv_heads * group, kv_heads, D, 64, 1), 9000)
