@@ -390,8 +390,11 @@ int basq_rope_append(const void* q, int64_t ldq, const void* k, int64_t ldk, con
  *   max_len    host: the longest length there can be; the work is laid out for it.  At most table_stride * page_size, and 2^31 - 2^16
  *   q_len      up to 32768 (else BASQ_EUNSUPPORTED)
  *   out        out, bf16 [B * q_len, heads, D], token stride ldo; may be q.   lse   out, fp32 [B * q_len, heads], or NULL
- *   workspace  basq_paged_attention_workspace_bytes, 256-byte aligned (BASQ_EWORKSPACE where it is smaller); NULL where that is 0
+ *   workspace  256-byte aligned (BASQ_EWORKSPACE where it is too small); NULL where basq_paged_attention_workspace_bytes is 0
  * The result does not depend on where pages lie.  B == 0 does nothing.
+ * basq_paged_attention_workspace_bytes: what a call of this shape may need, and any with fewer sequences, new tokens or tokens, or a
+ * shorter window (0 is the longest), of the same heads: a program asks once, for its largest.  At most 12.8 MB and 8 bytes for each
+ * sequence, kv head and 16 of its query rows; 0 where no context is longer than 512 tokens, and for an unsupported shape.
  */
 size_t basq_paged_attention_workspace_bytes(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t head_dim,
                                             int32_t max_len, int32_t window);

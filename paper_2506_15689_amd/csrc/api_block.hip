@@ -39,6 +39,11 @@ int64_t attention_segments(int32_t B, int32_t q_len, int32_t heads, int32_t kv_h
     return (int64_t)B * kv_heads * (((int64_t)(heads / kv_heads) * q_len + 15) / 16);
 }
 
+// (the kernel counts tokens in 32 bits: a little room above the longest context, and below zero for what new tokens do not see)
+bool attention_counts(int32_t q_len, int32_t heads, int32_t max_len) {
+    return q_len <= 32768 && (int64_t)q_len * heads <= 0x3FFFFFFFll && max_len <= 0x7FFF0000;
+}
+
 // parts of 16 rows of D sums with their reference and sum, and a segment's place (PagedAttentionArgs)
 size_t parts_bytes(int32_t workers, int32_t head_dim, int64_t segments) {
     return workers > 0 ? 2 * (size_t)workers * 16 * (4 * (size_t)head_dim + 8) + 8 * (size_t)segments : 0;
@@ -152,12 +157,10 @@ int basq_rope_append(const void* q, int64_t ldq, const void* k, int64_t ldk, con
 
 size_t basq_paged_attention_workspace_bytes(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t head_dim,
                                             int32_t max_len, int32_t window) {
-    if (B < 1 || q_len < 1 || heads < 1 || kv_heads < 1 || heads % kv_heads != 0 || (head_dim != 64 && head_dim != 128) || max_len < 0) return 0;
-    // (whether scores are capped is not known here: what the larger of both needs)
-    int workers = paged_attention_plan(B, q_len, heads, kv_heads, head_dim, max_len, window, false).workers;
-    const int capped = paged_attention_plan(B, q_len, heads, kv_heads, head_dim, max_len, window, true).workers;
-    if (capped > workers) workers = capped;
-    return workers < 0 ? 0 : parts_bytes(workers, head_dim, attention_segments(B, q_len, heads, kv_heads));
+    if (B < 1 || q_len < 1 || heads < 1 || kv_heads < 1 || heads % kv_heads != 0 || (head_dim != 64 && head_dim != 128) || max_len < 0 || window < 0) return 0;
+    if (heads + (int64_t)kv_heads > 65536 || !attention_counts(q_len, heads, max_len)) return 0;
+    const int workers = paged_attention_most_workers(B, q_len, heads, kv_heads, head_dim, max_len, window);
+    return parts_bytes(workers, head_dim, attention_segments(B, q_len, heads, kv_heads));
 }
 
 int basq_paged_attention(const void* q, int64_t ldq, int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t head_dim,
@@ -167,9 +170,8 @@ int basq_paged_attention(const void* q, int64_t ldq, int32_t B, int32_t q_len, i
     if (B < 0 || q_len < 1) return fail(BASQ_EINVAL, "B must be >= 0 and q_len >= 1 (got %d, %d)", B, q_len);
     int rc = check_heads(heads, kv_heads, head_dim, true);
     if (rc != BASQ_OK) return rc;
-    // (the kernel counts tokens in 32 bits: a little room above the longest context, and below zero for what new tokens do not see)
-    if (q_len > 32768 || (int64_t)q_len * heads > 0x3FFFFFFFll) return fail(BASQ_EUNSUPPORTED, "q_len up to 32768 and q_len * heads < 2^30 are supported (got %d, %d)", q_len, heads);
-    if (max_len > 0x7FFF0000) return fail(BASQ_EUNSUPPORTED, "max_len up to 2^31 - 2^16 is supported (got %d)", max_len);
+    if (!attention_counts(q_len, heads, max_len))
+        return fail(BASQ_EUNSUPPORTED, "q_len up to 32768, q_len * heads < 2^30 and max_len up to 2^31 - 2^16 are supported (got %d, %d, %d)", q_len, heads, max_len);
     if (bits != 4) return fail(BASQ_EUNSUPPORTED, "only bits == 4 is implemented (got %d)", bits);
     if (max_len < 0) return fail(BASQ_EINVAL, "max_len must be >= 0 (got %d)", max_len);
     if (!isfinite(scale)) return fail(BASQ_EINVAL, "scale must be finite (got %g)", (double)scale);

@@ -184,6 +184,7 @@ struct AttentionPlan {
     int32_t workers, waves;
 };
 AttentionPlan paged_attention_plan(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t max_len, int32_t window, bool cap);
+int paged_attention_most_workers(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t max_len, int32_t window);
 int launch_paged_attention(PagedAttentionArgs a, hipStream_t s);  // paged_attention.hip
 
 // 28 x 28 Paley type-I matrix, row-major, built on the host at first use (hadamard28.hip).

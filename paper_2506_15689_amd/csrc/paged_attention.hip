@@ -52,6 +52,7 @@ typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 constexpr int PA_STEP = 32;                                      // tokens of a wave's step
 constexpr int PA_UNIT = 4 * PA_STEP;                             // a step of each of four waves: what work is counted in
 constexpr int PA_START = 2;                                       // what the start and the end of a part cost, in units
+constexpr int PA_BRIEF = 4;                                      // contexts of that many units are short: never shared
 constexpr int PA_STAGES = 2;                                      // steps of a wave in LDS
 constexpr float UNSET = -1e30f;                                  // M of a row that has seen no token
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
@@ -732,7 +733,7 @@ int launch(const PagedAttentionArgs& a, hipStream_t s) {
     const int64_t segments = (int64_t)a.B * a.kv_heads * a.row_tiles;
     // Where segments go whole, each has a workgroup of its own, and the next free compute unit takes the next one; but where all are
     // short, starting is most of it, and a workgroup prepares its next segment beside the one that it works on.
-    const bool brief = a.workers == 0 && longest_units(a.q_len, a.max_len, a.window) <= 4;
+    const bool brief = a.workers == 0 && longest_units(a.q_len, a.max_len, a.window) <= PA_BRIEF;
     const unsigned blocks = (unsigned)(a.workers > 0 ? a.workers : brief && segments > resident(D, a.group * a.q_len) ? resident(D, a.group * a.q_len) : segments < (1 << 20) ? segments : 1 << 20);
     if (a.waves == 8) launch_waves<D, 8>(a, blocks, s);
     else launch_waves<D, 4>(a, blocks, s);
@@ -759,7 +760,7 @@ int launch(const PagedAttentionArgs& a, hipStream_t s) {
 AttentionPlan paged_attention_plan(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t max_len, int32_t window, bool cap) {
     const int64_t segments = (int64_t)B * kv_heads * (((int64_t)(heads / kv_heads) * q_len + 15) / 16);
     const int64_t units = longest_units(q_len, max_len, window);
-    if (segments * (units + PA_START) > 0x7FFF0000ll || (int64_t)B * q_len * heads > 0x7FFFFFFFll) return {-1, 4};
+    if ((int64_t)B * q_len * heads > 0x7FFFFFFFll || segments * (units + PA_START) > 0x7FFF0000ll) return {-1, 4};
     const int64_t most = resident(head_dim, heads / kv_heads * (int64_t)q_len);
     constexpr double CUS = 256, ALONE = 0.73, ALONE_EIGHT = 0.88, EACH = 0.47, END_EIGHT = 0.6, JOIN = 6.0, FILLED = 0.55;
     const double tanhs = cap ? 0.22 : 0.0;                       // of a step's scores
@@ -779,8 +780,19 @@ AttentionPlan paged_attention_plan(int32_t B, int32_t q_len, int32_t heads, int3
     // longest: 4096 tokens 30 and 38 us, 8192 50 and 38, 16384 89 and 39, 131072 648 and 63; all ragged up to 8192 172 and 173, up to 16384 318
     // and 308).
     const bool plenty = (segments >= 2 * most && units <= 64) || (segments >= 2 * (int64_t)CUS && units <= 32);
-    if (units > 4 && !plenty && shared < four && shared < eight) return {(int)(segments * units < most ? segments * units : most), 4};
+    if (units > PA_BRIEF && !plenty && shared < four && shared < eight) return {(int)(segments * units < most ? segments * units : most), 4};
     return {0, eight < four ? 8 : 4};
+}
+
+// The most workers of a call of this shape or of a smaller one (which may share where this one does not): each takes a unit at least, and the
+// chip holds 768 where all have few rows.  -1 as above.
+int paged_attention_most_workers(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t max_len, int32_t window) {
+    if (paged_attention_plan(B, q_len, heads, kv_heads, head_dim, max_len, window, false).workers < 0) return -1;
+    const int64_t segments = (int64_t)B * kv_heads * (((int64_t)(heads / kv_heads) * q_len + 15) / 16);
+    const int64_t units = longest_units(q_len, max_len, window);
+    if (units <= PA_BRIEF) return 0;
+    const int64_t most = resident(head_dim, 1);
+    return (int)(segments * units < most ? segments * units : most);
 }
 
 int launch_paged_attention(PagedAttentionArgs a, hipStream_t s) {

@@ -244,3 +244,32 @@ def test_long_contexts_are_shared_whatever_the_batch(lib, Bn):
     long_call = dict(B=Bn, heads=64, kv_heads=8, ldq=8192, ldo=8192, max_len=131072, table_stride=8192)
     assert B.basq_paged_attention_workspace_bytes(Bn, 1, 64, 8, 128, 131072) > 0
     assert attention(lib, **long_call) == B.BASQ_EINVAL and "workspace" in B.basq_last_error()
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the calls that are not refused would be launched, on places that are not there")
+def test_a_workspace_for_the_largest_call_does_for_smaller_ones(lib):
+    """A program asks for its largest batch and context once; batches shrink and contexts end."""
+    W = B.basq_paged_attention_workspace_bytes
+    shared = 0
+    for heads, kv_heads, D in [(32, 8, 128), (64, 8, 128), (32, 32, 128), (28, 4, 64), (71, 1, 128)]:
+        for most_B, most_new, most_len, window in [(64, 1, 4096, 0), (64, 4, 8192, 0), (300, 1, 2048, 0), (16, 8, 40000, 3000), (1, 1, 100000, 0)]:
+            room = W(most_B, most_new, heads, kv_heads, D, most_len, window)
+            assert room % 8 == 0 and room <= 768 * 2 * 16 * (4 * D + 8) + 8 * most_B * kv_heads * -(-(heads // kv_heads) * most_new // 16)
+            for Bn in {1, 2, 3, most_B // 4 + 1, most_B // 2 + 1, most_B}:
+                for q_len in {1, most_new}:
+                    for max_len in {1, 500, 513, 1000, 2049, most_len // 2, most_len}:
+                        for w in {0, 600, window} if window == 0 else {600, window}:
+                            if Bn > most_B or max_len > most_len:
+                                continue
+                            for cap in (0.0, 30.0):
+                                call = dict(B=Bn, q_len=q_len, heads=heads, kv_heads=kv_heads, head_dim=D, ldq=heads * D, ldo=heads * D, max_len=max_len,
+                                            table_stride=1 << 16, window=w, softcap=cap, workspace=FAKE)
+                                need = 0
+                                if attention(lib, **call, workspace_bytes=0) == B.BASQ_EWORKSPACE:
+                                    need = int(B.basq_last_error().split()[-2])
+                                    shared += 1
+                                assert need <= W(Bn, q_len, heads, kv_heads, D, max_len, w) <= room
+    assert shared > 100
+    # what the call refuses needs none
+    assert W(4, 32769, 32, 8, 128, 8192) == W(4, 1, 32, 8, 128, 0x7FFF0001) == W(4, 1, 65536, 1, 128, 8192) == W(4, 1, 32, 8, 128, 8192, -1) == 0
+    assert W(2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1, 1, 128, 2 ** 31 - 1) == 0
