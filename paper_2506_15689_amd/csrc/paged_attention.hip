@@ -19,8 +19,9 @@
 // with subnormal operands, the more the smaller they are: with patterns of 0 .. 15 scores are 2.4e-6 off, with 16 times that 3.5e-7
 // (q of standard deviation 1.8, D = 128; fp32 arithmetic 2.5e-7), so the keys' codes are all brought to the second nibble; the values',
 // whose products end in bf16, are not.  Query rows are brought to fp16 times a power of two of their own (a bf16 value fits it exactly
-// while it is within 2^-30 of the row's largest); weights p_t vs_t are rounded to fp16 (2^-11 relative at most, against 2^-8 of the
-// bf16 output) near 2^5 of their running maximum, far from either end of fp16.  l, M and both sums are fp32.
+// while it is within 2^-30 of the row's largest); weights p_t vs_t are rounded to fp16 near 2^5 of their running maximum: 2^-11 of each
+// (against 2^-8 of the bf16 output), and of those under 2^-19 of the largest, 2^-30 of that.  Vectors without codes, those of zeros, do not
+// count as largest.  l, M and both sums are fp32.
 //
 // Codes and ranges come by direct loads into a ring of LDS stages that the wave has to itself, a step ahead of the one that is
 // worked on: registers hold none of it, and three workgroups of four waves fit a compute unit (loads into registers and two workgroups took
@@ -457,10 +458,27 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 || (D == 128 && !FOLD) ? 2 :
         // (Where a scale is next to 0, p itself counts once it nears the end of fp32.)
         if (__any(top > 0x1p15f || !set || !(least >= 0x1p-60f))) {
             asm volatile("");
+            // A vector without an extent is stored with a scale of 1, and codes of 0 if it is zero: it weighs nothing, but a reference set by
+            // that scale would leave the others, on whom the output depends, few bits.
+            bool without_extent = false;
+#pragma unroll
+            for (int r = 0; r < MINE; ++r) without_extent = without_extent || vs[r] == 1.0f;
+            if (__any(without_extent)) {
+                asm volatile("");
+#pragma unroll
+                for (int r = 0; r < MINE; ++r) {
+                    const uint64_t first = __ballot(v[r] != 0), second = FOLD ? __ballot(v[4 + r] != 0) : 0;
+                    const uint64_t some = FOLD && col & 8 ? second : first;
+                    const uint32_t of_pair = quarter & 2 ? (uint32_t)(some >> 32) : (uint32_t)some;
+                    if (vs[r] == 1.0f && (of_pair & (quarter & 1 ? 0xFFFF0000u : 0xFFFFu)) == 0) vs[r] = 0.0f;
+                }
+            }
             float best = -INFINITY;
+            top = 0.0f;
 #pragma unroll
             for (int r = 0; r < MINE; ++r) {
                 best = fmaxf(best, sc[r] + fmaxf(__builtin_amdgcn_logf(vs[r]), -60.0f));
+                w[r] = p[r] * vs[r];
                 top = fmaxf(top, fmaxf(fabsf(w[r]), p[r] * 0x1p-60f));
             }
             best = row_max(best);

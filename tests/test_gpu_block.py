@@ -659,3 +659,39 @@ def test_attention_of_one_long_context_among_many_short_ones(D, kv_heads, group)
     lengths = [(29 * i) % 100 for i in range(130)]
     lengths[77] = 9000
     check_attention(*attention_case(27, lengths, kv_heads * group, kv_heads, D, 64, 1), 9000)
+
+
+@pytest.mark.parametrize("D,heads,kv_heads", [(64, 2, 2), (64, 12, 1), (128, 16, 2), (128, 10, 1)])
+@pytest.mark.parametrize("lead", [6.0, 14.0, 17.0, 25.0, 40.0])
+def test_attention_of_zero_values_with_the_largest_scores(D, heads, kv_heads, lead):
+    """Tokens whose values are all 0 and whose scores are `lead` above the others', as append stores them (a scale of 1, codes of 0): all
+    that is in the output comes from the others, by weights of e^-lead, and is to be as exact as without them."""
+    T, P = 400, 16
+    g = gen(28)
+    q = (randn(g, kv_heads, D)[None, :, None] + 0.02 * randn(g, 1, kv_heads, heads // kv_heads, D)).flatten(1, 2).to(BF16)
+    k, v = 0.1 * randn(g, T, kv_heads, D), 0.15 * randn(g, T, kv_heads, D)
+    base = q.float().unflatten(1, (kv_heads, -1)).mean(2)[0]
+    for t in (0, 37, 130, 131, 250, 399):
+        k[t] = lead * math.sqrt(D) * base / (base * base).sum(-1, keepdim=True)
+        v[t] = 0
+    cache = B.alloc_kv_cache(T // P, kv_heads, D, P)
+    B.basq_rope_append(None, k.to(BF16), v.to(BF16), None, None, torch.arange(T, dtype=torch.int32, device=DEV), cache, 1.0, 1.0, None, rotate=False)
+    table = torch.arange(T // P, dtype=torch.int32, device=DEV)[None]
+    for first in (0, 1):                                             # with such a token at the start, and without
+        lengths = torch.tensor([T - P * first], dtype=torch.int32, device=DEV)
+        check_attention(q, cache, table[:, first:].contiguous(), lengths, T - P * first)
+        wide = torch.nn.functional.pad(table[:, first:], (0, 1000), value=-1)
+        check_attention(q, cache, wide, lengths, 8000)
+
+
+def test_attention_of_zero_values_far_from_each_other():
+    """Such tokens in every step, above others that become smaller and smaller: the reference stays where the sums are."""
+    T, P, D = 1600, 16, 128
+    g = gen(29)
+    q, k, v = randn(g, 1, 4, D).to(BF16), 0.1 * randn(g, T, 4, D), 0.15 * randn(g, T, 4, D)
+    along = q.float()[0] * math.sqrt(D) / q.float()[0].pow(2).sum(-1, keepdim=True)
+    k += -0.15 * torch.arange(T, device=DEV)[:, None, None] * along
+    k[::32], v[::32] = 20 * along, 0
+    cache = B.alloc_kv_cache(T // P, 4, D, P)
+    B.basq_rope_append(None, k.to(BF16), v.to(BF16), None, None, torch.arange(T, dtype=torch.int32, device=DEV), cache, 1.0, 1.0, None, rotate=False)
+    check_attention(q, cache, torch.arange(T // P, dtype=torch.int32, device=DEV)[None], torch.tensor([T], dtype=torch.int32, device=DEV), T)
