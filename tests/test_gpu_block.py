@@ -695,3 +695,19 @@ def test_attention_of_zero_values_far_from_each_other():
     cache = B.alloc_kv_cache(T // P, 4, D, P)
     B.basq_rope_append(None, k.to(BF16), v.to(BF16), None, None, torch.arange(T, dtype=torch.int32, device=DEV), cache, 1.0, 1.0, None, rotate=False)
     check_attention(q, cache, torch.arange(T // P, dtype=torch.int32, device=DEV)[None], torch.tensor([T], dtype=torch.int32, device=DEV), T)
+
+
+@pytest.mark.parametrize("heads,kv_heads,D", [(8, 1, 128), (14, 1, 128), (8, 1, 64), (15, 1, 64)])
+def test_attention_of_a_row_does_not_depend_on_other_rows(heads, kv_heads, D):
+    """Whatever the other heads' and sequences' queries hold -- huge, tiny, zero or infinite values -- a row's bits stay."""
+    q, cache, table, lengths = attention_case(30, [600, 70], heads, kv_heads, D, 16, 1)
+    # rows of small values next to far smaller ones, and ordinary rows
+    q[:, ::2] = (0.15 * torch.sign(q[:, ::2].float()) * 2.0 ** -torch.randint(0, 24, q[:, ::2].shape, generator=gen(31), device=DEV)).to(BF16)
+    good, good_lse = attend(q, cache, table, lengths, 600)
+    for value in (1e6, 3e38, 1e-30, 0.0, float("inf")):
+        q2 = q.clone()
+        q2[0, 3], q2[1, 6] = value, value
+        out, lse = attend(q2, cache, table, lengths, 600)
+        rest = torch.ones(2, heads, dtype=torch.bool)
+        rest[0, 3] = rest[1, 6] = False
+        assert torch.equal(out[rest], good[rest]) and torch.equal(lse[rest], good_lse[rest]), value
