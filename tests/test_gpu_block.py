@@ -711,3 +711,113 @@ def test_attention_of_a_row_does_not_depend_on_other_rows(heads, kv_heads, D):
         rest = torch.ones(2, heads, dtype=torch.bool)
         rest[0, 3] = rest[1, 6] = False
         assert torch.equal(out[rest], good[rest]) and torch.equal(lse[rest], good_lse[rest]), value
+
+
+# ---- attention whose work is shared among workgroups and joined by a second launch
+
+def check_shared(q, cache, table, lengths, max_len, q_len=1, softcap=0.0, window=0, whole=False):
+    """check_attention of a call that is seen to share its contexts (or not to): without a workspace it is refused (or not)."""
+    table = torch.nn.functional.pad(table, (0, max(0, -(-max_len * (q.shape[2] + 16) // cache.shape[2]) - table.shape[1])), value=-1)
+    call = lambda: B.basq_paged_attention(q, cache, table, lengths, max_len, 1.0, torch.empty_like(q), None, q_len=q_len, softcap=softcap, window=window)  # noqa: E731
+    if whole:
+        call()
+    else:
+        with pytest.raises(B.BasqError, match="workspace is null"):
+            call()
+    check_attention(q, cache, table, lengths, max_len, q_len, softcap, window)
+
+
+@pytest.mark.parametrize("heads,kv_heads,D", [(8, 2, 128), (8, 2, 64), (24, 2, 128), (12, 1, 64)])
+@pytest.mark.parametrize("window,q_len,softcap", [(1900, 1, 0.0), (2048, 1, 20.0), (3999, 1, 0.0), (2000, 4, 0.0), (3000, 5, 30.0), (0, 3, 25.0)])
+def test_shared_attention_in_windows(heads, kv_heads, D, window, q_len, softcap):
+    """Parts that begin where a window does; several new tokens, of one row tile and of several; caps."""
+    check_shared(*attention_case(window + q_len + D, [5003, 0, 1, 2999, 130, q_len, 4100], heads, kv_heads, D, 16, q_len), 30000, q_len, softcap, window)
+
+
+@pytest.mark.parametrize("q_len,heads,kv_heads,D", [(2, 8, 2, 128), (4, 28, 4, 64), (5, 3, 1, 128), (33, 4, 1, 64), (8, 71, 1, 128), (17, 2, 2, 64)])
+def test_shared_attention_of_several_new_tokens(q_len, heads, kv_heads, D):
+    check_shared(*attention_case(q_len + D, [q_len, 1700, q_len - 1, 90, 1, 0, 300], heads, kv_heads, D, 32, q_len), 9000, q_len)
+
+
+@pytest.mark.parametrize("D,window", [(64, 70), (128, 600)])
+def test_shared_attention_of_row_tiles_with_windows_of_their_own(D, window):
+    """Many new tokens: most units of a segment are outside a tile's window, some parts have none of its tokens."""
+    check_shared(*attention_case(32, [3500], 2, 1, D, 16, 3000), 4000, 3000, window=window)
+
+
+@pytest.mark.parametrize("softcap", [1e-3, 5.0, 50.0, 1e6])
+@pytest.mark.parametrize("heads,D", [(4, 64), (4, 128), (40, 64), (40, 128)])
+def test_shared_attention_softcap(softcap, heads, D):
+    check_shared(*attention_case(33, [1, 40, 3777], heads, 4, D, 16, 1), 9000, softcap=softcap)
+
+
+@pytest.mark.parametrize("scale_of_values", [1e-12, 1e12])
+def test_shared_attention_of_small_and_large_values(scale_of_values):
+    check_shared(*attention_case(34, [3900, 64], 8, 2, 128, 16, 1, scale_of_values=scale_of_values), 9000)
+
+
+@pytest.mark.parametrize("heads,kv_heads,D,q_len", [(8, 2, 128, 1), (20, 2, 64, 3)])
+def test_shared_attention_in_place_and_in_a_graph(heads, kv_heads, D, q_len):
+    """The output in the query's place across both launches, eager, on a side stream, and replayed between eager calls."""
+    q, cache, table, lengths = attention_case(35, [9000, 50, 3000], heads, kv_heads, D, 16, q_len)
+    need = B.basq_paged_attention_workspace_bytes(3, q_len, heads, kv_heads, D, 9000)
+    with pytest.raises(B.BasqError, match="workspace is null"):
+        B.basq_paged_attention(q, cache, table, lengths, 9000, 0.1, torch.empty_like(q), None, q_len=q_len)
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    want, want_lse = torch.empty_like(q), torch.empty(3 * q_len, heads, device=DEV)
+    B.basq_paged_attention(q, cache, table, lengths, 9000, 0.1, want, ws, q_len=q_len, lse=want_lse)
+    q2, lse = q.clone(), torch.empty_like(want_lse)
+
+    def step():
+        q2.copy_(q)
+        B.basq_paged_attention(q2, cache, table, lengths, 9000, 0.1, q2, ws, q_len=q_len, lse=lse)
+
+    same = lambda: torch.equal(q2, want) and torch.equal(lse, want_lse)  # noqa: E731
+    step()
+    assert same()
+    side = torch.cuda.Stream()
+    lse.zero_()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    assert same()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(4):
+        lse.zero_()
+        ws.fill_(0xFF)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same()
+        step()
+        torch.cuda.synchronize()
+        assert same()
+
+
+def test_shared_attention_of_parts_of_more_than_32_steps():
+    """Workgroups whose share of one context is more than the 32 steps whose pages a wave holds at once: 64 sequences whose tables name the
+    same pages, with three queries between them."""
+    q, cache, table, _ = attention_case(36, [8192, 1, 1], 8, 8, 64, 64, 1)
+    n = [8192, 8191, 5000]
+    want, want_lse, slack, slack_lse = ref.paged_attention(q, cache, table[:1].expand(3, -1), torch.tensor(n), 8192, 0.125, 1, 0.0, 0)
+    pick = torch.arange(64) % 3
+    lengths = torch.tensor(n, dtype=torch.int32)[pick].to(DEV)
+    q64, table64 = q[pick.to(DEV)].contiguous(), table[:1].expand(64, -1).contiguous()
+    with pytest.raises(B.BasqError, match="workspace is null"):
+        B.basq_paged_attention(q64, cache, table64, lengths, 8192, 0.125, torch.empty_like(q64), None)
+    # (its shares: all units and two more for each segment, by 768 workgroups)
+    units = sum(-(-x // 128) + 2 for x in lengths.tolist()) * 8
+    assert units / 768 > 33
+    out, lse = attend(q64, cache, table64, lengths, 8192, scale=0.125)
+    check_stored(out.cpu(), want[pick], slack[pick])
+    assert ((ref.f64(lse) - want_lse[pick]).abs() <= slack_lse[pick]).all()
+
+
+@pytest.mark.parametrize("D,heads", [(64, 8), (128, 8), (128, 80)])
+def test_whole_contexts_of_more_than_32_steps(D, heads):
+    """One workgroup to a segment, of up to 64 steps of each wave."""
+    lengths = [(29 * i) % 60 for i in range(192)]
+    lengths[5], lengths[90], lengths[191] = 8192, 4097, 5000
+    check_shared(*attention_case(37, lengths, heads, 8, D, 64, 1), 8192, whole=True)
