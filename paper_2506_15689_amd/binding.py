@@ -155,6 +155,17 @@ def _stream(stream: Optional[torch.cuda.Stream]) -> int:
     return _raw_stream(_raw_device())
 
 
+def _stream_on(stream: Optional[torch.cuda.Stream], device: int) -> int:
+    """The handle of `stream`, which has to be one of this GPU, or of the GPU's current stream."""
+    if stream is not None:
+        if getattr(stream, "device_index", device) != device:
+            raise ValueError(f"the stream is on GPU {stream.device_index}, the tensors are on GPU {device}")
+        return stream.cuda_stream
+    if _raw_stream is None or not torch.cuda.is_initialized():
+        return torch.cuda.current_stream(device).cuda_stream
+    return _raw_stream(device)
+
+
 def _check(rc: int) -> None:
     if rc != BASQ_OK:
         raise BasqError(rc, load().basq_last_error().decode("utf-8", "replace"))
@@ -359,6 +370,7 @@ ROPE_PLAIN, ROPE_LINEAR, ROPE_BANDS, ROPE_YARN = 0, 1, 2, 3      # BASQ_ROPE_* o
 
 
 # Calls of a decode step are a few microseconds of GPU work each: their arguments are checked and marshalled in a compiled module.
+# They run on the GPU of their tensors, which need not be the current one, on its current stream or one of its own.
 _block = None
 
 
@@ -380,7 +392,7 @@ def basq_add_rms_norm(X: torch.Tensor, residual: Optional[torch.Tensor], weight:
                       y8_scale: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
     """X, residual, res_out, Y bf16 [M, K] (any row strides); weight bf16 [K]; Y8 float8_e4m3fn [M, K] with y8_scale fp32 [M].
     res_out = X + residual, Y = its norm; res_out and Y may be X or residual."""
-    rc = (_block or _load_block()).add_rms_norm(X, residual, weight, eps, Y, res_out, Y8, y8_scale, _stream, stream)
+    rc = (_block or _load_block()).add_rms_norm(X, residual, weight, eps, Y, res_out, Y8, y8_scale, _stream_on, stream)
     if rc != BASQ_OK:
         _check(rc)
 
@@ -391,7 +403,9 @@ def basq_rope_table(cos_sin: torch.Tensor, base: float, *, scaling: int = ROPE_P
     positions, rot_dim = cos_sin.shape
     if cos_sin.dtype != torch.float32 or not cos_sin.is_contiguous() or not cos_sin.is_cuda:
         raise ValueError(f"cos_sin must be contiguous fp32 on the GPU, not {cos_sin.dtype} {tuple(cos_sin.shape)}")
-    _check(load().basq_rope_table(rot_dim, positions, base, scaling, factor, low, high, original_len, _p(cos_sin), _stream(stream)))
+    handle = _stream_on(stream, cos_sin.get_device())
+    with torch.cuda.device(cos_sin.device):
+        _check(load().basq_rope_table(rot_dim, positions, base, scaling, factor, low, high, original_len, _p(cos_sin), handle))
 
 
 def basq_kv_page_bytes(kv_heads: int, head_dim: int, page_size: int) -> int:
@@ -407,7 +421,7 @@ def basq_rope_append(q: Optional[torch.Tensor], k: Optional[torch.Tensor], v: Op
     positions, slots int32 [T]; cos_sin fp32 [rows, rot_dim]; cache uint8 [pages, kv_heads, page_size * (D + 16)]
     (alloc_kv_cache).  q alone: k, v, slots and cache None; keys and values alone: q and q_out None."""
     rc = (_block or _load_block()).rope_append(q, k, v, positions, cos_sin, slots, cache, clip_lo, clip_hi, q_out, k_hat, v_hat, interleaved,
-                                               rotate, bits, _stream, stream)
+                                               rotate, bits, _stream_on, stream)
     if rc != BASQ_OK:
         _check(rc)
 
@@ -424,7 +438,7 @@ def basq_paged_attention(q: torch.Tensor, cache: torch.Tensor, page_table: torch
     """q, out bf16 [B * q_len, heads, D] (any token strides); cache uint8 [pages, kv_heads, page_size * (D + 16)]; page_table
     int32 [B, pages of a sequence] (any row stride); lengths int32 [B]; lse fp32 [B * q_len, heads] or None."""
     rc = (_block or _load_block()).paged_attention(q, cache, page_table, lengths, max_len, scale, out, workspace, q_len, softcap, window, lse,
-                                                   bits, _stream, stream)
+                                                   bits, _stream_on, stream)
     if rc != BASQ_OK:
         _check(rc)
 

@@ -4,6 +4,7 @@
 // them names and defaults) and returns the C ABI's code; a tensor that does not fit is a ValueError.
 #include <Python.h>
 
+#include <c10/core/DeviceGuard.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <stdarg.h>
@@ -108,15 +109,26 @@ bool truth(PyObject* o) {
     if (v < 0) throw Refused{};
     return v != 0;
 }
-// the handle that `handle_of(stream)` names; asked for behind the checks, which work without a GPU
-void* stream_of(PyObject* handle_of, PyObject* stream) {
-    PyObject* handle = PyObject_CallOneArg(handle_of, stream);
-    if (!handle) throw Refused{};
-    const long long v = PyLong_AsLongLong(handle);
-    Py_DECREF(handle);
-    if (v == -1 && PyErr_Occurred()) throw Refused{};
-    return reinterpret_cast<void*>((intptr_t)v);
-}
+// The stream of a call, and its GPU made the current one while this lives (a launch goes to the current GPU, whatever the stream is).
+// `handle_of(stream, device)` names the handle; it is asked behind the checks, which work without a GPU.
+class Launch {
+public:
+    Launch(const Call& c, PyObject* handle_of, PyObject* of) {
+        PyObject* index = PyLong_FromLong(c.device);
+        PyObject* handle = index ? PyObject_CallFunctionObjArgs(handle_of, of, index, nullptr) : nullptr;
+        Py_XDECREF(index);
+        if (!handle) throw Refused{};
+        const long long v = PyLong_AsLongLong(handle);
+        Py_DECREF(handle);
+        if (v == -1 && PyErr_Occurred()) throw Refused{};
+        stream = reinterpret_cast<void*>((intptr_t)v);
+        guard_.reset_device(c10::Device(c10::DeviceType::CUDA, (c10::DeviceIndex)c.device));
+    }
+    void* stream;
+
+private:
+    c10::OptionalDeviceGuard guard_;
+};
 
 // runs `body`; no C++ exception leaves a Python entry point
 template <class Body>
@@ -168,8 +180,8 @@ PyObject* add_rms_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
         void *h = data(res_out), *y = data(Y);
         uint8_t* y8 = data<uint8_t>(Y8);
         float* scale = data<float>(y8_scale);
-        void* stream = stream_of(args[8], args[9]);
-        return without_gil([&] { return basq_add_rms_norm(x, r, w, M, K, ldx, ldr, eps, h, ldro, y, ldy, y8, ldy8, scale, stream); });
+        const Launch on(c, args[8], args[9]);
+        return without_gil([&] { return basq_add_rms_norm(x, r, w, M, K, ldx, ldr, eps, h, ldro, y, ldy, y8, ldy8, scale, on.stream); });
     });
 }
 
@@ -230,10 +242,10 @@ PyObject* rope_append(PyObject*, PyObject* const* args, Py_ssize_t n) {
         const float* table = data<float>(cos_sin);
         uint8_t* blocks = data<uint8_t>(cache);
         void *turned = data(q_out), *kh = data(k_hat), *vh = data(v_hat);
-        void* stream = stream_of(args[15], args[16]);
+        const Launch on(c, args[15], args[16]);
         return without_gil([&] {
             return basq_rope_append(qs, ldq, ks, ldk, vs, ldv, T, heads, kv_heads, head_dim, at, table, table_rows, rot, interleaved, rotate, clip_lo,
-                                    clip_hi, bits, to, blocks, pages, page_size, turned, ldqo, kh, vh, ldh, stream);
+                                    clip_hi, bits, to, blocks, pages, page_size, turned, ldqo, kh, vh, ldh, on.stream);
         });
     });
 }
@@ -276,10 +288,10 @@ PyObject* paged_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
         const int32_t *page_of = data<int32_t>(&table), *lens = data<int32_t>(&lengths);
         void *result = data(&out), *parts = data(workspace);
         float* sums = data<float>(lse);
-        void* stream = stream_of(args[13], args[14]);
+        const Launch on(c, args[13], args[14]);
         return without_gil([&] {
             return basq_paged_attention(rows_q, ldq, sequences, q_len, all_heads, kv_heads, head_dim, bits, blocks, pages, page_size, page_of, table_stride,
-                                        lens, max_len, scale, softcap, window, result, ldo, sums, parts, room, stream);
+                                        lens, max_len, scale, softcap, window, result, ldo, sums, parts, room, on.stream);
         });
     });
 }

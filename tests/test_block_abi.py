@@ -273,3 +273,47 @@ def test_a_workspace_for_the_largest_call_does_for_smaller_ones(lib):
     # what the call refuses needs none
     assert W(4, 32769, 32, 8, 128, 8192) == W(4, 1, 32, 8, 128, 0x7FFF0001) == W(4, 1, 65536, 1, 128, 8192) == W(4, 1, 32, 8, 128, 8192, -1) == 0
     assert W(2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1, 1, 128, 2 ** 31 - 1) == 0
+
+
+def test_calls_go_to_the_gpu_of_their_tensors(lib, monkeypatch):
+    """Which is not always the current one: its current stream is asked for, a stream of another GPU is refused."""
+    from torch._subclasses.fake_tensor import FakeTensorMode
+
+    class Asked(Exception):
+        pass
+
+    def handle_of(stream, device):
+        raise Asked(stream, device)
+
+    monkeypatch.setattr(B, "_stream_on", handle_of)
+    with FakeTensorMode():
+        new = lambda dtype, *s: torch.empty(s, dtype=dtype, device="cuda:1")  # noqa: E731
+        x, q, k = new(BF16, 3, 64), new(BF16, 3, 4, 64), new(BF16, 3, 2, 64)
+        cache, i32 = new(torch.uint8, 5, 2, 16 * 80), lambda *s: new(torch.int32, *s)  # noqa: E731
+        for call in [lambda **kw: B.basq_add_rms_norm(x, None, new(BF16, 64), 1e-5, x, **kw),
+                     lambda **kw: B.basq_rope_append(q, k, k, None, None, i32(3), cache, 0.9, 0.9, q, **kw),
+                     lambda **kw: B.basq_paged_attention(q, cache, i32(3, 4), i32(3), 64, 0.1, q, None, **kw),
+                     lambda **kw: B.basq_rope_table(new(torch.float32, 8, 64), 1e4, **kw)]:
+            with pytest.raises(Asked) as asked:
+                call()
+            assert asked.value.args == (None, 1)
+            with pytest.raises(Asked) as asked:
+                call(stream="a stream")
+            assert asked.value.args == ("a stream", 1)
+        with pytest.raises(ValueError, match="is not on the GPU of the other tensors"):
+            B.basq_add_rms_norm(x, torch.empty((3, 64), dtype=BF16, device="cuda:0"), new(BF16, 64), 1e-5, x)
+
+
+@pytest.mark.parametrize("documented", [False, True])
+def test_the_stream_of_a_gpu(monkeypatch, documented):
+    class Stream:
+        cuda_stream = 0x5678
+        device_index = 1
+
+    monkeypatch.setattr(B, "_raw_stream", None if documented else lambda device: 0x1000 + device)
+    monkeypatch.setattr(B.torch.cuda, "is_initialized", lambda: True)
+    monkeypatch.setattr(B.torch.cuda, "current_stream", lambda device: type("S", (), {"cuda_stream": 0x1000 + device}))
+    assert B._stream_on(None, 3) == 0x1003
+    assert B._stream_on(Stream, 1) == 0x5678
+    with pytest.raises(ValueError, match="the stream is on GPU 1, the tensors are on GPU 0"):
+        B._stream_on(Stream, 0)
