@@ -69,16 +69,27 @@ class Cache:
 
     def grow(self, seq: int, tokens: int):
         """Room for more tokens: (their positions, their slots)."""
-        start = self.lengths[seq]
-        self.lengths[seq] += tokens
-        if self.lengths[seq] > self.most:
-            raise ValueError(f"sequence {seq} is longer than {self.most} tokens")
-        while len(self.of[seq]) * self.page_size < self.lengths[seq]:
-            if not self.free:
-                raise MemoryError("no free page")
-            self.of[seq].append(self.free.pop())
-        at = range(start, self.lengths[seq])
-        return list(at), [self.of[seq][t // self.page_size] * self.page_size + t % self.page_size for t in at]
+        return self.grow_all([seq], tokens)
+
+    def grow_all(self, seqs, tokens: int):
+        """Room for as many tokens of each sequence, one sequence behind the other; or, with an exception, of none."""
+        if len(set(seqs)) != len(seqs):
+            raise ValueError("a sequence is named twice")
+        lengths = [self.lengths[s] + tokens for s in seqs]
+        for s, n in zip(seqs, lengths):
+            if n > self.most:
+                raise ValueError(f"sequence {s} is longer than {self.most} tokens")
+        missing = [-(-n // self.page_size) - len(self.of[s]) for s, n in zip(seqs, lengths)]
+        if sum(missing) > len(self.free):
+            raise MemoryError("no free page")
+        positions, slots = [], []
+        for s, n, pages in zip(seqs, lengths, missing):
+            self.of[s] += [self.free.pop() for _ in range(pages)]
+            at = range(self.lengths[s], n)
+            positions += at
+            slots += [self.of[s][t // self.page_size] * self.page_size + t % self.page_size for t in at]
+            self.lengths[s] = n
+        return positions, slots
 
     def table(self, seqs):
         """(page table, lengths) of some sequences, on the GPU."""
@@ -108,9 +119,7 @@ class AttentionBlock:
         with x added)."""
         dev = x.device
         heads, kv_heads, D = self.heads, self.kv_heads, self.head_dim
-        room = [self.cache.grow(s, tokens) for s in seqs]
-        positions = torch.tensor(sum((r[0] for r in room), []), dtype=torch.int32, device=dev)
-        slots = torch.tensor(sum((r[1] for r in room), []), dtype=torch.int32, device=dev)
+        positions, slots = (torch.tensor(n, dtype=torch.int32, device=dev) for n in self.cache.grow_all(seqs, tokens))
         table, lengths = self.cache.table(seqs)
         longest = max(self.cache.lengths[s] for s in seqs)
 
