@@ -436,7 +436,7 @@ def basq_paged_attention(q: torch.Tensor, cache: torch.Tensor, page_table: torch
                          softcap: float = 0.0, window: int = 0, lse: Optional[torch.Tensor] = None, bits: int = 4,
                          stream: Optional[torch.cuda.Stream] = None) -> None:
     """q, out bf16 [B * q_len, heads, D] (any token strides); cache uint8 [pages, kv_heads, page_size * (D + 16)]; page_table
-    int32 [B, pages of a sequence] (any row stride); lengths int32 [B]; lse fp32 [B * q_len, heads] or None."""
+    int32 [B, pages of a sequence] (rows as far apart as they are wide, or further); lengths int32 [B]; lse fp32 [B * q_len, heads] or None."""
     rc = (_block or _load_block()).paged_attention(q, cache, page_table, lengths, max_len, scale, out, workspace, q_len, softcap, window, lse,
                                                    bits, _stream_on, stream)
     if rc != BASQ_OK:

@@ -406,7 +406,8 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 || (D == 128 && !FOLD) ? 2 :
         }
         if constexpr (CAP) {
             // log2(e) cap tanh(y), y = x / (log2(e) cap).  Up to 3/8 by its series, under 2^-24 of the value off, which is all that most
-            // steps need; beyond, 1 - 2 / (e^2y + 1), whose rounding is that of 1.
+            // steps need; beyond, 1 - 2 / (e^2y + 1) by the instructions for 1 / x and 2^x, each a unit in the last place off at most: some 2^-23
+            // together, as the rounding of the 1 is.
             bool far = false;
             float y[MINE];
 #pragma unroll

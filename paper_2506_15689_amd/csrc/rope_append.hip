@@ -9,8 +9,8 @@
 // A head of D channels lies on D/8 lanes, eight neighbouring channels (16 bytes) each, so a wavefront takes 512 channels (four
 // or eight heads) per step.  The pair of a channel under rope is in the lane itself (interleaved) or rot/16 lanes away (halves);
 // the transform's stages over channel bits 0-2 are in the lane, the others are DPP operands; the range is a DPP reduction over the
-// head's lanes.  Nothing goes through LDS memory, and a token's cosines and sines stay in registers for all its heads.  A zero out of the
-// transform is positive.
+// head's lanes; only the pairs rot/16 lanes away change lanes by the LDS unit, four instructions a step (no LDS memory).  A token's cosines
+// and sines stay in registers for all its heads.  A zero out of the transform is positive.
 //
 // Bound by memory, with vector instructions not far behind (about 150 for a step of queries).  4096 tokens of 64 and 8 heads of 128 channels
 // move 173 MB in 33.6 us, 5.2 TB/s, 32768 tokens in 246 us, 5.6 (a large copy reaches 4.8).  With the lanes' butterflies as two or three
