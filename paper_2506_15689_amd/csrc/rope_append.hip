@@ -13,7 +13,7 @@
 // and sines stay in registers for all its heads.  A zero out of the transform is positive.
 //
 // Bound by memory, with vector instructions not far behind (about 150 for a step of queries).  4096 tokens of 64 and 8 heads of 128 channels
-// move 173 MB in 33.6 us, 5.2 TB/s, 32768 tokens in 246 us, 5.6 (a large copy reaches 4.8).  With the lanes' butterflies as two or three
+// move 173 MB in 33.4 us, 5.2 TB/s, 32768 tokens in 246 us, 5.6 (a large copy reaches 4.8).  With the lanes' butterflies as two or three
 // instructions each and branches around loads and stores 35.4 .. 36.5, and 17.9 instead of 15.7 for 1946 tokens of 40 and 40 heads of 64
 // channels.  (The first heads are requested once the token's position is known: requested beside it, 1 .. 2 % less, but padding's would be read.)
 // Sixteen tokens: 3.6 us, the launch and four loads, one after the other.
