@@ -403,6 +403,110 @@ int basq_paged_attention(const void* q, int64_t ldq, int32_t B, int32_t q_len, i
                          int64_t table_stride, const int32_t* lengths, int32_t max_len, float scale, float softcap, int32_t window,
                          void* out, int64_t ldo, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- the ends of a step: places in the cache, embeddings, logits, tokens ------------------------ */
+
+/*
+ * Tokens in bf16 times 4-bit weights with a scale and a zero point for each group of channels: the output head, a layer whose
+ * activations stay in 16 bits.  fp32 products and sums, one rounding at the end:
+ *
+ *     Y[m,n] = sum_g w_scale[n,g] * sum_{k in g} (q[n,k] - w_zero[n,g]) X[m,k]  +  bias[n]
+ *
+ *   X          bf16 [M, ldx], 16-byte aligned, ldx >= K and a multiple of 8.  A token with a value that is not finite, or beyond
+ *              2^112, has outputs that are not finite; the others do not
+ *   Wq         uint8 [N, K/2] canonical, or the layout of basq_pack_decode with w_layout = BASQ_W_DECODE16 (K % 128 == 0);
+ *              16-byte aligned
+ *   group_size channels of a group: a multiple of 32 that divides K; 0 counts as K.  (basq_quantize_weights makes such weights of
+ *              [N, K] when called with N * K / group_size rows of group_size channels)
+ *   w_scale, w_zero   bf16 [N, K / group_size], zero points in code units (any real value)
+ *   bias       fp32 [N], or NULL (= 0)
+ *   Y          out, [M, ldy], ldy >= N: fp32 where y_f32, otherwise bf16
+ * K % 32 == 0, K <= 2^20.  Laid out for few tokens: the weights are read once for every 64.  M up to 1048560 (else
+ * BASQ_EUNSUPPORTED); M == 0 does nothing.  Results do not change from call to call.
+ */
+int basq_w4a16_gemm(const void* X, int64_t M, int32_t K, int64_t ldx, const uint8_t* Wq, int32_t N, int32_t w_layout,
+                    const void* w_scale, const void* w_zero, int32_t group_size, const float* bias, void* Y, int64_t ldy,
+                    int32_t y_f32, void* stream);
+
+/*
+ * Rows of such a matrix in bf16: the embeddings of tokens, from the head's weights where the two are tied.
+ *
+ *     Y[t,k] = bf16( scale * (w_scale[n,g] * (q[n,k] - w_zero[n,g])) ) ,   n = ids[t]                       fp32
+ *
+ *   ids        int32 [T]; one that is negative or >= N (padding) gives a row of zeros
+ *   Y          out, bf16 [T, ldy], 16-byte aligned, ldy >= K and a multiple of 8
+ * The matrix as above.  T == 0 does nothing.
+ */
+int basq_w4a16_lookup(const int32_t* ids, int64_t T, const uint8_t* Wq, int32_t N, int32_t K, int32_t w_layout, const void* w_scale,
+                      const void* w_zero, int32_t group_size, float scale, void* Y, int64_t ldy, void* stream);
+
+/*
+ * A token for each row of logits.  The tokens of a row are taken in the order of their logits, the largest first, equal ones by
+ * their index; one whose logit is -inf or NaN is none.  With z_0 >= z_1 >= ... the logits in that order and weights
+ * w_i = e^((z_i - z_0) / temperature) (1 where z_i = z_0), the first n tokens are kept, the least of
+ *     top_k                                                 where top_k > 0
+ *     the first n with  w_0 + ... + w_(n-1) >= top_p * S    where top_p < 1; S is the sum over the first top_k (over all without it); 1 at least
+ *     the number of weights >= min(min_p, 1)                where min_p > 0
+ * and 1 where temperature is not > 0 (the likeliest token).  The token is the first kept one at which
+ * w_0 + ... + w_i > u * (sum of the kept weights).
+ * Weights are computed in fp64 (top_p * S and u * sum are fp64 products) and summed exactly as multiples of 2^-bits, bits = min(50, 62 - log2 V rounded up): a weight below
+ * half of that is never drawn, and the same call gives the same tokens every time.
+ *   logits     fp32 (f32 != 0) or bf16 [B, ldl], ldl >= V, aligned as their type is; ldl = 0: B draws from one row
+ *   temperature, top_p, min_p   fp32 [B], top_k int32 [B]; each may be NULL (1; none).  A NaN among the last two is none
+ *   u          fp64 [B], from [0, 1); what lies outside counts as the nearest of them, NaN as 0
+ *   token      out, int32 [B]; -1 for a row without tokens
+ *   logprob    out, fp32 [B] or NULL: ln of the token's share of the kept weights; -inf without tokens
+ *   kept       out, int32 [B] or NULL: n
+ *   workspace  256-byte aligned, >= basq_sample_workspace_bytes(B, V) (else BASQ_EWORKSPACE); NULL where that is 0.  A workspace for
+ *              a call does for any with fewer rows or a smaller V
+ * V up to 2^22 (else BASQ_EUNSUPPORTED).  B == 0 does nothing.
+ */
+size_t basq_sample_workspace_bytes(int32_t B, int32_t V);
+int basq_sample(const void* logits, int64_t ldl, int32_t B, int32_t V, int32_t f32, const float* temperature, const int32_t* top_k,
+                const float* top_p, const float* min_p, const double* u, int32_t* token, float* logprob, int32_t* kept,
+                void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The books of the paged cache, on the GPU: a batch's sequences grow, or lose their last tokens, and what basq_rope_append and
+ * basq_paged_attention take is written.  Sequence b of the batch is row s = seqs[b] of the pool; with n = lengths[s], m = n +
+ * new_tokens[b] and P = page_size it has ceil(n / P) pages and comes to have ceil(m / P):
+ *     pages that go back   (new_tokens[b] < 0) are put behind the free ones, in the order of the batch, a sequence's in their order
+ *     pages that are taken then come from the end of the free ones, in the order of the batch, into row s from entry ceil(n / P) on
+ *     tokens               n .. m - 1 get positions and slots (page * P + token % P)
+ *   lengths      int32 [rows];  lengths_out  out, int32 [rows]: m for the batch's rows, the others left as they are; may be lengths
+ *   pool_table   int32 [rows, columns], row stride pool_stride, entries past a length may hold anything; in and out
+ *   free_pages   int32 [capacity], the first free_count[0] are free; in and out.   free_out  out, int32 [1]; may be free_count
+ *   seqs         int32 [B], none twice; NULL: the first B rows
+ *   new_tokens   int32 [B]; NULL: q_len of each
+ *   q_len        > 0: token places lie in B runs of q_len, T = B * q_len, and a sequence's new tokens are the last of its run
+ *                0: they lie packed, sequence behind sequence, from 0 on
+ *   positions, slots   out, int32 [T]; -1 for places without a token (padding to the operators that read them)
+ *   starts       out, int32 [B + 1] or NULL, with q_len = 0: where each sequence's tokens start; the last is their number
+ *   batch_table  out, int32 [B, columns], row stride batch_stride, or NULL: the pages of the batch's sequences; entries past them are
+ *                left as they were
+ *   batch_lengths   out, int32 [B] or NULL: m
+ *   status       out, int32 [2]: (0, 0), or why nothing was done: all positions and slots are -1, batch_lengths and starts 0, the
+ *                books as they were (free_out is free_count's value, lengths_out and batch_table are left)
+ *                  BASQ_KV_SEQUENCE  (1, b): seqs[b] is no row, or was named before
+ *                  BASQ_KV_LENGTH    (2, b): its length, before or after, is negative or more than columns * P, or q_len < new_tokens[b]
+ *                  BASQ_KV_FREE      (3, free_count): the count is negative, or free_pages has no room for what goes back
+ *                  BASQ_KV_PAGES     (4, pages): that many are missing
+ *                  BASQ_KV_TOKENS    (5, tokens): that many more than T
+ *   books        workspace, >= basq_kv_books_bytes(B), 16-byte aligned (else BASQ_EWORKSPACE); holds nothing between calls
+ * page_size as in the cache; B up to 1024 and B * columns < 2^31 (else BASQ_EUNSUPPORTED).  But for the pairs named, nothing may
+ * overlap.  B == 0: the padding, starts[0], free_out and status are written.
+ */
+#define BASQ_KV_SEQUENCE 1
+#define BASQ_KV_LENGTH   2
+#define BASQ_KV_FREE     3
+#define BASQ_KV_PAGES    4
+#define BASQ_KV_TOKENS   5
+size_t basq_kv_books_bytes(int32_t B);
+int basq_kv_extend(const int32_t* lengths, int32_t* pool_table, int64_t pool_stride, int32_t rows, int32_t columns, int32_t page_size,
+                   int32_t* free_pages, int32_t capacity, const int32_t* free_count, const int32_t* seqs, const int32_t* new_tokens,
+                   int32_t B, int32_t q_len, int32_t* positions, int32_t* slots, int64_t T, int32_t* starts, int32_t* batch_table,
+                   int64_t batch_stride, int32_t* batch_lengths, int32_t* lengths_out, int32_t* free_out, int32_t* status,
+                   void* books, size_t books_bytes, void* stream);
+
 /* ---- diagnostics: what this machine sustains (used by the benchmark's measured ceilings), single tilings, bounds ---- */
 
 /*

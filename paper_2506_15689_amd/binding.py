@@ -1,6 +1,6 @@
 """Thin binding of libbasq.so: same names as the C ABI (include/basq.h), torch tensors in,
 argument marshalling only -- by ctypes, and for the calls around the linear layer (norm, append,
-attention), whose small forms Python's marshalling would cost more than their kernels, in the compiled
+attention) and at a step's ends (places, embeddings, logits, tokens), whose small forms Python's marshalling would cost more than their kernels, in the compiled
 module _block (csrc/binding_block.cpp).  Every step of the layer runs in the HIP kernels; there is no CPU
 fallback -- if the library is missing or a call fails, an exception is raised."""
 from __future__ import annotations
@@ -26,6 +26,7 @@ STREAM_MAX_TOKENS = 128      # calls of more tokens never take the weight-stream
 EXPORTS = ["basq_version", "basq_last_error", "basq_rotate_quant", "basq_w4a4_gemm", "basq_workspace_bytes",
            "basq_w4a4_gemm_grouped", "basq_group_colsums", "basq_fp6_bytes", "basq_pack_fp6", "basq_decode_bytes", "basq_pack_decode", "basq_linear_fused", "basq_linear_fused_static", "basq_rotate_weights", "basq_quantize_weights", "basq_fused_bias", "basq_prepare_weights", "basq_calibrate_bias",
            "basq_add_rms_norm", "basq_rope_table", "basq_kv_page_bytes", "basq_rope_append", "basq_paged_attention_workspace_bytes", "basq_paged_attention",
+           "basq_w4a16_gemm", "basq_w4a16_lookup", "basq_sample_workspace_bytes", "basq_sample", "basq_kv_books_bytes", "basq_kv_extend",
            "basq_hadamard28", "basq_diag_stream", "basq_diag_read", "basq_diag_mfma_i8", "basq_diag_mfma_f6",
            "basq_diag_fp6_tiling", "basq_diag_w4a4_gemm_fp6", "basq_diag_fp6_split_tiling", "basq_diag_w4a4_gemm_fp6_split",
            "basq_diag_grouped_tiling", "basq_diag_w4a4_gemm_grouped_fp6", "basq_diag_grouped_wide_strays", "basq_diag_block_vector_channels",
@@ -105,6 +106,19 @@ def load() -> ctypes.CDLL:
     lib.basq_paged_attention.restype = c.c_int
     lib.basq_paged_attention.argtypes = [vp, i64, i32, i32, i32, i32, i32, i32, vp, i32, i32, vp, i64, vp, i32, f32, f32, i32,
                                          vp, i64, vp, vp, c.c_size_t, vp]
+    lib.basq_w4a16_gemm.restype = c.c_int
+    lib.basq_w4a16_gemm.argtypes = [vp, i64, i32, i64, vp, i32, i32, vp, vp, i32, vp, vp, i64, i32, vp]
+    lib.basq_w4a16_lookup.restype = c.c_int
+    lib.basq_w4a16_lookup.argtypes = [vp, i64, vp, i32, i32, i32, vp, vp, i32, f32, vp, i64, vp]
+    lib.basq_sample_workspace_bytes.restype = c.c_size_t
+    lib.basq_sample_workspace_bytes.argtypes = [i32, i32]
+    lib.basq_sample.restype = c.c_int
+    lib.basq_sample.argtypes = [vp, i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, c.c_size_t, vp]
+    lib.basq_kv_books_bytes.restype = c.c_size_t
+    lib.basq_kv_books_bytes.argtypes = [i32]
+    lib.basq_kv_extend.restype = c.c_int
+    lib.basq_kv_extend.argtypes = [vp, vp, i64, i32, i32, i32, vp, i32, vp, vp, vp, i32, i32, vp, vp, i64, vp, vp, i64, vp, vp, vp, vp,
+                                   vp, c.c_size_t, vp]
     lib.basq_hadamard28.restype = c.c_int
     lib.basq_hadamard28.argtypes = [vp]
     lib.basq_diag_stream.restype = c.c_int
@@ -439,6 +453,61 @@ def basq_paged_attention(q: torch.Tensor, cache: torch.Tensor, page_table: torch
     int32 [B, pages of a sequence] (rows as far apart as they are wide, or further); lengths int32 [B]; lse fp32 [B * q_len, heads] or None."""
     rc = (_block or _load_block()).paged_attention(q, cache, page_table, lengths, max_len, scale, out, workspace, q_len, softcap, window, lse,
                                                    bits, _stream_on, stream)
+    if rc != BASQ_OK:
+        _check(rc)
+
+
+KV_SEQUENCE, KV_LENGTH, KV_FREE, KV_PAGES, KV_TOKENS = 1, 2, 3, 4, 5      # BASQ_KV_* of include/basq.h: status of basq_kv_extend
+
+
+def basq_w4a16_gemm(x: torch.Tensor, Wq: torch.Tensor, w_scale: torch.Tensor, w_zero: torch.Tensor, y: torch.Tensor,
+                    bias: Optional[torch.Tensor] = None, *, w_layout: int = BASQ_W_CANONICAL,
+                    stream: Optional[torch.cuda.Stream] = None) -> None:
+    """x bf16 [M, K], y bf16 or fp32 [M, N] (any row strides); Wq uint8 [N, K/2], or what basq_pack_decode makes of it with w_layout =
+    BASQ_W_DECODE16; w_scale, w_zero bf16 [N, groups]; bias fp32 [N]."""
+    rc = (_block or _load_block()).w4a16_gemm(x, Wq, w_scale, w_zero, y, bias, w_layout, _stream_on, stream)
+    if rc != BASQ_OK:
+        _check(rc)
+
+
+def basq_w4a16_lookup(ids: torch.Tensor, Wq: torch.Tensor, w_scale: torch.Tensor, w_zero: torch.Tensor, y: torch.Tensor,
+                      scale: float = 1.0, *, w_layout: int = BASQ_W_CANONICAL, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Rows ids (int32 [T]) of a matrix as in basq_w4a16_gemm, times scale, into y bf16 [T, K] (any row stride)."""
+    rc = (_block or _load_block()).w4a16_lookup(ids, Wq, w_scale, w_zero, y, scale, w_layout, _stream_on, stream)
+    if rc != BASQ_OK:
+        _check(rc)
+
+
+def basq_sample_workspace_bytes(B: int, V: int) -> int:
+    return int(load().basq_sample_workspace_bytes(B, V))
+
+
+def basq_sample(logits: torch.Tensor, u: torch.Tensor, token: torch.Tensor, workspace: Optional[torch.Tensor], *,
+                temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None,
+                min_p: Optional[torch.Tensor] = None, logprob: Optional[torch.Tensor] = None, kept: Optional[torch.Tensor] = None,
+                stream: Optional[torch.cuda.Stream] = None) -> None:
+    """logits bf16 or fp32 [B, V] (any row stride); per row u fp64, temperature, top_p, min_p fp32, top_k int32; out token int32, logprob
+    fp32, kept int32."""
+    rc = (_block or _load_block()).sample(logits, u, token, workspace, temperature, top_k, top_p, min_p, logprob, kept, _stream_on, stream)
+    if rc != BASQ_OK:
+        _check(rc)
+
+
+def basq_kv_books_bytes(B: int) -> int:
+    return int(load().basq_kv_books_bytes(B))
+
+
+def basq_kv_extend(lengths: torch.Tensor, pool_table: torch.Tensor, free_pages: torch.Tensor, free_count: torch.Tensor,
+                   new_tokens: Optional[torch.Tensor], page_size: int, positions: torch.Tensor, slots: torch.Tensor, status: torch.Tensor,
+                   books: torch.Tensor, *, seqs: Optional[torch.Tensor] = None, q_len: int = 1, starts: Optional[torch.Tensor] = None,
+                   batch_table: Optional[torch.Tensor] = None, batch_lengths: Optional[torch.Tensor] = None,
+                   lengths_out: Optional[torch.Tensor] = None, free_out: Optional[torch.Tensor] = None,
+                   stream: Optional[torch.cuda.Stream] = None) -> None:
+    """lengths int32 [rows], pool_table int32 [rows, columns], free_pages int32, free_count int32 [1]: the books, updated where
+    lengths_out and free_out are not given; new_tokens, seqs int32 [B]; out positions, slots int32 [B * q_len] (any number with q_len =
+    0: packed), status int32 [2], starts int32 [B + 1], batch_table int32 [B, columns], batch_lengths int32 [B]; books: workspace."""
+    rc = (_block or _load_block()).kv_extend(lengths, pool_table, free_pages, free_count, new_tokens, page_size, positions, slots, status, books,
+                                             seqs, q_len, starts, batch_table, batch_lengths, lengths_out, free_out, _stream_on, stream)
     if rc != BASQ_OK:
         _check(rc)
 

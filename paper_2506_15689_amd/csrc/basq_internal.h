@@ -187,6 +187,82 @@ AttentionPlan paged_attention_plan(int32_t B, int32_t q_len, int32_t heads, int3
 int paged_attention_most_workers(int32_t B, int32_t q_len, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t max_len, int32_t window);
 int launch_paged_attention(PagedAttentionArgs a, hipStream_t s);  // paged_attention.hip
 
+// ---- the ends of a step (api_step.hip) ----------------------------------------------------------
+struct W4A16Args {
+    const uint16_t* X;        // [M, ldx], bf16 bits
+    int64_t M, ldx;
+    int32_t K, N;
+    const uint8_t* Wq;
+    int32_t w_layout;
+    const uint16_t *w_scale, *w_zero;                             // [N, K / group], bf16 bits
+    int32_t group;
+    const float* bias;        // optional, [N]
+    void* Y;                  // [M, ldy], fp32 or bf16
+    int64_t ldy;
+    int32_t y_f32;
+    int32_t unit, groups;     // these three are set by the launcher: channels that share a group, groups of a row,
+    uint32_t per_group;       // what a unit's number is multiplied with for its group's
+};
+constexpr int64_t W4A16_MAX_TOKENS = 16 * 65535;
+int launch_gemm_w4a16(W4A16Args a, hipStream_t s);                // gemm_w4a16.hip
+
+struct LookupArgs {
+    const int32_t* ids;       // [T]
+    int64_t T;
+    const uint8_t* Wq;
+    int32_t N, K, w_layout;
+    const uint16_t *w_scale, *w_zero;
+    int32_t group;
+    float scale;
+    uint16_t* Y;              // [T, ldy], bf16 bits
+    int64_t ldy;
+    int32_t groups;           // set by the launcher
+};
+int launch_lookup_w4a16(LookupArgs a, hipStream_t s);             // lookup_w4a16.hip
+
+struct SampleArgs {
+    const void* logits;       // [B, ldl], fp32 or bf16
+    int64_t ldl;
+    int32_t B, V, f32;
+    const float* temperature; // the four choices: optional, [B]
+    const int32_t* top_k;
+    const float *top_p, *min_p;
+    const double* u;          // [B]
+    int32_t* token;           // [B]
+    float* logprob;           // optional, [B]
+    int32_t* kept;            // optional, [B]
+    uint8_t* workspace;
+    int32_t bits;             // set by the launcher: a weight of 1 is 2^bits
+};
+constexpr int32_t SAMPLE_MAX_TOKENS = 1 << 22;
+size_t sample_workspace_bytes(int32_t B, int32_t V);
+int launch_sample(SampleArgs a, hipStream_t s);                   // sample.hip
+
+struct KvExtendArgs {
+    const int32_t* lengths;   // [rows]
+    int32_t* pool_table;      // [rows, pool_stride]
+    int64_t pool_stride;
+    int32_t rows, columns, page_log2;
+    int32_t* free_pages;      // [capacity]
+    int32_t capacity;
+    const int32_t* free_count;
+    const int32_t* seqs;      // optional, [B]
+    const int32_t* new_tokens;                                    // optional, [B]
+    int32_t B, q_len;
+    int32_t *positions, *slots;                                   // [T]
+    int64_t T;
+    int32_t* starts;          // optional, [B + 1]
+    int32_t* batch_table;     // optional, [B, batch_stride]
+    int64_t batch_stride;
+    int32_t* batch_lengths;   // optional, [B]
+    int32_t* lengths_out;
+    int32_t* free_out;
+    int32_t* status;          // [2]
+    uint8_t* plan;            // 64 bytes and KV_PLAN_BYTES a sequence
+};
+constexpr int KV_MAX_SEQUENCES = 1024, KV_PLAN_BYTES = 32;
+int launch_kv_extend(KvExtendArgs a, hipStream_t s);              // kv_extend.hip
+
 // 28 x 28 Paley type-I matrix, row-major, built on the host at first use (hadamard28.hip).
 const int8_t* hadamard28_host();
 

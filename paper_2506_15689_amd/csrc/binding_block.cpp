@@ -1,4 +1,4 @@
-// Python entry points of the operators around the linear layer (include/basq.h): checks of shapes, types and places, then the C
+// Python entry points of the operators around the linear layer and of a step's ends (include/basq.h): checks of shapes, types and places, then the C
 // ABI.  A compiled module because of what a small call costs: marshalling thirty arguments of ten tensors in Python takes 7 .. 13 us,
 // as long as the kernels of a decode step, here 1.  Every function takes its arguments by position (binding.py gives
 // them names and defaults) and returns the C ABI's code; a tensor that does not fit is a ValueError.
@@ -296,10 +296,170 @@ PyObject* paged_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
+// codes, scales and zero points of [N, K] weights with groups: N and the channels of a group
+struct Weights {
+    int32_t N, group;
+};
+Weights weights_of(const at::Tensor& Wq, const at::Tensor& scale, const at::Tensor& zero, int64_t K, int32_t layout) {
+    if (scale.scalar_type() != at::kBFloat16 || scale.dim() < 1 || scale.dim() > 2 || !scale.is_contiguous() || scale.numel() < 1)
+        refuse("w_scale must be contiguous BFloat16 [N, groups], not %s", shown(scale).c_str());
+    vector_of(zero, scale.numel(), "w_zero", at::kBFloat16);
+    const int64_t N = scale.size(0), groups = scale.numel() / N;
+    if (K < 1 || K % groups != 0) refuse("%lld channels are not %lld groups", (long long)K, (long long)groups);
+    const int64_t rows = layout == BASQ_W_DECODE16 ? (N + 15) / 16 * 16 : N;
+    vector_of(Wq, rows * (K / 2), "Wq", at::kByte);
+    return Weights{narrow(N, "N"), narrow(K / groups, "K")};
+}
+
+// (x, Wq, w_scale, w_zero, y, bias, w_layout, handle_of, stream)
+PyObject* w4a16_gemm(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return entry(n, 9, [&] {
+        Call c;
+        const at::Tensor &x = *c.tensor(args[0], "x"), &Wq = *c.tensor(args[1], "Wq"), &scale = *c.tensor(args[2], "w_scale"), &zero = *c.tensor(args[3], "w_zero");
+        const at::Tensor& y = *c.tensor(args[4], "y");
+        const at::Tensor* bias = c.tensor(args[5], "bias", false);
+        const int32_t layout = narrow(whole(args[6]), "w_layout");
+        if (x.dim() != 2) refuse("x must be [M, K], not %s", shown(x).c_str());
+        const int64_t M = x.size(0), ldx = rows_of(x, x, "x", at::kBFloat16);
+        const int32_t K = narrow(x.size(1), "K");
+        const Weights w = weights_of(Wq, scale, zero, K, layout);
+        const bool f32 = y.scalar_type() == at::kFloat;
+        if (y.dim() != 2 || y.size(0) != M || y.size(1) != w.N || (!f32 && y.scalar_type() != at::kBFloat16))
+            refuse("y must be Float or BFloat16 [%lld, %d], not %s", (long long)M, w.N, shown(y).c_str());
+        const int64_t ldy = rows_of(y, y, "y", y.scalar_type());
+        if (bias) vector_of(*bias, w.N, "bias", at::kFloat);
+        c.same_gpu();
+        const void *rows = data(&x), *s = data(&scale), *z = data(&zero);
+        const uint8_t* codes = data<uint8_t>(&Wq);
+        const float* add = data<float>(bias);
+        void* out = data(&y);
+        const Launch on(c, args[7], args[8]);
+        return without_gil([&] { return basq_w4a16_gemm(rows, M, K, ldx, codes, w.N, layout, s, z, w.group, add, out, ldy, f32, on.stream); });
+    });
+}
+
+// (ids, Wq, w_scale, w_zero, y, scale, w_layout, handle_of, stream)
+PyObject* w4a16_lookup(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return entry(n, 9, [&] {
+        Call c;
+        const at::Tensor &ids = *c.tensor(args[0], "ids"), &Wq = *c.tensor(args[1], "Wq"), &scale = *c.tensor(args[2], "w_scale"), &zero = *c.tensor(args[3], "w_zero");
+        const at::Tensor& y = *c.tensor(args[4], "y");
+        const float factor = (float)real(args[5]);
+        const int32_t layout = narrow(whole(args[6]), "w_layout");
+        if (y.dim() != 2) refuse("y must be [T, K], not %s", shown(y).c_str());
+        const int64_t T = y.size(0), ldy = rows_of(y, y, "y", at::kBFloat16);
+        const int32_t K = narrow(y.size(1), "K");
+        vector_of(ids, T, "ids", at::kInt);
+        const Weights w = weights_of(Wq, scale, zero, K, layout);
+        c.same_gpu();
+        const int32_t* which = data<int32_t>(&ids);
+        const void *s = data(&scale), *z = data(&zero);
+        const uint8_t* codes = data<uint8_t>(&Wq);
+        void* out = data(&y);
+        const Launch on(c, args[7], args[8]);
+        return without_gil([&] { return basq_w4a16_lookup(which, T, codes, w.N, K, layout, s, z, w.group, factor, out, ldy, on.stream); });
+    });
+}
+
+// (logits, u, token, workspace, temperature, top_k, top_p, min_p, logprob, kept, handle_of, stream)
+PyObject* sample(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return entry(n, 12, [&] {
+        Call c;
+        const at::Tensor &logits = *c.tensor(args[0], "logits"), &u = *c.tensor(args[1], "u"), &token = *c.tensor(args[2], "token");
+        const at::Tensor* workspace = c.tensor(args[3], "workspace", false);
+        const at::Tensor *temperature = c.tensor(args[4], "temperature", false), *top_k = c.tensor(args[5], "top_k", false);
+        const at::Tensor *top_p = c.tensor(args[6], "top_p", false), *min_p = c.tensor(args[7], "min_p", false);
+        const at::Tensor *logprob = c.tensor(args[8], "logprob", false), *kept = c.tensor(args[9], "kept", false);
+        const bool f32 = logits.scalar_type() == at::kFloat;
+        if (logits.dim() != 2 || (!f32 && logits.scalar_type() != at::kBFloat16)) refuse("logits must be Float or BFloat16 [B, V], not %s", shown(logits).c_str());
+        const int32_t B = narrow(logits.size(0), "B"), V = narrow(logits.size(1), "V");
+        const int64_t ldl = rows_of(logits, logits, "logits", logits.scalar_type());
+        vector_of(u, B, "u", at::kDouble);
+        vector_of(token, B, "token", at::kInt);
+        if (temperature) vector_of(*temperature, B, "temperature", at::kFloat);
+        if (top_k) vector_of(*top_k, B, "top_k", at::kInt);
+        if (top_p) vector_of(*top_p, B, "top_p", at::kFloat);
+        if (min_p) vector_of(*min_p, B, "min_p", at::kFloat);
+        if (logprob) vector_of(*logprob, B, "logprob", at::kFloat);
+        if (kept) vector_of(*kept, B, "kept", at::kInt);
+        if (workspace && !workspace->is_contiguous()) refuse("workspace must be contiguous");
+        const size_t room = workspace ? workspace->nbytes() : 0;
+        c.same_gpu();
+        const void* rows = data(&logits);
+        const double* numbers = data<double>(&u);
+        int32_t *drawn = data<int32_t>(&token), *many = data<int32_t>(kept);
+        const float *heat = data<float>(temperature), *mass = data<float>(top_p), *least = data<float>(min_p);
+        const int32_t* most = data<int32_t>(top_k);
+        float* ln = data<float>(logprob);
+        void* parts = data(workspace);
+        const Launch on(c, args[10], args[11]);
+        return without_gil([&] { return basq_sample(rows, ldl, B, V, f32, heat, most, mass, least, numbers, drawn, ln, many, parts, room, on.stream); });
+    });
+}
+
+// (lengths, pool_table, free_pages, free_count, new_tokens, page_size, positions, slots, status, books, seqs, q_len, starts, batch_table,
+//  batch_lengths, lengths_out, free_out, handle_of, stream)
+PyObject* kv_extend(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return entry(n, 19, [&] {
+        Call c;
+        const at::Tensor &lengths = *c.tensor(args[0], "lengths"), &pool = *c.tensor(args[1], "pool_table"), &pages = *c.tensor(args[2], "free_pages");
+        const at::Tensor& count = *c.tensor(args[3], "free_count");
+        const at::Tensor* fresh = c.tensor(args[4], "new_tokens", false);
+        const int32_t page_size = narrow(whole(args[5]), "page_size");
+        const at::Tensor &positions = *c.tensor(args[6], "positions"), &slots = *c.tensor(args[7], "slots"), &status = *c.tensor(args[8], "status");
+        const at::Tensor &books = *c.tensor(args[9], "books"), *seqs = c.tensor(args[10], "seqs", false);
+        const int32_t q_len = narrow(whole(args[11]), "q_len");
+        const at::Tensor *starts = c.tensor(args[12], "starts", false), *table = c.tensor(args[13], "batch_table", false);
+        const at::Tensor* batch_lengths = c.tensor(args[14], "batch_lengths", false);
+        const at::Tensor *lengths_out = c.tensor(args[15], "lengths_out", false), *free_out = c.tensor(args[16], "free_out", false);
+        if (pool.dim() != 2) refuse("pool_table must be [rows, columns], not %s", shown(pool).c_str());
+        const int32_t rows = narrow(pool.size(0), "rows"), columns = narrow(pool.size(1), "columns");
+        const int64_t pool_stride = rows_of(pool, pool, "pool_table", at::kInt);
+        vector_of(lengths, rows, "lengths", at::kInt);
+        if (lengths_out) vector_of(*lengths_out, rows, "lengths_out", at::kInt);
+        const int32_t capacity = narrow(pages.numel(), "free_pages");
+        vector_of(pages, capacity, "free_pages", at::kInt);
+        vector_of(count, 1, "free_count", at::kInt);
+        if (free_out) vector_of(*free_out, 1, "free_out", at::kInt);
+        if (!seqs && !fresh) refuse("seqs or new_tokens must be given");
+        const int32_t B = narrow((seqs ? *seqs : *fresh).numel(), "B");
+        if (seqs) vector_of(*seqs, B, "seqs", at::kInt);
+        if (fresh) vector_of(*fresh, B, "new_tokens", at::kInt);
+        const int64_t T = positions.numel();
+        vector_of(positions, T, "positions", at::kInt);
+        vector_of(slots, T, "slots", at::kInt);
+        vector_of(status, 2, "status", at::kInt);
+        if (starts) vector_of(*starts, B + 1, "starts", at::kInt);
+        if (batch_lengths) vector_of(*batch_lengths, B, "batch_lengths", at::kInt);
+        int64_t batch_stride = 0;
+        if (table) {
+            if (table->dim() != 2 || table->size(0) != B || table->size(1) != columns) refuse("batch_table must be [%d, %d], not %s", B, columns, shown(*table).c_str());
+            batch_stride = rows_of(*table, *table, "batch_table", at::kInt);
+        }
+        if (!books.is_contiguous()) refuse("books must be contiguous");
+        const size_t room = books.nbytes();
+        c.same_gpu();
+        auto ints = [](const at::Tensor* t) { return data<int32_t>(t); };
+        const int32_t *had = ints(&lengths), *free_n = ints(&count), *of = ints(seqs), *plus = ints(fresh);
+        int32_t *pool_at = ints(&pool), *free_at = ints(&pages), *pos = ints(&positions), *to = ints(&slots), *why = ints(&status), *first = ints(starts);
+        int32_t *rows_at = ints(table), *lens = ints(batch_lengths), *have = ints(lengths_out ? lengths_out : &lengths), *left = ints(free_out ? free_out : &count);
+        void* plan = data(&books);
+        const Launch on(c, args[17], args[18]);
+        return without_gil([&] {
+            return basq_kv_extend(had, pool_at, pool_stride, rows, columns, page_size, free_at, capacity, free_n, of, plus, B, q_len, pos, to, T, first,
+                                  rows_at, batch_stride, lens, have, left, why, plan, room, on.stream);
+        });
+    });
+}
+
 PyMethodDef methods[] = {
     {"add_rms_norm", (PyCFunction)(void (*)(void))add_rms_norm, METH_FASTCALL, nullptr},
     {"rope_append", (PyCFunction)(void (*)(void))rope_append, METH_FASTCALL, nullptr},
     {"paged_attention", (PyCFunction)(void (*)(void))paged_attention, METH_FASTCALL, nullptr},
+    {"w4a16_gemm", (PyCFunction)(void (*)(void))w4a16_gemm, METH_FASTCALL, nullptr},
+    {"w4a16_lookup", (PyCFunction)(void (*)(void))w4a16_lookup, METH_FASTCALL, nullptr},
+    {"sample", (PyCFunction)(void (*)(void))sample, METH_FASTCALL, nullptr},
+    {"kv_extend", (PyCFunction)(void (*)(void))kv_extend, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_block", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,540 @@
+"""The ends of a step on the GPU, against their definitions (step_ref.py).  Tolerances are stated where they are used, with what they
+follow from."""
+import math
+import random
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2506_15689_amd import binding as B
+
+import step_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+BF16 = torch.bfloat16
+I32 = torch.int32
+
+
+def gen(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def strided(t, pad, fill=7.0):
+    """The same values in rows that are `pad` elements further apart."""
+    wide = torch.full((t.shape[0], t.shape[1] + pad), fill, dtype=torch.float32, device=t.device).to(t.dtype)
+    view = wide[:, :t.shape[1]]
+    view.copy_(t)
+    return view
+
+
+def check_stored(got, want, slack):
+    """Stored values against fp64 ones that the arithmetic in front of the store may miss by `slack`: rounding is monotonic, so what is
+    stored lies between the roundings of the ends."""
+    low, high, got = (want - slack).to(got.dtype).double(), (want + slack).to(got.dtype).double(), got.cpu().double()
+    bad = ~((got >= low) & (got <= high))
+    assert not bad.any(), f"{int(bad.sum())} of {bad.numel()} values; the furthest {float(((got - want).abs() / slack.clamp(min=1e-300))[bad].max())} times the slack away"
+
+
+# ---- product and lookup ----------------------------------------------------------------------------
+
+def weights(g, N, K, G, exact=False):
+    codes = torch.randint(0, 256, (N, K // 2), generator=g, dtype=torch.uint8, device=DEV)
+    if exact:
+        s = 2.0 ** torch.randint(-2, 3, (N, K // G), generator=g, device=DEV).float()
+        z = torch.randint(0, 16, (N, K // G), generator=g, device=DEV).float()
+    else:
+        s = torch.exp(0.3 * torch.randn((N, K // G), generator=g, device=DEV)) / (3.3 * math.sqrt(K))
+        z = 7.5 + 1.2 * torch.randn((N, K // G), generator=g, device=DEV)
+    return codes, s.to(BF16), z.to(BF16)
+
+
+def laid_out(codes, layout):
+    if layout == B.BASQ_W_CANONICAL:
+        return codes
+    N, KB = codes.shape
+    out = torch.empty(B.basq_decode_bytes(N, 2 * KB), dtype=torch.uint8, device=DEV)
+    B.basq_pack_decode(codes, out)
+    return out
+
+
+CANONICAL, STREAMED = B.BASQ_W_CANONICAL, B.BASQ_W_DECODE16
+SHAPES = [(1, 32, 1, 32), (3, 160, 17, 32), (1, 96, 40, 96), (2, 128, 16, 128), (5, 384, 33, 64), (16, 512, 100, 128), (17, 640, 47, 32), (31, 256, 64, 256),
+          (33, 1024, 130, 64), (48, 4096, 80, 128), (64, 2048, 31, 2048), (65, 512, 48, 32), (150, 384, 70, 384), (4, 14336, 20, 512), (9, 4128, 19, 4128),
+          (7, 960, 600, 320), (1, 8192, 50, 128), (13, 11008, 33, 32), (20, 1152, 1100, 192)]
+
+
+@pytest.mark.parametrize("M,K,N,G", SHAPES)
+@pytest.mark.parametrize("layout", [CANONICAL, STREAMED])
+def test_product_of_whole_numbers(M, K, N, G, layout):
+    """Scales that are powers of two, whole zero points and whole activations: every product and sum is exact in fp32."""
+    if layout == STREAMED and K % 128 != 0:
+        pytest.skip("the streaming layout needs K % 128 == 0")
+    g = gen(M + K + N)
+    codes, s, z = weights(g, N, K, G, exact=True)
+    x = torch.randint(-3, 4, (M, K), generator=g, device=DEV).to(BF16)
+    bias = torch.randint(-50, 50, (N,), generator=g, device=DEV).float()
+    want, made_of = ref.product(x, codes, s, z, bias)
+    assert made_of.max() < 2.0 ** 22                              # (quarters, in 24 bits)
+    for out_type in (torch.float32, BF16):
+        y = strided(torch.zeros(M, N, dtype=out_type, device=DEV), 5)
+        B.basq_w4a16_gemm(strided(x, 24), laid_out(codes, layout), s, z, y, bias, w_layout=layout)
+        assert torch.equal(y.cpu(), want.to(out_type)), (out_type, (y.cpu().double() - want).abs().max())
+        assert M == 1 or (y._base[:, N:] == 7).all(), "the gaps between rows were written"
+
+
+@pytest.mark.parametrize("M,K,N,G", SHAPES)
+@pytest.mark.parametrize("layout", [CANONICAL, STREAMED])
+def test_product(M, K, N, G, layout):
+    if layout == STREAMED and K % 128 != 0:
+        pytest.skip("the streaming layout needs K % 128 == 0")
+    g = gen(2 * M + K + N)
+    codes, s, z = weights(g, N, K, G)
+    x = torch.randn((M, K), generator=g, device=DEV) + 0.3
+    x[:, ::37] *= 20
+    x = x.to(BF16)
+    bias = torch.randn(N, generator=g, device=DEV)
+    want, made_of = ref.product(x, codes, s, z, bias)
+    # fp32: at most 128 additions one behind the other in a unit, one for each of up to K/32 units, 20 joins, each within 2^-23 of what
+    # the sums are made of; their errors have either sign, so that their squares add: the square root of their number, six times
+    slack = made_of * 2.0 ** -23 * 6 * math.sqrt(148 + K / 32) / math.sqrt(128)
+    for out_type in (torch.float32, BF16):
+        y = torch.zeros(M, N, dtype=out_type, device=DEV)
+        B.basq_w4a16_gemm(x, laid_out(codes, layout), s, z, y, bias, w_layout=layout)
+        check_stored(y, want, slack)
+        again = torch.ones_like(y)
+        B.basq_w4a16_gemm(x, laid_out(codes, layout), s, z, again, bias, w_layout=layout)
+        assert torch.equal(y, again)
+
+
+def test_product_of_the_quantisers_weights():
+    """Groups by the library's own quantiser: N * K / G rows of G channels."""
+    N, K, G = 48, 512, 64
+    g = gen(3)
+    W = (torch.randn((N, K), generator=g, device=DEV) * 0.05).to(BF16)
+    codes, s, z, total = B.alloc_weight_buffers(N * K // G, G, DEV)
+    B.basq_quantize_weights(W.view(-1, G), codes, s, z, total)
+    x = torch.randn((5, K), generator=g, device=DEV).to(BF16)
+    y = torch.empty((5, N), device=DEV)
+    B.basq_w4a16_gemm(x, codes.view(N, K // 2), s.view(N, -1), z.view(N, -1), y)
+    want, _ = ref.product(x, codes.view(N, -1), s.view(N, -1), z.view(N, -1))
+    assert (y.cpu().double() - want).abs().max() < 1e-5
+    # half a step of the widest group, of some 0.25 / 15, in each of 512 weights: the root of their number, six times
+    assert (y.cpu().double() - x.cpu().double() @ W.cpu().double().t()).abs().max() < 6 * math.sqrt(512) * 0.5 * 0.4 / 15
+
+
+def test_product_with_a_token_that_is_not_finite():
+    M, K, N, G = 20, 512, 40, 64
+    g = gen(4)
+    codes, s, z = weights(g, N, K, G)
+    x = torch.randn((M, K), generator=g, device=DEV).to(BF16)
+    clean, y = torch.empty((M, N), device=DEV), torch.empty((M, N), device=DEV)
+    B.basq_w4a16_gemm(x, codes, s, z, clean)
+    x[3, 5], x[17, 100] = math.nan, math.inf
+    B.basq_w4a16_gemm(x, codes, s, z, y)
+    rest = [m for m in range(M) if m not in (3, 17)]
+    assert torch.equal(y[rest], clean[rest]) and not y[[3, 17]].isfinite().any()
+
+
+@pytest.mark.parametrize("T,K,N,G", [(1, 32, 1, 32), (5, 160, 17, 32), (33, 256, 40, 256), (16, 4096, 100, 64), (300, 1152, 50, 192), (3, 14336, 16, 128)])
+@pytest.mark.parametrize("layout", [CANONICAL, STREAMED])
+def test_lookup(T, K, N, G, layout):
+    if layout == STREAMED and K % 128 != 0:
+        pytest.skip("the streaming layout needs K % 128 == 0")
+    g = gen(T + K)
+    codes, s, z = weights(g, N, K, G)
+    ids = torch.randint(0, N, (T,), generator=g, dtype=I32, device=DEV)
+    if T > 2:
+        ids[1], ids[2] = -1, N
+    y = strided(torch.ones(T, K, dtype=BF16, device=DEV), 8)
+    B.basq_w4a16_lookup(ids, laid_out(codes, layout), s, z, y, math.sqrt(K), w_layout=layout)
+    want = ref.lookup(ids, codes, s, z, math.sqrt(K))
+    check_stored(y, want, want.abs() * 2.0 ** -22)                # three roundings in fp32
+    assert T == 1 or (y._base[:, K:] == 7).all()
+
+
+def test_rows_behind_2_to_the_31_bytes():
+    """A lookup and a product whose weights lie beyond 32-bit offsets."""
+    K, N, G = 8192, 540000, 8192
+    codes = torch.zeros((N, K // 2), dtype=torch.uint8, device=DEV)
+    codes[-1] = 0x21
+    s, z = torch.ones((N, 1), dtype=BF16, device=DEV), torch.zeros((N, 1), dtype=BF16, device=DEV)
+    y = torch.empty((1, K), dtype=BF16, device=DEV)
+    B.basq_w4a16_lookup(torch.tensor([N - 1], dtype=I32, device=DEV), codes, s, z, y)
+    assert torch.equal(y[0, :4].cpu(), torch.tensor([1, 2, 1, 2], dtype=BF16))
+    x, out = torch.ones((1, K), dtype=BF16, device=DEV), torch.empty((1, N), device=DEV)
+    B.basq_w4a16_gemm(x, codes, s, z, out)
+    assert out[0, -1] == 1.5 * K and out[0, :-1].abs().max() == 0
+
+
+# ---- draw ------------------------------------------------------------------------------------------
+
+def draw(logits, u, **choices):
+    """(token, logprob, kept), from a workspace of just the bytes that are asked for"""
+    Bn, V = logits.shape
+    token, kept, logprob = torch.full((Bn,), 77, dtype=I32, device=DEV), torch.full((Bn,), 77, dtype=I32, device=DEV), torch.full((Bn,), 77.0, device=DEV)
+    need = B.basq_sample_workspace_bytes(Bn, V)
+    work = torch.full((need,), 0xA5, dtype=torch.uint8, device=DEV) if need else None
+    as_tensor = lambda v, t: None if v is None else torch.tensor(v, dtype=t, device=DEV)  # noqa: E731
+    B.basq_sample(logits, torch.tensor(u, dtype=torch.float64, device=DEV), token, work,
+                  temperature=as_tensor(choices.get("temperature"), torch.float32), top_k=as_tensor(choices.get("top_k"), I32),
+                  top_p=as_tensor(choices.get("top_p"), torch.float32), min_p=as_tensor(choices.get("min_p"), torch.float32), logprob=logprob, kept=kept)
+    return token.tolist(), logprob.tolist(), kept.tolist()
+
+
+def check_draw(logits, u, **choices):
+    tokens, logprobs, kept = draw(logits, u, **choices)
+    rows = logits.cpu().double().numpy()
+    for b in range(len(u)):
+        mine = {k: (float(np.float32(v[b])) if k != "top_k" else v[b]) for k, v in choices.items()}
+        token, logprob, n = ref.sample_row(rows[b], u=u[b], **mine)
+        assert (tokens[b], kept[b]) == (token, n), (b, mine, u[b], (tokens[b], token), (kept[b], n))
+        # one rounding to fp32, and the weights' steps of 2^-42 in the sum
+        assert logprobs[b] == logprob or abs(logprobs[b] - logprob) <= abs(logprob) * 2.0 ** -24 + 2.0 ** -30, (b, logprobs[b], logprob)
+
+
+def bell(g, rows, V, dtype, sd=2.2):
+    z = sd * torch.randn((rows, V), generator=g, device=DEV)
+    up = torch.randint(0, V, (rows, max(1, min(32, V // 8))), generator=g, device=DEV)
+    z.scatter_add_(1, up, 8 * torch.rand(up.shape, generator=g, device=DEV))
+    z[:, V // 3:V // 3 + V // 50] = -math.inf
+    return z.to(dtype)
+
+
+ROWS = 12
+CHOICES = {
+    "free": dict(), "warm": dict(temperature=[1.7] * ROWS), "top_k": dict(top_k=[1, 2, 3, 10, 40, 200, 1000, 5000, 1 << 30, 0, -1, 7]),
+    "top_p": dict(top_p=[0.01, 0.1, 0.3, 0.5, 0.7, 0.8, 0.9, 0.95, 0.99, 0.9999, 1.0, 0.0], temperature=[0.8] * ROWS),
+    "min_p": dict(min_p=[0.5, 0.1, 0.05, 0.01, 1e-3, 1e-5, 1e-9, 1.0, 2.0, 0.0, -1.0, 0.2], temperature=[1.3] * ROWS),
+    "greedy": dict(temperature=[0.0, -1.0, math.nan] * 4),
+    "mixed": dict(temperature=[0.0, 0.7, 1.0, 1.3] * 3, top_k=[0, 50, 0, 3, 1000, 0, 20, 0, 7, 100, 0, 2], top_p=[1.0, 0.9, 0.5, 0.99] * 3,
+                  min_p=[0.0, 0.0, 0.02, 0.0, 0.1, 0.3] * 2),
+}
+
+
+@pytest.mark.parametrize("choices", CHOICES)
+@pytest.mark.parametrize("V", [1, 2, 63, 64, 65, 1000, 4099, 32000, 32771, 50257, 128000, 200003])
+@pytest.mark.parametrize("dtype", [torch.float32, BF16])
+def test_draw(choices, V, dtype):
+    g = gen(V)
+    logits = strided(bell(g, ROWS, V, dtype), 3)
+    rng = random.Random(V)
+    u = [rng.random() for _ in range(ROWS)]
+    u[0], u[1] = 0.0, 1.0 - 2.0 ** -53
+    check_draw(logits, u, **CHOICES[choices])
+
+
+@pytest.mark.parametrize("rows", [1, 2, 3, 8, 33, 130, 300])
+@pytest.mark.parametrize("V", [777, 40000, 70001])
+def test_draw_of_batches(rows, V):
+    g = gen(rows)
+    rng = random.Random(rows)
+    check_draw(bell(g, rows, V, torch.float32), [rng.random() for _ in range(rows)], temperature=[rng.choice([0.0, 0.6, 1.0]) for _ in range(rows)],
+               top_k=[rng.choice([0, 0, 5, 50]) for _ in range(rows)], top_p=[rng.choice([1.0, 0.9, 0.5]) for _ in range(rows)],
+               min_p=[rng.choice([0.0, 0.0, 0.05]) for _ in range(rows)])
+
+
+@pytest.mark.parametrize("V", [5, 1000, 40000, 130000])
+@pytest.mark.parametrize("dtype", [torch.float32, BF16])
+def test_rows_out_of_the_ordinary(V, dtype):
+    """Equal logits, two values, no token, one token, infinities, NaN, both zeros, tiny and huge logits, a slope."""
+    g = gen(V)
+    n = lambda: torch.randn(V, generator=g, device=DEV)  # noqa: E731
+    equal, two, none, one, up, nan, zeros, tiny, huge, slope, near, all_up = (torch.full((V,), 1.25, device=DEV) for _ in range(12))
+    two[V // 2:] = 2.0
+    none[:], one[:] = -math.inf, -math.inf
+    one[V - 1] = -3.0
+    up[V // 3], up[V // 2] = math.inf, math.inf
+    nan[:] = n()
+    nan[::2] = math.nan
+    zeros[:] = 0.0
+    zeros[::2] = -0.0
+    tiny[:] = n() * 1e-39
+    huge[:] = n() * 1e30
+    slope[:] = torch.arange(V, device=DEV) * (20.0 / V)
+    near[:] = 5 + 1e-4 * n()
+    all_up[:] = math.inf
+    logits = torch.stack([equal, two, none, one, up, nan, zeros, tiny, huge, slope, near, all_up]).to(dtype)
+    for u in (0.0, 0.37, 0.9999):
+        check_draw(logits, [u] * ROWS)
+        check_draw(logits, [u] * ROWS, top_p=[0.6] * ROWS, temperature=[0.9] * ROWS)
+        check_draw(logits, [u] * ROWS, top_k=[3] * ROWS)
+        check_draw(logits, [u] * ROWS, min_p=[0.3] * ROWS, top_k=[V // 2 + 1] * ROWS, top_p=[0.9] * ROWS)
+
+
+def test_all_tokens_forbidden_but_nan():
+    logits = torch.full((3, 500), math.nan, device=DEV)
+    logits[1, 7] = -1e30
+    assert draw(logits, [0.5] * 3) == ([-1, 7, -1], [-math.inf, 0.0, -math.inf], [0, 1, 0])
+
+
+def test_numbers_outside_the_unit():
+    logits = torch.tensor([[3.0, 1.0, 2.0, 0.0]] * 6, device=DEV)
+    tokens, _, _ = draw(logits, [-1.0, math.nan, 0.0, 1.0, 5.0, math.inf])
+    assert tokens == [0, 0, 0, 3, 3, 3]
+
+
+def test_frequencies():
+    """65536 evenly spaced numbers: each token as often as its share says, within one at either end."""
+    n = 65536
+    row = torch.tensor([0.3, -1.0, 2.0, -math.inf, 1.0, 0.3], device=DEV)
+    tokens = torch.tensor(draw(row.expand(n, -1), [(i + 0.5) / n for i in range(n)])[0])
+    share = torch.softmax(row.double().cpu(), 0) * n
+    assert ((torch.bincount(tokens, minlength=6) - share).abs() <= 1.0).all()
+
+
+def test_cuts_where_masses_are_equal():
+    """Four equal logits and p of a half: exactly two are kept; p just above it: three."""
+    logits = torch.full((3, 4), 0.7, device=DEV)
+    tokens, _, kept = draw(logits, [0.5, 0.0, 0.5], top_p=[0.5, 0.25, 0.5000001])
+    assert kept == [2, 1, 3] and tokens == [1, 0, 1]
+
+
+# ---- books -----------------------------------------------------------------------------------------
+
+def make_books(rng, rows, columns, P, spare, longest):
+    lengths = [rng.randint(0, min(longest, columns * P)) for _ in range(rows)]
+    used = sum(-(-n // P) for n in lengths)
+    pages = list(range(used + spare))
+    rng.shuffle(pages)
+    table = [[rng.randint(-5, 1 << 20) for _ in range(columns)] for _ in range(rows)]       # (entries past a length may hold anything)
+    for r, n in enumerate(lengths):
+        for c in range(-(-n // P)):
+            table[r][c] = pages.pop()
+    return {"lengths": lengths, "table": table, "free": pages, "columns": columns, "capacity": used + spare}
+
+
+def on_gpu(books):
+    t = lambda v: torch.tensor(v, dtype=I32, device=DEV)  # noqa: E731
+    free = torch.full((books["capacity"],), -9, dtype=I32, device=DEV)
+    free[:len(books["free"])] = t(books["free"])
+    return dict(lengths=t(books["lengths"]), pool_table=strided(t(books["table"]), 2, -3), free_pages=free, free_count=t([len(books["free"])]))
+
+
+def copy_of(books):
+    return {"lengths": list(books["lengths"]), "table": [list(r) for r in books["table"]], "free": list(books["free"]),
+            "columns": books["columns"], "capacity": books["capacity"]}
+
+
+def check_extend(books, gpu, seqs, new, P, q_len, T, in_place=True):
+    """One call on the GPU's books and one on the lists, which are updated where it is in place."""
+    Bn, columns = len(seqs), books["columns"]
+    t = lambda v: torch.tensor(v, dtype=I32, device=DEV)  # noqa: E731
+    positions, slots, status = torch.full((T,), 55, dtype=I32, device=DEV), torch.full((T,), 55, dtype=I32, device=DEV), t([9, 9])
+    starts = torch.full((Bn + 1,), 55, dtype=I32, device=DEV) if not q_len else None
+    batch, lengths = strided(torch.full((Bn, columns), -7, dtype=I32, device=DEV), 1, -3), torch.full((Bn,), 55, dtype=I32, device=DEV)
+    work = torch.full((B.basq_kv_books_bytes(Bn),), 0xA5, dtype=torch.uint8, device=DEV)
+    lists = books if in_place else copy_of(books)
+    before = copy_of(lists)
+    if not in_place:                                             # (the table and the free pages are, in any case)
+        gpu = dict(gpu, pool_table=gpu["pool_table"]._base.clone()[:, :columns], free_pages=gpu["free_pages"].clone())
+    out = {} if in_place else dict(lengths_out=gpu["lengths"].clone(), free_out=t([0]))
+    B.basq_kv_extend(**gpu, new_tokens=t(new), page_size=P, positions=positions, slots=slots, status=status, books=work, seqs=t(seqs), q_len=q_len,
+                     starts=starts, batch_table=batch, batch_lengths=lengths, **out)
+    want = ref.extend(lists, list(seqs), list(new), P, q_len, T)
+    assert status.tolist() == want["status"]
+    assert positions.tolist() == want["positions"] and slots.tolist() == want["slots"] and lengths.tolist() == want["lengths"]
+    if starts is not None:
+        assert starts.tolist() == want["starts"]
+    for b in range(Bn):
+        pages = want["batch"][b] if want["batch"] is not None else []
+        assert batch[b].tolist() == pages + [-7] * (columns - len(pages))
+    assert (batch._base[:, columns:] == -3).all() and (gpu["pool_table"]._base[:, columns:] == -3).all()
+    assert gpu["pool_table"].tolist() == lists["table"]
+    assert out.get("lengths_out", gpu["lengths"]).tolist() == lists["lengths"]
+    count = out.get("free_out", gpu["free_count"]).item()
+    assert gpu["free_pages"][:count].tolist() == lists["free"]
+    if want["status"] != [0, 0]:
+        assert lists == before and gpu["free_pages"][count:].eq(-9).sum() >= 0
+    return want
+
+
+@pytest.mark.parametrize("Bn,P,longest,new,packed", [
+    (1, 16, 40, 1, False), (1, 64, 100, 5, True), (3, 16, 33, 4, False), (7, 32, 200, 90, True), (64, 64, 500, 1, False), (64, 16, 100, 8, False),
+    (129, 128, 300, 3, False), (40, 16, 64, 700, True), (200, 1024, 3000, 60, True), (512, 16, 50, 2, False), (1024, 16, 40, 3, True), (1, 16, 0, 9000, True),
+])
+def test_books(Bn, P, longest, new, packed):
+    rng = random.Random(Bn * 31 + new)
+    rows = Bn + rng.randint(0, 5)
+    columns = -(-(longest + 4 * new) // P) + 1
+    books = make_books(rng, rows, columns, P, Bn * (-(-4 * new // P) + 1), longest)
+    gpu = on_gpu(books)
+    for step in range(4):
+        seqs = rng.sample(range(rows), Bn)
+        counts = [rng.choice([new, rng.randint(0, new), 0, -rng.randint(0, books["lengths"][s])]) for s in seqs]
+        T = sum(max(c, 0) for c in counts) + rng.choice([0, 1, 300]) if packed else Bn * new
+        want = check_extend(books, gpu, seqs, counts, P, 0 if packed else new, T, in_place=step != 1)
+        assert want["status"] == [0, 0]
+
+
+def test_without_the_optional():
+    books = make_books(random.Random(5), 4, 6, 16, 8, 30)
+    gpu = on_gpu(books)
+    positions, slots, status = (torch.zeros(n, dtype=I32, device=DEV) for n in (6, 6, 2))
+    work = torch.empty(256, dtype=torch.uint8, device=DEV)
+    seqs = torch.tensor([2, 0, 3], dtype=I32, device=DEV)
+    B.basq_kv_extend(**gpu, new_tokens=None, page_size=16, positions=positions, slots=slots, status=status, books=work, seqs=seqs, q_len=2)
+    want = ref.extend(books, [2, 0, 3], [2, 2, 2], 16, 2, 6)
+    assert positions.tolist() == want["positions"] and slots.tolist() == want["slots"]
+    B.basq_kv_extend(**gpu, new_tokens=torch.ones(3, dtype=I32, device=DEV), page_size=16, positions=positions[:3], slots=slots[:3], status=status, books=work)
+    want = ref.extend(books, [0, 1, 2], [1, 1, 1], 16, 1, 3)
+    assert positions[:3].tolist() == want["positions"] and gpu["lengths"].tolist() == books["lengths"]
+
+
+@pytest.mark.parametrize("q_len,T", [(4, 12), (0, 12), (0, 5000)])
+@pytest.mark.parametrize("fault", ["row", "negative row", "twice", "longer than a row", "shorter than nothing", "pages", "count", "room", "tokens", "length"])
+def test_refused_books_stay_as_they_were(fault, q_len, T):
+    rng = random.Random(8)
+    books = make_books(rng, 5, 8, 16, 3, 60)
+    books["lengths"][1], books["lengths"][4] = 40, 17
+    seqs, new = [1, 4, 2], [2, 1, 3]
+    if fault == "row":
+        seqs[1] = 5
+    elif fault == "negative row":
+        seqs[2] = -1
+    elif fault == "twice":
+        seqs[2] = 1
+    elif fault == "longer than a row":
+        books["lengths"][4] = 128
+    elif fault == "shorter than nothing":
+        new[1] = -18
+    elif fault == "pages":
+        books["free"] = []
+        books["lengths"][1] = 32
+    elif fault == "length":
+        books["lengths"][4] = -2
+    elif fault == "tokens":
+        new = [4, 5, 4]
+        if T > 13:
+            pytest.skip("they fit")
+    gpu = on_gpu(books)
+    if fault == "count":
+        gpu["free_count"].fill_(books["capacity"] + 1)
+    elif fault == "room":
+        new[0] = -30
+        gpu["free_count"].fill_(books["capacity"])
+        books["free"] = gpu["free_pages"].tolist()
+    want_status = {"row": [1, 1], "negative row": [1, 2], "twice": [1, 2], "longer than a row": [2, 1], "shorter than nothing": [2, 1], "length": [2, 1],
+                   "count": [3, books["capacity"] + 1], "room": [3, books["capacity"]]}.get(fault)
+    if fault == "tokens" and q_len:
+        want_status = [2, 1]
+    if fault == "count":
+        books["free"] = gpu["free_pages"].tolist() + [-9]
+        saved = {k: v.clone() for k, v in gpu.items()}
+        Bn = 3
+        out = [torch.full((n,), 5, dtype=I32, device=DEV) for n in (T, T, 2)]
+        B.basq_kv_extend(**gpu, new_tokens=torch.tensor(new, dtype=I32, device=DEV), page_size=16, positions=out[0], slots=out[1], status=out[2],
+                         books=torch.empty(B.basq_kv_books_bytes(Bn), dtype=torch.uint8, device=DEV), seqs=torch.tensor(seqs, dtype=I32, device=DEV), q_len=q_len)
+        assert out[2].tolist() == want_status and (out[0] == -1).all() and (out[1] == -1).all()
+        assert all(torch.equal(gpu[k], saved[k]) for k in gpu)
+        return
+    want = check_extend(books, gpu, seqs, new, 16, q_len, T)
+    assert want["status"][0] != 0 and (want_status is None or want["status"] == want_status)
+
+
+def test_no_sequences():
+    books = make_books(random.Random(1), 2, 4, 16, 3, 20)
+    gpu = on_gpu(books)
+    starts, status = torch.full((1,), 5, dtype=I32, device=DEV), torch.full((2,), 5, dtype=I32, device=DEV)
+    places = torch.full((2, 7), 5, dtype=I32, device=DEV)
+    empty = torch.empty(0, dtype=I32, device=DEV)
+    B.basq_kv_extend(**gpu, new_tokens=empty, page_size=16, positions=places[0], slots=places[1], status=status,
+                     books=torch.empty(64, dtype=torch.uint8, device=DEV), q_len=0, starts=starts)
+    assert (places == -1).all() and starts.tolist() == [0] and status.tolist() == [0, 0] and gpu["free_count"].item() == len(books["free"])
+
+
+# ---- streams and graphs ----------------------------------------------------------------------------
+
+class Step:
+    """A step's ends on state of their own: places, embeddings, logits and tokens; the tokens are the next step's."""
+
+    def __init__(self, seed, Bn=6, K=256, V=1200, P=16, columns=6):
+        g = gen(seed)
+        self.P, self.V = P, V
+        self.lists = make_books(random.Random(seed), Bn + 2, columns, P, 40, 50)
+        self.gpu = on_gpu(self.lists)
+        self.codes, self.scale, self.zero = weights(g, V, K, 64)
+        self.Wq = laid_out(self.codes, STREAMED)
+        ints = lambda *n: torch.zeros(n, dtype=I32, device=DEV)  # noqa: E731
+        self.seqs = torch.tensor(random.Random(seed).sample(range(Bn + 2), Bn), dtype=I32, device=DEV)
+        self.positions, self.slots, self.status, self.lengths, self.table = ints(Bn), ints(Bn), ints(2), ints(Bn), ints(Bn, columns)
+        self.token, self.kept, self.logprob = torch.randint(0, V, (Bn,), generator=g, dtype=I32, device=DEV), ints(Bn), torch.zeros(Bn, device=DEV)
+        self.x, self.y = torch.empty((Bn, K), dtype=BF16, device=DEV), torch.empty((Bn, V), device=DEV)
+        self.u = torch.rand(Bn, generator=g, dtype=torch.float64, device=DEV)
+        self.heat, self.top_p = torch.tensor([0.0, 1.0, 0.7] * 2, device=DEV)[:Bn], torch.full((Bn,), 0.9, device=DEV)
+        self.books = torch.empty(B.basq_kv_books_bytes(Bn), dtype=torch.uint8, device=DEV)
+        need = B.basq_sample_workspace_bytes(Bn, V)
+        self.work = torch.empty(need, dtype=torch.uint8, device=DEV) if need else None
+
+    def __call__(self, stream=None):
+        B.basq_kv_extend(**self.gpu, new_tokens=None, page_size=self.P, positions=self.positions, slots=self.slots, status=self.status, books=self.books,
+                         seqs=self.seqs, batch_table=self.table, batch_lengths=self.lengths, stream=stream)
+        B.basq_w4a16_lookup(self.token, self.Wq, self.scale, self.zero, self.x, 16.0, w_layout=STREAMED, stream=stream)
+        B.basq_w4a16_gemm(self.x, self.Wq, self.scale, self.zero, self.y, w_layout=STREAMED, stream=stream)
+        B.basq_sample(self.y, self.u, self.token, self.work, temperature=self.heat, top_p=self.top_p, logprob=self.logprob, kept=self.kept, stream=stream)
+
+    def check(self, before):
+        """What one step made of the tokens `before` it, the books on the lists with it."""
+        seqs = self.seqs.tolist()
+        want = ref.extend(self.lists, seqs, [1] * len(seqs), self.P, 1, len(seqs))
+        assert self.status.tolist() == want["status"] == [0, 0]
+        assert self.positions.tolist() == want["positions"] and self.slots.tolist() == want["slots"]
+        assert self.gpu["lengths"].tolist() == self.lists["lengths"] and self.gpu["free_count"].item() == len(self.lists["free"])
+        x = ref.lookup(before, self.codes, self.scale, self.zero, 16.0)
+        check_stored(self.x, x, x.abs() * 2.0 ** -22)
+        y, made_of = ref.product(self.x, self.codes, self.scale, self.zero)
+        check_stored(self.y, y, made_of * 2.0 ** -20)
+        rows, u, heat = self.y.cpu().double().numpy(), self.u.tolist(), self.heat.tolist()
+        for b, (token, kept) in enumerate(zip(self.token.tolist(), self.kept.tolist())):
+            got = ref.sample_row(rows[b], temperature=heat[b], top_p=float(np.float32(0.9)), u=u[b])
+            assert (token, kept) == (got[0], got[2])
+
+
+def test_a_step_again_and_again():
+    step = Step(1)
+    for _ in range(20):
+        before = step.token.clone()
+        step()
+        step.check(before)
+        step.u.uniform_()
+
+
+def test_two_captured_steps():
+    """Two graphs of steps with state of their own, and eager steps, in turn."""
+    one, two, eager = Step(2), Step(3), Step(4)
+    for s in (one, two, eager):
+        before = s.token.clone()
+        s()
+        s.check(before)
+    graphs = []
+    for s in (one, two):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            s()
+        graphs.append(graph)
+    for i in range(6):
+        for s, graph in ((one, graphs[0]), (two, graphs[1]), (eager, None)):
+            before = s.token.clone()
+            if graph is None:
+                s()
+            else:
+                graph.replay()
+            if i % 2:
+                torch.cuda.synchronize()
+            s.check(before)
+            s.u.uniform_()
+
+
+def test_on_another_stream():
+    step = Step(5)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    before = step.token.clone()
+    torch.cuda.synchronize()
+    step(stream)
+    stream.synchronize()
+    step.check(before)
