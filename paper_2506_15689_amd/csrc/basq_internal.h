@@ -220,6 +220,12 @@ struct LookupArgs {
 };
 int launch_lookup_w4a16(LookupArgs a, hipStream_t s);             // lookup_w4a16.hip
 
+constexpr int SAMPLE_CELLS = 1024, SAMPLE_FEW = 1024;
+struct SampleSlice {          // what one launch leaves the next of a slice of a row
+    uint64_t best;            // (key, ~index) of its largest logit
+    uint64_t mass[SAMPLE_CELLS];
+    int32_t count[SAMPLE_CELLS];
+};
 struct SampleArgs {
     const void* logits;       // [B, ldl], fp32 or bf16
     int64_t ldl;
@@ -232,9 +238,11 @@ struct SampleArgs {
     float* logprob;           // optional, [B]
     int32_t* kept;            // optional, [B]
     uint8_t* workspace;
-    int32_t bits;             // set by the launcher: a weight of 1 is 2^bits
+    int32_t bits;             // these three are set by the launcher: a weight of 1 is 2^bits
+    SampleSlice* slices;
+    int32_t slices_of_row;
 };
-constexpr int32_t SAMPLE_MAX_TOKENS = 1 << 22;
+constexpr int32_t SAMPLE_MAX_TOKENS = 1 << 22, SAMPLE_LONG = 1 << 20;
 size_t sample_workspace_bytes(int32_t B, int32_t V);
 int launch_sample(SampleArgs a, hipStream_t s);                   // sample.hip
 

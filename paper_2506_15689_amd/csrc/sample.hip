@@ -29,18 +29,17 @@ __device__ __forceinline__ float logit_of(unsigned key) {
     return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
 }
 
-// The weights of a row: 2^bits e^((z - top) / T) = 2^(bits + n + r), n whole and |r| <= 1/2.
+// The weights of a row: e^((z - top) / T) = 2^(n + r), n whole and |r| <= 1/2.
 struct Weights {
-    double top, per;                                      // per = log2(e) / T
-    unsigned top_key;
+    float top;
+    double per;                                           // log2(e) / T
     int bits;
-    // 2^r by its series, ln(2)^k / k!, the first term left out under 2^-47
-    __device__ __forceinline__ double scaled(unsigned key, int lift) const {
-        if (key == top_key) return ldexp(1.0, lift);
-        constexpr double magic = 6755399441055744.0;      // 1.5 * 2^52: adding it rounds to whole numbers
-        double y = ((double)logit_of(key) - top) * per;
-        y = fmax(y, -1020.0);                             // (-inf too, and NaN of two infinities)
-        const double n = (y + magic) - magic, r = y - n;
+    // 2^(lift + n + r); 2^r by its series, ln(2)^k / k!, the first term left out under 2^-47.  (lift: from 0 to 51)
+    __device__ __forceinline__ double scaled(float z, int lift) const {
+        constexpr double magic = 6755399441055744.0;      // 1.5 * 2^52: adding it rounds to whole numbers, which are the low bits
+        double y = ((double)z - (double)top) * per;
+        y = z == top ? 0.0 : fmax(y, -1000.0);            // (-inf and NaN, of infinities, become -1000: less than any step)
+        const double t = y + magic, r = y - (t - magic);
         double s = 4.44553827187081e-10;
         s = fma(s, r, 7.054911620801121e-09);
         s = fma(s, r, 1.0178086009239696e-07);
@@ -53,9 +52,10 @@ struct Weights {
         s = fma(s, r, 2.402265069591007e-01);
         s = fma(s, r, 6.931471805599453e-01);
         s = fma(s, r, 1.0);
-        return ldexp(s, (int)n + lift);
+        return __hiloint2double(__double2hiint(s) + (__double2loint(t) + lift) * (1 << 20), __double2loint(s));
     }
-    __device__ __forceinline__ uint64_t mass(unsigned key) const { return (uint64_t)__builtin_rint(scaled(key, bits)); }
+    // in steps of 2^-bits: adding 2^52 rounds, and the sum's low 52 bits are the number
+    __device__ __forceinline__ uint64_t mass(float z) const { return (uint64_t)__double_as_longlong(scaled(z, bits) + 4503599627370496.0) - 0x4330000000000000ull; }
 };
 
 // f(index, logit) for every token of the row, by the workgroup
@@ -114,7 +114,7 @@ __device__ void fill(Histogram& h, const void* row, int V, const Weights& w, int
         if (key <= LOWEST || (above < 32 && key >> above != prefix >> above)) return;
         const unsigned digit = key >> shift & (DIGITS - 1);
         atomicAdd(&h.count[digit], 1);
-        atomicAdd(&h.mass[digit], (unsigned long long)w.mass(key));
+        atomicAdd(&h.mass[digit], (unsigned long long)w.mass(z));
     });
     __syncthreads();
 }
@@ -162,7 +162,7 @@ __device__ Place find(Shared& s, const void* row, int V, const Weights& w, Goal 
     p.count = (int)count;
     p.mass = mass;
     p.equal = s.next.count[digit];
-    p.each = w.mass(p.key);
+    p.each = w.mass(logit_of(p.key));
     __syncthreads();
     if (goal == BY_KEY) p.nth = p.equal;
     else if (goal == BY_COUNT) p.nth = (int)(target - count);
@@ -170,87 +170,93 @@ __device__ Place find(Shared& s, const void* row, int V, const Weights& w, Goal 
     return p;
 }
 
-template <bool F32>
-__global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
-    __shared__ Shared s;
-    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = a.V;
-    const void* row = F32 ? (const void*)(static_cast<const float*>(a.logits) + b * a.ldl) : (const void*)(static_cast<const uint16_t*>(a.logits) + b * a.ldl);
-    // the likeliest token: the highest key, of equal ones the lowest index
-    uint64_t best = 0;
-    for_each<F32>(row, V, [&](int i, float z) {
-        const uint64_t v = (uint64_t)key_of(z) << 32 | (unsigned)~i;
-        best = v > best ? v : best;
-    });
-    if (tid == 0) s.top = 0;
-    __syncthreads();
-    atomicMax((unsigned long long*)&s.top, (unsigned long long)best);
-    __syncthreads();
-    best = s.top;
-    const float T = a.temperature ? a.temperature[b] : 1.0f;
-    const unsigned top_key = (unsigned)(best >> 32);
-    if (top_key <= LOWEST || !(T > 0.0f)) {                // no token at all, or the likeliest
-        if (tid == 0) {
-            const bool none = top_key <= LOWEST;
-            a.token[b] = none ? -1 : (int)~(unsigned)best;
-            if (a.logprob) a.logprob[b] = none ? -__builtin_inff() : 0.0f;
-            if (a.kept) a.kept[b] = none ? 0 : 1;
-        }
-        return;
+// what a request chose
+struct Choices {
+    float heat, p, least;
+    int k;
+    __device__ __forceinline__ Choices(const SampleArgs& a, int b) {
+        heat = a.temperature ? a.temperature[b] : 1.0f;
+        k = a.top_k ? a.top_k[b] : 0;
+        p = a.top_p ? a.top_p[b] : 1.0f;
+        least = a.min_p ? a.min_p[b] : 0.0f;
     }
+    __device__ __forceinline__ bool greedy() const { return !(heat > 0.0f); }
+    __device__ __forceinline__ double enough() const { return least < 1.0f ? (double)least : 1.0; }
+};
+// the running mass that top-p cuts at, of a mass that there is
+__device__ __forceinline__ uint64_t cut_target(float p, uint64_t mass) {
+    const double t = __builtin_ceil((double)p * (double)mass);
+    const uint64_t target = t >= 1.0 ? (uint64_t)t : 1;
+    return target < mass ? target : mass;
+}
+// the running mass that the draw reaches: the first beyond u * mass
+__device__ __forceinline__ uint64_t draw_target(double u, uint64_t mass) {
+    const double t = u > 0.0 ? u * (double)mass : 0.0;
+    const uint64_t target = t < 9.0e18 ? (uint64_t)t + 1 : mass;
+    return target < mass ? target : mass;
+}
+__device__ __forceinline__ void put(const SampleArgs& a, int b, int token, float logprob, int kept) {
+    a.token[b] = token;
+    if (a.logprob) a.logprob[b] = logprob;
+    if (a.kept) a.kept[b] = kept;
+}
+// ln of a token's share of the kept mass
+__device__ __forceinline__ float share(const Weights& w, float heat, float z, uint64_t mass) {
+    const double d = z == w.top ? 0.0 : ((double)z - (double)w.top) / (double)heat;
+    return (float)(d - log((double)mass * __hiloint2double((1023 - w.bits) << 20, 0)));
+}
+__device__ __forceinline__ const void* row_of(const SampleArgs& a, int b) {
+    return static_cast<const uint8_t*>(a.logits) + (int64_t)b * a.ldl * (a.f32 ? 4 : 2);
+}
+
+// A row by digits, whatever its logits are.  best: its likeliest token, (key, ~index).
+template <bool F32>
+__device__ void by_digits(const SampleArgs& a, int b, uint64_t best, Shared& s) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = a.V;
+    const void* row = row_of(a, b);
+    const Choices c(a, b);
+    const unsigned top_key = (unsigned)(best >> 32);
     Weights w;
-    w.top = (double)logit_of(top_key);
-    w.per = 1.4426950408889634 / (double)T;
-    w.top_key = top_key;
+    w.top = logit_of(top_key);
+    w.per = 1.4426950408889634 / (double)c.heat;
     w.bits = a.bits;
     fill<F32>(s.first, row, V, w, 0, 0);
-    uint64_t all_count = 0, all_mass = 0;
+    uint64_t kept = 0, mass = 0;
     {
-        uint64_t c = 0, m = 0;
-        for (int i = tid; i < DIGITS; i += THREADS) { c += s.first.count[i]; m += s.first.mass[i]; }
-        c = wave_scan(c, lane); m = wave_scan(m, lane);
-        if (lane == 63) { s.wave_counts[wave] = c; s.wave_masses[wave] = m; }
+        uint64_t n = 0, m = 0;
+        for (int i = tid; i < DIGITS; i += THREADS) { n += s.first.count[i]; m += s.first.mass[i]; }
+        n = wave_scan(n, lane); m = wave_scan(m, lane);
+        if (lane == 63) { s.wave_counts[wave] = n; s.wave_masses[wave] = m; }
         __syncthreads();
-        for (int i = 0; i < WAVES; ++i) { all_count += s.wave_counts[i]; all_mass += s.wave_masses[i]; }
+        for (int i = 0; i < WAVES; ++i) { kept += s.wave_counts[i]; mass += s.wave_masses[i]; }
         __syncthreads();
     }
-    uint64_t kept = all_count, mass = all_mass;
-    const int k = a.top_k ? a.top_k[b] : 0;
-    const float p = a.top_p ? a.top_p[b] : 1.0f, least = a.min_p ? a.min_p[b] : 0.0f;
-    if (k > 0 && (uint64_t)k < kept) {
-        const Place at = find<F32>(s, row, V, w, BY_COUNT, (uint64_t)k);
+    if (c.k > 0 && (uint64_t)c.k < kept) {
+        const Place at = find<F32>(s, row, V, w, BY_COUNT, (uint64_t)c.k);
         kept = at.tokens();
         mass = at.total();
     }
-    if (p < 1.0f) {
-        const double t = __builtin_ceil((double)p * (double)mass);
-        uint64_t target = t >= 1.0 ? (uint64_t)t : 1;
-        target = target < mass ? target : mass;
-        const Place at = find<F32>(s, row, V, w, BY_MASS, target);
+    if (c.p < 1.0f) {
+        const Place at = find<F32>(s, row, V, w, BY_MASS, cut_target(c.p, mass));
         if ((uint64_t)at.tokens() < kept) { kept = at.tokens(); mass = at.total(); }
     }
-    if (least > 0.0f) {
+    if (c.least > 0.0f) {
         // the lowest key whose weight is enough, by bisection: weights rise with keys
-        const double enough = least < 1.0f ? (double)least : 1.0;
         unsigned lo = LOWEST, hi = top_key;                // (hi is enough; lo is not, or is no token)
         while (hi - lo > 1) {
             const unsigned mid = lo + (hi - lo) / 2;
-            if (w.scaled(mid, 0) >= enough) hi = mid; else lo = mid;
+            if (w.scaled(logit_of(mid), 0) >= c.enough()) hi = mid; else lo = mid;
         }
         if (!F32) hi = hi & 0x80000000u ? (hi + 0xFFFFu) & 0xFFFF0000u : hi | 0xFFFFu;          // (the next bf16 number)
         const Place at = find<F32>(s, row, V, w, BY_KEY, 0, hi);
         if ((uint64_t)at.tokens() < kept) { kept = at.tokens(); mass = at.total(); }
     }
-    const double u = a.u[b];
-    const double t = u > 0.0 ? u * (double)mass : 0.0;
-    uint64_t target = t < 9.0e18 ? (uint64_t)t + 1 : mass;
-    target = target < mass ? target : mass;
-    const Place at = find<F32>(s, row, V, w, BY_MASS, target);
+    const Place at = find<F32>(s, row, V, w, BY_MASS, draw_target(a.u[b], mass));
     // the nth token with that key: the part of the row that holds it, then the token
     const int part = (V + DIGITS - 1) / DIGITS;
-    for (int i = tid; i < DIGITS; i += THREADS) s.next.count[i] = 0;
+    for (int i = tid; i < DIGITS; i += THREADS) { s.next.count[i] = 0; s.next.mass[i] = 0; }
     __syncthreads();
     for_each<F32>(row, V, [&](int i, float z) { if (key_of(z) == at.key) atomicAdd(&s.next.count[DIGITS - 1 - i / part], 1); });
-    for (int i = tid; i < DIGITS; i += THREADS) s.next.mass[i] = 0;
     __syncthreads();
     uint64_t before = 0, none = 0;
     const int in = DIGITS - 1 - descend(s, s.next, BY_COUNT, (uint64_t)at.nth, 0, before, none);
@@ -269,27 +275,578 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
             if (hit) token = i0 + __builtin_ctzll(hit);
             seen += __popcll(who);
         }
-        if (lane == 0) {
-            a.token[b] = token;
-            if (a.logprob) {
-                const double d = at.key == top_key ? 0.0 : (w.top - (double)logit_of(at.key)) / (double)T;
-                a.logprob[b] = (float)(-d - log(ldexp((double)mass, -w.bits)));
-            }
-            if (a.kept) a.kept[b] = (int)kept;
-        }
+        if (lane == 0) put(a, b, token, share(w, c.heat, logit_of(at.key), mass), (int)kept);
     }
 }
 
+template <bool F32>
+__global__ __launch_bounds__(THREADS) void sample_long_kernel(SampleArgs a) {
+    __shared__ Shared s;
+    const int b = blockIdx.x, tid = threadIdx.x;
+    uint64_t best = 0;
+    for_each<F32>(row_of(a, b), a.V, [&](int i, float z) {
+        const uint64_t v = (uint64_t)key_of(z) << 32 | (unsigned)~i;
+        best = v > best ? v : best;
+    });
+    if (tid == 0) s.top = 0;
+    __syncthreads();
+    atomicMax((unsigned long long*)&s.top, (unsigned long long)best);
+    __syncthreads();
+    best = s.top;
+    const bool none = (unsigned)(best >> 32) <= LOWEST;
+    if (none || Choices(a, b).greedy()) {
+        if (tid == 0) put(a, b, none ? -1 : (int)~(unsigned)best, none ? -__builtin_inff() : 0.0f, none ? 0 : 1);
+        return;
+    }
+    by_digits<F32>(a, b, best, s);
+}
+
+// ---- in two launches: slices of rows into cells, then a row's cells and what lies in few of them ------------------------------
+//
+// A logit's cell is its place on a grid of step 2^e, about T / 30 wide (T <= 1), so that 1023 cells cover all that has weight.  Cells
+// are counted from the highest logit's, the last holds whatever lies below; being a grid of its own, not of the row's maximum, it is the
+// same for all slices of a row before they know of each other.  The first launch reads the logits once: each slice stays in
+// registers while its maximum is found, then its histogram of counts and masses is.  The second joins a row's histograms
+// (masses are rescaled to the row's maximum), finds the cells in which the cuts and the draw may lie -- one or two each, mostly -- and
+// reads the row again for the tokens in them, some hundred, which are sorted and settle everything exactly.  Rows whose cells
+// hold more tokens than are sorted (nearly equal logits, or thousands of equal ones) go by digits.
+
+typedef unsigned v4u __attribute__((ext_vector_type(4)));
+
+// a piece of 16 bytes of a row: its logits
+template <bool F32>
+struct Piece {
+    static constexpr int N = F32 ? 4 : 8;
+    v4u v;
+    __device__ __forceinline__ float operator[](int e) const {
+        if constexpr (F32) return __uint_as_float(v[e]);
+        else return __uint_as_float(e & 1 ? v[e / 2] & 0xFFFF0000u : v[e / 2] << 16);
+    }
+};
+// A row in aligned pieces: element e of piece p is token N p + e - off; what is no token is -inf.
+template <bool F32>
+struct Pieces {
+    static constexpr int N = Piece<F32>::N;
+    const uint8_t* base;                                   // the first piece, aligned
+    int off, V, count;
+    __device__ __forceinline__ Pieces(const void* row, int tokens) : V(tokens) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(row);
+        off = (int)(at & 15) / (F32 ? 4 : 2);
+        base = reinterpret_cast<const uint8_t*>(at & ~(uintptr_t)15);
+        count = (V + off + N - 1) / N;
+    }
+    __device__ __forceinline__ int first(int p) const { return N * p - off; }
+    // (nothing outside the row is read)
+    __device__ __forceinline__ Piece<F32> load(int p) const {
+        Piece<F32> r;
+        if (first(p) >= 0 && first(p) + N <= V) {
+            r.v = *reinterpret_cast<const v4u*>(base + 16 * (int64_t)p);
+        } else {
+            constexpr unsigned none = F32 ? 0xFF800000u : 0xFF80FF80u;
+            r.v = v4u{none, none, none, none};
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const int i = first(p) + e;
+                if (p >= count || i < 0 || i >= V) continue;
+                if constexpr (F32) r.v[e] = reinterpret_cast<const unsigned*>(base)[N * p + e];
+                else r.v[e / 2] = (r.v[e / 2] & (e & 1 ? 0xFFFFu : 0xFFFF0000u)) | (unsigned)reinterpret_cast<const uint16_t*>(base)[N * p + e] << (e & 1 ? 16 : 0);
+            }
+        }
+        return r;
+    }
+};
+
+constexpr int CELLS = SAMPLE_CELLS, SORTED = 4096;
+// the grid of a temperature: cells to a unit
+__device__ __forceinline__ float cells_per_unit(float heat) {
+    // a step of 2^e >= 33 min(T, 1) / 1024, below twice that: 33 T under the maximum a weight is below 2^-47
+    const float least = 33.0f / CELLS * fminf(heat, 1.0f);
+    int e = (int)(__float_as_uint(least) >> 23) - 126;
+    e = e > -120 ? e : -120;
+    return __uint_as_float((unsigned)(127 - e) << 23);
+}
+__device__ __forceinline__ int cell_of(float z, float per_unit) { return (int)__builtin_floorf(z * per_unit); }       // (saturates)
+__device__ __forceinline__ int below(int top, int cell) {
+    const unsigned d = (unsigned)top - (unsigned)cell;
+    return d < CELLS - 1 ? (int)d : CELLS - 1;
+}
+// Few tokens are kept: they are weighed when they are known, and need no masses of cells.
+__device__ __forceinline__ bool few(const Choices& c) { return c.k > 0 && c.k <= SAMPLE_FEW; }
+
+template <class T>
+__device__ __forceinline__ T wave_max(T v) {
+#pragma unroll
+    for (int d = 32; d; d /= 2) {
+        const T o = __shfl_xor(v, d);
+        v = o > v ? o : v;
+    }
+    return v;
+}
+
+// R: pieces that a thread holds
+template <bool F32, int R>
+__global__ __launch_bounds__(THREADS) void sample_slice_kernel(SampleArgs a) {
+    __shared__ int count[CELLS];
+    __shared__ unsigned long long mass[CELLS];
+    __shared__ uint64_t tops[WAVES];
+    const int slice = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+    const Pieces<F32> row(row_of(a, b), a.V);
+    const Choices c(a, b);
+    const int p0 = slice * (THREADS * R);
+    Piece<F32> held[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) held[r] = row.load(p0 + r * THREADS + tid);
+    for (int i = tid; i < CELLS; i += THREADS) { count[i] = 0; mass[i] = 0; }
+    float top = -__builtin_inff();
+    int at = -1;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int e = 0; e < Piece<F32>::N; ++e) {
+            const float z = held[r][e];
+            if (z > top) { top = z; at = row.first(p0 + r * THREADS + tid) + e; }
+        }
+    uint64_t best = wave_max((uint64_t)key_of(top) << 32 | (unsigned)~at);
+    if ((tid & 63) == 0) tops[tid >> 6] = best;
+    __syncthreads();
+    best = tops[0];
+#pragma unroll
+    for (int i = 1; i < WAVES; ++i) best = tops[i] > best ? tops[i] : best;
+    SampleSlice& out = a.slices[(int64_t)b * a.slices_of_row + slice];
+    if (tid == 0) out.best = best;
+    if (c.greedy() || (unsigned)(best >> 32) <= LOWEST) return;
+    Weights w;
+    w.top = logit_of((unsigned)(best >> 32));
+    w.per = 1.4426950408889634 / (double)c.heat;
+    w.bits = a.bits;
+    const float per_unit = cells_per_unit(c.heat);
+    const int top_cell = cell_of(w.top, per_unit);
+    const bool weigh = !few(c);
+    // What min-p certainly drops is not weighed, where no other cut asks for the mass of all.
+    float least = -__builtin_inff();
+    if (c.least > 0.0f && !(c.p < 1.0f) && w.top < __builtin_inff()) least = w.top + 1.001f * c.heat * __logf((float)c.enough()) - 0.001f * (1.0f + fabsf(w.top));
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int e = 0; e < Piece<F32>::N; ++e) {
+            const float z = held[r][e];
+            if (z > -__builtin_inff()) {
+                const int j = below(top_cell, cell_of(z, per_unit));
+                atomicAdd(&count[j], 1);
+                if (weigh && z >= least) atomicAdd(&mass[j], (unsigned long long)w.mass(z));
+            }
+        }
+    __syncthreads();
+    for (int i = tid; i < CELLS; i += THREADS) { out.count[i] = count[i]; if (weigh) out.mass[i] = mass[i]; }
+}
+
+struct Cells {
+    uint64_t mass[CELLS];                                  // of the cells up to and with this one, from the highest
+    int count[CELLS];
+    uint64_t key[SORTED], running[SORTED];
+    uint64_t wave_counts[WAVES], wave_masses[WAVES];
+    int first, last, places[4], n;
+    int found_rank;
+    uint64_t found_mass, found_key;
+    int most_rank;
+};
+union RowShared {
+    Cells cells;
+    Shared digits;
+};
+
+// Sorts key[0 .. n) from the highest, n <= SORTED.  E: keys of a thread, tid + 1024 e
+template <int E>
+__device__ void sort_keys(uint64_t* key, int n) {
+    const int tid = threadIdx.x;
+    uint64_t v[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = tid + THREADS * e < n ? key[tid + THREADS * e] : 0;
+    int size = 64;
+    while (size < n) size *= 2;
+    for (int k = 2; k <= size; k *= 2) {
+        for (int j = k / 2; j > 0; j /= 2) {
+            if (j >= THREADS) {
+                // partners are a thread's own
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const int f = e ^ (j / THREADS);
+                    if (f > e && f < E) {
+                        const bool down = ((tid + THREADS * e) & k) == 0;
+                        const uint64_t x = v[e], y = v[f];
+                        const bool swap = down ? x < y : x > y;
+                        v[e] = swap ? y : x;
+                        v[f] = swap ? x : y;
+                    }
+                }
+            } else {
+                uint64_t o[E];
+                if (j >= 64) {
+                    __syncthreads();
+#pragma unroll
+                    for (int e = 0; e < E; ++e) key[tid + THREADS * e] = v[e];
+                    __syncthreads();
+#pragma unroll
+                    for (int e = 0; e < E; ++e) o[e] = key[(tid ^ j) + THREADS * e];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) o[e] = __shfl_xor(v[e], j);
+                }
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const bool down = ((tid + THREADS * e) & k) == 0, front = (tid & j) == 0;
+                    v[e] = down == front ? (v[e] > o[e] ? v[e] : o[e]) : (v[e] < o[e] ? v[e] : o[e]);
+                }
+            }
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < E; ++e) key[tid + THREADS * e] = v[e];
+    __syncthreads();
+}
+
+template <bool F32>
+__global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
+    __shared__ RowShared shared;
+    Cells& s = shared.cells;
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, S = a.slices_of_row;
+    const SampleSlice* slices = a.slices + (int64_t)b * S;
+    const Choices c(a, b);
+    uint64_t best = 0;
+    for (int i = 0; i < S; ++i) best = slices[i].best > best ? slices[i].best : best;
+    const bool none = (unsigned)(best >> 32) <= LOWEST;
+    if (none || c.greedy()) {
+        if (tid == 0) put(a, b, none ? -1 : (int)~(unsigned)best, none ? -__builtin_inff() : 0.0f, none ? 0 : 1);
+        return;
+    }
+    Weights w;
+    w.top = logit_of((unsigned)(best >> 32));
+    w.per = 1.4426950408889634 / (double)c.heat;
+    w.bits = a.bits;
+    const float per_unit = cells_per_unit(c.heat);
+    const int top_cell = cell_of(w.top, per_unit);
+    const bool weighed = !few(c);
+
+    // the row's histogram: a slice's cells, as far below the row's as its maximum is
+    static_assert(CELLS == THREADS, "a cell to a thread");
+    s.count[tid] = 0;
+    s.mass[tid] = 0;
+    __syncthreads();
+    for (int i = 0; i < S; ++i) {
+        const unsigned key = (unsigned)(slices[i].best >> 32);
+        if (key <= LOWEST) continue;
+        const float slice_top = logit_of(key);
+        const int n = slices[i].count[tid];
+        if (n == 0) continue;
+        const unsigned down = (unsigned)top_cell - (unsigned)cell_of(slice_top, per_unit);
+        const int j = down < CELLS && down + tid < CELLS - 1 && tid < CELLS - 1 ? (int)down + tid : CELLS - 1;
+        atomicAdd(&s.count[j], n);
+        if (weighed) {
+            const uint64_t m = slices[i].mass[tid];
+            atomicAdd((unsigned long long*)&s.mass[j], slice_top == w.top ? (unsigned long long)m : (unsigned long long)__builtin_rint((double)m * w.scaled(slice_top, 0)));
+        }
+    }
+    __syncthreads();
+    {
+        uint64_t n = (unsigned)s.count[tid], m = s.mass[tid];
+        n = wave_scan(n, lane); m = wave_scan(m, lane);
+        if (lane == 63) { s.wave_counts[wave] = n; s.wave_masses[wave] = m; }
+        if (tid == 0) { s.n = 0; s.first = s.last = CELLS - 1; for (int i = 0; i < 4; ++i) s.places[i] = CELLS - 1; }
+        __syncthreads();
+        for (int i = 0; i < wave; ++i) { n += s.wave_counts[i]; m += s.wave_masses[i]; }
+        s.count[tid] = (int)n;
+        s.mass[tid] = m;
+    }
+    __syncthreads();
+    const int my_count = s.count[tid], count_before = tid ? s.count[tid - 1] : 0;
+    const uint64_t my_mass = s.mass[tid], mass_before = tid ? s.mass[tid - 1] : 0;
+    const int all = s.count[CELLS - 1];
+    const uint64_t all_mass = s.mass[CELLS - 1];
+    // the first cell with so many tokens, or so much mass, up to its end: one thread finds it
+    auto cell_by_count = [&](int64_t n, int slot) { if (count_before < n && n <= my_count) s.places[slot] = tid; };
+    auto cell_by_mass = [&](double m, int slot) { if ((double)mass_before < m && m <= (double)my_mass) s.places[slot] = tid; };
+    auto cells_found = [&](int* to, int n) {
+        __syncthreads();
+        for (int i = 0; i < n; ++i) to[i] = s.places[i];
+        __syncthreads();
+        if (tid < 4) s.places[tid] = CELLS - 1;
+        __syncthreads();
+    };
+    const bool by_k = c.k > 0 && c.k < all, by_p = c.p < 1.0f, by_least = c.least > 0.0f;
+    // Up to three stretches of cells, one below the other, whose tokens have to be known: [from, to].  Sums by cell and sums by token
+    // differ by roundings, 2^-40 is ample.
+    constexpr double under = 1.0 - 0x1p-40, over = 1.0 + 0x1p-40;
+    int from[3] = {0, 0, 0}, to[3] = {-1, -1, -1};
+    int least_cell = CELLS, found[4];                      // (the first cell in which a weight may be too small)
+    if (!weighed) {
+        cell_by_count(by_k ? c.k : all, 0);
+        cells_found(found, 1);
+        to[0] = found[0];
+    } else {
+        int k_cell = CELLS, cut_lo = CELLS, cut_hi = CELLS;
+        double k_lo = (double)all_mass, k_hi = k_lo;
+        if (by_k) {
+            cell_by_count(c.k, 0);
+            cells_found(found, 1);
+            k_cell = cut_lo = cut_hi = found[0];
+            k_lo = k_cell ? (double)s.mass[k_cell - 1] : 0.0;
+            k_hi = (double)s.mass[k_cell];
+        }
+        if (by_p) {
+            const double t1 = fmin(fmax((double)c.p * k_hi * over, 1.0), k_hi), t0 = fmin(fmax((double)c.p * k_lo * under, 1.0), t1);
+            cell_by_mass(t0, 0);
+            cell_by_mass(t1, 1);
+            cells_found(found, 2);
+            cut_lo = found[0] < cut_lo ? found[0] : cut_lo;
+            cut_hi = found[1] < cut_hi ? found[1] : cut_hi;
+        }
+        if (by_least) {
+            // the logit of a weight of min-p, give or take what its computation may be off
+            const double z = (double)w.top + (double)c.heat * log(c.enough()), off = 1e-9 * (1.0 + fabs(z) + fabs((double)w.top));
+            const double hi = fmin(__builtin_floor((z + off) * (double)per_unit), 2147483647.0), lo = fmax(__builtin_floor((z - off) * (double)per_unit), -2147483648.0);
+            least_cell = hi >= (double)top_cell ? 0 : below(top_cell, (int)hi);
+            const int least_end = lo >= (double)top_cell ? 0 : below(top_cell, (int)lo);
+            cut_lo = least_cell < cut_lo ? least_cell : cut_lo;
+            cut_hi = least_end < cut_hi ? least_end : cut_hi;
+        }
+        const double u = a.u[b];
+        const double share = u > 0.0 ? (u < 1.0 ? u : 1.0) : 0.0;
+        const bool cut = cut_lo < CELLS;
+        const double lo = cut ? (cut_lo ? (double)s.mass[cut_lo - 1] : 0.0) : (double)all_mass, hi = cut ? (double)s.mass[cut_hi] : (double)all_mass;
+        cell_by_mass(fmax(share * lo * under, 1.0), 0);
+        cell_by_mass(fmin(fmax(share * hi * over + 1.0, 1.0), hi), 1);
+        cells_found(found, 2);
+        from[0] = found[0];
+        to[0] = found[1];
+        if (cut) {
+            // the cuts' cells; top-k's, for what is top-p's share, also where it is not the first cut.  (Cells without mass add nothing to it.)
+            from[1] = cut_lo;
+            to[1] = cut_hi;
+            if (by_k && by_p && k_hi > k_lo && k_cell > cut_hi) from[2] = to[2] = k_cell;
+            if (from[1] <= to[0] + 1) {                    // one stretch
+                from[0] = from[1] < from[0] ? from[1] : from[0];
+                to[0] = to[1] > to[0] ? to[1] : to[0];
+                from[1] = from[2];
+                to[1] = to[2];
+                to[2] = -1;
+            }
+        }
+    }
+    int base_count[3], tokens[3];
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+        const bool there = to[q] >= from[q];
+        base_count[q] = there && from[q] ? s.count[from[q] - 1] : 0;
+        tokens[q] = there ? s.count[to[q]] - base_count[q] : 0;
+    }
+    const int n = tokens[0] + tokens[1] + tokens[2];
+    if (n > SORTED || (by_least && c.least < 1e-12f)) {    // (uniform: every thread has the same numbers)
+        __syncthreads();
+        by_digits<F32>(a, b, best, shared.digits);
+        return;
+    }
+    // the tokens of those cells, as (key, ~index)
+    {
+        const Pieces<F32> row(row_of(a, b), a.V);
+        constexpr int R = 8;
+        auto take = [&](float z, int i) {
+            if (!(z > -__builtin_inff())) return;
+            const int j = below(top_cell, cell_of(z, per_unit));
+            if ((j >= from[0] && j <= to[0]) || (j >= from[1] && j <= to[1]) || (j >= from[2] && j <= to[2])) {
+                const int at = atomicAdd(&s.n, 1);
+                if (at < SORTED) s.key[at] = (uint64_t)key_of(z) << 32 | (unsigned)~i;
+            }
+        };
+        for (int p0 = 0; p0 < row.count; p0 += R * THREADS) {
+            Piece<F32> held[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) held[r] = row.load(p0 + r * THREADS + tid);
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int e = 0; e < Piece<F32>::N; ++e) take(held[r][e], row.first(p0 + r * THREADS + tid) + e);
+        }
+    }
+    __syncthreads();
+    if (n <= THREADS) sort_keys<1>(s.key, n); else sort_keys<SORTED / THREADS>(s.key, n);
+
+    // their running masses: E tokens of a thread, side by side
+    constexpr int E = SORTED / THREADS;
+    uint64_t each[E], run[E];
+    int rank[E];                                           // -1: none
+    const int per_thread = n <= THREADS ? 1 : E;
+    {
+        uint64_t sum = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int i = tid * per_thread + e;
+            const bool there = e < per_thread && i < n;
+            each[e] = there ? w.mass(logit_of((unsigned)(s.key[i] >> 32))) : 0;
+            sum += each[e];
+            run[e] = sum;
+            rank[e] = -1;
+        }
+        const uint64_t in = wave_scan(sum, lane);
+        if (lane == 63) s.wave_masses[wave] = in;
+        __syncthreads();
+        uint64_t front = in - sum;
+        for (int i = 0; i < wave; ++i) front += s.wave_masses[i];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int i = tid * per_thread + e;
+            run[e] += front;
+            if (e < per_thread && i < n) s.running[i] = run[e];
+        }
+    }
+    __syncthreads();
+    {
+        // places in the whole order: behind a stretch lies what is between it and the next
+        int start = 0;
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+            if (tokens[q] == 0) continue;
+            const uint64_t shift = (weighed && from[q] ? s.mass[from[q] - 1] : 0) - (start ? s.running[start - 1] : 0);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const int i = tid * per_thread + e;
+                if (e >= per_thread || i < start || i >= start + tokens[q]) continue;
+                rank[e] = base_count[q] + i - start;
+                run[e] += shift;
+            }
+            start += tokens[q];
+        }
+    }
+    // the first of them whose running mass reaches the target
+    auto reach = [&](uint64_t target) {
+        __syncthreads();
+        if (tid == 0) s.found_rank = -1;
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (rank[e] >= 0 && run[e] >= target && run[e] - each[e] < target) {
+                s.found_rank = rank[e];
+                s.found_mass = run[e];
+                s.found_key = s.key[tid * per_thread + e];
+            }
+        __syncthreads();
+        return s.found_rank;
+    };
+    int kept = all;
+    uint64_t mass = all_mass;
+    bool lost = false;                                     // (a target between the cells that it had to be in: never, but for rounding)
+    if (by_k) {
+        if (tid == 0) s.found_rank = -1;
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (rank[e] == c.k - 1) { s.found_rank = rank[e]; s.found_mass = run[e]; }
+        __syncthreads();
+        kept = c.k;
+        if (s.found_rank >= 0) {
+            mass = s.found_mass;
+        } else {
+            // not among them: another cut comes first, or its cell has no mass
+            int j = 0;
+            for (int step = CELLS / 2; step; step /= 2) if (s.count[j + step - 1] < c.k) j += step;
+            mass = s.mass[j];
+        }
+    } else if (!weighed) {
+        mass = n > 0 ? s.running[n - 1] : 0;
+    }
+    if (by_p) {
+        const int r = reach(cut_target(c.p, mass));
+        const uint64_t m = s.found_mass;
+        // (not found: top-k or min-p cuts in front of it)
+        if (r >= 0 && r + 1 < kept) { kept = r + 1; mass = m; }
+    }
+    if (by_least) {
+        // the last that weighs enough; where none of them does, the cells in front hold it
+        __syncthreads();
+        if (tid == 0) s.most_rank = -1;
+        __syncthreads();
+        int most = -1;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (rank[e] >= 0 && w.scaled(logit_of((unsigned)(s.key[tid * per_thread + e] >> 32)), 0) >= c.enough()) most = rank[e];
+        most = wave_max(most);
+        if (lane == 0 && most >= 0) atomicMax(&s.most_rank, most);
+        __syncthreads();
+        most = s.most_rank;
+        if (tid == 0) s.found_rank = -1;
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (most >= 0 && rank[e] == most) { s.found_rank = most; s.found_mass = run[e]; }
+        __syncthreads();
+        int m_kept = most + 1;
+        uint64_t m_mass = most >= 0 ? s.found_mass : 0;
+        const int whole = weighed && least_cell > 0 ? s.count[least_cell - 1] : 0;          // (cells that weigh enough altogether)
+        if (whole > m_kept) { m_kept = whole; m_mass = s.mass[least_cell - 1]; }
+        if (m_kept < kept) { kept = m_kept; mass = m_mass; }
+    }
+    if (reach(draw_target(a.u[b], mass)) < 0) lost = true;
+    if (lost) {
+        __syncthreads();
+        by_digits<F32>(a, b, best, shared.digits);
+        return;
+    }
+    if (tid == 0) put(a, b, (int)~(unsigned)s.found_key, share(w, c.heat, logit_of((unsigned)(s.found_key >> 32)), mass), kept);
+}
+
+// Slices of a row: as many tokens as a workgroup holds in registers, few where the rows alone do not fill the chip.
+constexpr int R_FEW = 2, R_MANY = 8;
+int pieces_of(int32_t V, bool f32) { return (V + 15 / (f32 ? 4 : 2)) / (f32 ? 4 : 8) + 1; }
+int slices_of(int32_t V, bool f32, int r) { return (pieces_of(V, f32) + THREADS * r - 1) / (THREADS * r); }
+
 }  // namespace
 
-size_t sample_workspace_bytes(int32_t, int32_t) { return 0; }
+// A workspace holds the slices of 4096 / (slices of a row) rows; a call of more runs in parts, one after the other.
+// (The slices are the most in fp32, and where rows are few.)
+constexpr int64_t SLICES_AT_ONCE = 4096;
+
+size_t sample_workspace_bytes(int32_t B, int32_t V) {
+    if (V > SAMPLE_LONG) V = SAMPLE_LONG;                  // (rows by digits need none)
+    const int64_t row = slices_of(V, true, R_MANY), most = row > SLICES_AT_ONCE ? row : SLICES_AT_ONCE;
+    const int64_t many = row * B < most ? row * B : most, few_rows = 256 + slices_of(V, true, R_FEW);
+    return (size_t)(many > few_rows ? many : few_rows) * sizeof(SampleSlice);
+}
 
 int launch_sample(SampleArgs a, hipStream_t s) {
+    const bool f32 = a.f32 != 0;
     int log2 = 0;
     while ((1ll << log2) < a.V) ++log2;
     a.bits = 62 - log2 < 50 ? 62 - log2 : 50;
-    if (a.f32) hipLaunchKernelGGL(sample_row_kernel<true>, dim3(a.B), dim3(THREADS), 0, s, a);
-    else hipLaunchKernelGGL(sample_row_kernel<false>, dim3(a.B), dim3(THREADS), 0, s, a);
+    if (a.V > SAMPLE_LONG) {
+        if (f32) hipLaunchKernelGGL(sample_long_kernel<true>, dim3(a.B), dim3(THREADS), 0, s, a);
+        else hipLaunchKernelGGL(sample_long_kernel<false>, dim3(a.B), dim3(THREADS), 0, s, a);
+        return check_hip(hipGetLastError(), "sample launch");
+    }
+    a.slices = reinterpret_cast<SampleSlice*>(a.workspace);
+    const int fine = slices_of(a.V, f32, R_FEW);
+    const bool few_rows = (int64_t)fine * a.B <= 256;
+    a.slices_of_row = few_rows ? fine : slices_of(a.V, f32, R_MANY);
+    const int32_t at_once = a.slices_of_row < SLICES_AT_ONCE ? (int32_t)(SLICES_AT_ONCE / a.slices_of_row) : 1;
+    for (int32_t b0 = 0; b0 < a.B; b0 += at_once) {
+        const int32_t rows = a.B - b0 < at_once ? a.B - b0 : at_once;
+        SampleArgs p = a;
+        p.logits = static_cast<const uint8_t*>(a.logits) + (int64_t)b0 * a.ldl * (f32 ? 4 : 2);
+        if (p.temperature) p.temperature += b0;
+        if (p.top_k) p.top_k += b0;
+        if (p.top_p) p.top_p += b0;
+        if (p.min_p) p.min_p += b0;
+        p.u += b0;
+        p.token += b0;
+        if (p.logprob) p.logprob += b0;
+        if (p.kept) p.kept += b0;
+        const dim3 grid(a.slices_of_row, rows), block(THREADS);
+        if (f32 && few_rows) hipLaunchKernelGGL((sample_slice_kernel<true, R_FEW>), grid, block, 0, s, p);
+        else if (f32) hipLaunchKernelGGL((sample_slice_kernel<true, R_MANY>), grid, block, 0, s, p);
+        else if (few_rows) hipLaunchKernelGGL((sample_slice_kernel<false, R_FEW>), grid, block, 0, s, p);
+        else hipLaunchKernelGGL((sample_slice_kernel<false, R_MANY>), grid, block, 0, s, p);
+        if (f32) hipLaunchKernelGGL(sample_row_kernel<true>, dim3(rows), block, 0, s, p);
+        else hipLaunchKernelGGL(sample_row_kernel<false>, dim3(rows), block, 0, s, p);
+    }
     return check_hip(hipGetLastError(), "sample launch");
 }
 

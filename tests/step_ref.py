@@ -35,8 +35,9 @@ def lookup(ids, Wq, w_scale, w_zero, scale):
 
 
 def sample_row(row, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, u=0.0):
-    """(token, ln of its share, kept) of one row of fp64 logits; sums in the extended type, the
-    products of them with u and top_p rounded to fp64."""
+    """(token, ln of its share, kept) of one row of fp64 logits; weights in the extended type, summed as
+    multiples of 2^-bits, the products of the sums with u and top_p rounded to fp64."""
+    V = row.size
     row = np.where(np.isnan(row), -math.inf, row)
     index = np.flatnonzero(row > -math.inf)
     if index.size == 0:
@@ -51,8 +52,9 @@ def sample_row(row, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, u=0.0):
     n = w.size
     if top_k > 0:
         n = min(n, top_k)
-    total = w[:n].sum()
-    running = np.cumsum(w)
+    bits = min(50, 62 - (V - 1).bit_length())
+    steps = np.rint(w * np.longdouble(2.0 ** bits)).astype(np.uint64)
+    running = np.cumsum(steps).astype(np.longdouble)              # (64 bits: exact)
     first = n
     if top_p < 1:
         first = min(first, int(np.searchsorted(running, np.float64(top_p) * np.float64(running[n - 1]), side="left")) + 1)
@@ -62,8 +64,8 @@ def sample_row(row, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, u=0.0):
     total = running[n - 1]
     u = 0.0 if not u > 0 else min(u, 1.0)
     at = int(np.searchsorted(running[:n], np.float64(u) * np.float64(total), side="right"))
-    at = min(at, int(np.flatnonzero(w[:n] > 2.0 ** -60)[-1]))
-    return int(index[at]), float(np.log(w[at] / total)), n
+    at = min(at, int(np.flatnonzero(steps[:n])[-1]))
+    return int(index[at]), float(np.log(w[at] / total * np.longdouble(2.0 ** bits))), n
 
 
 def extend(books, seqs, new, page_size, q_len, T):

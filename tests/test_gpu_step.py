@@ -266,6 +266,37 @@ def test_rows_out_of_the_ordinary(V, dtype):
         check_draw(logits, [u] * ROWS, min_p=[0.3] * ROWS, top_k=[V // 2 + 1] * ROWS, top_p=[0.9] * ROWS)
 
 
+@pytest.mark.parametrize("V", [3001, 90001])
+@pytest.mark.parametrize("dtype", [torch.float32, BF16])
+@pytest.mark.parametrize("shape", ["far up", "far down", "flat", "flatter", "masked by a number", "steep", "one above all"])
+def test_logits_of_other_shapes(V, dtype, shape):
+    """The grid of cells is the temperature's: rows that fill few of its cells, or many, lie anywhere on it or reach below it."""
+    g = gen(V)
+    z = torch.randn((ROWS, V), generator=g, device=DEV)
+    z = {"far up": 2 * z + 300, "far down": 2 * z - 5000, "flat": 0.3 * z, "flatter": 0.003 * z, "steep": 40 * z,
+         "masked by a number": torch.where(z > 0, 2 * z, torch.full_like(z, -1e9)), "one above all": z}[shape]
+    if shape == "one above all":
+        z[:, V // 7] = 25.0
+    z = z.to(dtype)
+    rng = random.Random(V)
+    u = [rng.random() for _ in range(ROWS - 1)] + [1 - 2.0 ** -40]
+    heat = [0.05, 0.5, 1.0, 3.0, 10.0, 100.0] * 2
+    check_draw(z, u, temperature=heat)
+    check_draw(z, u, temperature=heat, top_p=[0.5, 0.9, 0.999, 0.1] * 3)
+    check_draw(z, u, temperature=heat, top_k=[1500, 2000, V // 2, V - 1] * 3, top_p=[0.7, 0.99, 1.0] * 4)
+    check_draw(z, u, temperature=heat, top_k=[1500, 30, 0] * 4, min_p=[0.05, 1e-4, 1e-10, 1e-14] * 3)
+    check_draw(z, u, temperature=heat, top_p=[0.99, 0.6, 1.0] * 4, min_p=[0.2, 1e-3, 1e-13, 0.9] * 3)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, BF16])
+def test_long_rows(dtype):
+    g = gen(9)
+    for V in ((1 << 20) - 3, (1 << 20) + 5):
+        z = bell(g, 5, V, dtype)
+        check_draw(z, [0.1, 0.9, 0.5, 0.99, 0.7], temperature=[1.0, 0.7, 0.0, 1.2, 1.0], top_p=[1.0, 0.9, 1.0, 0.95, 1.0], top_k=[0, 0, 0, 3000, 20],
+                   min_p=[0.0, 0.0, 0.0, 0.0, 0.05])
+
+
 def test_all_tokens_forbidden_but_nan():
     logits = torch.full((3, 500), math.nan, device=DEV)
     logits[1, 7] = -1e30
