@@ -223,8 +223,7 @@ int launch_lookup_w4a16(LookupArgs a, hipStream_t s);             // lookup_w4a1
 constexpr int SAMPLE_CELLS = 1024, SAMPLE_FEW = 1024;
 struct SampleSlice {          // what one launch leaves the next of a slice of a row
     uint64_t best;            // (key, ~index) of its largest logit
-    uint64_t mass[SAMPLE_CELLS];
-    int32_t count[SAMPLE_CELLS];
+    uint64_t cells[SAMPLE_CELLS];
 };
 struct SampleArgs {
     const void* logits;       // [B, ldl], fp32 or bf16

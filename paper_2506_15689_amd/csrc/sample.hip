@@ -303,13 +303,19 @@ __global__ __launch_bounds__(THREADS) void sample_long_kernel(SampleArgs a) {
 
 // ---- in two launches: slices of rows into cells, then a row's cells and what lies in few of them ------------------------------
 //
-// A logit's cell is its place on a grid of step 2^e, about T / 30 wide (T <= 1), so that 1023 cells cover all that has weight.  Cells
-// are counted from the highest logit's, the last holds whatever lies below; being a grid of its own, not of the row's maximum, it is the
-// same for all slices of a row before they know of each other.  The first launch reads the logits once: each slice stays in
-// registers while its maximum is found, then its histogram of counts and masses is.  The second joins a row's histograms
-// (masses are rescaled to the row's maximum), finds the cells in which the cuts and the draw may lie -- one or two each, mostly -- and
-// reads the row again for the tokens in them, some hundred, which are sorted and settle everything exactly.  Rows whose cells
-// hold more tokens than are sorted (nearly equal logits, or thousands of equal ones) go by digits.
+// A logit's cell is its place on a grid of step 2^e between 36/1024 and 72/1024 of the temperature, so that 1023 cells cover all that has
+// weight.  Cells are counted from the highest logit's, the last holds whatever lies below; the grid is the temperature's, not the
+// row's, so it is the same for all slices of a row before they know of each other.  The first launch reads the logits once: a slice stays
+// in registers while its maximum is found, then its histogram is.  The second joins a row's histograms, finds the cells in which
+// the cuts and the draw may lie -- one or two each, mostly -- and reads the row again for the tokens in them, some hundred,
+// which are sorted and settle everything exactly.  Rows whose cells hold more tokens than are sorted (nearly equal logits, thousands of
+// equal ones, a high temperature) go by digits.
+//
+// A token's weight is the weight at its cell's lower edge times e^x, x = (z - edge) / T below 0.0704: the histogram sums e^x - 1, and
+// one exponential for each cell follows in the second launch.  e^x - 1 is six terms of its series in fp64, times 2^36, in the lower
+// 48 bits of a cell's 64, the number of tokens in the upper 16: one LDS atomic a token.  (With an exponential and two atomics for each
+// token the first launch took 67 us on 256 rows of 128000 logits, LDS and the vector units at their limits in turn.)  The series and the
+// rounding are good for 2^-37 of a token's weight; of logits on the grid, as coarse ones are, e^x - 1 is 0 and sums are exact.
 
 typedef unsigned v4u __attribute__((ext_vector_type(4)));
 
@@ -357,19 +363,25 @@ struct Pieces {
 };
 
 constexpr int CELLS = SAMPLE_CELLS, SORTED = 4096;
-// the grid of a temperature: cells to a unit
-__device__ __forceinline__ float cells_per_unit(float heat) {
-    // a step of 2^e >= 33 min(T, 1) / 1024, below twice that: 33 T under the maximum a weight is below 2^-47
-    const float least = 33.0f / CELLS * fminf(heat, 1.0f);
-    int e = (int)(__float_as_uint(least) >> 23) - 126;
-    e = e > -120 ? e : -120;
-    return __uint_as_float((unsigned)(127 - e) << 23);
-}
-__device__ __forceinline__ int cell_of(float z, float per_unit) { return (int)__builtin_floorf(z * per_unit); }       // (saturates)
+// the grid of a temperature
+struct Grid {
+    float per_unit, step;
+    __device__ __forceinline__ explicit Grid(float heat) {
+        int e = (int)(__float_as_uint(36.0f / CELLS * heat) >> 23) - 126;                       // 2^e: the next power of two
+        e = e < -120 ? -120 : e > 120 ? 120 : e;
+        per_unit = __uint_as_float((unsigned)(127 - e) << 23);
+        step = __uint_as_float((unsigned)(127 + e) << 23);
+    }
+    __device__ __forceinline__ int cell(float z) const { return (int)__builtin_floorf(z * per_unit); }       // (saturates)
+    // Cells next to this logit are numbers of 24 bits: edges are exact.
+    __device__ __forceinline__ bool fine(float z) const { return fabsf(z * per_unit) < 4194304.0f; }
+};
 __device__ __forceinline__ int below(int top, int cell) {
     const unsigned d = (unsigned)top - (unsigned)cell;
     return d < CELLS - 1 ? (int)d : CELLS - 1;
 }
+constexpr int COUNT_AT = 48;
+constexpr double PARTS = 68719476736.0;                   // 2^36
 // Few tokens are kept: they are weighed when they are known, and need no masses of cells.
 __device__ __forceinline__ bool few(const Choices& c) { return c.k > 0 && c.k <= SAMPLE_FEW; }
 
@@ -383,11 +395,11 @@ __device__ __forceinline__ T wave_max(T v) {
     return v;
 }
 
-// R: pieces that a thread holds
+// R: pieces that a thread holds; 2^15 logits of a workgroup at most, which a cell's 48 bits hold
 template <bool F32, int R>
 __global__ __launch_bounds__(THREADS) void sample_slice_kernel(SampleArgs a) {
-    __shared__ int count[CELLS];
-    __shared__ unsigned long long mass[CELLS];
+    static_assert(THREADS * R * Piece<F32>::N <= 32768, "");
+    __shared__ unsigned long long cells[CELLS + 1];        // (the last takes what is no token)
     __shared__ uint64_t tops[WAVES];
     const int slice = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
     const Pieces<F32> row(row_of(a, b), a.V);
@@ -396,7 +408,7 @@ __global__ __launch_bounds__(THREADS) void sample_slice_kernel(SampleArgs a) {
     Piece<F32> held[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) held[r] = row.load(p0 + r * THREADS + tid);
-    for (int i = tid; i < CELLS; i += THREADS) { count[i] = 0; mass[i] = 0; }
+    cells[tid] = 0;
     float top = -__builtin_inff();
     int at = -1;
 #pragma unroll
@@ -415,29 +427,34 @@ __global__ __launch_bounds__(THREADS) void sample_slice_kernel(SampleArgs a) {
     SampleSlice& out = a.slices[(int64_t)b * a.slices_of_row + slice];
     if (tid == 0) out.best = best;
     if (c.greedy() || (unsigned)(best >> 32) <= LOWEST) return;
-    Weights w;
-    w.top = logit_of((unsigned)(best >> 32));
-    w.per = 1.4426950408889634 / (double)c.heat;
-    w.bits = a.bits;
-    const float per_unit = cells_per_unit(c.heat);
-    const int top_cell = cell_of(w.top, per_unit);
-    const bool weigh = !few(c);
-    // What min-p certainly drops is not weighed, where no other cut asks for the mass of all.
-    float least = -__builtin_inff();
-    if (c.least > 0.0f && !(c.p < 1.0f) && w.top < __builtin_inff()) least = w.top + 1.001f * c.heat * __logf((float)c.enough()) - 0.001f * (1.0f + fabsf(w.top));
+    const Grid grid(c.heat);
+    const int top_cell = grid.cell(logit_of((unsigned)(best >> 32)));
+    if (few(c)) {
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+        for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int e = 0; e < Piece<F32>::N; ++e) {
-            const float z = held[r][e];
-            if (z > -__builtin_inff()) {
-                const int j = below(top_cell, cell_of(z, per_unit));
-                atomicAdd(&count[j], 1);
-                if (weigh && z >= least) atomicAdd(&mass[j], (unsigned long long)w.mass(z));
+            for (int e = 0; e < Piece<F32>::N; ++e) {
+                const float z = held[r][e];
+                if (z > -__builtin_inff()) atomicAdd(&cells[below(top_cell, grid.cell(z))], 1ull << COUNT_AT);
             }
-        }
+    } else {
+        // x = d g, d the place in the cell; coefficients g^k / k!
+        const double g = (double)grid.step / (double)c.heat;
+        const double c1 = PARTS * g, c2 = c1 * g * (1.0 / 2), c3 = c2 * g * (1.0 / 3), c4 = c3 * g * (1.0 / 4), c5 = c4 * g * (1.0 / 5), c6 = c5 * g * (1.0 / 6);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int e = 0; e < Piece<F32>::N; ++e) {
+                const float z = held[r][e], y = z * grid.per_unit, edge = __builtin_floorf(y);
+                const double d = (double)(y - edge);
+                const double v = fma(fma(fma(fma(fma(fma(c6, d, c5), d, c4), d, c3), d, c2), d, c1), d, 4503599627370496.0);
+                const int j = z > -__builtin_inff() ? below(top_cell, (int)edge) : CELLS;
+                const unsigned hi = ((unsigned)__double2hiint(v) & 0xFFFFu) | 1u << (COUNT_AT - 32);
+                atomicAdd(&cells[j], (unsigned long long)hi << 32 | (unsigned)__double2loint(v));
+            }
+    }
     __syncthreads();
-    for (int i = tid; i < CELLS; i += THREADS) { out.count[i] = count[i]; if (weigh) out.mass[i] = mass[i]; }
+    out.cells[tid] = cells[tid];
 }
 
 struct Cells {
@@ -524,37 +541,55 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
     w.top = logit_of((unsigned)(best >> 32));
     w.per = 1.4426950408889634 / (double)c.heat;
     w.bits = a.bits;
-    const float per_unit = cells_per_unit(c.heat);
-    const int top_cell = cell_of(w.top, per_unit);
-    const bool weighed = !few(c);
+    const Grid grid(c.heat);
+    if (!grid.fine(w.top)) {
+        by_digits<F32>(a, b, best, shared.digits);
+        return;
+    }
+    const int top_cell = grid.cell(w.top);
 
     // the row's histogram: a slice's cells, as far below the row's as its maximum is
     static_assert(CELLS == THREADS, "a cell to a thread");
     s.count[tid] = 0;
     s.mass[tid] = 0;
     __syncthreads();
-    for (int i = 0; i < S; ++i) {
-        const unsigned key = (unsigned)(slices[i].best >> 32);
-        if (key <= LOWEST) continue;
-        const float slice_top = logit_of(key);
-        const int n = slices[i].count[tid];
-        if (n == 0) continue;
-        const unsigned down = (unsigned)top_cell - (unsigned)cell_of(slice_top, per_unit);
-        const int j = down < CELLS && down + tid < CELLS - 1 && tid < CELLS - 1 ? (int)down + tid : CELLS - 1;
-        atomicAdd(&s.count[j], n);
-        if (weighed) {
-            const uint64_t m = slices[i].mass[tid];
-            atomicAdd((unsigned long long*)&s.mass[j], slice_top == w.top ? (unsigned long long)m : (unsigned long long)__builtin_rint((double)m * w.scaled(slice_top, 0)));
+    constexpr int AT_ONCE = 8;
+    for (int i0 = 0; i0 < S; i0 += AT_ONCE) {
+        uint64_t cell[AT_ONCE];
+        unsigned key[AT_ONCE];
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const int at = i0 + i < S ? i0 + i : S - 1;
+            key[i] = i0 + i < S ? (unsigned)(slices[at].best >> 32) : 0;
+            cell[i] = slices[at].cells[tid];               // (of a slice without tokens: whatever is there)
+        }
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const int n = (int)(cell[i] >> COUNT_AT);
+            if (key[i] <= LOWEST || n == 0) continue;
+            const unsigned down = (unsigned)top_cell - (unsigned)grid.cell(logit_of(key[i]));
+            const int j = down < CELLS && down + tid < CELLS - 1 && tid < CELLS - 1 ? (int)down + tid : CELLS - 1;
+            atomicAdd(&s.count[j], n);
+            atomicAdd((unsigned long long*)&s.mass[j], cell[i] & ((1ull << COUNT_AT) - 1));
         }
     }
     __syncthreads();
     {
-        uint64_t n = (unsigned)s.count[tid], m = s.mass[tid];
+        uint64_t n = (unsigned)s.count[tid], m = 0;
+        if (!few(c) && n && tid < CELLS - 1) {
+            const double edge = (double)(top_cell - tid) * (double)grid.step, sum = (double)n + (double)s.mass[tid] * (1.0 / PARTS);
+            m = (uint64_t)__builtin_rint(sum * w.scaled((float)edge, w.bits));
+        }
         n = wave_scan(n, lane); m = wave_scan(m, lane);
         if (lane == 63) { s.wave_counts[wave] = n; s.wave_masses[wave] = m; }
-        if (tid == 0) { s.n = 0; s.first = s.last = CELLS - 1; for (int i = 0; i < 4; ++i) s.places[i] = CELLS - 1; }
+        if (tid == 0) s.n = 0;
+        if (tid < 4) s.places[tid] = CELLS - 1;
         __syncthreads();
-        for (int i = 0; i < wave; ++i) { n += s.wave_counts[i]; m += s.wave_masses[i]; }
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) {
+            n += i < wave ? s.wave_counts[i] : 0;
+            m += i < wave ? s.wave_masses[i] : 0;
+        }
         s.count[tid] = (int)n;
         s.mass[tid] = m;
     }
@@ -562,6 +597,8 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
     const int my_count = s.count[tid], count_before = tid ? s.count[tid - 1] : 0;
     const uint64_t my_mass = s.mass[tid], mass_before = tid ? s.mass[tid - 1] : 0;
     const int all = s.count[CELLS - 1];
+    // few tokens are kept, or there are: all that matter are weighed one by one
+    const bool weighed = !few(c) && all > SORTED;
     const uint64_t all_mass = s.mass[CELLS - 1];
     // the first cell with so many tokens, or so much mass, up to its end: one thread finds it
     auto cell_by_count = [&](int64_t n, int slot) { if (count_before < n && n <= my_count) s.places[slot] = tid; };
@@ -575,8 +612,8 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
     };
     const bool by_k = c.k > 0 && c.k < all, by_p = c.p < 1.0f, by_least = c.least > 0.0f;
     // Up to three stretches of cells, one below the other, whose tokens have to be known: [from, to].  Sums by cell and sums by token
-    // differ by roundings, 2^-40 is ample.
-    constexpr double under = 1.0 - 0x1p-40, over = 1.0 + 0x1p-40;
+    // differ by 2^-37 of them, 2^-35 is ample.
+    constexpr double under = 1.0 - 0x1p-35, over = 1.0 + 0x1p-35;
     int from[3] = {0, 0, 0}, to[3] = {-1, -1, -1};
     int least_cell = CELLS, found[4];                      // (the first cell in which a weight may be too small)
     if (!weighed) {
@@ -604,7 +641,7 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
         if (by_least) {
             // the logit of a weight of min-p, give or take what its computation may be off
             const double z = (double)w.top + (double)c.heat * log(c.enough()), off = 1e-9 * (1.0 + fabs(z) + fabs((double)w.top));
-            const double hi = fmin(__builtin_floor((z + off) * (double)per_unit), 2147483647.0), lo = fmax(__builtin_floor((z - off) * (double)per_unit), -2147483648.0);
+            const double hi = fmin(__builtin_floor((z + off) * (double)grid.per_unit), 2147483647.0), lo = fmax(__builtin_floor((z - off) * (double)grid.per_unit), -2147483648.0);
             least_cell = hi >= (double)top_cell ? 0 : below(top_cell, (int)hi);
             const int least_end = lo >= (double)top_cell ? 0 : below(top_cell, (int)lo);
             cut_lo = least_cell < cut_lo ? least_cell : cut_lo;
@@ -649,15 +686,13 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
     // the tokens of those cells, as (key, ~index)
     {
         const Pieces<F32> row(row_of(a, b), a.V);
-        constexpr int R = 8;
-        auto take = [&](float z, int i) {
-            if (!(z > -__builtin_inff())) return;
-            const int j = below(top_cell, cell_of(z, per_unit));
-            if ((j >= from[0] && j <= to[0]) || (j >= from[1] && j <= to[1]) || (j >= from[2] && j <= to[2])) {
-                const int at = atomicAdd(&s.n, 1);
-                if (at < SORTED) s.key[at] = (uint64_t)key_of(z) << 32 | (unsigned)~i;
-            }
-        };
+        constexpr int R = 4;
+        float lo[3], hi[3];                                // of a stretch; none: nothing is at least infinity
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+            lo[q] = tokens[q] == 0 ? __builtin_inff() : to[q] == CELLS - 1 ? -3.402823466e38f : (float)(top_cell - to[q]) * grid.step;
+            hi[q] = (float)(top_cell - from[q] + 1) * grid.step;
+        }
         for (int p0 = 0; p0 < row.count; p0 += R * THREADS) {
             Piece<F32> held[R];
 #pragma unroll
@@ -665,7 +700,13 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
 #pragma unroll
             for (int r = 0; r < R; ++r)
 #pragma unroll
-                for (int e = 0; e < Piece<F32>::N; ++e) take(held[r][e], row.first(p0 + r * THREADS + tid) + e);
+                for (int e = 0; e < Piece<F32>::N; ++e) {
+                    const float z = held[r][e];
+                    if ((z >= lo[0] && z < hi[0]) || (z >= lo[1] && z < hi[1]) || (z >= lo[2] && z < hi[2])) {
+                        const int at = atomicAdd(&s.n, 1);
+                        if (at < SORTED) s.key[at] = (uint64_t)key_of(z) << 32 | (unsigned)~(row.first(p0 + r * THREADS + tid) + e);
+                    }
+                }
         }
     }
     __syncthreads();
@@ -691,7 +732,9 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
         if (lane == 63) s.wave_masses[wave] = in;
         __syncthreads();
         uint64_t front = in - sum;
-        for (int i = 0; i < wave; ++i) front += s.wave_masses[i];
+        
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) front += i < wave ? s.wave_masses[i] : 0;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const int i = tid * per_thread + e;
@@ -795,8 +838,10 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
 }
 
 // Slices of a row: as many tokens as a workgroup holds in registers, few where the rows alone do not fill the chip.
-constexpr int R_FEW = 2, R_MANY = 8;
+// (In 16 bits a piece is twice as many.)
 int pieces_of(int32_t V, bool f32) { return (V + 15 / (f32 ? 4 : 2)) / (f32 ? 4 : 8) + 1; }
+constexpr int few_pieces(bool f32) { return f32 ? 2 : 1; }
+constexpr int many_pieces(bool f32) { return f32 ? 8 : 4; }
 int slices_of(int32_t V, bool f32, int r) { return (pieces_of(V, f32) + THREADS * r - 1) / (THREADS * r); }
 
 }  // namespace
@@ -807,8 +852,8 @@ constexpr int64_t SLICES_AT_ONCE = 4096;
 
 size_t sample_workspace_bytes(int32_t B, int32_t V) {
     if (V > SAMPLE_LONG) V = SAMPLE_LONG;                  // (rows by digits need none)
-    const int64_t row = slices_of(V, true, R_MANY), most = row > SLICES_AT_ONCE ? row : SLICES_AT_ONCE;
-    const int64_t many = row * B < most ? row * B : most, few_rows = 256 + slices_of(V, true, R_FEW);
+    const int64_t row = slices_of(V, true, many_pieces(true)), most = row > SLICES_AT_ONCE ? row : SLICES_AT_ONCE;
+    const int64_t many = row * B < most ? row * B : most, few_rows = 256 + slices_of(V, true, few_pieces(true));
     return (size_t)(many > few_rows ? many : few_rows) * sizeof(SampleSlice);
 }
 
@@ -823,9 +868,9 @@ int launch_sample(SampleArgs a, hipStream_t s) {
         return check_hip(hipGetLastError(), "sample launch");
     }
     a.slices = reinterpret_cast<SampleSlice*>(a.workspace);
-    const int fine = slices_of(a.V, f32, R_FEW);
+    const int fine = slices_of(a.V, f32, few_pieces(f32));
     const bool few_rows = (int64_t)fine * a.B <= 256;
-    a.slices_of_row = few_rows ? fine : slices_of(a.V, f32, R_MANY);
+    a.slices_of_row = few_rows ? fine : slices_of(a.V, f32, many_pieces(f32));
     const int32_t at_once = a.slices_of_row < SLICES_AT_ONCE ? (int32_t)(SLICES_AT_ONCE / a.slices_of_row) : 1;
     for (int32_t b0 = 0; b0 < a.B; b0 += at_once) {
         const int32_t rows = a.B - b0 < at_once ? a.B - b0 : at_once;
@@ -840,10 +885,10 @@ int launch_sample(SampleArgs a, hipStream_t s) {
         if (p.logprob) p.logprob += b0;
         if (p.kept) p.kept += b0;
         const dim3 grid(a.slices_of_row, rows), block(THREADS);
-        if (f32 && few_rows) hipLaunchKernelGGL((sample_slice_kernel<true, R_FEW>), grid, block, 0, s, p);
-        else if (f32) hipLaunchKernelGGL((sample_slice_kernel<true, R_MANY>), grid, block, 0, s, p);
-        else if (few_rows) hipLaunchKernelGGL((sample_slice_kernel<false, R_FEW>), grid, block, 0, s, p);
-        else hipLaunchKernelGGL((sample_slice_kernel<false, R_MANY>), grid, block, 0, s, p);
+        if (f32 && few_rows) hipLaunchKernelGGL((sample_slice_kernel<true, few_pieces(true)>), grid, block, 0, s, p);
+        else if (f32) hipLaunchKernelGGL((sample_slice_kernel<true, many_pieces(true)>), grid, block, 0, s, p);
+        else if (few_rows) hipLaunchKernelGGL((sample_slice_kernel<false, few_pieces(false)>), grid, block, 0, s, p);
+        else hipLaunchKernelGGL((sample_slice_kernel<false, many_pieces(false)>), grid, block, 0, s, p);
         if (f32) hipLaunchKernelGGL(sample_row_kernel<true>, dim3(rows), block, 0, s, p);
         else hipLaunchKernelGGL(sample_row_kernel<false>, dim3(rows), block, 0, s, p);
     }
