@@ -70,13 +70,44 @@ __device__ __forceinline__ void for_each(const void* row, int V, F f) {
     }
 }
 
-// sums over the lanes in front of this one, and this one
-__device__ __forceinline__ uint64_t wave_scan(uint64_t v, int lane) {
+// the value of another lane: CTRL, ROWS and BANKS as in the instruction's modifier; lanes that it leaves out give `old`
+template <int CTRL, int ROWS = 0xF, int BANKS = 0xF>
+__device__ __forceinline__ uint64_t moved(uint64_t old, uint64_t v) {
+    const unsigned lo = __builtin_amdgcn_update_dpp((int)old, (int)v, CTRL, ROWS, BANKS, false);
+    const unsigned hi = __builtin_amdgcn_update_dpp((int)(old >> 32), (int)(v >> 32), CTRL, ROWS, BANKS, false);
+    return (uint64_t)hi << 32 | lo;
+}
+// sums over the lanes in front of this one, and this one: within rows of 16, then row by row
+__device__ __forceinline__ uint64_t wave_scan(uint64_t v) {
+    v += moved<0x111>(0, v);                               // (row_shr 1, 2, 4, 8)
+    v += moved<0x112>(0, v);
+    v += moved<0x114>(0, v);
+    v += moved<0x118>(0, v);
+    v += moved<0x142, 0xA>(0, v);                          // (the last lane of rows 0 and 2, to rows 1 and 3)
+    v += moved<0x143, 0xC>(0, v);                          // (lane 31, to rows 2 and 3)
+    return v;
+}
+// the value of lane ^ J
+template <int J>
+__device__ __forceinline__ uint64_t across(uint64_t v) {
+    if constexpr (J == 1) return moved<0xB1>(0, v);        // (quad_perm 1 0 3 2)
+    else if constexpr (J == 2) return moved<0x4E>(0, v);   // (quad_perm 2 3 0 1)
+    else if constexpr (J == 4) return moved<0x114, 0xF, 0xA>(moved<0x104, 0xF, 0x5>(0, v), v);
+    else if constexpr (J == 8) return moved<0x128>(0, v);  // (row_ror 8)
+    else {
+        const bool upper = threadIdx.x & J;
+        unsigned w[2] = {(unsigned)v, (unsigned)(v >> 32)};
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const uint64_t o = __shfl_up(v, d);
-        if (lane >= d) v += o;
+        for (int i = 0; i < 2; ++i) {
+            const auto p = J == 16 ? __builtin_amdgcn_permlane16_swap(w[i], w[i], false, false) : __builtin_amdgcn_permlane32_swap(w[i], w[i], false, false);
+            w[i] = upper ? p[0] : p[1];
+        }
+        return (uint64_t)w[1] << 32 | w[0];
     }
+}
+__device__ __forceinline__ uint64_t wave_max(uint64_t v) {
+    auto take = [&](uint64_t o) { v = o > v ? o : v; };
+    take(across<1>(v)); take(across<2>(v)); take(across<4>(v)); take(across<8>(v)); take(across<16>(v)); take(across<32>(v));
     return v;
 }
 
@@ -124,7 +155,7 @@ __device__ int descend(Shared& s, const Histogram& h, Goal goal, uint64_t target
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int hi = DIGITS - 1 - 2 * tid, lo = hi - 1;      // this thread's digits
     const uint64_t c0 = h.count[hi], c1 = h.count[lo], m0 = h.mass[hi], m1 = h.mass[lo];
-    const uint64_t c = wave_scan(c0 + c1, lane), m = wave_scan(m0 + m1, lane);
+    const uint64_t c = wave_scan(c0 + c1), m = wave_scan(m0 + m1);
     if (lane == 63) { s.wave_counts[wave] = c; s.wave_masses[wave] = m; }
     if (tid == 0) s.found_digit = -1;
     __syncthreads();
@@ -225,7 +256,7 @@ __device__ void by_digits(const SampleArgs& a, int b, uint64_t best, Shared& s) 
     {
         uint64_t n = 0, m = 0;
         for (int i = tid; i < DIGITS; i += THREADS) { n += s.first.count[i]; m += s.first.mass[i]; }
-        n = wave_scan(n, lane); m = wave_scan(m, lane);
+        n = wave_scan(n); m = wave_scan(m);
         if (lane == 63) { s.wave_counts[wave] = n; s.wave_masses[wave] = m; }
         __syncthreads();
         for (int i = 0; i < WAVES; ++i) { kept += s.wave_counts[i]; mass += s.wave_masses[i]; }
@@ -303,7 +334,7 @@ __global__ __launch_bounds__(THREADS) void sample_long_kernel(SampleArgs a) {
 
 // ---- in two launches: slices of rows into cells, then a row's cells and what lies in few of them ------------------------------
 //
-// A logit's cell is its place on a grid of step 2^e between 36/1024 and 72/1024 of the temperature, so that 1023 cells cover all that has
+// A logit's cell is its place on a grid of step 2^e between 36/2048 and 72/2048 of the temperature, so that 2047 cells cover all that has
 // weight.  Cells are counted from the highest logit's, the last holds whatever lies below; the grid is the temperature's, not the
 // row's, so it is the same for all slices of a row before they know of each other.  The first launch reads the logits once: a slice stays
 // in registers while its maximum is found, then its histogram is.  The second joins a row's histograms, finds the cells in which
@@ -311,8 +342,8 @@ __global__ __launch_bounds__(THREADS) void sample_long_kernel(SampleArgs a) {
 // which are sorted and settle everything exactly.  Rows whose cells hold more tokens than are sorted (nearly equal logits, thousands of
 // equal ones, a high temperature) go by digits.
 //
-// A token's weight is the weight at its cell's lower edge times e^x, x = (z - edge) / T below 0.0704: the histogram sums e^x - 1, and
-// one exponential for each cell follows in the second launch.  e^x - 1 is six terms of its series in fp64, times 2^36, in the lower
+// A token's weight is the weight at its cell's lower edge times e^x, x = (z - edge) / T below 0.0352: the histogram sums e^x - 1, and
+// one exponential for each cell follows in the second launch.  e^x - 1 is five terms of its series in fp64, times 2^36, in the lower
 // 48 bits of a cell's 64, the number of tokens in the upper 16: one LDS atomic a token.  (With an exponential and two atomics for each
 // token the first launch took 67 us on 256 rows of 128000 logits, LDS and the vector units at their limits in turn.)  The series and the
 // rounding are good for 2^-37 of a token's weight; of logits on the grid, as coarse ones are, e^x - 1 is 0 and sums are exact.
@@ -385,16 +416,6 @@ constexpr double PARTS = 68719476736.0;                   // 2^36
 // Few tokens are kept: they are weighed when they are known, and need no masses of cells.
 __device__ __forceinline__ bool few(const Choices& c) { return c.k > 0 && c.k <= SAMPLE_FEW; }
 
-template <class T>
-__device__ __forceinline__ T wave_max(T v) {
-#pragma unroll
-    for (int d = 32; d; d /= 2) {
-        const T o = __shfl_xor(v, d);
-        v = o > v ? o : v;
-    }
-    return v;
-}
-
 // R: pieces that a thread holds; 2^15 logits of a workgroup at most, which a cell's 48 bits hold
 template <bool F32, int R>
 __global__ __launch_bounds__(THREADS) void sample_slice_kernel(SampleArgs a) {
@@ -408,7 +429,8 @@ __global__ __launch_bounds__(THREADS) void sample_slice_kernel(SampleArgs a) {
     Piece<F32> held[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) held[r] = row.load(p0 + r * THREADS + tid);
-    cells[tid] = 0;
+#pragma unroll
+    for (int i = 0; i < CELLS; i += THREADS) cells[i + tid] = 0;
     float top = -__builtin_inff();
     int at = -1;
 #pragma unroll
@@ -440,21 +462,22 @@ __global__ __launch_bounds__(THREADS) void sample_slice_kernel(SampleArgs a) {
     } else {
         // x = d g, d the place in the cell; coefficients g^k / k!
         const double g = (double)grid.step / (double)c.heat;
-        const double c1 = PARTS * g, c2 = c1 * g * (1.0 / 2), c3 = c2 * g * (1.0 / 3), c4 = c3 * g * (1.0 / 4), c5 = c4 * g * (1.0 / 5), c6 = c5 * g * (1.0 / 6);
+        const double c1 = PARTS * g, c2 = c1 * g * (1.0 / 2), c3 = c2 * g * (1.0 / 3), c4 = c3 * g * (1.0 / 4), c5 = c4 * g * (1.0 / 5);
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int e = 0; e < Piece<F32>::N; ++e) {
                 const float z = held[r][e], y = z * grid.per_unit, edge = __builtin_floorf(y);
                 const double d = (double)(y - edge);
-                const double v = fma(fma(fma(fma(fma(fma(c6, d, c5), d, c4), d, c3), d, c2), d, c1), d, 4503599627370496.0);
+                const double v = fma(fma(fma(fma(fma(c5, d, c4), d, c3), d, c2), d, c1), d, 4503599627370496.0);
                 const int j = z > -__builtin_inff() ? below(top_cell, (int)edge) : CELLS;
                 const unsigned hi = ((unsigned)__double2hiint(v) & 0xFFFFu) | 1u << (COUNT_AT - 32);
                 atomicAdd(&cells[j], (unsigned long long)hi << 32 | (unsigned)__double2loint(v));
             }
     }
     __syncthreads();
-    out.cells[tid] = cells[tid];
+#pragma unroll
+    for (int i = 0; i < CELLS; i += THREADS) out.cells[i + tid] = cells[i + tid];
 }
 
 struct Cells {
@@ -472,50 +495,55 @@ union RowShared {
     Shared digits;
 };
 
-// Sorts key[0 .. n) from the highest, n <= SORTED.  E: keys of a thread, tid + 1024 e
+// Sorts key[0 .. n) from the highest, n <= SORTED, by a bitonic network: E keys of a thread, i = tid + 1024 e; `down` where a run of k
+// keys is to fall.  Partners are a thread's own, another wave's, through LDS, or another lane's.
+__device__ __forceinline__ uint64_t chosen(uint64_t v, uint64_t o, bool larger) { return (v > o) == larger ? v : o; }
+template <int E, int J>
+__device__ __forceinline__ void sort_in_wave(uint64_t (&v)[E], int k) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const int i = threadIdx.x + THREADS * e;
+        v[e] = chosen(v[e], across<J>(v[e]), ((i & k) == 0) == ((i & J) == 0));
+    }
+    if constexpr (J > 1) sort_in_wave<E, J / 2>(v, k);
+}
 template <int E>
 __device__ void sort_keys(uint64_t* key, int n) {
     const int tid = threadIdx.x;
     uint64_t v[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) v[e] = tid + THREADS * e < n ? key[tid + THREADS * e] : 0;
-    int size = 64;
-    while (size < n) size *= 2;
-    for (int k = 2; k <= size; k *= 2) {
-        for (int j = k / 2; j > 0; j /= 2) {
+    sort_in_wave<E, 1>(v, 2);
+    sort_in_wave<E, 2>(v, 4);
+    sort_in_wave<E, 4>(v, 8);
+    sort_in_wave<E, 8>(v, 16);
+    sort_in_wave<E, 16>(v, 32);
+    sort_in_wave<E, 32>(v, 64);
+    for (int k = 128; k < 2 * n; k *= 2) {
+        for (int j = k / 2; j >= 64; j /= 2) {
             if (j >= THREADS) {
-                // partners are a thread's own
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    const int f = e ^ (j / THREADS);
-                    if (f > e && f < E) {
-                        const bool down = ((tid + THREADS * e) & k) == 0;
-                        const uint64_t x = v[e], y = v[f];
-                        const bool swap = down ? x < y : x > y;
-                        v[e] = swap ? y : x;
-                        v[f] = swap ? x : y;
-                    }
+                    const int f = e | (j / THREADS);
+                    if (f == e || f >= E) continue;
+                    const bool larger = ((tid + THREADS * e) & k) == 0;
+                    const uint64_t x = v[e], y = v[f];
+                    v[e] = chosen(x, y, larger);
+                    v[f] = chosen(y, x, !larger);
                 }
             } else {
-                uint64_t o[E];
-                if (j >= 64) {
-                    __syncthreads();
+                __syncthreads();
 #pragma unroll
-                    for (int e = 0; e < E; ++e) key[tid + THREADS * e] = v[e];
-                    __syncthreads();
-#pragma unroll
-                    for (int e = 0; e < E; ++e) o[e] = key[(tid ^ j) + THREADS * e];
-                } else {
-#pragma unroll
-                    for (int e = 0; e < E; ++e) o[e] = __shfl_xor(v[e], j);
-                }
+                for (int e = 0; e < E; ++e) key[tid + THREADS * e] = v[e];
+                __syncthreads();
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    const bool down = ((tid + THREADS * e) & k) == 0, front = (tid & j) == 0;
-                    v[e] = down == front ? (v[e] > o[e] ? v[e] : o[e]) : (v[e] < o[e] ? v[e] : o[e]);
+                    const int i = tid + THREADS * e;
+                    v[e] = chosen(v[e], key[i ^ j], ((i & k) == 0) == ((i & j) == 0));
                 }
             }
         }
+        sort_in_wave<E, 32>(v, k);
     }
     __syncthreads();
 #pragma unroll
@@ -549,60 +577,82 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
     const int top_cell = grid.cell(w.top);
 
     // the row's histogram: a slice's cells, as far below the row's as its maximum is
-    static_assert(CELLS == THREADS, "a cell to a thread");
-    s.count[tid] = 0;
-    s.mass[tid] = 0;
+    static_assert(CELLS == 2 * THREADS, "two cells to a thread");
+    s.count[tid] = s.count[tid + THREADS] = 0;
+    s.mass[tid] = s.mass[tid + THREADS] = 0;
+    if (tid == 0) s.n = 0;
+    if (tid < 4) s.places[tid] = CELLS - 1;
     __syncthreads();
-    constexpr int AT_ONCE = 8;
+    constexpr int AT_ONCE = 4;
     for (int i0 = 0; i0 < S; i0 += AT_ONCE) {
-        uint64_t cell[AT_ONCE];
+        uint64_t cell[AT_ONCE][2];
         unsigned key[AT_ONCE];
 #pragma unroll
         for (int i = 0; i < AT_ONCE; ++i) {
             const int at = i0 + i < S ? i0 + i : S - 1;
             key[i] = i0 + i < S ? (unsigned)(slices[at].best >> 32) : 0;
-            cell[i] = slices[at].cells[tid];               // (of a slice without tokens: whatever is there)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) cell[i][h] = slices[at].cells[tid + h * THREADS];          // (of a slice without tokens: whatever is there)
         }
 #pragma unroll
         for (int i = 0; i < AT_ONCE; ++i) {
-            const int n = (int)(cell[i] >> COUNT_AT);
-            if (key[i] <= LOWEST || n == 0) continue;
+            if (key[i] <= LOWEST) continue;
             const unsigned down = (unsigned)top_cell - (unsigned)grid.cell(logit_of(key[i]));
-            const int j = down < CELLS && down + tid < CELLS - 1 && tid < CELLS - 1 ? (int)down + tid : CELLS - 1;
-            atomicAdd(&s.count[j], n);
-            atomicAdd((unsigned long long*)&s.mass[j], cell[i] & ((1ull << COUNT_AT) - 1));
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int n = (int)(cell[i][h] >> COUNT_AT), own = tid + h * THREADS;
+                if (n == 0) continue;
+                const int j = down < CELLS && down + own < CELLS - 1 && own < CELLS - 1 ? (int)down + own : CELLS - 1;
+                atomicAdd(&s.count[j], n);
+                atomicAdd((unsigned long long*)&s.mass[j], cell[i][h] & ((1ull << COUNT_AT) - 1));
+            }
         }
     }
     __syncthreads();
+    // this thread's two cells, and what lies in front of them
+    int count_to[3];
+    uint64_t mass_to[3];
     {
-        uint64_t n = (unsigned)s.count[tid], m = 0;
-        if (!few(c) && n && tid < CELLS - 1) {
-            const double edge = (double)(top_cell - tid) * (double)grid.step, sum = (double)n + (double)s.mass[tid] * (1.0 / PARTS);
-            m = (uint64_t)__builtin_rint(sum * w.scaled((float)edge, w.bits));
+        uint64_t n[2], m[2] = {0, 0};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int j = 2 * tid + h;
+            n[h] = (unsigned)s.count[j];
+            if (!few(c) && n[h] && j < CELLS - 1) {
+                const double edge = (double)(top_cell - j) * (double)grid.step, sum = (double)(int)n[h] + (double)s.mass[j] * (1.0 / PARTS);
+                m[h] = (uint64_t)__builtin_rint(sum * w.scaled((float)edge, w.bits));
+            }
         }
-        n = wave_scan(n, lane); m = wave_scan(m, lane);
-        if (lane == 63) { s.wave_counts[wave] = n; s.wave_masses[wave] = m; }
-        if (tid == 0) s.n = 0;
-        if (tid < 4) s.places[tid] = CELLS - 1;
+        const uint64_t n_in = wave_scan(n[0] + n[1]), m_in = wave_scan(m[0] + m[1]);
+        if (lane == 63) { s.wave_counts[wave] = n_in; s.wave_masses[wave] = m_in; }
         __syncthreads();
+        uint64_t nb = n_in - n[0] - n[1], mb = m_in - m[0] - m[1];
 #pragma unroll
         for (int i = 0; i < WAVES; ++i) {
-            n += i < wave ? s.wave_counts[i] : 0;
-            m += i < wave ? s.wave_masses[i] : 0;
+            nb += i < wave ? s.wave_counts[i] : 0;
+            mb += i < wave ? s.wave_masses[i] : 0;
         }
-        s.count[tid] = (int)n;
-        s.mass[tid] = m;
+        count_to[0] = (int)nb; count_to[1] = (int)(nb + n[0]); count_to[2] = (int)(nb + n[0] + n[1]);
+        mass_to[0] = mb; mass_to[1] = mb + m[0]; mass_to[2] = mb + m[0] + m[1];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) { s.count[2 * tid + h] = count_to[h + 1]; s.mass[2 * tid + h] = mass_to[h + 1]; }
     }
     __syncthreads();
-    const int my_count = s.count[tid], count_before = tid ? s.count[tid - 1] : 0;
-    const uint64_t my_mass = s.mass[tid], mass_before = tid ? s.mass[tid - 1] : 0;
     const int all = s.count[CELLS - 1];
     // few tokens are kept, or there are: all that matter are weighed one by one
     const bool weighed = !few(c) && all > SORTED;
     const uint64_t all_mass = s.mass[CELLS - 1];
     // the first cell with so many tokens, or so much mass, up to its end: one thread finds it
-    auto cell_by_count = [&](int64_t n, int slot) { if (count_before < n && n <= my_count) s.places[slot] = tid; };
-    auto cell_by_mass = [&](double m, int slot) { if ((double)mass_before < m && m <= (double)my_mass) s.places[slot] = tid; };
+    auto cell_by_count = [&](int64_t n, int slot) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (count_to[h] < n && n <= count_to[h + 1]) s.places[slot] = 2 * tid + h;
+    };
+    auto cell_by_mass = [&](double m, int slot) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if ((double)mass_to[h] < m && m <= (double)mass_to[h + 1]) s.places[slot] = 2 * tid + h;
+    };
     auto cells_found = [&](int* to, int n) {
         __syncthreads();
         for (int i = 0; i < n; ++i) to[i] = s.places[i];
@@ -693,16 +743,24 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
             lo[q] = tokens[q] == 0 ? __builtin_inff() : to[q] == CELLS - 1 ? -3.402823466e38f : (float)(top_cell - to[q]) * grid.step;
             hi[q] = (float)(top_cell - from[q] + 1) * grid.step;
         }
+        const bool third = tokens[2] > 0;
+        auto wanted = [&](float z) { return ((z >= lo[0]) & (z < hi[0])) | ((z >= lo[1]) & (z < hi[1])) | (third & (z >= lo[2]) & (z < hi[2])); };
         for (int p0 = 0; p0 < row.count; p0 += R * THREADS) {
             Piece<F32> held[R];
 #pragma unroll
             for (int r = 0; r < R; ++r) held[r] = row.load(p0 + r * THREADS + tid);
+            bool any = false;
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int e = 0; e < Piece<F32>::N; ++e) any |= wanted(held[r][e]);
+            if (!any) continue;                            // (of most pieces nothing is wanted)
 #pragma unroll
             for (int r = 0; r < R; ++r)
 #pragma unroll
                 for (int e = 0; e < Piece<F32>::N; ++e) {
                     const float z = held[r][e];
-                    if ((z >= lo[0] && z < hi[0]) || (z >= lo[1] && z < hi[1]) || (z >= lo[2] && z < hi[2])) {
+                    if (wanted(z)) {
                         const int at = atomicAdd(&s.n, 1);
                         if (at < SORTED) s.key[at] = (uint64_t)key_of(z) << 32 | (unsigned)~(row.first(p0 + r * THREADS + tid) + e);
                     }
@@ -710,7 +768,9 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
         }
     }
     __syncthreads();
-    if (n <= THREADS) sort_keys<1>(s.key, n); else sort_keys<SORTED / THREADS>(s.key, n);
+    if (n <= THREADS) sort_keys<1>(s.key, n);
+    else if (n <= 2 * THREADS) sort_keys<2>(s.key, n);
+    else sort_keys<4>(s.key, n);
 
     // their running masses: E tokens of a thread, side by side
     constexpr int E = SORTED / THREADS;
@@ -728,7 +788,7 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
             run[e] = sum;
             rank[e] = -1;
         }
-        const uint64_t in = wave_scan(sum, lane);
+        const uint64_t in = wave_scan(sum);
         if (lane == 63) s.wave_masses[wave] = in;
         __syncthreads();
         uint64_t front = in - sum;
@@ -790,7 +850,7 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
             mass = s.found_mass;
         } else {
             // not among them: another cut comes first, or its cell has no mass
-            int j = 0;
+            int j = 0;                                     // (the cell that reaches it)
             for (int step = CELLS / 2; step; step /= 2) if (s.count[j + step - 1] < c.k) j += step;
             mass = s.mass[j];
         }
@@ -812,7 +872,7 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
 #pragma unroll
         for (int e = 0; e < E; ++e)
             if (rank[e] >= 0 && w.scaled(logit_of((unsigned)(s.key[tid * per_thread + e] >> 32)), 0) >= c.enough()) most = rank[e];
-        most = wave_max(most);
+        most = (int)wave_max((uint64_t)(most + 1)) - 1;
         if (lane == 0 && most >= 0) atomicMax(&s.most_rank, most);
         __syncthreads();
         most = s.most_rank;
@@ -846,9 +906,9 @@ int slices_of(int32_t V, bool f32, int r) { return (pieces_of(V, f32) + THREADS 
 
 }  // namespace
 
-// A workspace holds the slices of 4096 / (slices of a row) rows; a call of more runs in parts, one after the other.
+// A workspace holds the slices of 2048 / (slices of a row) rows; a call of more runs in parts, one after the other.
 // (The slices are the most in fp32, and where rows are few.)
-constexpr int64_t SLICES_AT_ONCE = 4096;
+constexpr int64_t SLICES_AT_ONCE = 2048;
 
 size_t sample_workspace_bytes(int32_t B, int32_t V) {
     if (V > SAMPLE_LONG) V = SAMPLE_LONG;                  // (rows by digits need none)
