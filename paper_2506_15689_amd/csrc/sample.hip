@@ -360,36 +360,46 @@ struct Piece {
         else return __uint_as_float(e & 1 ? v[e / 2] & 0xFFFF0000u : v[e / 2] << 16);
     }
 };
-// A row in aligned pieces: element e of piece p is token N p + e - off; what is no token is -inf.
+// A row in aligned pieces, element e of piece p token head + N p + e, and what lies in front of the first and behind the last of them,
+// which a thread takes one each of.  Loads of pieces have no branch around them, which would wait for each in turn: pieces past the
+// last are the last again, and made -inf where a block reaches past it.
 template <bool F32>
 struct Pieces {
     static constexpr int N = Piece<F32>::N;
-    const uint8_t* base;                                   // the first piece, aligned
-    int off, V, count;
-    __device__ __forceinline__ Pieces(const void* row, int tokens) : V(tokens) {
-        const uintptr_t at = reinterpret_cast<uintptr_t>(row);
-        off = (int)(at & 15) / (F32 ? 4 : 2);
-        base = reinterpret_cast<const uint8_t*>(at & ~(uintptr_t)15);
-        count = (V + off + N - 1) / N;
+    const void* row;
+    const v4u* first;
+    int V, head, count;
+    __device__ __forceinline__ Pieces(const void* logits, int tokens) : row(logits), V(tokens) {
+        head = (int)(-(intptr_t)(uintptr_t)logits & 15) / (F32 ? 4 : 2);
+        head = head < V ? head : V;
+        count = (V - head) / N;
+        first = reinterpret_cast<const v4u*>(static_cast<const uint8_t*>(logits) + head * (F32 ? 4 : 2));
     }
-    __device__ __forceinline__ int first(int p) const { return N * p - off; }
-    // (nothing outside the row is read)
-    __device__ __forceinline__ Piece<F32> load(int p) const {
-        Piece<F32> r;
-        if (first(p) >= 0 && first(p) + N <= V) {
-            r.v = *reinterpret_cast<const v4u*>(base + 16 * (int64_t)p);
-        } else {
-            constexpr unsigned none = F32 ? 0xFF800000u : 0xFF80FF80u;
-            r.v = v4u{none, none, none, none};
+    __device__ __forceinline__ int token(int p, int e) const { return head + N * p + e; }
+    // pieces p0 + tid + THREADS r
+    template <int R>
+    __device__ __forceinline__ void load(Piece<F32> (&held)[R], int p0) const {
+        constexpr unsigned none = F32 ? 0xFF800000u : 0xFF80FF80u;
+        if (p0 < count) {
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const int i = first(p) + e;
-                if (p >= count || i < 0 || i >= V) continue;
-                if constexpr (F32) r.v[e] = reinterpret_cast<const unsigned*>(base)[N * p + e];
-                else r.v[e / 2] = (r.v[e / 2] & (e & 1 ? 0xFFFFu : 0xFFFF0000u)) | (unsigned)reinterpret_cast<const uint16_t*>(base)[N * p + e] << (e & 1 ? 16 : 0);
+            for (int r = 0; r < R; ++r) {
+                const int p = p0 + r * THREADS + (int)threadIdx.x;
+                held[r].v = first[p < count ? p : count - 1];
             }
         }
-        return r;
+        if (p0 + R * THREADS <= count) return;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (p0 + r * THREADS + (int)threadIdx.x >= count) held[r].v = v4u{none, none, none, none};
+    }
+    // this thread's token outside the pieces; -1: none
+    __device__ __forceinline__ int edge() const {
+        const int tail = V - head - N * count, tid = threadIdx.x;
+        return tid < head ? tid : tid < head + tail ? V - tail + tid - head : -1;
+    }
+    __device__ __forceinline__ float at(int i) const {
+        if (i < 0) return -__builtin_inff();
+        return F32 ? static_cast<const float*>(row)[i] : bf16_to_f32(static_cast<const uint16_t*>(row)[i]);
     }
 };
 
@@ -419,7 +429,7 @@ __device__ __forceinline__ bool few(const Choices& c) { return c.k > 0 && c.k <=
 // R: pieces that a thread holds; 2^15 logits of a workgroup at most, which a cell's 48 bits hold
 template <bool F32, int R>
 __global__ __launch_bounds__(THREADS) void sample_slice_kernel(SampleArgs a) {
-    static_assert(THREADS * R * Piece<F32>::N <= 32768, "");
+    static_assert(THREADS * R * Piece<F32>::N <= 32768, "and a few at the row's ends");
     __shared__ unsigned long long cells[CELLS + 1];        // (the last takes what is no token)
     __shared__ uint64_t tops[WAVES];
     const int slice = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
@@ -427,8 +437,9 @@ __global__ __launch_bounds__(THREADS) void sample_slice_kernel(SampleArgs a) {
     const Choices c(a, b);
     const int p0 = slice * (THREADS * R);
     Piece<F32> held[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) held[r] = row.load(p0 + r * THREADS + tid);
+    row.load(held, p0);
+    const int edge_token = slice == 0 ? row.edge() : -1;
+    const float edge_logit = row.at(edge_token);
 #pragma unroll
     for (int i = 0; i < CELLS; i += THREADS) cells[i + tid] = 0;
     float top = -__builtin_inff();
@@ -438,9 +449,10 @@ __global__ __launch_bounds__(THREADS) void sample_slice_kernel(SampleArgs a) {
 #pragma unroll
         for (int e = 0; e < Piece<F32>::N; ++e) {
             const float z = held[r][e];
-            if (z > top) { top = z; at = row.first(p0 + r * THREADS + tid) + e; }
+            if (z > top) { top = z; at = row.token(p0 + r * THREADS + tid, e); }
         }
-    uint64_t best = wave_max((uint64_t)key_of(top) << 32 | (unsigned)~at);
+    const uint64_t own = (uint64_t)key_of(top) << 32 | (unsigned)~at, at_edge = (uint64_t)key_of(edge_logit) << 32 | (unsigned)~edge_token;
+    uint64_t best = wave_max(own > at_edge ? own : at_edge);
     if ((tid & 63) == 0) tops[tid >> 6] = best;
     __syncthreads();
     best = tops[0];
@@ -452,28 +464,31 @@ __global__ __launch_bounds__(THREADS) void sample_slice_kernel(SampleArgs a) {
     const Grid grid(c.heat);
     const int top_cell = grid.cell(logit_of((unsigned)(best >> 32)));
     if (few(c)) {
+        auto add = [&](float z) {
+            if (z > -__builtin_inff()) atomicAdd(&cells[below(top_cell, grid.cell(z))], 1ull << COUNT_AT);
+        };
+        add(edge_logit);
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int e = 0; e < Piece<F32>::N; ++e) {
-                const float z = held[r][e];
-                if (z > -__builtin_inff()) atomicAdd(&cells[below(top_cell, grid.cell(z))], 1ull << COUNT_AT);
-            }
+            for (int e = 0; e < Piece<F32>::N; ++e) add(held[r][e]);
     } else {
         // x = d g, d the place in the cell; coefficients g^k / k!
         const double g = (double)grid.step / (double)c.heat;
         const double c1 = PARTS * g, c2 = c1 * g * (1.0 / 2), c3 = c2 * g * (1.0 / 3), c4 = c3 * g * (1.0 / 4), c5 = c4 * g * (1.0 / 5);
+        auto add = [&](float z) {
+            const float y = z * grid.per_unit, edge = __builtin_floorf(y);
+            const double d = (double)(y - edge);
+            const double v = fma(fma(fma(fma(fma(c5, d, c4), d, c3), d, c2), d, c1), d, 4503599627370496.0);
+            const int j = z > -__builtin_inff() ? below(top_cell, (int)edge) : CELLS;
+            const unsigned hi = ((unsigned)__double2hiint(v) & 0xFFFFu) | 1u << (COUNT_AT - 32);
+            atomicAdd(&cells[j], (unsigned long long)hi << 32 | (unsigned)__double2loint(v));
+        };
+        if (edge_token >= 0) add(edge_logit);
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int e = 0; e < Piece<F32>::N; ++e) {
-                const float z = held[r][e], y = z * grid.per_unit, edge = __builtin_floorf(y);
-                const double d = (double)(y - edge);
-                const double v = fma(fma(fma(fma(fma(c5, d, c4), d, c3), d, c2), d, c1), d, 4503599627370496.0);
-                const int j = z > -__builtin_inff() ? below(top_cell, (int)edge) : CELLS;
-                const unsigned hi = ((unsigned)__double2hiint(v) & 0xFFFFu) | 1u << (COUNT_AT - 32);
-                atomicAdd(&cells[j], (unsigned long long)hi << 32 | (unsigned)__double2loint(v));
-            }
+            for (int e = 0; e < Piece<F32>::N; ++e) add(held[r][e]);
     }
     __syncthreads();
 #pragma unroll
@@ -549,6 +564,58 @@ __device__ void sort_keys(uint64_t* key, int n) {
 #pragma unroll
     for (int e = 0; e < E; ++e) key[tid + THREADS * e] = v[e];
     __syncthreads();
+}
+
+// The tokens of the row in Q stretches of cells, into key[], in any order.  A lane tests a block of its logits by three vector instructions
+// each (the middle of logit and bounds; is it the logit; a bit more of a mask), the next block under way meanwhile; hits
+// leave their index only, and the logits of all of them are fetched at the end.  (Tests by masks of the wave, or hits one by one in
+// between, are chains of latencies: 13 .. 28 us for 128000 logits.)
+template <bool F32, int Q>
+__device__ void collect(Cells& s, const Pieces<F32>& row, const int (&from)[3], const int (&to)[3], int top_cell, const Grid& grid) {
+    constexpr int R = 4, N = Piece<F32>::N;
+    const int tid = threadIdx.x;
+    float lo[Q], hi[Q];                                    // of a stretch, both within
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        const int end = __float_as_int((float)(top_cell - from[q] + 1) * grid.step);            // the first beyond
+        lo[q] = to[q] == CELLS - 1 ? -3.402823466e38f : (float)(top_cell - to[q]) * grid.step;
+        hi[q] = __int_as_float(end > 0 ? end - 1 : end == 0 ? (int)0x80000001 : end + 1);
+    }
+    auto wanted = [&](float z) {
+        bool in = __builtin_amdgcn_fmed3f(z, lo[0], hi[0]) == z;
+#pragma unroll
+        for (int q = 1; q < Q; ++q) in |= __builtin_amdgcn_fmed3f(z, lo[q], hi[q]) == z;
+        return in;
+    };
+    auto keep = [&](int token) {
+        const int at = atomicAdd(&s.n, 1);
+        if (at < SORTED) s.key[at] = (unsigned)token;
+    };
+    const int edge = row.edge();
+    if (edge >= 0 && wanted(row.at(edge))) keep(edge);
+    Piece<F32> held[R], next[R];
+    row.load(next, 0);
+    for (int p0 = 0; p0 < row.count; p0 += R * THREADS) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) held[r] = next[r];
+        row.load(next, p0 + R * THREADS);
+        unsigned hits = 0;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int e = 0; e < N; ++e) hits = hits + hits + (wanted(held[r][e]) ? 1u : 0u);
+        while (hits) {
+            const int i = R * N - 1 - __builtin_ctz(hits);
+            hits &= hits - 1;
+            keep(row.token(p0 + i / N * THREADS + tid, i % N));
+        }
+    }
+    __syncthreads();
+    const int n = s.n < SORTED ? s.n : SORTED;
+    for (int i = tid; i < n; i += THREADS) {
+        const int token = (int)s.key[i];
+        s.key[i] = (uint64_t)key_of(row.at(token)) << 32 | (unsigned)~token;
+    }
 }
 
 template <bool F32>
@@ -736,36 +803,9 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
     // the tokens of those cells, as (key, ~index)
     {
         const Pieces<F32> row(row_of(a, b), a.V);
-        constexpr int R = 4;
-        float lo[3], hi[3];                                // of a stretch; none: nothing is at least infinity
-#pragma unroll
-        for (int q = 0; q < 3; ++q) {
-            lo[q] = tokens[q] == 0 ? __builtin_inff() : to[q] == CELLS - 1 ? -3.402823466e38f : (float)(top_cell - to[q]) * grid.step;
-            hi[q] = (float)(top_cell - from[q] + 1) * grid.step;
-        }
-        const bool third = tokens[2] > 0;
-        auto wanted = [&](float z) { return ((z >= lo[0]) & (z < hi[0])) | ((z >= lo[1]) & (z < hi[1])) | (third & (z >= lo[2]) & (z < hi[2])); };
-        for (int p0 = 0; p0 < row.count; p0 += R * THREADS) {
-            Piece<F32> held[R];
-#pragma unroll
-            for (int r = 0; r < R; ++r) held[r] = row.load(p0 + r * THREADS + tid);
-            bool any = false;
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int e = 0; e < Piece<F32>::N; ++e) any |= wanted(held[r][e]);
-            if (!any) continue;                            // (of most pieces nothing is wanted)
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int e = 0; e < Piece<F32>::N; ++e) {
-                    const float z = held[r][e];
-                    if (wanted(z)) {
-                        const int at = atomicAdd(&s.n, 1);
-                        if (at < SORTED) s.key[at] = (uint64_t)key_of(z) << 32 | (unsigned)~(row.first(p0 + r * THREADS + tid) + e);
-                    }
-                }
-        }
+        if (to[1] < from[1]) collect<F32, 1>(s, row, from, to, top_cell, grid);
+        else if (to[2] < from[2]) collect<F32, 2>(s, row, from, to, top_cell, grid);
+        else collect<F32, 3>(s, row, from, to, top_cell, grid);
     }
     __syncthreads();
     if (n <= THREADS) sort_keys<1>(s.key, n);
@@ -899,7 +939,7 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
 
 // Slices of a row: as many tokens as a workgroup holds in registers, few where the rows alone do not fill the chip.
 // (In 16 bits a piece is twice as many.)
-int pieces_of(int32_t V, bool f32) { return (V + 15 / (f32 ? 4 : 2)) / (f32 ? 4 : 8) + 1; }
+int pieces_of(int32_t V, bool f32) { return V / (f32 ? 4 : 8) + 1; }
 constexpr int few_pieces(bool f32) { return f32 ? 2 : 1; }
 constexpr int many_pieces(bool f32) { return f32 ? 8 : 4; }
 int slices_of(int32_t V, bool f32, int r) { return (pieces_of(V, f32) + THREADS * r - 1) / (THREADS * r); }
