@@ -411,7 +411,7 @@ int basq_paged_attention(const void* q, int64_t ldq, int32_t B, int32_t q_len, i
  *
  *     Y[m,n] = sum_g w_scale[n,g] * sum_{k in g} (q[n,k] - w_zero[n,g]) X[m,k]  +  bias[n]
  *
- *   X          bf16 [M, ldx], 16-byte aligned, ldx >= K and a multiple of 8.  A token with a value that is not finite, or beyond
+ *   X          bf16 [M, ldx], 16-byte aligned, ldx >= K, a multiple of 8, up to 2^23.  A token with a value that is not finite, or beyond
  *              2^112, has outputs that are not finite; the others do not
  *   Wq         uint8 [N, K/2] canonical, or the layout of basq_pack_decode with w_layout = BASQ_W_DECODE16 (K % 128 == 0);
  *              16-byte aligned

@@ -46,6 +46,7 @@ int basq_w4a16_gemm(const void* X, int64_t M, int32_t K, int64_t ldx, const uint
     if (M == 0) return BASQ_OK;
     if (!X || !aligned(X, 16)) return fail(BASQ_EINVAL, "X is null or not 16-byte aligned");
     if (ldx < K || ldx % 8 != 0) return fail(BASQ_EINVAL, "ldx must be >= K and a multiple of 8 (got %lld)", (long long)ldx);
+    if (ldx > 1 << 23) return fail(BASQ_EUNSUPPORTED, "ldx up to 2^23 is supported (got %lld)", (long long)ldx);
     if (!Y || !aligned(Y, y_f32 ? 4 : 2)) return fail(BASQ_EINVAL, "Y is null or not aligned as its type is");
     if (ldy < N) return fail(BASQ_EINVAL, "ldy must be >= N (got %lld)", (long long)ldy);
     W4A16Args a{};

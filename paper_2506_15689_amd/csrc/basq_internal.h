@@ -205,6 +205,10 @@ struct W4A16Args {
 };
 constexpr int64_t W4A16_MAX_TOKENS = 16 * 65535;
 int launch_gemm_w4a16(W4A16Args a, hipStream_t s);                // gemm_w4a16.hip
+void launch_w4a16_streamed_few(const W4A16Args& a, hipStream_t s);                               // up to 16 tokens; gemm_w4a16_*.hip
+void launch_w4a16_streamed_many(const W4A16Args& a, hipStream_t s);
+void launch_w4a16_canonical_few(const W4A16Args& a, hipStream_t s);
+void launch_w4a16_canonical_many(const W4A16Args& a, hipStream_t s);
 
 struct LookupArgs {
     const int32_t* ids;       // [T]

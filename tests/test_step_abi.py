@@ -41,7 +41,7 @@ MATRIX = [
 
 @pytest.mark.parametrize("kw,code", MATRIX + [
     (dict(M=-1), B.BASQ_EINVAL), (dict(M=16 * 65535 + 1), B.BASQ_EUNSUPPORTED), (dict(X=None), B.BASQ_EINVAL), (dict(X=ODD), B.BASQ_EINVAL),
-    (dict(ldx=248), B.BASQ_EINVAL), (dict(ldx=260), B.BASQ_EINVAL), (dict(bias=OFF), B.BASQ_EINVAL), (dict(Y=BYTE), B.BASQ_EINVAL),
+    (dict(ldx=248), B.BASQ_EINVAL), (dict(ldx=260), B.BASQ_EINVAL), (dict(ldx=(1 << 23) + 8), B.BASQ_EUNSUPPORTED), (dict(bias=OFF), B.BASQ_EINVAL), (dict(Y=BYTE), B.BASQ_EINVAL),
     (dict(Y=OFF, y_f32=1), B.BASQ_EINVAL), (dict(ldy=47), B.BASQ_EINVAL),
 ])
 def test_product_refuses(lib, kw, code):
