@@ -220,7 +220,8 @@ struct LookupArgs {
     float scale;
     uint16_t* Y;              // [T, ldy], bf16 bits
     int64_t ldy;
-    int32_t groups;           // set by the launcher
+    int32_t groups;           // these two are set by the launcher, as in W4A16Args, for units of 32 channels
+    uint32_t per_group;
 };
 int launch_lookup_w4a16(LookupArgs a, hipStream_t s);             // lookup_w4a16.hip
 

@@ -136,7 +136,7 @@ struct Shared {
 __device__ __forceinline__ int shift_of(int level) { return level == 0 ? 21 : level == 1 ? 10 : 0; }
 
 template <bool F32>
-__device__ void fill(Histogram& h, const void* row, int V, const Weights& w, int level, unsigned prefix) {
+__device__ __forceinline__ void fill(Histogram& h, const void* row, int V, const Weights& w, int level, unsigned prefix) {
     for (int i = threadIdx.x; i < DIGITS; i += THREADS) { h.count[i] = 0; h.mass[i] = 0; }
     __syncthreads();
     const int shift = shift_of(level), above = level == 0 ? 32 : shift_of(level - 1);
@@ -151,7 +151,7 @@ __device__ void fill(Histogram& h, const void* row, int V, const Weights& w, int
 }
 
 // The digit, counted from the highest, in which the goal is reached; behind[] get what lies in front of it.
-__device__ int descend(Shared& s, const Histogram& h, Goal goal, uint64_t target, int key_digit, uint64_t& count, uint64_t& mass) {
+__device__ __forceinline__ int descend(Shared& s, const Histogram& h, Goal goal, uint64_t target, int key_digit, uint64_t& count, uint64_t& mass) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int hi = DIGITS - 1 - 2 * tid, lo = hi - 1;      // this thread's digits
     const uint64_t c0 = h.count[hi], c1 = h.count[lo], m0 = h.mass[hi], m1 = h.mass[lo];
@@ -177,7 +177,7 @@ __device__ int descend(Shared& s, const Histogram& h, Goal goal, uint64_t target
 
 // target: at least 1, and reached.  BY_KEY: all tokens whose key is `key` or higher.
 template <bool F32>
-__device__ Place find(Shared& s, const void* row, int V, const Weights& w, Goal goal, uint64_t target, unsigned key = 0) {
+__device__ __forceinline__ Place find(Shared& s, const void* row, int V, const Weights& w, Goal goal, uint64_t target, unsigned key = 0) {
     uint64_t count = 0, mass = 0;
     unsigned prefix = 0;
     int digit = 0;
@@ -242,7 +242,7 @@ __device__ __forceinline__ const void* row_of(const SampleArgs& a, int b) {
 
 // A row by digits, whatever its logits are.  best: its likeliest token, (key, ~index).
 template <bool F32>
-__device__ void by_digits(const SampleArgs& a, int b, uint64_t best, Shared& s) {
+__device__ __forceinline__ void by_digits(const SampleArgs& a, int b, uint64_t best, Shared& s) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = a.V;
     const void* row = row_of(a, b);
     const Choices c(a, b);
@@ -332,21 +332,15 @@ __global__ __launch_bounds__(THREADS) void sample_long_kernel(SampleArgs a) {
     by_digits<F32>(a, b, best, s);
 }
 
-// ---- in two launches: slices of rows into cells, then a row's cells and what lies in few of them ------------------------------
+// ---- bf16: by the numbers themselves -------------------------------------------------------------------------------------------
 //
-// A logit's cell is its place on a grid of step 2^e between 36/2048 and 72/2048 of the temperature, so that 2047 cells cover all that has
-// weight.  Cells are counted from the highest logit's, the last holds whatever lies below; the grid is the temperature's, not the
-// row's, so it is the same for all slices of a row before they know of each other.  The first launch reads the logits once: a slice stays
-// in registers while its maximum is found, then its histogram is.  The second joins a row's histograms, finds the cells in which
-// the cuts and the draw may lie -- one or two each, mostly -- and reads the row again for the tokens in them, some hundred,
-// which are sorted and settle everything exactly.  Rows whose cells hold more tokens than are sorted (nearly equal logits, thousands of
-// equal ones, a high temperature) go by digits.
+// There are 65536 of them: a workgroup counts how often each occurs in its row, in LDS, two counters of 16 bits to a word, and needs
+// no weight but one for each number that occurs, some thousand of 128000.  Counts and masses of 64 numbers at a time are summed and scanned
+// over the workgroup; a place is found among the 1024 sums and then among the 64 numbers of one.  (With cells as for fp32, below, for which
+// every token is weighed, 256 rows of 128000 logits took 63 us.)  A counter that overflows, of a number that more than 65535 tokens
+// have, shows in the sum of all: such rows go by digits.
 //
-// A token's weight is the weight at its cell's lower edge times e^x, x = (z - edge) / T below 0.0352: the histogram sums e^x - 1, and
-// one exponential for each cell follows in the second launch.  e^x - 1 is five terms of its series in fp64, times 2^36, in the lower
-// 48 bits of a cell's 64, the number of tokens in the upper 16: one LDS atomic a token.  (With an exponential and two atomics for each
-// token the first launch took 67 us on 256 rows of 128000 logits, LDS and the vector units at their limits in turn.)  The series and the
-// rounding are good for 2^-37 of a token's weight; of logits on the grid, as coarse ones are, e^x - 1 is 0 and sums are exact.
+// The row stays in registers for the last step, the index of the token that is the nth with the number found.
 
 typedef unsigned v4u __attribute__((ext_vector_type(4)));
 
@@ -377,6 +371,7 @@ struct Pieces {
     }
     __device__ __forceinline__ int token(int p, int e) const { return head + N * p + e; }
     // pieces p0 + tid + THREADS r
+    __device__ __forceinline__ void load_one(Piece<F32>& held, int p) const { held.v = first[p < count ? p : count - 1]; }
     template <int R>
     __device__ __forceinline__ void load(Piece<F32> (&held)[R], int p0) const {
         constexpr unsigned none = F32 ? 0xFF800000u : 0xFF80FF80u;
@@ -402,6 +397,305 @@ struct Pieces {
         return F32 ? static_cast<const float*>(row)[i] : bf16_to_f32(static_cast<const uint16_t*>(row)[i]);
     }
 };
+
+typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+
+// Numbers from the largest on: +inf is 0; what is no token, -inf and NaN, comes from NONE on.  Two in a word.
+constexpr unsigned NONE = 0xFF01u, ZERO = 0x7F80u;         // (ZERO + 1 is -0)
+__device__ __forceinline__ us2 numbers_of(unsigned two) {
+    const unsigned negative = two >> 15 & 0x00010001u;
+    return __builtin_bit_cast(us2, two ^ (0x7FFF7FFFu & ~(negative * 0xFFFFu))) - us2{0x7F, 0x7F};
+}
+__device__ __forceinline__ float logit_of_number(unsigned n) {
+    n += 0x7Fu;
+    return __uint_as_float((n < 0x8000u ? n ^ 0x7FFFu : n) << 16);
+}
+
+struct Numbers {
+    unsigned counters[32768];
+    int count[1024];                                       // of 64 numbers and all in front
+    uint64_t mass[1024];
+    uint64_t wave_counts[WAVES], wave_masses[WAVES];
+    int top, last, tokens, zeros, found, before, token;
+    int parts[1024];
+    __device__ __forceinline__ unsigned occurs(unsigned n) const { return counters[n >> 1] >> (n & 1 ? 16 : 0) & 0xFFFFu; }
+};
+union NumbersShared {
+    Numbers numbers;
+    Shared digits;
+};
+
+// f(piece, its number) for what a thread holds of a row, or, R = 0, reads again
+template <int R, class F, class G>
+__device__ __forceinline__ void each_piece(const Pieces<false>& row, Piece<false> (&held)[R ? R : 1], F f, G before) {
+    if constexpr (R > 0) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            before(r);
+            Piece<false> piece = held[r];
+            asm volatile("" : "+v"(piece.v));              // (one after the other, in the registers of one)
+            if (r * THREADS + (int)threadIdx.x < row.count) f(piece, r * THREADS + (int)threadIdx.x);
+        }
+    } else {
+        Piece<false> some[4];
+        for (int p0 = 0; p0 < row.count; p0 += 4 * THREADS) {
+            row.load(some, p0);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (p0 + r * THREADS + (int)threadIdx.x < row.count) f(some[r], p0 + r * THREADS + (int)threadIdx.x);
+        }
+    }
+}
+
+template <int R>
+__global__ __launch_bounds__(THREADS) void sample_numbers_kernel(SampleArgs a) {
+    __shared__ NumbersShared shared;
+    Numbers& s = shared.numbers;
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const Pieces<false> row(row_of(a, b), a.V);
+    const Choices c(a, b);
+#pragma unroll
+    for (int i = 0; i < 32768; i += 4 * THREADS) *reinterpret_cast<uint4*>(&s.counters[i + 4 * tid]) = make_uint4(0, 0, 0, 0);
+    s.count[tid] = 0;
+    s.mass[tid] = 0;
+    if (tid == 0) { s.top = NONE; s.last = 0; s.tokens = 0; }
+    __syncthreads();
+    // (Behind the barrier, which waits for loads; the edge first, as they are waited for in their order: pieces are counted as they arrive.)
+    const int edge_token = row.edge();
+    const float edge_logit = row.at(edge_token);
+    Piece<false> held[R ? R : 1];
+    // (a wave's loads are issued one by one as there is room for them: the first are counted before the last are asked for)
+    constexpr int AHEAD = R < 6 ? R : 6;
+    if (R > 0 && row.count > 0)
+#pragma unroll
+        for (int r = 0; r < AHEAD; ++r) row.load_one(held[r], r * THREADS + tid);
+    // how often each number occurs; the largest logit; the tokens
+    us2 least = {0xFFFF, 0xFFFF}, most = {0, 0};
+    int tokens = 0;
+    auto count = [&](unsigned n) {
+        if (n < NONE) {                                    // (thousands of forbidden tokens would wait for one another at one counter)
+            atomicAdd(&s.counters[n >> 1], n & 1 ? 0x10000u : 1u);
+            ++tokens;
+        }
+    };
+    each_piece<R>(row, held, [&](const Piece<false>& piece, int) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const us2 two = numbers_of(piece.v[w]);
+            least = __builtin_elementwise_min(least, two);
+            most = __builtin_elementwise_max(most, two);
+            count(two.x);
+            count(two.y);
+        }
+    }, [&](int r) {
+        if (r + AHEAD < R && (r + AHEAD) * THREADS < row.count) row.load_one(held[r + AHEAD < R ? r + AHEAD : 0], (r + AHEAD) * THREADS + tid);
+        __builtin_amdgcn_sched_barrier(0);
+    });
+    if (edge_token >= 0) {
+        const us2 edge = numbers_of(__float_as_uint(edge_logit) >> 16 | 0xFF800000u);          // (and -inf)
+        least = __builtin_elementwise_min(least, edge);
+        most = __builtin_elementwise_max(most, edge);
+        count(edge.x);
+    }
+    {
+        const uint64_t best = wave_max((uint64_t)(0xFFFFu - (least.x < least.y ? least.x : least.y)));
+        const uint64_t far = wave_max((uint64_t)(most.x > most.y ? most.x : most.y));
+        const uint64_t in = wave_scan((uint64_t)tokens);
+        if (lane == 63) { atomicMin(&s.top, 0xFFFF - (int)best); atomicMax(&s.last, (int)far); atomicAdd(&s.tokens, (int)in); }
+    }
+    __syncthreads();
+    const unsigned top = (unsigned)s.top;
+    const int all = s.tokens;
+    if (all == 0) {
+        if (tid == 0) put(a, b, -1, -__builtin_inff(), 0);
+        return;
+    }
+    if (tid == 0) {                                        // zeros are equal
+        const unsigned two = s.counters[ZERO >> 1];
+        s.zeros = (int)((two & 0xFFFFu) + (two >> 16));
+        s.counters[ZERO >> 1] = (unsigned)s.zeros & 0xFFFFu;
+    }
+    Weights w;
+    w.top = logit_of_number(top);
+    w.per = 1.4426950408889634 / (double)c.heat;
+    w.bits = a.bits;
+    uint64_t kept = 1, mass = 0;
+    unsigned number = top;
+    int nth = 1;
+    __syncthreads();
+    if (!c.greedy()) {
+        // 64 numbers at a time: half a wave's words, from the largest number's on
+        const int end = (s.last < (int)NONE ? s.last : (int)NONE - 1) >> 1;
+        constexpr int AT_ONCE = 4;
+        for (int i0 = (int)(top >> 1) & ~(THREADS - 1); i0 <= end; i0 += AT_ONCE * THREADS) {
+            unsigned two[AT_ONCE];
+#pragma unroll
+            for (int e = 0; e < AT_ONCE; ++e) two[e] = i0 + e * THREADS + tid < 32768 ? s.counters[i0 + e * THREADS + tid] : 0;
+#pragma unroll
+            for (int e = 0; e < AT_ONCE; ++e) {
+                if (__ballot(two[e] != 0) == 0) continue;
+                const int i = i0 + e * THREADS + tid;
+                const unsigned n0 = two[e] & 0xFFFFu, n1 = two[e] >> 16;
+                uint64_t n = n0 + n1, m = 0;
+                if (n0) m = n0 * w.mass(logit_of_number(2 * i));
+                if (n1) m += n1 * w.mass(logit_of_number(2 * i + 1));
+                n = wave_scan(n);
+                m = wave_scan(m);
+                const uint64_t n_low = __shfl((unsigned long long)n, 31), m_low = __shfl((unsigned long long)m, 31);
+                if (lane == 63) { n -= n_low; m -= m_low; }
+                if ((lane & 31) == 31) { s.count[i >> 5] = (int)n; s.mass[i >> 5] = m; }
+            }
+        }
+        __syncthreads();
+        const uint64_t own_n = (unsigned)s.count[tid], own_m = s.mass[tid];
+        uint64_t n = wave_scan(own_n), m = wave_scan(own_m);
+        if (lane == 63) { s.wave_counts[wave] = n; s.wave_masses[wave] = m; }
+        if (tid == 0) s.found = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) {
+            n += i < wave ? s.wave_counts[i] : 0;
+            m += i < wave ? s.wave_masses[i] : 0;
+        }
+        s.count[tid] = (int)n;
+        s.mass[tid] = m;
+        __syncthreads();
+        if (s.count[1023] != all || s.zeros > 0xFFFF) {    // (a counter was too small)
+            __syncthreads();
+            by_digits<false>(a, b, (uint64_t)key_of(w.top) << 32, shared.digits);
+            return;
+        }
+        mass = s.mass[1023];
+        kept = (uint64_t)all;
+        // the place at which the count, or the mass, reaches a target: the 64 numbers, then the number and which of its tokens
+        struct Found { unsigned number; int nth; uint64_t count, mass; };
+        auto reach = [&](bool by_mass, uint64_t target) {
+            const uint64_t to = by_mass ? m : n, from = to - (by_mass ? own_m : own_n);
+            if (from < target && target <= to) s.found = tid;
+            __syncthreads();
+            const int at = s.found;
+            const unsigned x = 64u * at + lane;
+            const uint64_t times = s.occurs(x), each = times ? w.mass(logit_of_number(x)) : 0;
+            const uint64_t n_in = wave_scan(times) + (at ? (unsigned)s.count[at - 1] : 0), m_in = wave_scan(times * each) + (at ? s.mass[at - 1] : 0);
+            const uint64_t end = by_mass ? m_in : n_in, begin = end - (by_mass ? times * each : times);
+            const uint64_t hit = __ballot(begin < target && target <= end);
+            const int l = hit ? __builtin_ctzll(hit) : 0;
+            auto of = [&](uint64_t v) { return (uint64_t)__shfl((unsigned long long)v, l); };
+            const uint64_t each_l = of(each), begin_l = of(begin);
+            Found f;
+            f.number = 64u * at + l;
+            f.nth = (int)(by_mass ? (target - begin_l + each_l - 1) / (each_l ? each_l : 1) : target - begin_l);
+            f.count = of(n_in - times) + f.nth;
+            f.mass = of(m_in - times * each) + f.nth * each_l;
+            __syncthreads();
+            return f;
+        };
+        if (c.k > 0 && (uint64_t)c.k < kept) {
+            const Found f = reach(false, (uint64_t)c.k);
+            kept = f.count;
+            mass = f.mass;
+        }
+        if (c.p < 1.0f) {
+            const Found f = reach(true, cut_target(c.p, mass));
+            if (f.count < kept) { kept = f.count; mass = f.mass; }
+        }
+        if (c.least > 0.0f) {
+            // weights fall with numbers: the last 64 whose first weighs enough, then all in front and those of them that do
+            auto enough = [&](unsigned x) { return x <= top || (x < NONE && w.scaled(logit_of_number(x), 0) >= c.enough()); };
+            if (tid == 0) s.found = 0;
+            __syncthreads();
+            const uint64_t yes = __ballot(enough(64u * tid));
+            if (lane == 0 && yes) atomicMax(&s.found, 64 * wave + 63 - __builtin_clzll(yes));
+            __syncthreads();
+            const int at = s.found;
+            const unsigned x = 64u * at + lane;
+            const uint64_t times = enough(x) ? s.occurs(x) : 0, each = times ? w.mass(logit_of_number(x)) : 0;
+            const uint64_t n_in = __shfl((unsigned long long)wave_scan(times), 63) + (at ? (unsigned)s.count[at - 1] : 0);
+            const uint64_t m_in = __shfl((unsigned long long)wave_scan(times * each), 63) + (at ? s.mass[at - 1] : 0);
+            if (n_in < kept) { kept = n_in; mass = m_in; }
+            __syncthreads();
+        }
+        const Found f = reach(true, draw_target(a.u[b], mass));
+        number = f.number;
+        nth = f.nth;
+    }
+    // the nth token with that number: the part of the row that holds it, then the token.  (Parts of 2^log2 tokens, 1024 at most.  The first of all,
+    // where the likeliest is wanted, does not need its counter, which may have been too small.)
+    const unsigned thousands = (unsigned)(a.V - 1) >> 10;
+    const int log2 = thousands ? 32 - __builtin_clz(thousands) : 0;
+    s.parts[tid] = 0;
+    if (tid == 0) { s.found = 0; s.before = 0; s.token = 0x7FFFFFFF; }
+    __syncthreads();
+    // The number's bits, in both halves of a word; a half that differs from them in nothing is found by what it borrows.  (The upper one's
+    // borrow may be the lower one's: each is looked at before it counts.)
+    const unsigned bits = __float_as_uint(logit_of_number(number)) >> 16, both = bits | bits << 16, relevant = number == ZERO ? 0x7FFF7FFFu : 0xFFFFFFFFu;
+    const bool first = nth == 1 && c.greedy();
+    const bool only = !first && s.occurs(number) == 1;
+    auto mark = [&](unsigned differs, int token) {
+        if (differs) return;
+        if (first) atomicMin(&s.token, token);
+        else if (only) s.token = token;
+        else atomicAdd(&s.parts[token >> log2], 1);
+    };
+    each_piece<R>(row, held, [&](const Piece<false>& piece, int p) {
+        unsigned x[4], zeros = 0;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            x[w] = (piece.v[w] ^ both) & relevant;
+            zeros |= (x[w] - 0x00010001u) & ~x[w];
+        }
+        if ((zeros & 0x80008000u) == 0) return;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            mark(x[w] & 0xFFFFu, row.token(p, 2 * w));
+            mark(x[w] >> 16, row.token(p, 2 * w + 1));
+        }
+    }, [](int) {});
+    if (edge_token >= 0) mark((__float_as_uint(edge_logit) >> 16 ^ bits) & relevant & 0xFFFFu, edge_token);
+    __syncthreads();
+    if (!first && !only) {
+        const uint64_t own = (unsigned)s.parts[tid];
+        uint64_t n = wave_scan(own);
+        if (lane == 63) s.wave_counts[wave] = n;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) n += i < wave ? s.wave_counts[i] : 0;
+        if (n - own < (uint64_t)nth && (uint64_t)nth <= n) { s.found = tid; s.before = (int)(n - own); }
+        __syncthreads();
+        if (wave == 0) {
+            int seen = s.before, token = -1;
+            const int from = s.found << log2, to = from + (1 << log2) < a.V ? from + (1 << log2) : a.V;
+            for (int i0 = from; i0 < to && token < 0; i0 += 64) {
+                const int i = i0 + lane < to ? i0 + lane : to - 1;
+                const bool mine = i0 + lane < to && ((static_cast<const uint16_t*>(row.row)[i] ^ bits) & relevant & 0xFFFFu) == 0;
+                const uint64_t who = __ballot(mine);
+                const int rank = seen + __popcll(who & ((1ull << lane) - 1)) + 1;
+                const uint64_t hit = __ballot(mine && rank == nth);
+                if (hit) token = i0 + __builtin_ctzll(hit);
+                seen += __popcll(who);
+            }
+            if (lane == 0) s.token = token;
+        }
+        __syncthreads();
+    }
+    if (tid == 0) put(a, b, s.token, c.greedy() ? 0.0f : share(w, c.heat, logit_of_number(number), mass), (int)kept);
+}
+
+// ---- in two launches: slices of rows into cells, then a row's cells and what lies in few of them ------------------------------
+//
+// A logit's cell is its place on a grid of step 2^e between 36/2048 and 72/2048 of the temperature, so that 2047 cells cover all that has
+// weight.  Cells are counted from the highest logit's, the last holds whatever lies below; the grid is the temperature's, not the
+// row's, so it is the same for all slices of a row before they know of each other.  The first launch reads the logits once: a slice stays
+// in registers while its maximum is found, then its histogram is.  The second joins a row's histograms, finds the cells in which
+// the cuts and the draw may lie -- one or two each, mostly -- and reads the row again for the tokens in them, some hundred,
+// which are sorted and settle everything exactly.  Rows whose cells hold more tokens than are sorted (nearly equal logits, thousands of
+// equal ones, a high temperature) go by digits.
+//
+// A token's weight is the weight at its cell's lower edge times e^x, x = (z - edge) / T below 0.0352: the histogram sums e^x - 1, and
+// one exponential for each cell follows in the second launch.  e^x - 1 is five terms of its series in fp64, times 2^36, in the lower
+// 48 bits of a cell's 64, the number of tokens in the upper 16: one LDS atomic a token.  (With an exponential and two atomics for each
+// token the first launch took 67 us on 256 rows of 128000 logits, LDS and the vector units at their limits in turn.)  The series and the
+// rounding are good for 2^-37 of a token's weight; of logits on the grid, as coarse ones are, e^x - 1 is 0 and sums are exact.
 
 constexpr int CELLS = SAMPLE_CELLS, SORTED = 4096;
 // the grid of a temperature
@@ -962,9 +1256,14 @@ int launch_sample(SampleArgs a, hipStream_t s) {
     int log2 = 0;
     while ((1ll << log2) < a.V) ++log2;
     a.bits = 62 - log2 < 50 ? 62 - log2 : 50;
-    if (a.V > SAMPLE_LONG) {
-        if (f32) hipLaunchKernelGGL(sample_long_kernel<true>, dim3(a.B), dim3(THREADS), 0, s, a);
-        else hipLaunchKernelGGL(sample_long_kernel<false>, dim3(a.B), dim3(THREADS), 0, s, a);
+    const dim3 row_grid(a.B), block(THREADS);
+    if (a.V > SAMPLE_LONG || !f32) {
+        constexpr int WORD = THREADS * 8;                  // logits of a piece of each thread
+        if (f32) hipLaunchKernelGGL(sample_long_kernel<true>, row_grid, block, 0, s, a);
+        else if (a.V > SAMPLE_LONG) hipLaunchKernelGGL(sample_long_kernel<false>, row_grid, block, 0, s, a);
+        else if (a.V <= 4 * WORD) hipLaunchKernelGGL(sample_numbers_kernel<4>, row_grid, block, 0, s, a);
+        else if (a.V <= 16 * WORD) hipLaunchKernelGGL(sample_numbers_kernel<16>, row_grid, block, 0, s, a);
+        else hipLaunchKernelGGL(sample_numbers_kernel<0>, row_grid, block, 0, s, a);
         return check_hip(hipGetLastError(), "sample launch");
     }
     a.slices = reinterpret_cast<SampleSlice*>(a.workspace);
@@ -984,13 +1283,10 @@ int launch_sample(SampleArgs a, hipStream_t s) {
         p.token += b0;
         if (p.logprob) p.logprob += b0;
         if (p.kept) p.kept += b0;
-        const dim3 grid(a.slices_of_row, rows), block(THREADS);
-        if (f32 && few_rows) hipLaunchKernelGGL((sample_slice_kernel<true, few_pieces(true)>), grid, block, 0, s, p);
-        else if (f32) hipLaunchKernelGGL((sample_slice_kernel<true, many_pieces(true)>), grid, block, 0, s, p);
-        else if (few_rows) hipLaunchKernelGGL((sample_slice_kernel<false, few_pieces(false)>), grid, block, 0, s, p);
-        else hipLaunchKernelGGL((sample_slice_kernel<false, many_pieces(false)>), grid, block, 0, s, p);
-        if (f32) hipLaunchKernelGGL(sample_row_kernel<true>, dim3(rows), block, 0, s, p);
-        else hipLaunchKernelGGL(sample_row_kernel<false>, dim3(rows), block, 0, s, p);
+        const dim3 grid(a.slices_of_row, rows);
+        if (few_rows) hipLaunchKernelGGL((sample_slice_kernel<true, few_pieces(true)>), grid, block, 0, s, p);
+        else hipLaunchKernelGGL((sample_slice_kernel<true, many_pieces(true)>), grid, block, 0, s, p);
+        hipLaunchKernelGGL(sample_row_kernel<true>, dim3(rows), block, 0, s, p);
     }
     return check_hip(hipGetLastError(), "sample launch");
 }
