@@ -225,7 +225,7 @@ struct LookupArgs {
 };
 int launch_lookup_w4a16(LookupArgs a, hipStream_t s);             // lookup_w4a16.hip
 
-constexpr int SAMPLE_CELLS = 2048, SAMPLE_FEW = 1024;
+constexpr int SAMPLE_CELLS = 2048, SAMPLE_FEW = 128;
 struct SampleSlice {          // what one launch leaves the next of a slice of a row
     uint64_t best;            // (key, ~index) of its largest logit
     uint64_t cells[SAMPLE_CELLS];

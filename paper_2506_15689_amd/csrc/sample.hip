@@ -12,6 +12,8 @@
 // 2^-37 of the mass at most.  Sums in fp32 would move the draw of one row in forty to a neighbour, by their 2^-23.)
 #include "basq_internal.h"
 
+#include <type_traits>
+
 namespace basq {
 
 namespace {
@@ -720,19 +722,18 @@ constexpr double PARTS = 68719476736.0;                   // 2^36
 // Few tokens are kept: they are weighed when they are known, and need no masses of cells.
 __device__ __forceinline__ bool few(const Choices& c) { return c.k > 0 && c.k <= SAMPLE_FEW; }
 
-// R: pieces that a thread holds; 2^15 logits of a workgroup at most, which a cell's 48 bits hold
+// The likeliest of the logits that a workgroup holds, (key, ~index), and their cells, counted from its.  Cells are not made where only the
+// likeliest is wanted, or there is none.  R: pieces that a thread holds; 2^15 logits of a workgroup at most, which a cell's 48 bits hold.
+struct Tally {
+    unsigned long long cells[CELLS + 1];                   // (the last takes what is no token)
+    uint64_t tops[WAVES];
+};
 template <bool F32, int R>
-__global__ __launch_bounds__(THREADS) void sample_slice_kernel(SampleArgs a) {
+__device__ __forceinline__ uint64_t tally(Tally& s, const Pieces<F32>& row, const Piece<F32> (&held)[R], int p0, int edge_token, const Choices& c) {
     static_assert(THREADS * R * Piece<F32>::N <= 32768, "and a few at the row's ends");
-    __shared__ unsigned long long cells[CELLS + 1];        // (the last takes what is no token)
-    __shared__ uint64_t tops[WAVES];
-    const int slice = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
-    const Pieces<F32> row(row_of(a, b), a.V);
-    const Choices c(a, b);
-    const int p0 = slice * (THREADS * R);
-    Piece<F32> held[R];
-    row.load(held, p0);
-    const int edge_token = slice == 0 ? row.edge() : -1;
+    const int tid = threadIdx.x;
+    auto& cells = s.cells;
+    auto& tops = s.tops;
     const float edge_logit = row.at(edge_token);
 #pragma unroll
     for (int i = 0; i < CELLS; i += THREADS) cells[i + tid] = 0;
@@ -752,9 +753,7 @@ __global__ __launch_bounds__(THREADS) void sample_slice_kernel(SampleArgs a) {
     best = tops[0];
 #pragma unroll
     for (int i = 1; i < WAVES; ++i) best = tops[i] > best ? tops[i] : best;
-    SampleSlice& out = a.slices[(int64_t)b * a.slices_of_row + slice];
-    if (tid == 0) out.best = best;
-    if (c.greedy() || (unsigned)(best >> 32) <= LOWEST) return;
+    if (c.greedy() || (unsigned)(best >> 32) <= LOWEST) return best;
     const Grid grid(c.heat);
     const int top_cell = grid.cell(logit_of((unsigned)(best >> 32)));
     if (few(c)) {
@@ -785,8 +784,24 @@ __global__ __launch_bounds__(THREADS) void sample_slice_kernel(SampleArgs a) {
             for (int e = 0; e < Piece<F32>::N; ++e) add(held[r][e]);
     }
     __syncthreads();
+    return best;
+}
+
+template <bool F32, int R>
+__global__ __launch_bounds__(THREADS) void sample_slice_kernel(SampleArgs a) {
+    __shared__ Tally s;
+    const int slice = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+    const Pieces<F32> row(row_of(a, b), a.V);
+    const Choices c(a, b);
+    const int p0 = slice * (THREADS * R);
+    Piece<F32> held[R];
+    row.load(held, p0);
+    const uint64_t best = tally<F32, R>(s, row, held, p0, slice == 0 ? row.edge() : -1, c);
+    SampleSlice& out = a.slices[(int64_t)b * a.slices_of_row + slice];
+    if (tid == 0) out.best = best;
+    if (c.greedy() || (unsigned)(best >> 32) <= LOWEST) return;
 #pragma unroll
-    for (int i = 0; i < CELLS; i += THREADS) out.cells[i + tid] = cells[i + tid];
+    for (int i = 0; i < CELLS; i += THREADS) out.cells[i + tid] = s.cells[i + tid];
 }
 
 struct Cells {
@@ -864,9 +879,11 @@ __device__ void sort_keys(uint64_t* key, int n) {
 // each (the middle of logit and bounds; is it the logit; a bit more of a mask), the next block under way meanwhile; hits
 // leave their index only, and the logits of all of them are fetched at the end.  (Tests by masks of the wave, or hits one by one in
 // between, are chains of latencies: 13 .. 28 us for 128000 logits.)
-template <bool F32, int Q>
-__device__ void collect(Cells& s, const Pieces<F32>& row, const int (&from)[3], const int (&to)[3], int top_cell, const Grid& grid) {
-    constexpr int R = 4, N = Piece<F32>::N;
+template <bool F32, int Q, int HELD>
+__device__ __forceinline__ void collect(Cells& s, const Pieces<F32>& row, const Piece<F32> (&have)[HELD ? HELD : 1], const int (&from)[3], const int (&to)[3], int top_cell, const Grid& grid) {
+    constexpr int R = 8, N = Piece<F32>::N;
+    static_assert(HELD == 0 || HELD == R, "");
+    static_assert(R * N <= 32, "a mask");
     const int tid = threadIdx.x;
     float lo[Q], hi[Q];                                    // of a stretch, both within
 #pragma unroll
@@ -887,12 +904,7 @@ __device__ void collect(Cells& s, const Pieces<F32>& row, const int (&from)[3], 
     };
     const int edge = row.edge();
     if (edge >= 0 && wanted(row.at(edge))) keep(edge);
-    Piece<F32> held[R], next[R];
-    row.load(next, 0);
-    for (int p0 = 0; p0 < row.count; p0 += R * THREADS) {
-#pragma unroll
-        for (int r = 0; r < R; ++r) held[r] = next[r];
-        row.load(next, p0 + R * THREADS);
+    auto block = [&](const Piece<F32> (&held)[R], int p0) {
         unsigned hits = 0;
 #pragma unroll
         for (int r = 0; r < R; ++r)
@@ -903,6 +915,18 @@ __device__ void collect(Cells& s, const Pieces<F32>& row, const int (&from)[3], 
             hits &= hits - 1;
             keep(row.token(p0 + i / N * THREADS + tid, i % N));
         }
+    };
+    if constexpr (HELD) {
+        block(have, 0);
+    } else {
+        Piece<F32> held[R], next[R];
+        row.load(next, 0);
+        for (int p0 = 0; p0 < row.count; p0 += R * THREADS) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) held[r] = next[r];
+            row.load(next, p0 + R * THREADS);
+            block(held, p0);
+        }
     }
     __syncthreads();
     const int n = s.n < SORTED ? s.n : SORTED;
@@ -912,15 +936,24 @@ __device__ void collect(Cells& s, const Pieces<F32>& row, const int (&from)[3], 
     }
 }
 
-template <bool F32>
+// HELD: the row is that many pieces of each thread, and no slices were made of it; 0: it is joined from slices.
+template <bool F32, int HELD>
 __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
     __shared__ RowShared shared;
+    __shared__ typename std::conditional<(HELD > 0), Tally, int>::type fresh;
     Cells& s = shared.cells;
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, S = a.slices_of_row;
     const SampleSlice* slices = a.slices + (int64_t)b * S;
     const Choices c(a, b);
+    const Pieces<F32> row(row_of(a, b), a.V);
+    Piece<F32> held[HELD ? HELD : 1];
     uint64_t best = 0;
-    for (int i = 0; i < S; ++i) best = slices[i].best > best ? slices[i].best : best;
+    if constexpr (HELD > 0) {
+        row.load(held, 0);
+        best = tally<F32, HELD>(fresh, row, held, 0, row.edge(), c);
+    } else {
+        for (int i = 0; i < S; ++i) best = slices[i].best > best ? slices[i].best : best;
+    }
     const bool none = (unsigned)(best >> 32) <= LOWEST;
     if (none || c.greedy()) {
         if (tid == 0) put(a, b, none ? -1 : (int)~(unsigned)best, none ? -__builtin_inff() : 0.0f, none ? 0 : 1);
@@ -944,8 +977,16 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
     if (tid == 0) s.n = 0;
     if (tid < 4) s.places[tid] = CELLS - 1;
     __syncthreads();
+    if constexpr (HELD > 0) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint64_t cell = fresh.cells[tid + h * THREADS];
+            s.count[tid + h * THREADS] = (int)(cell >> COUNT_AT);
+            s.mass[tid + h * THREADS] = cell & ((1ull << COUNT_AT) - 1);
+        }
+    }
     constexpr int AT_ONCE = 4;
-    for (int i0 = 0; i0 < S; i0 += AT_ONCE) {
+    for (int i0 = 0; HELD == 0 && i0 < S; i0 += AT_ONCE) {
         uint64_t cell[AT_ONCE][2];
         unsigned key[AT_ONCE];
 #pragma unroll
@@ -1095,12 +1136,9 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
         return;
     }
     // the tokens of those cells, as (key, ~index)
-    {
-        const Pieces<F32> row(row_of(a, b), a.V);
-        if (to[1] < from[1]) collect<F32, 1>(s, row, from, to, top_cell, grid);
-        else if (to[2] < from[2]) collect<F32, 2>(s, row, from, to, top_cell, grid);
-        else collect<F32, 3>(s, row, from, to, top_cell, grid);
-    }
+    if (to[1] < from[1]) collect<F32, 1, HELD>(s, row, held, from, to, top_cell, grid);
+    else if (to[2] < from[2]) collect<F32, 2, HELD>(s, row, held, from, to, top_cell, grid);
+    else collect<F32, 3, HELD>(s, row, held, from, to, top_cell, grid);
     __syncthreads();
     if (n <= THREADS) sort_keys<1>(s.key, n);
     else if (n <= 2 * THREADS) sort_keys<2>(s.key, n);
@@ -1257,6 +1295,10 @@ int launch_sample(SampleArgs a, hipStream_t s) {
     while ((1ll << log2) < a.V) ++log2;
     a.bits = 62 - log2 < 50 ? 62 - log2 : 50;
     const dim3 row_grid(a.B), block(THREADS);
+    if (f32 && a.V <= 32768) {
+        hipLaunchKernelGGL((sample_row_kernel<true, 8>), row_grid, block, 0, s, a);
+        return check_hip(hipGetLastError(), "sample launch");
+    }
     if (a.V > SAMPLE_LONG || !f32) {
         constexpr int WORD = THREADS * 8;                  // logits of a piece of each thread
         if (f32) hipLaunchKernelGGL(sample_long_kernel<true>, row_grid, block, 0, s, a);
@@ -1286,7 +1328,7 @@ int launch_sample(SampleArgs a, hipStream_t s) {
         const dim3 grid(a.slices_of_row, rows);
         if (few_rows) hipLaunchKernelGGL((sample_slice_kernel<true, few_pieces(true)>), grid, block, 0, s, p);
         else hipLaunchKernelGGL((sample_slice_kernel<true, many_pieces(true)>), grid, block, 0, s, p);
-        hipLaunchKernelGGL(sample_row_kernel<true>, dim3(rows), block, 0, s, p);
+        hipLaunchKernelGGL((sample_row_kernel<true, 0>), dim3(rows), block, 0, s, p);
     }
     return check_hip(hipGetLastError(), "sample launch");
 }
