@@ -79,14 +79,32 @@ __device__ __forceinline__ uint64_t moved(uint64_t old, uint64_t v) {
     const unsigned hi = __builtin_amdgcn_update_dpp((int)(old >> 32), (int)(v >> 32), CTRL, ROWS, BANKS, false);
     return (uint64_t)hi << 32 | lo;
 }
-// sums over the lanes in front of this one, and this one: within rows of 16, then row by row
-__device__ __forceinline__ uint64_t wave_scan(uint64_t v) {
-    v += moved<0x111>(0, v);                               // (row_shr 1, 2, 4, 8)
-    v += moved<0x112>(0, v);
-    v += moved<0x114>(0, v);
-    v += moved<0x118>(0, v);
-    v += moved<0x142, 0xA>(0, v);                          // (the last lane of rows 0 and 2, to rows 1 and 3)
-    v += moved<0x143, 0xC>(0, v);                          // (lane 31, to rows 2 and 3)
+template <int CTRL, int ROWS = 0xF, int BANKS = 0xF>
+__device__ __forceinline__ unsigned moved(unsigned old, unsigned v) {
+    return (unsigned)__builtin_amdgcn_update_dpp((int)old, (int)v, CTRL, ROWS, BANKS, false);
+}
+// sums of the lanes of half a wave up to this one, within rows of 16, then over two; then of the wave
+template <class T>
+__device__ __forceinline__ T half_scan(T v) {
+    const T none = 0;
+    v += moved<0x111>(none, v);                            // (row_shr 1, 2, 4, 8)
+    v += moved<0x112>(none, v);
+    v += moved<0x114>(none, v);
+    v += moved<0x118>(none, v);
+    v += moved<0x142, 0xA>(none, v);                       // (the last lane of rows 0 and 2, to rows 1 and 3)
+    return v;
+}
+template <class T>
+__device__ __forceinline__ T wave_scan(T v) {
+    v = half_scan(v);
+    v += moved<0x143, 0xC>((T)0, v);                       // (lane 31, to rows 2 and 3)
+    return v;
+}
+// the largest of all lanes, in lane 63
+__device__ __forceinline__ unsigned wave_most(unsigned v) {
+    auto take = [&](unsigned o) { v = o > v ? o : v; };
+    take(moved<0x111>(0u, v)); take(moved<0x112>(0u, v)); take(moved<0x114>(0u, v)); take(moved<0x118>(0u, v));
+    take(moved<0x142, 0xA>(0u, v)); take(moved<0x143, 0xC>(0u, v));
     return v;
 }
 // the value of lane ^ J
@@ -500,9 +518,8 @@ __global__ __launch_bounds__(THREADS) void sample_numbers_kernel(SampleArgs a) {
         count(edge.x);
     }
     {
-        const uint64_t best = wave_max((uint64_t)(0xFFFFu - (least.x < least.y ? least.x : least.y)));
-        const uint64_t far = wave_max((uint64_t)(most.x > most.y ? most.x : most.y));
-        const uint64_t in = wave_scan((uint64_t)tokens);
+        const unsigned best = wave_most(0xFFFFu - (least.x < least.y ? least.x : least.y)), far = wave_most(most.x > most.y ? most.x : most.y);
+        const unsigned in = wave_scan((unsigned)tokens);
         if (lane == 63) { atomicMin(&s.top, 0xFFFF - (int)best); atomicMax(&s.last, (int)far); atomicAdd(&s.tokens, (int)in); }
     }
     __syncthreads();
@@ -538,19 +555,15 @@ __global__ __launch_bounds__(THREADS) void sample_numbers_kernel(SampleArgs a) {
                 if (__ballot(two[e] != 0) == 0) continue;
                 const int i = i0 + e * THREADS + tid;
                 const unsigned n0 = two[e] & 0xFFFFu, n1 = two[e] >> 16;
-                uint64_t n = n0 + n1, m = 0;
-                if (n0) m = n0 * w.mass(logit_of_number(2 * i));
-                if (n1) m += n1 * w.mass(logit_of_number(2 * i + 1));
-                n = wave_scan(n);
-                m = wave_scan(m);
-                const uint64_t n_low = __shfl((unsigned long long)n, 31), m_low = __shfl((unsigned long long)m, 31);
-                if (lane == 63) { n -= n_low; m -= m_low; }
+                // (weights of both, whether they occur or not: one after the other they would be waited for)
+                const unsigned n = half_scan(n0 + n1);
+                const uint64_t m = half_scan(n0 * w.mass(logit_of_number(2 * i)) + n1 * w.mass(logit_of_number(2 * i + 1)));
                 if ((lane & 31) == 31) { s.count[i >> 5] = (int)n; s.mass[i >> 5] = m; }
             }
         }
         __syncthreads();
         const uint64_t own_n = (unsigned)s.count[tid], own_m = s.mass[tid];
-        uint64_t n = wave_scan(own_n), m = wave_scan(own_m);
+        uint64_t n = wave_scan((unsigned)own_n), m = wave_scan(own_m);
         if (lane == 63) { s.wave_counts[wave] = n; s.wave_masses[wave] = m; }
         if (tid == 0) s.found = 0;
         __syncthreads();
@@ -577,8 +590,8 @@ __global__ __launch_bounds__(THREADS) void sample_numbers_kernel(SampleArgs a) {
             __syncthreads();
             const int at = s.found;
             const unsigned x = 64u * at + lane;
-            const uint64_t times = s.occurs(x), each = times ? w.mass(logit_of_number(x)) : 0;
-            const uint64_t n_in = wave_scan(times) + (at ? (unsigned)s.count[at - 1] : 0), m_in = wave_scan(times * each) + (at ? s.mass[at - 1] : 0);
+            const uint64_t times = s.occurs(x), each = x < NONE ? w.mass(logit_of_number(x)) : 0;
+            const uint64_t n_in = wave_scan((unsigned)times) + (at ? (unsigned)s.count[at - 1] : 0), m_in = wave_scan(times * each) + (at ? s.mass[at - 1] : 0);
             const uint64_t end = by_mass ? m_in : n_in, begin = end - (by_mass ? times * each : times);
             const uint64_t hit = __ballot(begin < target && target <= end);
             const int l = hit ? __builtin_ctzll(hit) : 0;
@@ -586,7 +599,15 @@ __global__ __launch_bounds__(THREADS) void sample_numbers_kernel(SampleArgs a) {
             const uint64_t each_l = of(each), begin_l = of(begin);
             Found f;
             f.number = 64u * at + l;
-            f.nth = (int)(by_mass ? (target - begin_l + each_l - 1) / (each_l ? each_l : 1) : target - begin_l);
+            const uint64_t beyond = target - begin_l;
+            if (by_mass) {
+                // beyond / each, rounded up: below 2^16, so a quotient of doubles is off by one at most
+                f.nth = (int)__builtin_ceil((double)beyond / (double)each_l);
+                if ((uint64_t)(f.nth - 1) * each_l >= beyond) --f.nth;
+                if ((uint64_t)f.nth * each_l < beyond) ++f.nth;
+            } else {
+                f.nth = (int)beyond;
+            }
             f.count = of(n_in - times) + f.nth;
             f.mass = of(m_in - times * each) + f.nth * each_l;
             __syncthreads();
@@ -657,7 +678,7 @@ __global__ __launch_bounds__(THREADS) void sample_numbers_kernel(SampleArgs a) {
     __syncthreads();
     if (!first && !only) {
         const uint64_t own = (unsigned)s.parts[tid];
-        uint64_t n = wave_scan(own);
+        uint64_t n = wave_scan((unsigned)own);
         if (lane == 63) s.wave_counts[wave] = n;
         __syncthreads();
 #pragma unroll
@@ -1025,7 +1046,7 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
                 m[h] = (uint64_t)__builtin_rint(sum * w.scaled((float)edge, w.bits));
             }
         }
-        const uint64_t n_in = wave_scan(n[0] + n[1]), m_in = wave_scan(m[0] + m[1]);
+        const uint64_t n_in = wave_scan((unsigned)(n[0] + n[1])), m_in = wave_scan(m[0] + m[1]);
         if (lane == 63) { s.wave_counts[wave] = n_in; s.wave_masses[wave] = m_in; }
         __syncthreads();
         uint64_t nb = n_in - n[0] - n[1], mb = m_in - m[0] - m[1];
