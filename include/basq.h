@@ -411,8 +411,8 @@ int basq_paged_attention(const void* q, int64_t ldq, int32_t B, int32_t q_len, i
  *
  *     Y[m,n] = sum_g w_scale[n,g] * sum_{k in g} (q[n,k] - w_zero[n,g]) X[m,k]  +  bias[n]
  *
- *   X          bf16 [M, ldx], 16-byte aligned, ldx >= K, a multiple of 8, up to 2^23.  A token with a value that is not finite, or beyond
- *              2^112, has outputs that are not finite; the others do not
+ *   X          bf16 [M, ldx], 16-byte aligned, ldx >= K, a multiple of 8, up to 2^23.  A token with a value that is not finite has
+ *              outputs that are not finite, and one with values beyond 2^100 may have; they leave the others alone
  *   Wq         uint8 [N, K/2] canonical, or the layout of basq_pack_decode with w_layout = BASQ_W_DECODE16 (K % 128 == 0);
  *              16-byte aligned
  *   group_size channels of a group: a multiple of 32 that divides K; 0 counts as K.  (basq_quantize_weights makes such weights of
@@ -420,7 +420,7 @@ int basq_paged_attention(const void* q, int64_t ldq, int32_t B, int32_t q_len, i
  *   w_scale, w_zero   bf16 [N, K / group_size], zero points in code units (any real value)
  *   bias       fp32 [N], or NULL (= 0)
  *   Y          out, [M, ldy], ldy >= N: fp32 where y_f32, otherwise bf16
- * K % 32 == 0, K <= 2^20.  Laid out for few tokens: the weights are read once for every 64.  M up to 1048560 (else
+ * K % 32 == 0.  Laid out for few tokens: the weights are read once for every 64.  K up to 2^20, N up to 2^28, M up to 1048560 (else
  * BASQ_EUNSUPPORTED); M == 0 does nothing.  Results do not change from call to call.
  */
 int basq_w4a16_gemm(const void* X, int64_t M, int32_t K, int64_t ldx, const uint8_t* Wq, int32_t N, int32_t w_layout,
@@ -434,7 +434,7 @@ int basq_w4a16_gemm(const void* X, int64_t M, int32_t K, int64_t ldx, const uint
  *
  *   ids        int32 [T]; one that is negative or >= N (padding) gives a row of zeros
  *   Y          out, bf16 [T, ldy], 16-byte aligned, ldy >= K and a multiple of 8
- * The matrix as above.  T == 0 does nothing.
+ * The matrix as above.  T up to 2^30 (else BASQ_EUNSUPPORTED); T == 0 does nothing.
  */
 int basq_w4a16_lookup(const int32_t* ids, int64_t T, const uint8_t* Wq, int32_t N, int32_t K, int32_t w_layout, const void* w_scale,
                       const void* w_zero, int32_t group_size, float scale, void* Y, int64_t ldy, void* stream);
@@ -480,7 +480,8 @@ int basq_sample(const void* logits, int64_t ldl, int32_t B, int32_t V, int32_t f
  *   new_tokens   int32 [B]; NULL: q_len of each
  *   q_len        > 0: token places lie in B runs of q_len, T = B * q_len, and a sequence's new tokens are the last of its run
  *                0: they lie packed, sequence behind sequence, from 0 on
- *   positions, slots   out, int32 [T]; -1 for places without a token (padding to the operators that read them)
+ *   positions, slots   out, int32 [T]; -1 for places without a token (padding to the operators that read them), slots also where the page
+ *                      in the table or among the free ones is negative, or the slot would not be an int32
  *   starts       out, int32 [B + 1] or NULL, with q_len = 0: where each sequence's tokens start; the last is their number
  *   batch_table  out, int32 [B, columns], row stride batch_stride, or NULL: the pages of the batch's sequences; entries past them are
  *                left as they were

@@ -13,6 +13,7 @@ int check_matrix(const uint8_t* Wq, int32_t N, int32_t K, int32_t w_layout, cons
     if (N < 1) return fail(BASQ_EINVAL, "N must be >= 1 (got %d)", N);
     if (K < 32 || K % 32 != 0) return fail(BASQ_EINVAL, "K must be a positive multiple of 32 (got %d)", K);
     if (K > 1 << 20) return fail(BASQ_EUNSUPPORTED, "K up to 2^20 is supported (got %d)", K);
+    if (N > 1 << 28) return fail(BASQ_EUNSUPPORTED, "N up to 2^28 is supported (got %d)", N);
     if (w_layout != BASQ_W_CANONICAL && w_layout != BASQ_W_DECODE16) return fail(BASQ_EINVAL, "unknown w_layout %d", w_layout);
     if (w_layout == BASQ_W_DECODE16 && K % 128 != 0) return fail(BASQ_EINVAL, "the streaming layout needs K %% 128 == 0 (got %d)", K);
     if (*group == 0) *group = K;
@@ -61,6 +62,7 @@ int basq_w4a16_gemm(const void* X, int64_t M, int32_t K, int64_t ldx, const uint
 int basq_w4a16_lookup(const int32_t* ids, int64_t T, const uint8_t* Wq, int32_t N, int32_t K, int32_t w_layout, const void* w_scale,
                       const void* w_zero, int32_t group_size, float scale, void* Y, int64_t ldy, void* stream) {
     if (T < 0 || T > 0x7FFFFFFFll) return fail(BASQ_EINVAL, "T must be 0 .. 2^31 - 1 (got %lld)", (long long)T);
+    if (T > 1 << 30) return fail(BASQ_EUNSUPPORTED, "T up to 2^30 is supported (got %lld)", (long long)T);
     int rc = check_matrix(Wq, N, K, w_layout, w_scale, w_zero, &group_size);
     if (rc != BASQ_OK) return rc;
     if (!isfinite(scale)) return fail(BASQ_EINVAL, "scale must be finite (got %g)", (double)scale);

@@ -569,3 +569,108 @@ def test_on_another_stream():
     step(stream)
     stream.synchronize()
     step.check(before)
+
+
+# ---- calls that documentation allows and that are rarer ---------------------------------------------
+
+@pytest.mark.parametrize("M,K,N,G,layout", [(2, 1 << 20, 17, 128, CANONICAL), (17, 1 << 20, 16, 1 << 19, STREAMED), (1, 1 << 20, 1, 32, CANONICAL), (70, 256, 13000, 64, STREAMED),
+                                            (3, 128, 100000, 128, STREAMED), (40, 512, 100000, 128, STREAMED), (1100, 160, 33, 160, CANONICAL)])
+def test_products_that_are_long_or_wide(M, K, N, G, layout):
+    test_product(M, K, N, G, layout)
+
+
+def test_lookup_of_many_tokens():
+    """More of them than one dimension of a launch has."""
+    T, K, N = 70001, 32, 50
+    g = gen(11)
+    codes, s, z = weights(g, N, K, 32)
+    ids = torch.randint(-2, N + 2, (T,), generator=g, dtype=I32, device=DEV)
+    y = torch.full((T, K), 7.0, dtype=BF16, device=DEV)
+    B.basq_w4a16_lookup(ids, codes, s, z, y, 3.0)
+    x = ref.lookup(ids, codes, s, z, 3.0)
+    check_stored(y, x, x.abs() * 2.0 ** -22)
+
+
+def test_draws_in_parts():
+    """1100 rows in two slices each: more than the workspace holds at once.  Some rows against the definition, all against calls of few."""
+    rows, V = 1100, 40000
+    g = gen(12)
+    logits = bell(g, rows, V, torch.float32)
+    rng = random.Random(12)
+    u, heat = [rng.random() for _ in range(rows)], [rng.choice([0.0, 0.7, 1.0, 1.4]) for _ in range(rows)]
+    k, p = [rng.choice([0, 0, 5, 300]) for _ in range(rows)], [rng.choice([1.0, 0.9, 0.3]) for _ in range(rows)]
+    whole = draw(logits, u, temperature=heat, top_k=k, top_p=p)
+    for at in range(0, rows, 220):
+        part = slice(at, at + 220)
+        some = draw(logits[part], u[part], temperature=heat[part], top_k=k[part], top_p=p[part])
+        assert all(a[part] == b for a, b in zip(whole, some))
+    pick = [0, 1, 511, 512, 1022, 1023, 1024, 1025, 1099]
+    check_draw(logits[pick], [u[i] for i in pick], temperature=[heat[i] for i in pick], top_k=[k[i] for i in pick], top_p=[p[i] for i in pick])
+
+
+@pytest.mark.parametrize("V", [900, 50000])
+@pytest.mark.parametrize("dtype", [torch.float32, BF16])
+def test_temperatures_at_the_ends(V, dtype):
+    heat = [math.inf, 3e38, 1e30, 1e4, 1e-4, 1e-20, 1e-37, 1e-42, -0.0, -math.inf]
+    rng = random.Random(13)
+    check_draw(bell(gen(13), len(heat), V, dtype), [rng.random() for _ in heat], temperature=heat, top_p=[0.9, 1.0] * 5)
+
+
+def test_two_captured_draws_share_a_workspace():
+    """One behind the other, with different rows, temperatures and numbers of rows."""
+    g = gen(14)
+    V, calls = 40000, []
+    work = torch.full((B.basq_sample_workspace_bytes(5, V),), 0xA5, dtype=torch.uint8, device=DEV)
+    for rows, heat in ((5, 0.8), (3, 1.5)):
+        c = dict(logits=bell(g, rows, V, torch.float32), u=torch.rand(rows, generator=g, dtype=torch.float64, device=DEV), token=torch.zeros(rows, dtype=I32, device=DEV),
+                 heat=torch.full((rows,), heat, device=DEV), top_p=torch.full((rows,), 0.95, device=DEV))
+        calls.append(c)
+
+    def run(c):
+        B.basq_sample(c["logits"], c["u"], c["token"], work, temperature=c["heat"], top_p=c["top_p"])
+
+    graphs = []
+    for c in calls:
+        run(c)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            run(c)
+        graphs.append(graph)
+    for _ in range(4):
+        for c in calls:
+            c["u"].uniform_()
+            c["logits"][:, ::7] += 0.5                            # (tokens of the step before would be found out)
+        graphs[0].replay()
+        graphs[1].replay()
+        for c in calls:
+            rows, u = c["logits"].cpu().double().numpy(), c["u"].tolist()
+            want = [ref.sample_row(r, temperature=float(np.float32(h)), top_p=float(np.float32(0.95)), u=x)[0] for r, h, x in zip(rows, c["heat"].tolist(), u)]
+            assert c["token"].tolist() == want
+
+
+@pytest.mark.parametrize("T", [8, 5000])
+def test_pages_that_are_none(T):
+    """A negative page, in the table or among the free ones: its tokens have places, but no slots."""
+    ints = lambda v: torch.tensor(v, dtype=I32, device=DEV)  # noqa: E731
+    table, free = ints([[4, -1, 9], [-2, 0, 0]]), ints([-5, 7])
+    lengths, count, status = ints([18, 15]), ints([2]), ints([9, 9])
+    positions, slots = torch.full((T,), 55, dtype=I32, device=DEV), torch.full((T,), 55, dtype=I32, device=DEV)
+    work = torch.zeros(B.basq_kv_books_bytes(2), dtype=torch.uint8, device=DEV)
+    B.basq_kv_extend(lengths, table, free, count, ints([2, 4]), 16, positions, slots, status, work, q_len=0)
+    assert status.tolist() == [0, 0] and lengths.tolist() == [20, 19] and count.tolist() == [1]
+    assert positions.tolist() == [18, 19, 15, 16, 17, 18] + [-1] * (T - 6)
+    assert slots.tolist() == [-1, -1, -1, 112, 113, 114] + [-1] * (T - 6)
+    assert table.tolist() == [[4, -1, 9], [-2, 7, 0]]
+
+
+@pytest.mark.parametrize("Bn,packed", [(3, True), (200, True), (130, False)])
+def test_sequences_that_only_lose_tokens(Bn, packed):
+    """Every one of them to nothing, and from nothing on again."""
+    rng = random.Random(Bn)
+    books = make_books(rng, Bn, 6, 16, 2, 90)
+    gpu = on_gpu(books)
+    seqs = list(range(Bn))
+    had = list(books["lengths"])
+    check_extend(books, gpu, seqs, [-n for n in had], 16, 0 if packed else 90, 5 if packed else 90 * Bn)
+    assert books["lengths"] == [0] * Bn and len(books["free"]) == books["capacity"]
+    check_extend(books, gpu, seqs[::-1], had, 16, 0 if packed else 90, sum(had) if packed else 90 * Bn)

@@ -35,7 +35,7 @@ MATRIX = [
     (dict(w_layout=2), B.BASQ_EINVAL), (dict(w_layout=1, K=160, group_size=32), B.BASQ_EINVAL), (dict(group_size=16), B.BASQ_EINVAL),
     (dict(group_size=48), B.BASQ_EINVAL), (dict(group_size=96), B.BASQ_EINVAL), (dict(group_size=-32), B.BASQ_EINVAL), (dict(Wq=None), B.BASQ_EINVAL),
     (dict(Wq=ODD), B.BASQ_EINVAL), (dict(w_scale=None), B.BASQ_EINVAL), (dict(w_zero=None), B.BASQ_EINVAL), (dict(w_scale=BYTE), B.BASQ_EINVAL),
-    (dict(w_zero=BYTE), B.BASQ_EINVAL), (dict(Y=None), B.BASQ_EINVAL),
+    (dict(w_zero=BYTE), B.BASQ_EINVAL), (dict(Y=None), B.BASQ_EINVAL), (dict(N=(1 << 28) + 1), B.BASQ_EUNSUPPORTED),
 ]
 
 
@@ -56,7 +56,7 @@ def lookup(lib, **kw):
 
 
 @pytest.mark.parametrize("kw,code", MATRIX + [
-    (dict(T=-1), B.BASQ_EINVAL), (dict(T=1 << 31), B.BASQ_EINVAL), (dict(ids=None), B.BASQ_EINVAL), (dict(ids=OFF), B.BASQ_EINVAL),
+    (dict(T=-1), B.BASQ_EINVAL), (dict(T=1 << 31), B.BASQ_EINVAL), (dict(T=(1 << 30) + 1), B.BASQ_EUNSUPPORTED), (dict(ids=None), B.BASQ_EINVAL), (dict(ids=OFF), B.BASQ_EINVAL),
     (dict(Y=ODD), B.BASQ_EINVAL), (dict(ldy=248), B.BASQ_EINVAL), (dict(ldy=260), B.BASQ_EINVAL), (dict(scale=float("inf")), B.BASQ_EINVAL),
 ])
 def test_lookup_refuses(lib, kw, code):
