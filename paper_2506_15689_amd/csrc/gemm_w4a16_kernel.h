@@ -8,7 +8,9 @@
 // rounded to bf16 would put 2^-9 on each; with 128 + q, the next such form, eight times as much cancels in the difference.)  The
 // sums of x over a group are one more product, with ones.
 //
-// One pass over the weights, which bound it: each lane requests its batch of 16-byte pieces before it takes any up.  A workgroup
+// One pass over the weights, which bound it where they are large (16 x 8192 x 128000, 565 MB: 140 us, 4.0 TB/s, the memory path alone 116);
+// smaller calls are bound by the waits of a step, of which each wave has few (1 x 4096 x 4096 4.2 us, 13 x 14336 x 4096 16.7, 48 x 4096 x
+// 11008 17.8; their bytes 1.3, 4.9 and 4.3).  Each lane requests its batch of 16-byte pieces before it takes any up.  A workgroup
 // owns TILES tiles of 16 weight rows, its waves share K in chunks of 128 channels; D = x (rows) times weights (columns), so a
 // lane's results belong to one weight row and take one scale.
 //
@@ -50,13 +52,13 @@ __device__ __forceinline__ v4u transposed(v4u r) {
 }
 
 // NW: waves that take different tiles and share the tokens' channels.   KW: groups of them that share K.   STEPS: chunks of a step.
-// XSTEPS: chunks of
-// which the tokens are in LDS at once.   TILES: weight tiles of a wave.   TT: tiles of 16 tokens, of which ROWS are there (all, but of one tile).   UNIT: channels that certainly
-// share a group: 128, 64 or 32.   SIDE: scales of a step's chunks lie side by side, all of them there.
+// XSTEPS: chunks of which the tokens are in LDS at once.   TILES: weight tiles of a wave.   TT: tiles of 16 tokens, of which ROWS are
+// there (all, but of one tile).   UNIT: channels that certainly share a group: 128, 64 or 32.   SIDE: scales of a step's chunks lie
+// side by side, all of them there.
 //
 // Tokens go through LDS: read row by row, a row's 256 bytes of a chunk by 16 lanes, and put down in the order of the operands, in places
 // that 16 rows reach without conflicts.  (Read as operands straight from memory, 16 bytes of 16 rows at a time, they cost more than the
-// weights: 16 x 8192 x 128000 162 us, as built 129.)  A step's weights, scales and tokens are under way while the step before is
+// weights: 16 x 8192 x 128000 162 us, through LDS 129 at the time.)  A step's weights, scales and tokens are under way while the step before is
 // multiplied, and nothing else is: with more steps under way the waits, which count loads in their order, saved nothing.
 template <bool STREAM_LAYOUT, int NW, int KW, int STEPS, int XSTEPS, int TILES, int TT, int ROWS, int UNIT, bool SIDE>
 __global__ __launch_bounds__(NW * KW * 64) void gemm_w4a16_kernel(W4A16Args a) {

