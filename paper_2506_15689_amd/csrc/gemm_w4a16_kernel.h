@@ -8,9 +8,9 @@
 // rounded to bf16 would put 2^-9 on each; with 128 + q, the next such form, eight times as much cancels in the difference.)  The
 // sums of x over a group are one more product, with ones.
 //
-// One pass over the weights, which bound it where they are large (16 x 8192 x 128000, 565 MB: 140 us, 4.0 TB/s, the memory path alone 116);
-// smaller calls are bound by the waits of a step, of which each wave has few (1 x 4096 x 4096 4.2 us, 13 x 14336 x 4096 16.7, 48 x 4096 x
-// 11008 17.8; their bytes 1.3, 4.9 and 4.3).  Each lane requests its batch of 16-byte pieces before it takes any up.  A workgroup
+// One pass over the weights, which bound it where they are large (16 x 8192 x 128000, 565 MB: 118 us, 4.8 TB/s, vector instructions half of the time);
+// smaller calls are bound by the waits of a step, of which each wave has few (1 x 4096 x 4096 4.2 us, 13 x 14336 x 4096 16.4, 48 x 4096 x
+// 11008 17.4; their bytes 1.3, 4.9 and 4.3).  Each lane requests its batch of 16-byte pieces before it takes any up.  A workgroup
 // owns TILES tiles of 16 weight rows, its waves share K in chunks of 128 channels; D = x (rows) times weights (columns), so a
 // lane's results belong to one weight row and take one scale.
 //
@@ -31,9 +31,9 @@ typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 
 constexpr int TILE = 16;
 
-// 8 codes -> 16 + code in bf16: pairs (0,4) (1,5) (2,6) (3,7) of the dword's channels
-__device__ __forceinline__ v8b widen(unsigned v) {
-    constexpr unsigned mask = 0x00780078u, base = 0x41804180u;
+// 8 codes -> 16 + code in bf16: pairs (0,4) (1,5) (2,6) (3,7) of the dword's channels.  (The constants come in registers, of either kind,
+// as only then they go into one and-or.)
+__device__ __forceinline__ v8b widen(unsigned v, unsigned mask, unsigned base) {
     const v4u r = {(v << 3 & mask) | base, (v >> 1 & mask) | base, (v >> 5 & mask) | base, (v >> 9 & mask) | base};
     return __builtin_bit_cast(v8b, r);
 }
@@ -61,7 +61,7 @@ __device__ __forceinline__ v4u transposed(v4u r) {
 // weights: 16 x 8192 x 128000 162 us, through LDS 129 at the time.)  A step's weights, scales and tokens are under way while the step before is
 // multiplied, and nothing else is: with more steps under way the waits, which count loads in their order, saved nothing.
 template <bool STREAM_LAYOUT, int NW, int KW, int STEPS, int XSTEPS, int TILES, int TT, int ROWS, int UNIT, bool SIDE>
-__global__ __launch_bounds__(NW * KW * 64) void gemm_w4a16_kernel(W4A16Args a) {
+__global__ __launch_bounds__(NW * KW * 64, 2) void gemm_w4a16_kernel(W4A16Args a) {
     constexpr int UNITS = 128 / UNIT;                                          // of a chunk
     constexpr int NT = TILES * TT, WG_TILES = NW * TILES;
     constexpr int BUFS = NW > 1 ? 2 : 1;                                       // (a wave by itself reads before it writes again)
@@ -69,7 +69,9 @@ __global__ __launch_bounds__(NW * KW * 64) void gemm_w4a16_kernel(W4A16Args a) {
     constexpr int XS = BUFS * KW * XSTEPS * CHUNK, PART = KW * NW * NT * 64;
     constexpr int FOURS = CHUNK / 64;                                          // a load of a wave is 4 rows of a chunk
     constexpr int LOADS = (XSTEPS * FOURS + NW - 1) / NW;                       // pieces of tokens that a lane fetches for a step
-    __shared__ v4u lds[XS > PART ? XS : PART];
+    constexpr bool BLOCKS = SIDE && NW > 1 && KW == 1 && XSTEPS == STEPS;                 // scales by way of LDS
+    static_assert(!BLOCKS || (STEPS == 4 && TILES == 1), "");
+    __shared__ v4u lds[XS > PART ? XS : PART], scales[BLOCKS ? NW * KW * 64 : 1];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int nw = wave % NW, kw = wave / NW;
@@ -100,6 +102,9 @@ __global__ __launch_bounds__(NW * KW * 64) void gemm_w4a16_kernel(W4A16Args a) {
         s_lane[t] = (unsigned)(n - nt0) * (unsigned)groups;
     }
 
+    unsigned mask = 0x00780078u, base = 0x41804180u;
+    asm("" : "+s"(mask));
+    asm("" : "+v"(base));
     const v4f zero = {0.f, 0.f, 0.f, 0.f};
     const v4u ones_bits = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
     const v8b ones = __builtin_bit_cast(v8b, ones_bits);
@@ -112,13 +117,26 @@ __global__ __launch_bounds__(NW * KW * 64) void gemm_w4a16_kernel(W4A16Args a) {
         v4u w[TILES][STEPS];
         unsigned sw[TILES][PAIRS], zp[TILES][PAIRS];                           // two in each
     };
+    // Scales in blocks of 16 groups, a lane with half of a row's scales or zero points: of 4 groups at a time, 8 bytes of 16 lines, the lines
+    // came from L2 again for every step, as many bytes as the weights.  (Halves that reach past a row's end end there; 8 groups at least.)
+    v4u block = {0, 0, 0, 0};
+    int block_at = -1;
+    auto first_of = [&](int c0) { return (c0 < chunks ? c0 : chunks - STEPS) * UNITS; };        // (past the last: the last, with tokens of 0)
+    auto block_of = [&](int c0) { return first_of(c0) & ~15; };
     auto fetch = [&](Batch& to, int c0) {
 #pragma unroll
         for (int i = 0; i < STEPS; ++i)
 #pragma unroll
             for (int t = 0; t < TILES; ++t)
                 to.w[t][i] = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(rsrc_w, w_lane + (t * TILE * KB + (c0 + i) * WSTEP), 0, 2 /* once */));
-        if constexpr (SIDE) {
+        if constexpr (BLOCKS) {
+            const int from = block_of(c0);
+            if (from != block_at) {
+                block_at = from;
+                const int half = sub & 1, start = from + 8 * half < groups - 8 ? from + 8 * half : groups - 8;
+                __builtin_memcpy(&block, (sub & 2 ? z_base[0] : s_base[0]) + start + s_lane[0], 16);
+            }
+        } else if constexpr (SIDE) {
             const int c = c0 < chunks ? c0 : 0;
 #pragma unroll
             for (int t = 0; t < TILES; ++t) {
@@ -158,12 +176,24 @@ __global__ __launch_bounds__(NW * KW * 64) void gemm_w4a16_kernel(W4A16Args a) {
             const int at = (i * NW + nw) % (XSTEPS * FOURS), r = 4 * (at % FOURS % (ROWS / 4)) + sub;
             lds[(buf * KW + kw) * (XSTEPS * CHUNK) + at / FOURS * CHUNK + at % FOURS * 64 + sub * 16 + (row ^ r)] = in_pairs(x_next[i]);
         }
+        if constexpr (BLOCKS) scales[wave * 64 + lane] = block;
         if constexpr (NW > 1) __syncthreads();
         else __builtin_amdgcn_wave_barrier();
     };
     auto number = [](const unsigned (&pairs)[PAIRS], int i) { return __uint_as_float(i & 1 ? pairs[i / 2] & 0xFFFF0000u : pairs[i / 2] << 16); };
     const int own = row & (ROWS - 1);
-    auto multiply = [&](const Batch& of, int i0, int buf) {
+    auto multiply = [&](Batch& of, int c0, int i0, int buf) {
+        if constexpr (BLOCKS) {
+            constexpr int SPAN = STEPS * UNITS, PARTS = (SPAN + 7) / 8, EACH = SPAN / PARTS;
+            const int first = first_of(c0);
+#pragma unroll
+            for (int h = 0; h < PARTS; ++h) {
+                const int g = first + 8 * h, half = g >> 3 & 1, start = (g & ~7) < groups - 8 ? g & ~7 : groups - 8;
+                const uint8_t* from = reinterpret_cast<const uint8_t*>(scales + wave * 64 + half * 16 + row) + (g - start) * 2;
+                __builtin_memcpy(of.sw[0] + h * (EACH / 2), __builtin_assume_aligned(from, 8), EACH * 2);
+                __builtin_memcpy(of.zp[0] + h * (EACH / 2), __builtin_assume_aligned(from + 512, 8), EACH * 2);
+            }
+        }
         const v4u* xs = lds + (buf * KW + kw) * (XSTEPS * CHUNK);
 #pragma unroll
         for (int j = 0; j < XSTEPS; ++j) {
@@ -195,7 +225,7 @@ __global__ __launch_bounds__(NW * KW * 64) void gemm_w4a16_kernel(W4A16Args a) {
                     for (int q = 0; q < PARTS; ++q) {
                         unsigned word = d[t][u * PARTS + q];
                         if constexpr (TT > 1) asm volatile("" : "+v"(word));
-                        const v8b codes = widen(word);
+                        const v8b codes = widen(word, mask, base);
 #pragma unroll
                         for (int tt = 0; tt < TT; ++tt) r[tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[tt][q], codes, r[tt], 0, 0, 0);
                     }
@@ -227,11 +257,11 @@ __global__ __launch_bounds__(NW * KW * 64) void gemm_w4a16_kernel(W4A16Args a) {
         for (int s = 0; s < steps; s += 2) {
             put_tokens(0);
             if (s + 1 < steps) { fetch(two, c + NEXT); fetch_tokens(c + NEXT); }
-            multiply(one, 0, 0);
+            multiply(one, c, 0, 0);
             if (s + 1 >= steps) break;
             put_tokens(BUFS - 1);
             if (s + 2 < steps) { fetch(one, c + 2 * NEXT); fetch_tokens(c + 2 * NEXT); }
-            multiply(two, 0, BUFS - 1);
+            multiply(two, c + NEXT, 0, BUFS - 1);
             c += 2 * NEXT;
         }
     } else {
@@ -242,7 +272,7 @@ __global__ __launch_bounds__(NW * KW * 64) void gemm_w4a16_kernel(W4A16Args a) {
                 const int buf = i / XSTEPS & (BUFS - 1);
                 put_tokens(buf);
                 if (i + XSTEPS < STEPS) fetch_tokens(c + i + XSTEPS);
-                multiply(one, i, buf);
+                multiply(one, c, i, buf);
             }
             c += NEXT;
             if (s + 1 < steps) { fetch(one, c); fetch_tokens(c); }
@@ -291,7 +321,8 @@ template <bool SL, int UNIT, bool SIDE, int ROWS>
 void launch_16(const W4A16Args& a, hipStream_t s) {
     const int tiles = tiles_of(a), chunks = (a.K + 127) / 128;
     const bool fours = !SIDE || chunks % 4 == 0;                               // (scales side by side need whole steps)
-    if (tiles > MANY_TILES && fours) launch_shape<SL, 4, 1, 4, 4, 1, 1, ROWS, UNIT, SIDE>(a, s);
+    const bool blocks = fours && (!SIDE || a.groups >= 8);
+    if (tiles > MANY_TILES && blocks) launch_shape<SL, 4, 1, 4, 4, 1, 1, ROWS, UNIT, SIDE>(a, s);
     else if (tiles > FEW_TILES && fours) launch_shape<SL, 4, 2, 4, 4, 1, 1, ROWS, UNIT, SIDE>(a, s);
     else if (chunks < 16 || (SIDE && chunks % 2 != 0)) launch_shape<SL, 1, 8, 1, 1, 1, 1, ROWS, UNIT, SIDE>(a, s);
     else if (ROWS < 16 || tiles <= 256) {
