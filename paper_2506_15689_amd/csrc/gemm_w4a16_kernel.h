@@ -8,9 +8,9 @@
 // rounded to bf16 would put 2^-9 on each; with 128 + q, the next such form, eight times as much cancels in the difference.)  The
 // sums of x over a group are one more product, with ones.
 //
-// One pass over the weights, which bound it where they are large (16 x 8192 x 128000, 565 MB: 118 us, 4.8 TB/s, vector instructions half of the time);
+// One pass over the weights, which bound it where they are large (16 x 8192 x 128000, 565 MB: 117 us, 4.8 TB/s, vector instructions half of the time);
 // smaller calls are bound by the waits of a step, of which each wave has few (1 x 4096 x 4096 4.2 us, 13 x 14336 x 4096 16.4, 48 x 4096 x
-// 11008 17.4; their bytes 1.3, 4.9 and 4.3).  Each lane requests its batch of 16-byte pieces before it takes any up.  A workgroup
+// 11008 17.2; their bytes 1.3, 4.9 and 4.3).  Each lane requests its batch of 16-byte pieces before it takes any up.  A workgroup
 // owns TILES tiles of 16 weight rows, its waves share K in chunks of 128 channels; D = x (rows) times weights (columns), so a
 // lane's results belong to one weight row and take one scale.
 //
@@ -58,8 +58,10 @@ __device__ __forceinline__ v4u transposed(v4u r) {
 //
 // Tokens go through LDS: read row by row, a row's 256 bytes of a chunk by 16 lanes, and put down in the order of the operands, in places
 // that 16 rows reach without conflicts.  (Read as operands straight from memory, 16 bytes of 16 rows at a time, they cost more than the
-// weights: 16 x 8192 x 128000 162 us, through LDS 129 at the time.)  A step's weights, scales and tokens are under way while the step before is
-// multiplied, and nothing else is: with more steps under way the waits, which count loads in their order, saved nothing.
+// weights: 16 x 8192 x 128000 162 us, through LDS 129 at the time.)  A step's weights, scales and tokens are under way while the step before
+// is multiplied: tokens first, which have to be in LDS first, as waits count loads in their order, and requested past the end too, where
+// they come back as 0 at once, as a branch around them would make the wait behind it one for all of them (16 x 4096 x 32000 20.0 us with
+// the branches, without 18.3).
 template <bool STREAM_LAYOUT, int NW, int KW, int STEPS, int XSTEPS, int TILES, int TT, int ROWS, int UNIT, bool SIDE>
 __global__ __launch_bounds__(NW * KW * 64, 2) void gemm_w4a16_kernel(W4A16Args a) {
     constexpr int UNITS = 128 / UNIT;                                          // of a chunk
@@ -128,14 +130,9 @@ __global__ __launch_bounds__(NW * KW * 64, 2) void gemm_w4a16_kernel(W4A16Args a
         for (int i = 0; i < STEPS; ++i)
 #pragma unroll
             for (int t = 0; t < TILES; ++t)
-                to.w[t][i] = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(rsrc_w, w_lane + (t * TILE * KB + (c0 + i) * WSTEP), 0, 2 /* once */));
+                to.w[t][i] = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(rsrc_w, w_lane + (c0 + i < chunks ? t * TILE * KB + (c0 + i) * WSTEP : BEYOND), 0, 2 /* once */));
         if constexpr (BLOCKS) {
-            const int from = block_of(c0);
-            if (from != block_at) {
-                block_at = from;
-                const int half = sub & 1, start = from + 8 * half < groups - 8 ? from + 8 * half : groups - 8;
-                __builtin_memcpy(&block, (sub & 2 ? z_base[0] : s_base[0]) + start + s_lane[0], 16);
-            }
+            // (with the tokens)
         } else if constexpr (SIDE) {
             const int c = c0 < chunks ? c0 : 0;
 #pragma unroll
@@ -162,6 +159,14 @@ __global__ __launch_bounds__(NW * KW * 64, 2) void gemm_w4a16_kernel(W4A16Args a
     };
     v4u x_next[LOADS];
     auto fetch_tokens = [&](int c0) {
+        if constexpr (BLOCKS) {
+            const int from = block_of(c0);
+            if (from != block_at) {
+                block_at = from;
+                const int half = sub & 1, start = from + 8 * half < groups - 8 ? from + 8 * half : groups - 8;
+                __builtin_memcpy(&block, (sub & 2 ? z_base[0] : s_base[0]) + start + s_lane[0], 16);
+            }
+        }
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int at = (i * NW + nw) % (XSTEPS * FOURS), c = c0 + at / FOURS;               // (past the last: the first again)
@@ -169,6 +174,7 @@ __global__ __launch_bounds__(NW * KW * 64, 2) void gemm_w4a16_kernel(W4A16Args a
             if (c >= chunks || (!STREAM_LAYOUT && 128 * c + 8 * row >= a.K)) from = BEYOND;
             x_next[i] = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(rsrc_x, from, 0, 0));
         }
+        __builtin_amdgcn_sched_barrier(0);
     };
     auto put_tokens = [&](int buf) {
 #pragma unroll
@@ -250,17 +256,20 @@ __global__ __launch_bounds__(NW * KW * 64, 2) void gemm_w4a16_kernel(W4A16Args a
     const int steps = (chunks + NEXT - 1) / NEXT;
     int c = kw * STEPS;
     Batch one;
-    fetch(one, c);
     fetch_tokens(c);
+    fetch(one, c);
     if constexpr (XSTEPS == STEPS) {
         Batch two;
         for (int s = 0; s < steps; s += 2) {
             put_tokens(0);
-            if (s + 1 < steps) { fetch(two, c + NEXT); fetch_tokens(c + NEXT); }
+            fetch_tokens(c + NEXT);
+            fetch(two, c + NEXT);
             multiply(one, c, 0, 0);
+            asm volatile("" ::: "memory");                                     // (or the loads would move behind the branch)
             if (s + 1 >= steps) break;
             put_tokens(BUFS - 1);
-            if (s + 2 < steps) { fetch(one, c + 2 * NEXT); fetch_tokens(c + 2 * NEXT); }
+            fetch_tokens(c + 2 * NEXT);
+            fetch(one, c + 2 * NEXT);
             multiply(two, c + NEXT, 0, BUFS - 1);
             c += 2 * NEXT;
         }
