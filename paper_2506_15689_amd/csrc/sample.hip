@@ -12,7 +12,7 @@
 //
 // Bound by latency: a row is read in full once or twice (256 rows of 128000 bf16 logits, 65.5 MB, would take 9.5 us at the rate of a
 // large read), but one row is a chain of some ten steps that a workgroup's waves wait for together: scan, find, scan, find.  One row of
-// 32000 bf16 logits 16 us; 256 rows of 128000 34.5; 64 rows of 128000 fp32 logits with top-k, top-p and min-p 46.
+// 32000 bf16 logits 16 us; 256 rows of 128000 32; 64 rows of 128000 fp32 logits with top-k, top-p and min-p 46.
 //
 // Masses are whole numbers: a token's weight e^((z - top) / T), computed in fp64, times 2^bits, rounded once.  Sums of them are exact
 // in any order, so LDS atomics give the same token every time, equal logits weigh the same, and the running mass at the last place
@@ -641,6 +641,11 @@ __global__ __launch_bounds__(THREADS) void sample_numbers_kernel(SampleArgs a) {
         else if (only) s.token = token;
         else atomicAdd(&s.parts[token >> log2], 1);
     };
+    // (Sixteen pieces and what stands between have not the registers: the last four are read again, from the cache.  256 rows of 128000 logits
+    // 34.2 us, with all of them kept, and some 20 MB of spilled ones, 37.2.)
+    constexpr int KEPT = R > 12 ? 12 : R;
+#pragma unroll
+    for (int r = KEPT; r < R; ++r) row.load_one(held[r], r * THREADS + tid);
     each_piece<R>(row, held, [&](const Piece<false>& piece, int p) {
         unsigned x[4], zeros = 0;
 #pragma unroll
