@@ -8,8 +8,8 @@
 // all of it is done or, with a status, nothing.
 //
 // Bound by the latency of a chain: what is known of a sequence, its page, its token.  Few tokens are placed by the same workgroup
-// (64 sequences, one token each: 5.1 us); many, or many sequences, by a second launch that fills the chip (48 prompts of 8192 tokens
-// together: 3.3 + 6.2).
+// (64 sequences, one token each: 5.0 us); many, or many sequences, by a second launch that fills the chip (48 packed prompts of up to 4096
+// tokens on pages of 16: 3.4 + 6.0).
 #include "basq_internal.h"
 #include "lane_ops.h"
 
