@@ -579,6 +579,26 @@ def test_products_that_are_long_or_wide(M, K, N, G, layout):
     test_product(M, K, N, G, layout)
 
 
+WIDE = [(N, K, G, M) for i, N in enumerate([4200, 8300, 12400, 96100]) for j, K in enumerate([512, 1024, 1536, 2560]) for k, G in enumerate([32, 64, 128, 256])
+        for M in [[1, 16, 45], [5, 30], [13, 60], [3, 16]][(i + j + k) % 4]]
+
+
+@pytest.mark.parametrize("N,K,G,M", WIDE)
+@pytest.mark.parametrize("layout", [CANONICAL, STREAMED])
+def test_wide_products_of_whole_numbers(N, K, G, M, layout):
+    """As above, exactly; of matrices of 263 to 6007 tiles, whose rows are looked at in three places."""
+    g = gen(N + K + G + M)
+    codes, s, z = weights(g, N, K, G, exact=True)
+    x = torch.randint(-3, 4, (M, K), generator=g, device=DEV).to(BF16)
+    y = torch.full((M, N), math.nan, device=DEV)
+    B.basq_w4a16_gemm(x, laid_out(codes, layout), s, z, y, w_layout=layout)
+    assert y.isfinite().all()
+    rows = torch.cat([torch.arange(130), torch.arange(N // 2, N // 2 + 130), torch.arange(N - 130, N)]).to(DEV)
+    want, made_of = ref.product(x, codes[rows], s[rows], z[rows])
+    assert made_of.max() < 2.0 ** 22
+    assert torch.equal(y[:, rows].cpu(), want.float())
+
+
 def test_lookup_of_many_tokens():
     """More of them than one dimension of a launch has."""
     T, K, N = 70001, 32, 50
