@@ -10,7 +10,7 @@
 //
 // One pass over the weights, which bound it where they are large (16 x 8192 x 128000, 565 MB: 117 us, 4.8 TB/s, vector instructions half of the time);
 // smaller calls are bound by the waits of a step, of which each wave has few (1 x 4096 x 4096 4.2 us, 13 x 14336 x 4096 16.4, 48 x 4096 x
-// 11008 17.2; their bytes 1.3, 4.9 and 4.3).  Each lane requests its batch of 16-byte pieces before it takes any up.  A workgroup
+// 11008 16.8; their bytes 1.3, 4.9 and 4.3).  Each lane requests its batch of 16-byte pieces before it takes any up.  A workgroup
 // owns TILES tiles of 16 weight rows, its waves share K in chunks of 128 channels; D = x (rows) times weights (columns), so a
 // lane's results belong to one weight row and take one scale.
 //
@@ -61,7 +61,7 @@ __device__ __forceinline__ v4u transposed(v4u r) {
 // weights: 16 x 8192 x 128000 162 us, through LDS 129 at the time.)  A step's weights, scales and tokens are under way while the step before
 // is multiplied: tokens first, which have to be in LDS first, as waits count loads in their order, and requested past the end too, where
 // they come back as 0 at once, as a branch around them would make the wait behind it one for all of them (16 x 4096 x 32000 20.0 us with
-// the branches, without 18.3).
+// the branches, 18.3 without).
 template <bool STREAM_LAYOUT, int NW, int KW, int STEPS, int XSTEPS, int TILES, int TT, int ROWS, int UNIT, bool SIDE>
 __global__ __launch_bounds__(NW * KW * 64, 2) void gemm_w4a16_kernel(W4A16Args a) {
     constexpr int UNITS = 128 / UNIT;                                          // of a chunk
@@ -319,9 +319,10 @@ void launch_shape(const W4A16Args& a, hipStream_t s) {
 
 // Up to 768 tiles a compute unit gets one workgroup, whose eight waves share K, on one to three of them; more tiles go to workgroups of
 // four waves with a tile each, so that four share the tokens, twice as many to share K unless that fills the chip anyway (us;
-// 1 x 8 is one wave's tiles and eight waves of K): 16 x 4096 x 4096 in groups of 128 1 x 8 6.3, 4 x 2 about 12; x 12288 on three tiles
-// 11.3, 4 x 2 12.8; x 32000 1 x 8 25, 4 x 2 20.8, 4 x 1 22.5; x 128000 4 x 2 68.5, 4 x 1 66.7.
-constexpr int FEW_TILES = 768, MANY_TILES = 6000;
+// 1 x 8 is one wave's tiles and eight waves of K): 16 x 4096 x 4096 in groups of 128 1 x 8 6.7, 4 x 2 8.8, 4 x 1 10.3; x 12288 on three
+// tiles 10.2, 4 x 2 9.6, 4 x 1 10.7; x 32000 1 x 8 26.1, 4 x 2 17.1 to 18.5, 4 x 1 16.6; x 128000 89, 64 and 57.  More tokens stay
+// with 4 x 2 longer.
+constexpr int FEW_TILES = 768, MANY_TILES = 1500, MANY_TILES_OF_MORE = 6000;
 int tiles_of(const W4A16Args& a) { return (a.N + TILE - 1) / TILE; }
 
 // up to 16 tokens.  Steps of as many chunks as each wave has work for: K = 1024 3.3 us with one, 4.1 with two; K = 4096 6.3 with four, 7.1
@@ -350,7 +351,7 @@ void launch_64(const W4A16Args& a, hipStream_t s) {
     const int tiles = tiles_of(a), chunks = (a.K + 127) / 128;
     constexpr int T = TT == 4 ? 2 : 1;
     if (SIDE && chunks % 2 != 0) launch_shape<SL, 1, 8, 1, 1, 1, TT, 16, UNIT, SIDE>(a, s);
-    else if (tiles > MANY_TILES && TT != 3) launch_shape<SL, 4, 1, 2, 1, T, TT, 16, UNIT, SIDE>(a, s);
+    else if (tiles > MANY_TILES_OF_MORE && TT != 3) launch_shape<SL, 4, 1, 2, 1, T, TT, 16, UNIT, SIDE>(a, s);
     else if (tiles > FEW_TILES) launch_shape<SL, 4, 2, 2, 1, T, TT, 16, UNIT, SIDE>(a, s);
     else if (tiles <= 256) launch_shape<SL, 1, 8, 2, 1, 1, TT, 16, UNIT, SIDE>(a, s);
     else if (tiles <= 512) launch_shape<SL, 1, 8, 2, 1, 2, TT, 16, UNIT, SIDE>(a, s);
