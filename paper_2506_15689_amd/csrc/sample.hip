@@ -717,6 +717,9 @@ struct Grid {
         step = __uint_as_float((unsigned)(127 + e) << 23);
     }
     __device__ __forceinline__ int cell(float z) const { return (int)__builtin_floorf(z * per_unit); }       // (saturates)
+    // The lowest logit of a cell.  That of cell 0 is not 0 where the step is 2 or more: the products of logits just below it, down to
+    // -2^-150 step, round to -0.  (2^-150 is half of the least number, a tie that goes to 0; for a smaller step this is -0.)
+    __device__ __forceinline__ float edge(int cell) const { return cell ? (float)cell * step : step * -0x1p-75f * 0x1p-75f; }
     // Cells next to this logit are numbers of 24 bits: edges are exact.
     __device__ __forceinline__ bool fine(float z) const { return fabsf(z * per_unit) < 4194304.0f; }
 };
@@ -895,9 +898,9 @@ __device__ __forceinline__ void collect(Cells& s, const Pieces<true>& row, const
     float lo[Q], hi[Q];                                    // of a stretch, both within
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
-        const int end = __float_as_int((float)(top_cell - from[q] + 1) * grid.step);            // the first beyond
-        lo[q] = to[q] == CELLS - 1 ? -3.402823466e38f : (float)(top_cell - to[q]) * grid.step;
-        hi[q] = __int_as_float(end > 0 ? end - 1 : end == 0 ? (int)0x80000001 : end + 1);
+        const int end = __float_as_int(grid.edge(top_cell - from[q] + 1));                      // the first beyond
+        lo[q] = to[q] == CELLS - 1 ? -3.402823466e38f : grid.edge(top_cell - to[q]);
+        hi[q] = __int_as_float(end > 0 ? end - 1 : end + 1);
     }
     auto wanted = [&](float z) {
         bool in = __builtin_amdgcn_fmed3f(z, lo[0], hi[0]) == z;
@@ -1215,7 +1218,8 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
     };
     int kept = all;
     uint64_t mass = all_mass;
-    bool lost = false;                                     // (a target between the cells that it had to be in: never, but for rounding)
+    // (a target between the cells that it had to be in, or keys that were counted and not collected, which are not there: never, but for rounding)
+    bool lost = s.n != n;
     if (by_k) {
         if (tid == 0) s.found_rank = -1;
         __syncthreads();

@@ -325,6 +325,48 @@ def test_cuts_where_masses_are_equal():
     assert kept == [2, 1, 3] and tokens == [1, 0, 1]
 
 
+@pytest.mark.parametrize("V", [2, 3, 500, 5000, 40000])
+@pytest.mark.parametrize("heat", [57.0, 100.0, 1e4, 1e30, 3e38, math.inf])
+def test_logits_just_below_zero(V, heat):
+    """At temperatures of 57 and more the grid of cells is coarser than 1, and a logit's place on it rounds to -0 for the least negative ones:
+    they lie beside 0, between tokens on both sides, where top-k cuts and where draws lead."""
+    g = gen(V)
+    spread = min(4 * heat, 1e38)
+    z = (2 * torch.rand((ROWS, V), generator=g, device=DEV) - 1) * spread
+    below = torch.tensor([-1e-45, -3e-45, -1e-44, -1e-40, -1e-38, -1e-30, -1e-17, -1e-10, -9e-10, 0.0], device=DEV)
+    n = min(V - 1, 10)
+    for r in range(ROWS):
+        z[r, torch.randperm(V, generator=g, device=DEV)[:n]] = below[r % 3:][:n] if n < 7 else below[:n]
+    z[0], z[0, V - 1] = -1.0, -1e-45                              # (alone on top)
+    rows = z.cpu()
+    assert (rows[0] > -1e-44).sum() == 1
+    above = [int((row > 0).sum()) for row in rows]
+    rng = random.Random(V)
+    for more in (1, 2, n, n + 1):
+        k = [a + more for a in above]
+        for u in ([rng.random() for _ in range(ROWS)], [1.0] * ROWS, [0.0] * ROWS):
+            check_draw(z, u, temperature=[heat] * ROWS, top_k=k)
+    for u in ([rng.random() for _ in range(ROWS)], [1.0] * ROWS):
+        check_draw(z, u, temperature=[heat] * ROWS)
+        check_draw(z, u, temperature=[heat] * ROWS, min_p=[0.5, 0.2, 0.05] * 4, top_p=[1.0, 0.9, 0.6, 0.99] * 3)
+    # numbers that lead to each of them
+    logits = z[1:2].cpu().double().numpy()[0]
+    w = np.sort(np.exp((logits - logits.max()) / float(np.float32(heat))))[::-1]
+    running = np.cumsum(w) / w.sum()
+    u = [float(running[min(above[1] + i, V - 1)] - w[0] / w.sum() * 1e-3) for i in range(-1, n + 1)]
+    check_draw(z[1:2].expand(len(u), -1), [min(max(x, 0.0), 1.0) for x in u], temperature=[heat] * len(u))
+
+
+def test_logits_that_all_lie_just_below_zero():
+    """Two tokens and three, as few as can be: the cell of 0 has them all, by the temperature."""
+    for row in ([0.0, -1e-45], [-1e-45, 0.0], [-1e-45, -1e-45], [-5e-10, 0.0], [0.5, 0.25, -1e-10], [-1e-30, -1e-20, -1e-40], [1.0, -1e-45, 2.0, -1.0]):
+        logits = torch.tensor([row] * 4, device=DEV)
+        for heat in (57.0, 100.0, 1e30, 3e38, math.inf):
+            for k in range(len(row) + 1):
+                check_draw(logits, [0.0, 0.3, 0.6, 0.99], temperature=[heat] * 4, top_k=[k] * 4)
+                check_draw(logits, [0.0, 0.3, 0.6, 0.99], temperature=[heat] * 4, top_k=[k] * 4, top_p=[0.7] * 4, min_p=[0.5] * 4)
+
+
 # ---- books -----------------------------------------------------------------------------------------
 
 def make_books(rng, rows, columns, P, spare, longest):
