@@ -720,8 +720,9 @@ struct Grid {
     // The lowest logit of a cell.  That of cell 0 is not 0 where the step is 2 or more: the products of logits just below it, down to
     // -2^-150 step, round to -0.  (2^-150 is half of the least number, a tie that goes to 0; for a smaller step this is -0.)
     __device__ __forceinline__ float edge(int cell) const { return cell ? (float)cell * step : step * -0x1p-75f * 0x1p-75f; }
-    // Cells next to this logit are numbers of 24 bits: edges are exact.
-    __device__ __forceinline__ bool fine(float z) const { return fabsf(z * per_unit) < 4194304.0f; }
+    // Cells next to this logit are numbers of 24 bits, edges are exact; and a cell is no wider than 72/2048 temperatures, as its sums need (one of
+    // 2^-120 is, for temperatures below 2.1e-35).
+    __device__ __forceinline__ bool fine(float z, float heat) const { return fabsf(z * per_unit) < 4194304.0f && step <= 72.0f / CELLS * heat; }
 };
 __device__ __forceinline__ int below(int top, int cell) {
     const unsigned d = (unsigned)top - (unsigned)cell;
@@ -974,7 +975,7 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
     w.per = 1.4426950408889634 / (double)c.heat;
     w.bits = a.bits;
     const Grid grid(c.heat);
-    if (!grid.fine(w.top)) {
+    if (!grid.fine(w.top, c.heat)) {
         by_digits<true>(a, b, best, shared.digits);
         return;
     }

@@ -367,6 +367,20 @@ def test_logits_that_all_lie_just_below_zero():
                 check_draw(logits, [0.0, 0.3, 0.6, 0.99], temperature=[heat] * 4, top_k=[k] * 4, top_p=[0.7] * 4, min_p=[0.5] * 4)
 
 
+@pytest.mark.parametrize("V", [3, 900, 5000, 40000])
+@pytest.mark.parametrize("heat", [1e-34, 2.5e-35, 2e-35, 1e-36, 1e-38, 1e-42])
+def test_tiny_logits_at_tiny_temperatures(V, heat):
+    """Where cells cannot be as narrow as the temperature, and where they just can."""
+    g = gen(V)
+    top = float(np.float32(heat)) * 30
+    z = (bell(g, ROWS, V, torch.float32).clamp(max=9.0).double() * top / 30).float()
+    rng = random.Random(V)
+    u = [rng.random() for _ in range(ROWS)]
+    check_draw(z, u, temperature=[heat] * ROWS)
+    check_draw(z, u, temperature=[heat] * ROWS, top_p=[0.9, 0.5, 0.99] * 4, min_p=[0.0, 0.1, 0.01, 1e-4] * 3)
+    check_draw(z, u, temperature=[heat] * ROWS, top_k=[1, 2, 10, 100, 1000, V // 2] * 2, top_p=[1.0, 0.8] * 6)
+
+
 # ---- books -----------------------------------------------------------------------------------------
 
 def make_books(rng, rows, columns, P, spare, longest):
