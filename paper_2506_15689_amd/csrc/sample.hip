@@ -1287,8 +1287,10 @@ int slices_of(int32_t V, int r) { return (V / 4 + 1 + THREADS * r - 1) / (THREAD
 
 }  // namespace
 
-// A workspace holds the slices of 2048 / (slices of a row) rows; a call of more runs in parts, one after the other.
+// A workspace holds the slices of 2048 / (slices of a row) rows; a call of more runs in parts, one after the other.  So does one of more
+// rows than a launch has workgroups (2^32 threads).
 constexpr int64_t SLICES_AT_ONCE = 2048;
+constexpr int32_t ROWS_AT_ONCE = 1 << 21;
 
 size_t sample_workspace_bytes(int32_t B, int32_t V) {
     if (V > SAMPLE_LONG) V = SAMPLE_LONG;                  // (rows by digits need none)
@@ -1297,34 +1299,49 @@ size_t sample_workspace_bytes(int32_t B, int32_t V) {
     return (size_t)(many > few_rows ? many : few_rows) * sizeof(SampleSlice);
 }
 
+namespace {
+
+// the rows of a part
+void launch_rows(const SampleArgs& a, bool few_rows, hipStream_t s) {
+    const dim3 rows(a.B), block(THREADS);
+    constexpr int WORD = THREADS * 8;                      // logits of a piece of each thread
+    if (a.V > SAMPLE_LONG) {
+        if (a.f32) hipLaunchKernelGGL(sample_long_kernel<true>, rows, block, 0, s, a);
+        else hipLaunchKernelGGL(sample_long_kernel<false>, rows, block, 0, s, a);
+    } else if (!a.f32) {
+        if (a.V <= 4 * WORD) hipLaunchKernelGGL(sample_numbers_kernel<4>, rows, block, 0, s, a);
+        else if (a.V <= 16 * WORD) hipLaunchKernelGGL(sample_numbers_kernel<16>, rows, block, 0, s, a);
+        else hipLaunchKernelGGL(sample_numbers_kernel<0>, rows, block, 0, s, a);
+    } else if (a.slices_of_row == 0) {
+        hipLaunchKernelGGL(sample_row_kernel<MANY_PIECES>, rows, block, 0, s, a);
+    } else {
+        const dim3 grid(a.slices_of_row, a.B);
+        if (few_rows) hipLaunchKernelGGL(sample_slice_kernel<FEW_PIECES>, grid, block, 0, s, a);
+        else hipLaunchKernelGGL(sample_slice_kernel<MANY_PIECES>, grid, block, 0, s, a);
+        hipLaunchKernelGGL(sample_row_kernel<0>, rows, block, 0, s, a);
+    }
+}
+
+}  // namespace
+
 int launch_sample(SampleArgs a, hipStream_t s) {
-    const bool f32 = a.f32 != 0;
     int log2 = 0;
     while ((1ll << log2) < a.V) ++log2;
     a.bits = 62 - log2 < 50 ? 62 - log2 : 50;
-    const dim3 row_grid(a.B), block(THREADS);
-    if (f32 && a.V <= 32768) {
-        hipLaunchKernelGGL(sample_row_kernel<MANY_PIECES>, row_grid, block, 0, s, a);
-        return check_hip(hipGetLastError(), "sample launch");
+    bool few_rows = false;
+    int32_t at_once = ROWS_AT_ONCE;
+    a.slices_of_row = 0;
+    if (a.f32 && a.V > 32768 && a.V <= SAMPLE_LONG) {
+        a.slices = reinterpret_cast<SampleSlice*>(a.workspace);
+        const int fine = slices_of(a.V, FEW_PIECES);
+        few_rows = (int64_t)fine * a.B <= 256;
+        a.slices_of_row = few_rows ? fine : slices_of(a.V, MANY_PIECES);
+        at_once = a.slices_of_row < SLICES_AT_ONCE ? (int32_t)(SLICES_AT_ONCE / a.slices_of_row) : 1;
     }
-    if (a.V > SAMPLE_LONG || !f32) {
-        constexpr int WORD = THREADS * 8;                  // logits of a piece of each thread
-        if (f32) hipLaunchKernelGGL(sample_long_kernel<true>, row_grid, block, 0, s, a);
-        else if (a.V > SAMPLE_LONG) hipLaunchKernelGGL(sample_long_kernel<false>, row_grid, block, 0, s, a);
-        else if (a.V <= 4 * WORD) hipLaunchKernelGGL(sample_numbers_kernel<4>, row_grid, block, 0, s, a);
-        else if (a.V <= 16 * WORD) hipLaunchKernelGGL(sample_numbers_kernel<16>, row_grid, block, 0, s, a);
-        else hipLaunchKernelGGL(sample_numbers_kernel<0>, row_grid, block, 0, s, a);
-        return check_hip(hipGetLastError(), "sample launch");
-    }
-    a.slices = reinterpret_cast<SampleSlice*>(a.workspace);
-    const int fine = slices_of(a.V, FEW_PIECES);
-    const bool few_rows = (int64_t)fine * a.B <= 256;
-    a.slices_of_row = few_rows ? fine : slices_of(a.V, MANY_PIECES);
-    const int32_t at_once = a.slices_of_row < SLICES_AT_ONCE ? (int32_t)(SLICES_AT_ONCE / a.slices_of_row) : 1;
-    for (int32_t b0 = 0; b0 < a.B; b0 += at_once) {
-        const int32_t rows = a.B - b0 < at_once ? a.B - b0 : at_once;
+    for (int64_t b0 = 0; b0 < a.B; b0 += at_once) {
         SampleArgs p = a;
-        p.logits = static_cast<const uint8_t*>(a.logits) + (int64_t)b0 * a.ldl * 4;
+        p.B = a.B - b0 < at_once ? (int32_t)(a.B - b0) : at_once;
+        p.logits = static_cast<const uint8_t*>(a.logits) + b0 * a.ldl * (a.f32 ? 4 : 2);
         if (p.temperature) p.temperature += b0;
         if (p.top_k) p.top_k += b0;
         if (p.top_p) p.top_p += b0;
@@ -1333,10 +1350,7 @@ int launch_sample(SampleArgs a, hipStream_t s) {
         p.token += b0;
         if (p.logprob) p.logprob += b0;
         if (p.kept) p.kept += b0;
-        const dim3 grid(a.slices_of_row, rows);
-        if (few_rows) hipLaunchKernelGGL(sample_slice_kernel<FEW_PIECES>, grid, block, 0, s, p);
-        else hipLaunchKernelGGL(sample_slice_kernel<MANY_PIECES>, grid, block, 0, s, p);
-        hipLaunchKernelGGL(sample_row_kernel<0>, dim3(rows), block, 0, s, p);
+        launch_rows(p, few_rows, s);
     }
     return check_hip(hipGetLastError(), "sample launch");
 }

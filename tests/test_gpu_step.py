@@ -684,6 +684,27 @@ def test_draws_in_parts():
     check_draw(logits[pick], [u[i] for i in pick], temperature=[heat[i] for i in pick], top_k=[k[i] for i in pick], top_p=[p[i] for i in pick])
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, BF16])
+def test_draws_of_more_rows_than_a_launch_has(dtype):
+    """2^22 and some from one row: 2^32 threads and more, so they go in parts."""
+    n = (1 << 22) + 5
+    row = torch.tensor([0.5, -1.0, -math.inf, 2.0, 1.0], device=DEV).to(dtype)
+    u = torch.arange(n, dtype=torch.float64, device=DEV) / n
+    token, kept, logprob = torch.full((n,), 77, dtype=I32, device=DEV), torch.full((n,), 77, dtype=I32, device=DEV), torch.full((n,), 77.0, device=DEV)
+    need = B.basq_sample_workspace_bytes(n, 5)
+    B.basq_sample(row.expand(n, -1), u, token, torch.empty(need, dtype=torch.uint8, device=DEV) if need else None, kept=kept, logprob=logprob)
+    assert (kept == 4).all()
+    # the order is that of the logits, so the tokens come in four runs, of their shares
+    share = torch.softmax(row.double(), 0)
+    order = [3, 4, 0, 1]
+    ends = (torch.cumsum(share[order], 0) * n).cpu()
+    want = torch.tensor(order, dtype=I32, device=DEV)[torch.searchsorted(ends[:3].to(DEV), torch.arange(n, dtype=torch.float64, device=DEV), right=True)]
+    assert (ends[:3] - ends[:3].round()).abs().min() > 1e-6        # (no number lies on an end)
+    assert torch.equal(token, want)
+    ln = torch.log(share)[token.long()]
+    assert ((logprob.double() - ln).abs() <= ln.abs() * 2.0 ** -23).all()
+
+
 @pytest.mark.parametrize("V", [900, 50000])
 @pytest.mark.parametrize("dtype", [torch.float32, BF16])
 def test_temperatures_at_the_ends(V, dtype):
