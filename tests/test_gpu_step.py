@@ -655,6 +655,30 @@ def test_wide_products_of_whole_numbers(N, K, G, M, layout):
     assert torch.equal(y[:, rows].cpu(), want.float())
 
 
+@pytest.mark.parametrize("M,K,layout", [(1, 32, CANONICAL), (17, 32, CANONICAL), (2, 128, STREAMED)])
+def test_products_of_more_rows_than_a_launch_has(M, K, layout):
+    """2^27 rows and some, which go in parts of 2^26, exactly; looked at beside the parts' ends."""
+    N = (1 << 27) + 33
+    g = gen(M)
+    room = (N + 15) // 16 * 16
+    Wq = torch.randint(0, 256, (room * K // 2,), generator=g, dtype=torch.uint8, device=DEV)
+    s = torch.randint(-2, 3, (N, 1), generator=g, dtype=torch.int8, device=DEV).to(BF16).exp2()
+    z = torch.randint(0, 16, (N, 1), generator=g, dtype=torch.uint8, device=DEV).to(BF16)
+    x = torch.randint(-3, 4, (M, K), generator=g, device=DEV).to(BF16)
+    bias = torch.randint(-50, 50, (N,), generator=g, dtype=torch.int8, device=DEV).float()
+    y = torch.full((M, N), math.nan, device=DEV)
+    B.basq_w4a16_gemm(x, Wq if layout == STREAMED else Wq[:N * K // 2], s, z, y, bias, w_layout=layout)
+    assert all(row.isfinite().all() for row in y)
+    for at in (0, (1 << 26) - 64, (1 << 27) - 64, N - 33):        # 64 rows and more: four blocks, or what is left
+        end = min(at + 128, N)
+        rows = Wq[at * K // 2:(end + 15) // 16 * 16 * K // 2]
+        if layout == STREAMED:
+            rows = rows.view(-1, K // 128, 4, 16, 16).permute(0, 3, 1, 2, 4).contiguous()
+        codes = rows.reshape(-1, K // 2)[:end - at]
+        want, _ = ref.product(x, codes, s[at:end], z[at:end], bias[at:end])
+        assert torch.equal(y[:, at:end].cpu(), want.float()), at
+
+
 def test_lookup_of_many_tokens():
     """More of them than one dimension of a launch has."""
     T, K, N = 70001, 32, 50
