@@ -457,8 +457,8 @@ int basq_w4a16_lookup(const int32_t* ids, int64_t T, const uint8_t* Wq, int32_t 
  *   token      out, int32 [B]; -1 for a row without tokens
  *   logprob    out, fp32 [B] or NULL: ln of the token's share of the kept weights; -inf without tokens
  *   kept       out, int32 [B] or NULL: n
- *   workspace  256-byte aligned, >= basq_sample_workspace_bytes(B, V) (else BASQ_EWORKSPACE); NULL where that is 0.  A workspace for
- *              a call does for any with fewer rows or a smaller V
+ *   workspace  256-byte aligned, >= basq_sample_workspace_bytes(B, V) (else BASQ_EWORKSPACE); NULL where that is 0, as for V up to
+ *              32768.  A workspace for a call does for any with fewer rows or a smaller V.  bf16 logits need none: NULL, or any
  * V up to 2^22 (else BASQ_EUNSUPPORTED).  B == 0 does nothing.
  */
 size_t basq_sample_workspace_bytes(int32_t B, int32_t V);

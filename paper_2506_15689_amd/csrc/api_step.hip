@@ -100,7 +100,7 @@ int basq_sample(const void* logits, int64_t ldl, int32_t B, int32_t V, int32_t f
     if (rc == BASQ_OK) rc = check_ints("kept", kept, false);
     if (rc != BASQ_OK) return rc;
     if (!u || !aligned(u, 8)) return fail(BASQ_EINVAL, "u is null or not 8-byte aligned");
-    const size_t need = sample_workspace_bytes(B, V);
+    const size_t need = f32 ? sample_workspace_bytes(B, V) : 0;
     if (need > 0) {
         if (!workspace || !aligned(workspace, 256)) return fail(BASQ_EINVAL, "workspace is null or not 256-byte aligned");
         if (workspace_bytes < need) return fail(BASQ_EWORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes, need);

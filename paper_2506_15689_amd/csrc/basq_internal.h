@@ -247,7 +247,8 @@ struct SampleArgs {
     int32_t slices_of_row;
 };
 constexpr int32_t SAMPLE_MAX_TOKENS = 1 << 22, SAMPLE_LONG = 1 << 20;
-size_t sample_workspace_bytes(int32_t B, int32_t V);
+constexpr int32_t SAMPLE_SHORT = 1 << 15;                         // fp32 rows of more tokens are read in slices, up to SAMPLE_LONG
+size_t sample_workspace_bytes(int32_t B, int32_t V);              // for fp32; bf16 needs none
 int launch_sample(SampleArgs a, hipStream_t s);                   // sample.hip
 
 struct KvExtendArgs {

@@ -1283,6 +1283,7 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
 // Slices of a row: as many pieces of a thread as it holds in registers, or two where the rows alone do not fill the chip.  (Eight, four:
 // 64 rows of 128000 logits 14.4 us the slices and 29.2 the rows, 15.5 and 31.2.)
 constexpr int FEW_PIECES = 2, MANY_PIECES = 8;
+static_assert(SAMPLE_SHORT == THREADS * MANY_PIECES * Piece<true>::N, "a row that a workgroup holds");
 int slices_of(int32_t V, int r) { return (V / 4 + 1 + THREADS * r - 1) / (THREADS * r); }
 
 }  // namespace
@@ -1293,7 +1294,8 @@ constexpr int64_t SLICES_AT_ONCE = 2048;
 constexpr int32_t ROWS_AT_ONCE = 1 << 21;
 
 size_t sample_workspace_bytes(int32_t B, int32_t V) {
-    if (V > SAMPLE_LONG) V = SAMPLE_LONG;                  // (rows by digits need none)
+    if (V <= SAMPLE_SHORT) return 0;
+    if (V > SAMPLE_LONG) V = SAMPLE_LONG;                  // (rows by digits need none, but what does for a call does for smaller ones)
     const int64_t row = slices_of(V, MANY_PIECES), most = row > SLICES_AT_ONCE ? row : SLICES_AT_ONCE;
     const int64_t many = row * B < most ? row * B : most, few_rows = 256 + slices_of(V, FEW_PIECES);
     return (size_t)(many > few_rows ? many : few_rows) * sizeof(SampleSlice);
@@ -1331,7 +1333,7 @@ int launch_sample(SampleArgs a, hipStream_t s) {
     bool few_rows = false;
     int32_t at_once = ROWS_AT_ONCE;
     a.slices_of_row = 0;
-    if (a.f32 && a.V > 32768 && a.V <= SAMPLE_LONG) {
+    if (a.f32 && a.V > SAMPLE_SHORT && a.V <= SAMPLE_LONG) {
         a.slices = reinterpret_cast<SampleSlice*>(a.workspace);
         const int fine = slices_of(a.V, FEW_PIECES);
         few_rows = (int64_t)fine * a.B <= 256;

@@ -381,6 +381,16 @@ def test_tiny_logits_at_tiny_temperatures(V, heat):
     check_draw(z, u, temperature=[heat] * ROWS, top_k=[1, 2, 10, 100, 1000, V // 2] * 2, top_p=[1.0, 0.8] * 6)
 
 
+@pytest.mark.parametrize("V,dtype", [(1, torch.float32), (1000, torch.float32), (32768, torch.float32), (1000, BF16), (32769, BF16), (50000, BF16), (150000, BF16), ((1 << 20) + 1, BF16)])
+def test_draws_without_a_workspace(V, dtype):
+    g = gen(V)
+    wide = bell(g, 3, V + 1, dtype)
+    for logits in (wide[:, :V], wide[:, 1:]):                     # (a row in pieces, and what is in front of and behind them)
+        token = torch.full((3,), 77, dtype=I32, device=DEV)
+        B.basq_sample(logits, torch.tensor([0.2, 0.5, 0.9], dtype=torch.float64, device=DEV), token, None)
+        assert token.tolist() == [ref.sample_row(row, u=u)[0] for row, u in zip(logits.cpu().double().numpy(), (0.2, 0.5, 0.9))]
+
+
 # ---- books -----------------------------------------------------------------------------------------
 
 def make_books(rng, rows, columns, P, spare, longest):

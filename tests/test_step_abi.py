@@ -95,6 +95,12 @@ def test_sample_workspace(lib):
             assert sample(lib, B=b, V=v, ldl=v, workspace_bytes=n - 1) == B.BASQ_EWORKSPACE
 
 
+def test_rows_that_a_workgroup_holds_need_no_workspace(lib):
+    for b in (1, 64, 5000, 1 << 22):
+        assert [B.basq_sample_workspace_bytes(b, v) for v in (1, 1000, 32768)] == [0] * 3
+        assert B.basq_sample_workspace_bytes(b, 32769) > 0
+
+
 def extend(lib, **kw):
     a = dict(lengths=FAKE, pool_table=FAKE, pool_stride=8, rows=6, columns=8, page_size=16, free_pages=FAKE, capacity=48, free_count=FAKE, seqs=FAKE,
              new_tokens=FAKE, B=3, q_len=2, positions=FAKE, slots=FAKE, T=6, starts=None, batch_table=FAKE, batch_stride=8, batch_lengths=FAKE,
