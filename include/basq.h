@@ -448,8 +448,9 @@ int basq_w4a16_lookup(const int32_t* ids, int64_t T, const uint8_t* Wq, int32_t 
  *     the number of weights >= min(min_p, 1)                where min_p > 0
  * and 1 where temperature is not > 0 (the likeliest token).  The token is the first kept one at which
  * w_0 + ... + w_i > u * (sum of the kept weights).
- * Weights are computed in fp64, to 2^-37 of theirs or better, and summed as whole multiples of 2^-bits, bits = min(50, 62 - log2 V
- * rounded up), top_p * S and u * sum being fp64 products: a weight below half of that is never drawn, and the same call gives the same
+ * Weights are computed in fp64, to 2^-36 of theirs or better, and summed as whole multiples of 2^-bits, bits = min(50, 62 - log2 V
+ * rounded up), each rounded to one, or, of fp32 logits, the sum of some neighbours: a running sum is off by 2^-36 of it and V 2^-(bits + 1)
+ * at most.  top_p * S and u * sum are fp64 products.  A weight below half of a step is never drawn, and the same call gives the same
  * tokens every time.
  *   logits     fp32 (f32 != 0) or bf16 [B, ldl], ldl >= V, aligned as their type is; ldl = 0: B draws from one row
  *   temperature, top_p, min_p   fp32 [B], top_k int32 [B]; each may be NULL (1; none).  A NaN among the last two is none

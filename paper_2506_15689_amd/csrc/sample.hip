@@ -3,7 +3,7 @@
 //
 // The tokens' order is that of their logits, so nothing is sorted but what lies next to a cut: a cut, and the draw itself, is the
 // first place of that order at which a running count or a running mass reaches a target.  Three ways lead to such places, by what the
-// row is like (all see the same masses, the second to 2^-37):
+// row is like (all see the same masses, the second to 2^-36 and its cells' roundings):
 //     bf16                       how often each of the 65536 numbers occurs, one workgroup and launch a row
 //     fp32                       cells of a grid, then the few tokens in the cells of the cuts; rows of up to 32768 in one launch, longer ones in two
 //     long rows, and those that  digits of the logits' bits, with a histogram of counts and masses over one digit at a time: any
@@ -16,8 +16,9 @@
 //
 // Masses are whole numbers: a token's weight e^((z - top) / T), computed in fp64, times 2^bits, rounded once.  Sums of them are exact
 // in any order, so LDS atomics give the same token every time, equal logits weigh the same, and the running mass at the last place
-// is the total.  (bits: 2^bits times the tokens of a row stays below 2^62; 45 for 128000 tokens, whose roundings together are about
-// 2^-37 of the mass at most.  Sums in fp32 would move the draw of one row in forty to a neighbour, by their 2^-23.)
+// is the total.  (bits: 2^bits times the tokens of a row stays below 2^62; 45 for 128000 tokens, whose roundings, half a step each, come to
+// about 2^-37 of the mass, and to 2^-29 if all had one sign.  Sums in fp32 would move the draw of one row in forty to a neighbour, by
+// their 2^-23.)
 #include "basq_internal.h"
 #include "lane_ops.h"
 
@@ -703,8 +704,9 @@ __global__ __launch_bounds__(THREADS) void sample_numbers_kernel(SampleArgs a) {
 // A token's weight is the weight at its cell's lower edge times e^x, x = (z - edge) / T below 0.0352: the histogram sums e^x - 1, and
 // one exponential for each cell follows in the second launch.  e^x - 1 is five terms of its series in fp64, times 2^36, in the lower
 // 48 bits of a cell's 64, the number of tokens in the upper 16: one LDS atomic a token.  (With an exponential and two atomics for each
-// token, 256 rows of 128000 bf16 logits took this launch 67 us, LDS and the vector units at their limits in turn.)  The series and the
-// rounding are good for 2^-37 of a token's weight; of logits on the grid, as coarse ones are, e^x - 1 is 0 and sums are exact.
+// token, 256 rows of 128000 logits, then in bf16, took this launch 67 us and took it 38 so, LDS and the vector units at their limits in turn.)  The series and the
+// rounding are good for 2^-36 of a token's weight (2^-37 the rounding, 2^-38.5 the first term left out); a cell's sum is rounded to whole
+// steps once, not token by token.  Of logits on the grid, as coarse ones are, e^x - 1 is 0.
 
 constexpr int CELLS = SAMPLE_CELLS, SORTED = 4096;
 // the grid of a temperature
@@ -1075,7 +1077,7 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
     };
     const bool by_k = c.k > 0 && c.k < all, by_p = c.p < 1.0f, by_least = c.least > 0.0f;
     // Up to three stretches of cells, one below the other, whose tokens have to be known: [from, to].  Sums by cell and sums by token
-    // differ by 2^-37 of them, 2^-35 is ample.
+    // differ by 2^-36 of them, and by half a step a token: a target that is not among the tokens found for it sends the row to the digits.
     constexpr double under = 1.0 - 0x1p-35, over = 1.0 + 0x1p-35;
     int from[3] = {0, 0, 0}, to[3] = {-1, -1, -1};
     int least_cell = CELLS, found[4];                      // (the first cell in which a weight may be too small)
