@@ -1081,6 +1081,7 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
     constexpr double under = 1.0 - 0x1p-35, over = 1.0 + 0x1p-35;
     int from[3] = {0, 0, 0}, to[3] = {-1, -1, -1};
     int least_cell = CELLS, found[4];                      // (the first cell in which a weight may be too small)
+    bool least_ends = false;                               // (all cells in which some may be are among those stretches)
     if (!weighed) {
         cell_by_count(by_k ? c.k : all, 0);
         cells_found(found, 1);
@@ -1111,6 +1112,7 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
             const int least_end = lo >= (double)top_cell ? 0 : below(top_cell, (int)lo);
             cut_lo = least_cell < cut_lo ? least_cell : cut_lo;
             cut_hi = least_end < cut_hi ? least_end : cut_hi;
+            least_ends = least_end <= cut_hi;
         }
         const double u = a.u[b];
         const double share = u > 0.0 ? (u < 1.0 ? u : 1.0) : 0.0;
@@ -1188,18 +1190,23 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
     }
     __syncthreads();
     {
-        // places in the whole order: behind a stretch lies what is between it and the next
+        // places in the whole order: behind a stretch lies what is between it and the next, which has the mass from its cells' on, so none of
+        // its tokens' goes beyond
         int start = 0;
 #pragma unroll
         for (int q = 0; q < 3; ++q) {
             if (tokens[q] == 0) continue;
             const uint64_t shift = (weighed && from[q] ? s.mass[from[q] - 1] : 0) - (start ? s.running[start - 1] : 0);
+            const uint64_t end = weighed ? s.mass[to[q]] : ~0ull;
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 const int i = tid * per_thread + e;
                 if (e >= per_thread || i < start || i >= start + tokens[q]) continue;
                 rank[e] = base_count[q] + i - start;
                 run[e] += shift;
+                const uint64_t in_front = run[e] - each[e];
+                run[e] = run[e] < end ? run[e] : end;
+                each[e] = run[e] - (in_front < end ? in_front : end);
             }
             start += tokens[q];
         }
@@ -1221,8 +1228,10 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
     };
     int kept = all;
     uint64_t mass = all_mass;
-    // (a target between the cells that it had to be in, or keys that were counted and not collected, which are not there: never, but for rounding)
+    // (a target between the tokens' sums and the cells', or keys that were counted and not collected, which are not there: next to never)
     bool lost = s.n != n;
+    uint64_t p_target = 0;
+    bool p_found = true;
     if (by_k) {
         if (tid == 0) s.found_rank = -1;
         __syncthreads();
@@ -1243,10 +1252,11 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
         mass = n > 0 ? s.running[n - 1] : 0;
     }
     if (by_p) {
-        const int r = reach(cut_target(c.p, mass));
+        p_target = cut_target(c.p, mass);
+        const int r = reach(p_target);
         const uint64_t m = s.found_mass;
-        // (not found: top-k or min-p cuts in front of it)
-        if (r >= 0 && r + 1 < kept) { kept = r + 1; mass = m; }
+        p_found = r >= 0;
+        if (p_found && r + 1 < kept) { kept = r + 1; mass = m; }
     }
     if (by_least) {
         // the last that weighs enough; where none of them does, the cells in front hold it
@@ -1271,8 +1281,11 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
         uint64_t m_mass = most >= 0 ? s.found_mass : 0;
         const int whole = weighed && least_cell > 0 ? s.count[least_cell - 1] : 0;          // (cells that weigh enough altogether)
         if (whole > m_kept) { m_kept = whole; m_mass = s.mass[least_cell - 1]; }
+        // (min-p cuts in front of it)
+        if (!p_found && least_ends && m_mass < p_target) p_found = true;
         if (m_kept < kept) { kept = m_kept; mass = m_mass; }
     }
+    if (!p_found) lost = true;
     if (reach(draw_target(a.u[b], mass)) < 0) lost = true;
     if (lost) {
         __syncthreads();

@@ -391,6 +391,39 @@ def test_draws_without_a_workspace(V, dtype):
         assert token.tolist() == [ref.sample_row(row, u=u)[0] for row, u in zip(logits.cpu().double().numpy(), (0.2, 0.5, 0.9))]
 
 
+def row_that_reaches_p_at_a_cells_end(V, p, tokens=4000):
+    """fp32 logits, for a temperature of 1, of which one weighs 1 and `tokens` equal ones, on the grid of 1/32, together about a half, each of them a
+    whole number of 2^-bits and 0.35 to 0.5 more; and as much behind them as makes p of all end in those parts."""
+    one = np.longdouble(2) ** min(50, 62 - (V - 1).bit_length())
+    weight = lambda z: np.exp(np.longdouble(z)) * one  # noqa: E731
+    z = next(-k / 32 for k in range(int(32 * math.log(2 * tokens)) - 20, 10000) if 0.35 < float(weight(-k / 32) % 1) < 0.5)
+    whole, parts = tokens * np.floor(weight(z)), np.rint(tokens * weight(z))
+    rest = (one + (whole + parts) / 2) / np.longdouble(np.float32(p)) - one - parts
+    low = z - 40 / 32
+    row = [0.0] + [z] * tokens + [low] * int(rest / weight(low))
+    assert rest > 0 and len(row) < V - 4
+    rest -= np.rint((len(row) - 1 - tokens) * weight(low))
+    while rest >= 1:
+        last = np.float32(np.log(rest / one))
+        last = last if weight(last) <= rest else np.nextafter(last, np.float32(-math.inf))
+        assert last < z
+        row.append(float(last))
+        rest -= np.rint(weight(last))
+    return torch.tensor(row + [-math.inf] * (V - len(row)), dtype=torch.float32, device=DEV)
+
+
+@pytest.mark.parametrize("V", [8200, 40000, 300000, 1 << 20])
+def test_top_p_between_a_cells_tokens_and_their_sum(V):
+    """The tokens' masses, rounded one by one, come to 1500 steps less than their sum's, and p lies in between."""
+    row = row_that_reaches_p_at_a_cells_end(V, 0.9)
+    n = 6
+    logits = torch.stack([row[torch.randperm(V, generator=gen(i), device=DEV)] for i in range(n)])
+    u = [0.0, 0.3, 0.6, 0.8, 0.999, 1.0]
+    check_draw(logits, u, top_p=[0.9] * n)
+    check_draw(logits, u, top_p=[0.9] * n, min_p=[1e-4, 1e-5, 1e-6, 2.5e-4, 0.5, 2e-5])
+    check_draw(logits, u, top_p=[0.9] * n, top_k=[1 << 30, 7000, 5000, 4001, 4000, 2])
+
+
 # ---- books -----------------------------------------------------------------------------------------
 
 def make_books(rng, rows, columns, P, spare, longest):
