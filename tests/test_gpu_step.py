@@ -838,3 +838,117 @@ def test_sequences_that_only_lose_tokens(Bn, packed):
     check_extend(books, gpu, seqs, [-n for n in had], 16, 0 if packed else 90, 5 if packed else 90 * Bn)
     assert books["lengths"] == [0] * Bn and len(books["free"]) == books["capacity"]
     check_extend(books, gpu, seqs[::-1], had, 16, 0 if packed else 90, sum(had) if packed else 90 * Bn)
+
+
+@pytest.mark.parametrize("q_len,T", [(40, 160), (0, 40), (0, 5000)])
+@pytest.mark.parametrize("why", ["pages", "tokens", "room", "later sequence"])
+def test_refused_books_where_pages_would_go_back(q_len, T, why):
+    """One sequence gives pages back, another is refused: not a value of the books changes, behind the free pages' count neither."""
+    books = make_books(random.Random(3), 4, 8, 16, 4, 100)
+    books["lengths"] = [90, 20, 33, 5]
+    need = [-(-n // 16) for n in books["lengths"]]
+    books["capacity"] = sum(need) + 4
+    pages = list(range(100, 100 + books["capacity"]))
+    for r, n in enumerate(need):
+        books["table"][r][:n] = [pages.pop() for _ in range(n)]
+    books["free"] = pages
+    seqs, new = [0, 1, 2, 3], [-70, 3, 2, 1]                      # (four pages back)
+    if why == "pages":
+        new[1:] = [40, 40, 40]                                    # (six wanted)
+        books["free"] = []
+    elif why == "tokens":
+        if q_len or T > 100:
+            pytest.skip("they fit")
+        new[1:] = [38, 3, 0]
+    elif why == "room":
+        books["capacity"] = 7
+    else:
+        seqs[3] = 4
+    gpu = on_gpu(books)
+    before = {k: v.clone() for k, v in gpu.items()}
+    want = check_extend(books, gpu, seqs, new, 16, q_len, T)
+    assert want["status"][0] == {"pages": 4, "tokens": 5, "room": 3, "later sequence": 1}[why]
+    assert all(torch.equal(gpu[k], before[k]) for k in gpu)
+
+
+@pytest.mark.parametrize("heads,kv_heads,D,P", [(4, 2, 64, 16), (8, 1, 128, 32)])
+def test_attention_on_these_books(heads, kv_heads, D, P):
+    """Places for tokens, their keys and values into the cache, attention over it: packed prompts, then captured steps of up to three tokens of
+    each sequence, some of which lose tokens.  The same tokens on a cache where every sequence has pages of its own side by side give the same."""
+    rng, g = random.Random(D), gen(D)
+    Bn, rows, columns, q_len = 3, 5, 12, 3
+    books = make_books(rng, rows, columns, P, 40, 0)
+    gpu = on_gpu(books)
+    seqs = rng.sample(range(rows), Bn)
+    ints = lambda *n: torch.zeros(n, dtype=I32, device=DEV)  # noqa: E731
+    t = lambda v: torch.tensor(v, dtype=I32, device=DEV)  # noqa: E731
+    which, status, table, lengths = t(seqs), ints(2), torch.full((Bn, columns), -1, dtype=I32, device=DEV), ints(Bn)
+    work = torch.empty(B.basq_kv_books_bytes(Bn), dtype=torch.uint8, device=DEV)
+    cos_sin = torch.empty((columns * P, D), device=DEV)
+    B.basq_rope_table(cos_sin, 10000.0)
+    cache, own = (B.alloc_kv_cache(n, kv_heads, D, P, DEV) for n in (books["capacity"], rows * columns))
+    at_home = torch.arange(rows * columns, dtype=I32, device=DEV).view(rows, columns)[which.long()]
+    room = B.basq_paged_attention_workspace_bytes(Bn, q_len, heads, kv_heads, D, columns * P)
+    parts = torch.empty(room, dtype=torch.uint8, device=DEV) if room else None
+    randn = lambda *n: torch.randn(n, generator=g, device=DEV).to(BF16)  # noqa: E731
+
+    def append(x, positions, slots, cache):
+        q = x[:, :heads].clone()
+        B.basq_rope_append(q, x[:, heads:heads + kv_heads], x[:, heads + kv_heads:], positions, cos_sin, slots, cache, 0.9, 0.9, q)
+        return q
+
+    def attend(q, cache, table, lengths):
+        out = torch.empty_like(q)
+        B.basq_paged_attention(q, cache, table, lengths, columns * P, 1 / math.sqrt(D), out, parts, q_len=q_len)
+        return out
+
+    def places_at_home(have, new, T):
+        """Positions and slots of a sequence's own pages."""
+        positions, slots = [], []
+        for s, n, m in zip(seqs, have, new):
+            run = [(p, s * columns * P + p) for p in range(n, n + m)]
+            run = [(-1, -1)] * (0 if T else q_len - len(run)) + run
+            positions += [p for p, _ in run]
+            slots += [at for _, at in run]
+        rest = [-1] * (T - len(positions))
+        return t(positions + rest), t(slots + rest)
+
+    # prompts, packed, with room to spare
+    have, new = [0] * Bn, [5 * P + 3, 1, 2 * P]
+    T = sum(new) + 7
+    positions, slots = ints(T), ints(T)
+    B.basq_kv_extend(**gpu, new_tokens=t(new), page_size=P, positions=positions, slots=slots, status=status, books=work, seqs=which, q_len=0,
+                     batch_table=table, batch_lengths=lengths)
+    x = randn(T, heads + 2 * kv_heads, D)
+    here, there = append(x, positions, slots, cache), append(x, *places_at_home(have, new, T), own)
+    assert status.tolist() == [0, 0] and torch.equal(here[:sum(new)], there[:sum(new)])
+    have = [n + m for n, m in zip(have, new)]
+
+    # steps; the captured one reads its tokens and their numbers from the same places each time
+    counts, x = ints(Bn), randn(Bn * q_len, heads + 2 * kv_heads, D)
+    positions, slots, out = ints(Bn * q_len), ints(Bn * q_len), torch.empty((Bn * q_len, heads, D), dtype=BF16, device=DEV)
+
+    def step():
+        B.basq_kv_extend(**gpu, new_tokens=counts, page_size=P, positions=positions, slots=slots, status=status, books=work, seqs=which, q_len=q_len,
+                         batch_table=table, batch_lengths=lengths)
+        out.copy_(attend(append(x, positions, slots, cache), cache, table, lengths))
+
+    graph = None
+    for i, new in enumerate([[3, 3, 3], [1, 2, 3], [-2 * P, 3, -5], [3, -1, 0], [2, 3, 3], [-3, 1, 3], [3, 3, 1], [0, 0, 2]]):
+        counts.copy_(t(new))
+        x.copy_(randn(*x.shape))
+        if i == 1:
+            torch.cuda.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                step()
+        if graph is None:
+            step()
+        else:
+            graph.replay()
+        q = append(x, *places_at_home(have, [max(n, 0) for n in new], 0), own)
+        have = [n + m for n, m in zip(have, new)]
+        want = attend(q, own, at_home, t(have))
+        assert status.tolist() == [0, 0] and lengths.tolist() == have, i
+        assert torch.equal(out, want) and out.isfinite().all() and out.abs().max() > 0, i
+    assert gpu["free_count"].item() == books["capacity"] - sum(-(-n // P) for n in have)
