@@ -10,7 +10,7 @@
 //
 // One pass over the weights, which bound it where they are large (16 x 8192 x 128000, 565 MB: 117 us, 4.8 TB/s, vector instructions half of the time);
 // smaller calls are bound by the waits of a step, of which each wave has few (1 x 4096 x 4096 4.2 us, 13 x 14336 x 4096 16.4, 48 x 4096 x
-// 11008 16.8; their bytes 1.3, 4.9 and 4.3).  Each lane requests its batch of 16-byte pieces before it takes any up.  A workgroup
+// 11008 17.0; their bytes 1.3, 4.9 and 4.3).  Each lane requests its batch of 16-byte pieces before it takes any up.  A workgroup
 // owns TILES tiles of 16 weight rows, its waves share K in chunks of 128 channels; D = x (rows) times weights (columns), so a
 // lane's results belong to one weight row and take one scale.
 //
@@ -321,7 +321,14 @@ void launch_shape(const W4A16Args& a, hipStream_t s) {
 // four waves with a tile each, so that four share the tokens, twice as many to share K unless that fills the chip anyway (us;
 // 1 x 8 is one wave's tiles and eight waves of K): 16 x 4096 x 4096 in groups of 128 1 x 8 6.7, 4 x 2 8.8, 4 x 1 10.3; x 12288 on three
 // tiles 10.2, 4 x 2 9.6, 4 x 1 10.7; x 32000 1 x 8 26.1, 4 x 2 17.1 to 18.5, 4 x 1 16.6; x 128000 89, 64 and 57.  More tokens stay
-// with 4 x 2 longer.
+// with 4 x 2 longer: 60 x 4096 x 32000 in groups of 128 42.3, 4 x 1 55.8; x 64000 81.4 and 69.0; x 128000 158 and 134 (in groups of 32 50.0 and
+// 65.0, 96.1 and 85.8, 186 and 167); 20 x 4096 x 64000 51.4 and 46.7, x 128000 98.4 and 91.3.  33 to 48 tokens always do, which costs
+// them: 40 x 4096 x 128000 176, 4 x 1 130 (in groups of 32 148 and 143).
+//
+// Scales that lie side by side (groups of 32, 64 or 128) are read a step at a time, so shapes with steps of four or two chunks take K of as
+// many: x 32000 in groups of 128, 16 tokens, K = 4096 (32 chunks) 17.1, 2816 and 2304 (22 and 18) 22.5 and 21.6, 1024 6.4, 1152 and 896 (9
+// and 7) 16.1 and 12.9.  K that ends inside a chunk has one shape in groups of 32 or 64: 16 x 2880 x 32000 74.2 and 50.7, where 2048
+// takes 14.7 and 12.1.
 constexpr int FEW_TILES = 768, MANY_TILES = 1500, MANY_TILES_OF_MORE = 6000;
 int tiles_of(const W4A16Args& a) { return (a.N + TILE - 1) / TILE; }
 
@@ -344,7 +351,7 @@ void launch_16(const W4A16Args& a, hipStream_t s) {
     }
 }
 // Up to 32, 48 or 64 tokens: their operands and sums take the registers of a second batch of weights, so a batch is long instead and the
-// tokens go through LDS chunk by chunk (48 x 4096 x 11008 in groups of 32 18.6 us, in batches of one chunk 21.6; 64 x 4096 x 32000
+// tokens go through LDS chunk by chunk (48 x 4096 x 11008 in groups of 32 18.6 us then, in batches of one chunk 21.6; 64 x 4096 x 32000
 // on two tiles a wave 43.4, on one 51).
 template <bool SL, int UNIT, bool SIDE, int TT>
 void launch_64(const W4A16Args& a, hipStream_t s) {

@@ -190,6 +190,8 @@ __global__ __launch_bounds__(256) void kv_place_kernel(KvExtendArgs a, int token
 
 int launch_kv_extend(KvExtendArgs a, hipStream_t s) {
     uint8_t* books = a.plan;
+    // (one launch, two: one token of 128 sequences 6.5 us and 8.1, of 200 8.6 and 8.0; some 4000 packed tokens of 16 sequences 6.4 and 8.0, 8000 9.0
+    // and 8.0)
     const bool one = a.T <= 4096 && a.B <= 128;
     a.plan = one ? nullptr : books;
     hipLaunchKernelGGL(kv_plan_kernel, dim3(1), dim3(THREADS), 0, s, a);

@@ -643,7 +643,7 @@ __global__ __launch_bounds__(THREADS) void sample_numbers_kernel(SampleArgs a) {
         else atomicAdd(&s.parts[token >> log2], 1);
     };
     // (Sixteen pieces and what stands between have not the registers: the last four are read again, from the cache.  256 rows of 128000 logits
-    // 34.2 us, with all of them kept, and some 20 MB of spilled ones, 37.2.)
+    // 34.2 us, with some 5 MB of spilled registers, with all of them kept, and some 20 MB, 37.2.)
     constexpr int KEPT = R > 12 ? 12 : R;
 #pragma unroll
     for (int r = KEPT; r < R; ++r) row.load_one(held[r], r * THREADS + tid);
@@ -1295,8 +1295,9 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a) {
     if (tid == 0) put(a, b, (int)~(unsigned)s.found_key, share(w, c.heat, logit_of((unsigned)(s.found_key >> 32)), mass), kept);
 }
 
-// Slices of a row: as many pieces of a thread as it holds in registers, or two where the rows alone do not fill the chip.  (Eight, four:
-// 64 rows of 128000 logits 14.4 us the slices and 29.2 the rows, 15.5 and 31.2.)
+// Slices of a row: as many pieces of a thread as it holds in registers, or two where those are 256 workgroups at most.  (Eight, four:
+// 64 rows of 128000 logits 14.4 us the slices and 29.2 the rows, 15.5 and 31.2.  Eight, two, the whole with top-p: 8 rows of 40000 47.8 us
+// and 28.6, 50 rows 50.1 and 31.6, but also 80 rows 50.5 and 34.0; 4 rows of 128000 39.9 and 43.3, 48 rows 47.2 and 59.1.)
 constexpr int FEW_PIECES = 2, MANY_PIECES = 8;
 static_assert(SAMPLE_SHORT == THREADS * MANY_PIECES * Piece<true>::N, "a row that a workgroup holds");
 int slices_of(int32_t V, int r) { return (V / 4 + 1 + THREADS * r - 1) / (THREADS * r); }
